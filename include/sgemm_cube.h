@@ -338,6 +338,139 @@ int sgemm_cube_auto_scaled(sgemm_cube_handle h, int M, int N, int K,
                            float* C_dev, int64_t ldc,
                            int accumulation_order, void* stream, int* chosen_out);
 
+/* ---- Language-model operators on and around the split product.
+ *
+ * A linear layer with its gradients, layer normalisation with its gradients, and log probabilities of
+ * given tokens with their gradient.  No call synchronises; once the handle's workspace has its size
+ * the calls can be captured into a graph.  As everywhere, calls on one handle that may overlap on the
+ * GPU need one handle per stream.  Sums, statistics and softmax sums are FP32 (the products' k-blocks as
+ * sgemm_cube, termwise); every result is the same from call to call.
+ */
+
+/* Operand of a linear layer: a row-major FP32 matrix (f32_dev, ld), or, with f32_dev NULL, one packed by
+ * sgemm_cube_pack (hi_dev, lo_dev, ld16, exp_dev).  Packing is what the layer does to an FP32 operand
+ * in its workspace on every call; an operand that is used again (a weight that is served, an operand
+ * of both the product and a gradient) is packed once by the caller instead.  4 bytes per element. */
+typedef struct sgemm_cube_operand {
+  const float* f32_dev;
+  int64_t ld;
+  const uint16_t* hi_dev;
+  const uint16_t* lo_dev;
+  int64_t ld16;
+  const int32_t* exp_dev;
+} sgemm_cube_operand;
+
+/* Layout of a weight with K inputs and N outputs. */
+enum {
+  SGEMM_CUBE_WEIGHT_KN = 0,   /* K x N row-major, the B of sgemm_cube */
+  SGEMM_CUBE_WEIGHT_NK = 1    /* N x K row-major, one row per output */
+};
+
+enum {
+  SGEMM_CUBE_ACT_NONE = 0,
+  SGEMM_CUBE_ACT_RELU = 1,       /* max(z, 0), slope 0 at 0 */
+  SGEMM_CUBE_ACT_GELU = 2,       /* z Phi(z), Phi the normal distribution function */
+  SGEMM_CUBE_ACT_GELU_TANH = 3,  /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+  SGEMM_CUBE_ACT_SILU = 4        /* z / (1 + exp(-z)) */
+};
+
+/* Scaling exponent and two-word split of a matrix, all on the device:
+ *   p = 15 - e_max, clamped to [-126, 126]; e_max as in sgemm_cube_hi_exponent_range (p = 0 if every
+ *   entry is zero, infinite or NaN); hi = fl16(2^p x), lo = fl16((2^p x - hi) 2^11).
+ * An entry keeps 22 bits while it is within 2^-29 of the largest; below that its error is at most 2^-51
+ * of the largest.  One infinite or NaN entry makes the results that depend on it NaN, no others.
+ *   X_dev  rows x cols FP32, ldx >= cols, any alignment                        (device, read)
+ *   hi_dev/lo_dev  rows x ld16 words each, 16-byte aligned, ld16 >= cols, ld16 % 8 == 0 (device, written;
+ *                  columns past cols are zero up to the next multiple of 8)
+ *   exp_dev  one int32                                                          (device, written)
+ * Errors: INVALID_ARG, MISALIGNED, CUDA_ERROR. */
+int sgemm_cube_pack(sgemm_cube_handle h, int rows, int cols,
+                    const float* X_dev, int64_t ldx,
+                    uint16_t* hi_dev, uint16_t* lo_dev, int64_t ld16, int32_t* exp_dev, void* stream);
+
+/* Linear layer:  z = X W + b,  Y = act(z) + R.
+ *   X  M x K;  W  K inputs, N outputs in weight_layout;  either may be FP32 or packed
+ *   bias_dev N FP32 or NULL;  R_dev M x N FP32 (ldr >= N) or NULL, may be Y_dev itself (then ldr == ldy)
+ *   Y_dev M x N FP32 (written);  Z_dev M x N FP32 or NULL: z is stored there for the backward pass
+ * FP32 matrices may have any alignment.  The product is the three-product form of sgemm_cube on packed
+ * operands; an FP32 X of at most 8 rows is multiplied in FP32 (W read once, no packing).  M, N, K >= 0;
+ * K == 0 gives Y = act(b) + R.
+ * Errors: INVALID_ARG, MISALIGNED (packed operands), ALLOC_FAILED, CUDA_ERROR. */
+int sgemm_cube_linear(sgemm_cube_handle h, int M, int N, int K,
+                      const sgemm_cube_operand* X, const sgemm_cube_operand* W, int weight_layout,
+                      const float* bias_dev, const float* R_dev, int64_t ldr, int activation,
+                      float* Y_dev, int64_t ldy, float* Z_dev, int64_t ldz, void* stream);
+
+/* Gradients of the linear layer for dY = dL/dY:  with dz = dY act'(z),
+ *   dX = dz W^T (M x K),  dW = X^T dz (in weight_layout),  dbias = column sums of dz (N).
+ * Each output may be NULL and is then not computed; X is looked at for dW only, W for dX only.  Z_dev is
+ * the z of the forward call (looked at unless activation is NONE).  The gradient of R is dY.  dz is
+ * packed like the other operands, so gradients of any magnitude keep their bits.  Outputs must not
+ * overlap the inputs or each other.  An empty sum (M == 0 for dW and dbias, N == 0 for dX) is zero.
+ * Errors: INVALID_ARG, MISALIGNED (packed operands), ALLOC_FAILED, CUDA_ERROR. */
+int sgemm_cube_linear_backward(sgemm_cube_handle h, int M, int N, int K,
+                               const float* dY_dev, int64_t lddy, const float* Z_dev, int64_t ldz,
+                               int activation, const sgemm_cube_operand* X, const sgemm_cube_operand* W,
+                               int weight_layout, float* dX_dev, int64_t lddx, float* dW_dev, int64_t lddw,
+                               float* dbias_dev, void* stream);
+
+/* Element types of the operators below. */
+enum {
+  SGEMM_CUBE_F32 = 0,
+  SGEMM_CUBE_F16 = 1,
+  SGEMM_CUBE_BF16 = 2
+};
+
+/* Layer normalisation of each row:  y = (x - mean) rstd w + b,  rstd = 1 / sqrt(var + eps), var the mean of
+ * (x - mean)^2.  Computed in FP32, rounded once to the element type.
+ *   X_dev, Y_dev  rows x cols of `dtype`, row-major, any alignment (Y_dev may be X_dev with ldy == ldx)
+ *   weight_dev, bias_dev  cols FP32 or NULL (1 and 0);  mean_dev, rstd_dev  rows FP32 or NULL (written,
+ *   for the backward pass)
+ * rows >= 0, cols >= 1, eps >= 0.  Errors: INVALID_ARG, CUDA_ERROR. */
+int sgemm_cube_layer_norm(sgemm_cube_handle h, int rows, int cols, int dtype,
+                          const void* X_dev, int64_t ldx, const float* weight_dev, const float* bias_dev,
+                          float eps, void* Y_dev, int64_t ldy, float* mean_dev, float* rstd_dev, void* stream);
+
+/* Its gradients for dY:  with u = dY w and n = (x - mean) rstd,
+ *   dX = rstd (u - mean(u) - n mean(u n)),  dweight = sum over rows of dY n,  dbias = sum over rows of dY.
+ * dX_dev rows x cols of `dtype` or NULL (may be dY_dev with lddx == lddy); dweight_dev, dbias_dev cols FP32
+ * or NULL (zero when rows == 0).  mean_dev and rstd_dev are the forward call's.
+ * Errors: INVALID_ARG, ALLOC_FAILED, CUDA_ERROR. */
+int sgemm_cube_layer_norm_backward(sgemm_cube_handle h, int rows, int cols, int dtype,
+                                   const void* dY_dev, int64_t lddy, const void* X_dev, int64_t ldx,
+                                   const float* weight_dev, const float* mean_dev, const float* rstd_dev,
+                                   void* dX_dev, int64_t lddx, float* dweight_dev, float* dbias_dev,
+                                   void* stream);
+
+/* Log probabilities of given tokens under softmax(scale * logits), row by row, in one pass over the logits:
+ *   logp_dev[r]     = scale x[r, t] - lse[r], t = tokens_dev[r]; 0 where t < 0 (no target), NaN where t >= vocab
+ *   entropy_dev[r]  = - sum_j p_j log p_j, a probability of zero contributing nothing      (or NULL)
+ *   stats_dev[r]    = {largest logit m, sum of exp(scale (x - m))}; lse = scale m + log of the second
+ *                     (rows x 2 FP32, for the backward pass; or NULL)
+ *   top_logp_dev, top_index_dev  rows x top_k: the largest log probabilities, descending, and their
+ *                     columns; equal logits are ordered by column (both NULL iff top_k == 0)
+ *   logits_dev      rows x vocab of `dtype`, row-major, any alignment; -inf marks a token that is not allowed
+ *   tokens_dev      rows int64, or NULL with logp_dev NULL
+ * 0 <= top_k <= 32 and <= vocab; vocab >= 1; scale positive and finite.  A row whose every logit is -inf has no
+ * distribution: logp and top_logp are -inf, entropy 0, top_index the first columns, stats {-inf, 0}, its
+ * gradient zero.  A row that holds NaN or +inf gives NaN (top_index then names valid columns, no more).
+ * Errors: INVALID_ARG, CUDA_ERROR. */
+int sgemm_cube_token_logprobs(sgemm_cube_handle h, int rows, int vocab, int dtype,
+                              const void* logits_dev, int64_t ld, const int64_t* tokens_dev, float scale,
+                              float* logp_dev, float* entropy_dev, float* stats_dev,
+                              int top_k, float* top_logp_dev, int64_t* top_index_dev, void* stream);
+
+/* Gradient of the logits for dlogp and dentropy (each rows FP32 or NULL, not both NULL):
+ *   dlogits[r, j] = scale (dlogp[r] (1[j == t] - p_j) - dentropy[r] p_j (log p_j + H))
+ * with the forward call's stats and (for dentropy) entropy.  A row without target takes no part in dlogp.
+ * dlogits_dev rows x vocab of `dtype`, may be logits_dev itself (then lddl == ld).
+ * Errors: INVALID_ARG, CUDA_ERROR. */
+int sgemm_cube_token_logprobs_backward(sgemm_cube_handle h, int rows, int vocab, int dtype,
+                                       const void* logits_dev, int64_t ld, const int64_t* tokens_dev,
+                                       float scale, const float* stats_dev, const float* entropy_dev,
+                                       const float* dlogp_dev, const float* dentropy_dev,
+                                       void* dlogits_dev, int64_t lddl, void* stream);
+
 /* Size in bytes of the fixed device scratch area used by sgemm_cube_unfused_static. */
 #define SGEMM_CUBE_STATIC_SCRATCH_BYTES (32u << 20)
 

@@ -17,6 +17,10 @@ STATIC_SCRATCH_BYTES = 32 << 20
 TERMWISE, ELEMENTWISE, ELEMENTWISE_REORDERED = 0, 1, 2
 OPT_TERMWISE_K_BLOCK, OPT_ELEMENTWISE_K_BLOCK, OPT_CTA_PAIR, OPT_STRATEGY, OPT_TIME_KERNEL, OPT_SPLIT_K = range(6)
 STRATEGY_AUTO, STRATEGY_FUSED, STRATEGY_TWO_PHASE = 0, 1, 2
+WEIGHT_KN, WEIGHT_NK = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
+F32, F16, BF16 = range(3)
+_DTYPE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
 EXPORTS = ["sgemm_cube_create", "sgemm_cube_destroy", "sgemm_cube_set_option", "sgemm_cube_split",
            "sgemm_cube", "sgemm_cube_unfused", "sgemm_cube_presplit", "sgemm_cube_hgemm",
@@ -25,6 +29,9 @@ EXPORTS = ["sgemm_cube_create", "sgemm_cube_destroy", "sgemm_cube_set_option", "
            "sgemm_cube_host", "sgemm_cube_unfused_static", "sgemm_cube_check", "sgemm_cube_launch_count", "sgemm_cube_last_kernel_ms", "sgemm_cube_mean_kernel_ms",
            "sgemm_cube_exponent_window", "sgemm_cube_choose_scale_exp", "sgemm_cube_residual_overflow_count",
            "sgemm_cube_last_kernel_clock", "sgemm_cube_debug_inject_error", "sgemm_cube_debug_wait_timeout",
+           "sgemm_cube_pack", "sgemm_cube_linear", "sgemm_cube_linear_backward",
+           "sgemm_cube_layer_norm", "sgemm_cube_layer_norm_backward",
+           "sgemm_cube_token_logprobs", "sgemm_cube_token_logprobs_backward",
            "sgemm_cube_status_string", "sgemm_cube_version"]
 
 _lib = None
@@ -34,6 +41,24 @@ class SgemmCubeError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
         super().__init__("%s failed: status %d (%s)" % (where, status, status_string(status)))
+
+
+class _Operand(ctypes.Structure):
+    _fields_ = [("f32_dev", ctypes.c_void_p), ("ld", ctypes.c_int64), ("hi_dev", ctypes.c_void_p),
+                ("lo_dev", ctypes.c_void_p), ("ld16", ctypes.c_int64), ("exp_dev", ctypes.c_void_p)]
+
+
+class PackedMatrix:
+    """Room for one packed operand of a linear layer: the FP16 words and the scaling exponent that
+    Handle.sgemm_cube_pack writes (4 bytes per element)."""
+
+    def __init__(self, rows, cols, device="cuda:0"):
+        self.shape = (int(rows), int(cols))
+        ld = (self.shape[1] + 7) // 8 * 8
+        self.hi = torch.empty((self.shape[0], ld), dtype=torch.float16, device=device)
+        self.lo = torch.empty_like(self.hi)
+        self.exp = torch.empty(1, dtype=torch.int32, device=device)
+        self.operand = _Operand(None, 0, self.hi.data_ptr(), self.lo.data_ptr(), ld, self.exp.data_ptr())
 
 
 def load():
@@ -64,6 +89,17 @@ def load():
     lib.sgemm_cube_choose_input_scaling.argtypes = [ctypes.POINTER(i64), ctypes.POINTER(i64), pi, pi, pi, pi]
     lib.sgemm_cube_scaled.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp]
     lib.sgemm_cube_auto_scaled.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, vp, i64, i32, vp, pi]
+    pop, f32 = ctypes.POINTER(_Operand), ctypes.c_float
+    lib.sgemm_cube_pack.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, vp]
+    lib.sgemm_cube_linear.argtypes = [vp, i32, i32, i32, pop, pop, i32, vp, vp, i64, i32, vp, i64, vp, i64, vp]
+    lib.sgemm_cube_linear_backward.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, i32, pop, pop, i32, vp, i64,
+                                               vp, i64, vp, vp]
+    lib.sgemm_cube_layer_norm.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, f32, vp, i64, vp, vp, vp]
+    lib.sgemm_cube_layer_norm_backward.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp,
+                                                   vp, vp]
+    lib.sgemm_cube_token_logprobs.argtypes = [vp, i32, i32, i32, vp, i64, vp, f32, vp, vp, vp, i32, vp, vp, vp]
+    lib.sgemm_cube_token_logprobs_backward.argtypes = [vp, i32, i32, i32, vp, i64, vp, f32, vp, vp, vp, vp, vp,
+                                                       i64, vp]
     lib.sgemm_cube_check.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_uint32)]
     lib.sgemm_cube_last_kernel_ms.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
     lib.sgemm_cube_mean_kernel_ms.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i32)]
@@ -114,6 +150,34 @@ def _ld(t):
 def _dev(t, dtype):
     assert t.is_cuda and t.dtype == dtype, "expected a CUDA tensor of dtype %s" % dtype
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _vector(t, n, dtype=torch.float32):
+    """Pointer of an optional contiguous vector of n elements."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == dtype and t.numel() == n and t.is_contiguous(), "contiguous %s vector" % dtype
+    return t.data_ptr()
+
+
+def _matrix(t, rows, cols, dtype=torch.float32):
+    """(pointer, leading dimension) of an optional row-major matrix."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.dtype == dtype and t.shape == (rows, cols), "expected %s (%d, %d)" % (dtype, rows, cols)
+    return t.data_ptr(), _ld(t)
+
+
+def _operand(t):
+    """An FP32 tensor or a PackedMatrix as the C struct."""
+    if isinstance(t, PackedMatrix):
+        return t.operand
+    assert t.is_cuda and t.dtype == torch.float32, "expected a CUDA tensor of dtype float32 or a PackedMatrix"
+    return _Operand(t.data_ptr(), _ld(t), None, None, 0, None)
+
+
+def _raw_stream(stream):
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
 def sgemm_cube_unfused_static(A, B, C, scale_exp=11, stream=None):
@@ -288,6 +352,89 @@ class Handle:
         _check(load().sgemm_cube_exponent_window(self._h, rows, cols, _dev(X, torch.float32), _ld(X),
                                                  out, _stream_ptr(stream)), "sgemm_cube_exponent_window")
         return [int(v) for v in out]
+
+    def sgemm_cube_pack(self, X, packed, stream=None):
+        """Scale, split and store X in a PackedMatrix of its shape."""
+        rows, cols = X.shape
+        assert packed.shape == (rows, cols)
+        x, ldx = _matrix(X, rows, cols)
+        o = packed.operand
+        _check(load().sgemm_cube_pack(self._h, rows, cols, x, ldx, o.hi_dev, o.lo_dev, o.ld16, o.exp_dev,
+                                      _raw_stream(stream)), "sgemm_cube_pack")
+
+    def sgemm_cube_linear(self, X, W, Y, bias=None, residual=None, activation=ACT_NONE, preact=None,
+                          weight_layout=WEIGHT_KN, stream=None):
+        """Y = act(X W + bias) + residual; X and W are FP32 tensors or PackedMatrix objects."""
+        (M, K), (a, b) = X.shape, W.shape
+        k2, N = (b, a) if weight_layout == WEIGHT_NK else (a, b)
+        assert K == k2, "X and W do not fit"
+        y, ldy = _matrix(Y, M, N)
+        r, ldr = _matrix(residual, M, N)
+        z, ldz = _matrix(preact, M, N)
+        _check(load().sgemm_cube_linear(self._h, M, N, K, _operand(X), _operand(W), weight_layout, _vector(bias, N),
+                                        r, ldr, activation, y, ldy, z, ldz, _raw_stream(stream)),
+               "sgemm_cube_linear")
+
+    def sgemm_cube_linear_backward(self, dY, X, W, dX=None, dW=None, dbias=None, preact=None,
+                                   activation=ACT_NONE, weight_layout=WEIGHT_KN, stream=None):
+        """Gradients of sgemm_cube_linear into whichever of dX, dW and dbias are given."""
+        (M, K), (a, b) = X.shape, W.shape
+        k2, N = (b, a) if weight_layout == WEIGHT_NK else (a, b)
+        assert K == k2, "X and W do not fit"
+        g, lddy = _matrix(dY, M, N)
+        z, ldz = _matrix(preact, M, N)
+        dx, lddx = _matrix(dX, M, K)
+        dw, lddw = _matrix(dW, a, b)
+        _check(load().sgemm_cube_linear_backward(self._h, M, N, K, g, lddy, z, ldz, activation, _operand(X),
+                                                 _operand(W), weight_layout, dx, lddx, dw, lddw, _vector(dbias, N),
+                                                 _raw_stream(stream)), "sgemm_cube_linear_backward")
+
+    def sgemm_cube_layer_norm(self, X, Y, weight=None, bias=None, eps=1e-5, mean=None, rstd=None, stream=None):
+        """Layer normalisation of the rows of X (float32, float16 or bfloat16) into Y."""
+        rows, cols = X.shape
+        x, ldx = _matrix(X, rows, cols, X.dtype)
+        y, ldy = _matrix(Y, rows, cols, X.dtype)
+        _check(load().sgemm_cube_layer_norm(self._h, rows, cols, _DTYPE[X.dtype], x, ldx, _vector(weight, cols),
+                                            _vector(bias, cols), eps, y, ldy, _vector(mean, rows),
+                                            _vector(rstd, rows), _raw_stream(stream)), "sgemm_cube_layer_norm")
+
+    def sgemm_cube_layer_norm_backward(self, dY, X, mean, rstd, dX=None, weight=None, dweight=None, dbias=None,
+                                       stream=None):
+        """Gradients of sgemm_cube_layer_norm into whichever of dX, dweight and dbias are given."""
+        rows, cols = X.shape
+        g, lddy = _matrix(dY, rows, cols, X.dtype)
+        x, ldx = _matrix(X, rows, cols, X.dtype)
+        dx, lddx = _matrix(dX, rows, cols, X.dtype)
+        _check(load().sgemm_cube_layer_norm_backward(self._h, rows, cols, _DTYPE[X.dtype], g, lddy, x, ldx,
+                                                     _vector(weight, cols), _vector(mean, rows), _vector(rstd, rows),
+                                                     dx, lddx, _vector(dweight, cols), _vector(dbias, cols),
+                                                     _raw_stream(stream)), "sgemm_cube_layer_norm_backward")
+
+    def sgemm_cube_token_logprobs(self, logits, tokens, logp, entropy=None, stats=None, top_logp=None,
+                                  top_index=None, scale=1.0, stream=None):
+        """Log probabilities of tokens (int64, negative: no target), entropy, softmax statistics (rows, 2)
+        and the top_logp.shape[1] most likely alternatives of every row."""
+        rows, vocab = logits.shape
+        x, ld = _matrix(logits, rows, vocab, logits.dtype)
+        assert (top_logp is None) == (top_index is None)
+        k = 0 if top_logp is None else top_logp.shape[1]
+        _check(load().sgemm_cube_token_logprobs(self._h, rows, vocab, _DTYPE[logits.dtype], x, ld,
+                                                _vector(tokens, rows, torch.int64), scale, _vector(logp, rows),
+                                                _vector(entropy, rows), _vector(stats, 2 * rows), k,
+                                                _vector(top_logp, rows * k), _vector(top_index, rows * k, torch.int64),
+                                                _raw_stream(stream)), "sgemm_cube_token_logprobs")
+
+    def sgemm_cube_token_logprobs_backward(self, logits, tokens, stats, dlogits, dlogp=None, entropy=None,
+                                           dentropy=None, scale=1.0, stream=None):
+        """Gradient of the logits for the gradients of logp and entropy; dlogits may be logits."""
+        rows, vocab = logits.shape
+        x, ld = _matrix(logits, rows, vocab, logits.dtype)
+        dx, lddl = _matrix(dlogits, rows, vocab, logits.dtype)
+        _check(load().sgemm_cube_token_logprobs_backward(self._h, rows, vocab, _DTYPE[logits.dtype], x, ld,
+                                                         _vector(tokens, rows, torch.int64), scale,
+                                                         _vector(stats, 2 * rows), _vector(entropy, rows),
+                                                         _vector(dlogp, rows), _vector(dentropy, rows), dx, lddl,
+                                                         _raw_stream(stream)), "sgemm_cube_token_logprobs_backward")
 
     def sgemm_cube_launch_count(self) -> int:
         return int(load().sgemm_cube_launch_count(self._h))

@@ -9,12 +9,12 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsgemm_cube.so")
-SOURCES = [os.path.join(CSRC, "sgemm_cube_api.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("sgemm_cube_api.cu", "linear_api.cu", "layer_norm.cu", "token_logprobs.cu")]
 DEPS = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + \
        [os.path.join(os.path.dirname(HERE), "include", "sgemm_cube.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
+              "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v", "--threads", "0"]
 
 
 def is_stale() -> bool:

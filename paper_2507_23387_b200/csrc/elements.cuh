@@ -1,0 +1,144 @@
+// FP32, FP16 and BF16 elements for the kernels that work in FP32 whatever the storage type: 16-byte
+// vectors and single elements, converted on load and rounded once (to nearest even) on store.
+#pragma once
+
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+namespace sgc {
+
+template <typename T>
+struct Elem;
+
+template <>
+struct Elem<float> {
+  static constexpr int kVec = 4;
+  static __device__ __forceinline__ void unpack(const uint4& r, float (&v)[4]) {
+    v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y);
+    v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&v)[4]) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+  }
+  static __device__ __forceinline__ float get(float x) { return x; }
+  static __device__ __forceinline__ float put(float x) { return x; }
+};
+
+template <>
+struct Elem<__half> {
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ void unpack(const uint4& r, float (&v)[8]) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&v)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ float get(__half x) { return __half2float(x); }
+  static __device__ __forceinline__ __half put(float x) { return __float2half_rn(x); }
+};
+
+template <>
+struct Elem<__nv_bfloat16> {
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ void unpack(const uint4& r, float (&v)[8]) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&v)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ float get(__nv_bfloat16 x) { return __bfloat162float(x); }
+  static __device__ __forceinline__ __nv_bfloat16 put(float x) { return __float2bfloat16_rn(x); }
+};
+
+// Which columns of a row a thread of a group of `threads` holds.  VEC: 16-byte vectors, vector i at
+// (i * threads + t) * kVec; otherwise (rows that are not 16-byte aligned) single elements, element i at
+// i * threads + t.  Either way a warp's accesses are contiguous.  PT elements a thread, columns past
+// `cols` read as `fill`.
+template <typename T, int PT, bool VEC>
+__device__ __forceinline__ void load_row(const T* __restrict__ row, int cols, int t, int threads, float fill,
+                                         float (&v)[PT]) {
+  if constexpr (VEC) {
+    constexpr int V = Elem<T>::kVec;
+    uint4 raw[PT / V];
+#pragma unroll
+    for (int i = 0; i < PT / V; ++i) {
+      const int c = (i * threads + t) * V;
+      raw[i] = c < cols ? __ldcs(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < PT / V; ++i) {
+      float e[V];
+      Elem<T>::unpack(raw[i], e);
+      const bool in = (i * threads + t) * V < cols;
+#pragma unroll
+      for (int q = 0; q < V; ++q) v[i * V + q] = in ? e[q] : fill;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < PT; ++i) {
+      const int c = i * threads + t;
+      v[i] = c < cols ? Elem<T>::get(row[c]) : fill;
+    }
+  }
+}
+template <typename T, int PT, bool VEC>
+__device__ __forceinline__ void store_row(T* row, int cols, int t, int threads, const float (&v)[PT]) {
+  if constexpr (VEC) {
+    constexpr int V = Elem<T>::kVec;
+#pragma unroll
+    for (int i = 0; i < PT / V; ++i) {
+      const int c = (i * threads + t) * V;
+      float e[V];
+#pragma unroll
+      for (int q = 0; q < V; ++q) e[q] = v[i * V + q];
+      if (c < cols) *reinterpret_cast<uint4*>(row + c) = Elem<T>::pack(e);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < PT; ++i) {
+      const int c = i * threads + t;
+      if (c < cols) row[c] = Elem<T>::put(v[i]);
+    }
+  }
+}
+// Column of the thread's element i.
+template <typename T, bool VEC>
+__device__ __forceinline__ int row_column(int i, int t, int threads) {
+  if constexpr (VEC) {
+    constexpr int V = Elem<T>::kVec;
+    return (i / V * threads + t) * V + i % V;
+  } else {
+    return i * threads + t;
+  }
+}
+
+// Whether rows of `ld` elements from p are 16-byte aligned and whole vectors long.
+inline bool rows_take_vectors(const void* p, int64_t ld, int cols, size_t elem) {
+  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * elem) % 16 == 0 && (cols * elem) % 16 == 0;
+}
+
+}  // namespace sgc

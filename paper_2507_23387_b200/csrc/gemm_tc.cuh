@@ -43,6 +43,7 @@
 
 #include <type_traits>
 
+#include "linear_epilogue.cuh"
 #include "ptx_sm100.cuh"
 
 namespace sgc {
@@ -291,14 +292,30 @@ __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[16]) 
 __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld_32x32b_x32(taddr, r); }
 __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[64]) { tmem_ld_32x32b_x64(taddr, r); }
 
+// What a kernel computes from its FP16 words.  kFormProduct: the library's plain product, row-major
+// A (M x K) and B (K x N).  The others are the products of a linear layer and of its gradients on
+// packed operands (linear_epilogue.cuh): one power-of-two exponent per operand is undone and the
+// layer's epilogue applied.  The two letters say which index of A and of B is contiguous in memory:
+// K the contracted one, M the other (row-major A is K, row-major B is M).
+enum LinearForm { kFormProduct = 0, kFormKM, kFormKK, kFormMM };
+
+struct TcLinearParams : TcGemmParams {
+  LinearEpilogue ep;
+};
+template <int FORM>
+using TcParams = std::conditional_t<FORM == kFormProduct, TcGemmParams, TcLinearParams>;
+
 // REORD: the reordered elementwise order (p.order == 2) has its own instantiations, so that its
 // accumulate path (two chunk buffers live at once) does not weigh on the register allocation of
 // the termwise / elementwise kernels.
-template <int NTERMS, bool FUSED, bool PAIR, bool REORD = false>
+template <int NTERMS, bool FUSED, bool PAIR, bool REORD = false, int FORM = kFormProduct>
 __global__ void __launch_bounds__(FUSED ? kFusedThreads : kTcThreads, 1)
 tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmA1,
                const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmB1,
-               const TcGemmParams p) {
+               const TcParams<FORM> p) {
+  constexpr bool A_MN = FORM == kFormMM;                            // A's rows (M) contiguous
+  constexpr bool B_MN = FORM != kFormKK;                            // B's columns (N) contiguous
+  static_assert(FORM == kFormProduct || (NTERMS == 3 && !FUSED && !REORD), "linear forms");
   using Cfg = TcCfg<NTERMS, PAIR, FUSED>;
   constexpr int BK = Cfg::BK;
   constexpr int STAGES = Cfg::STAGES;
@@ -648,7 +665,11 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
         drains[1]++;
         if (split_out) store_tile(p.Px + (long long)slice * p.pstride, p.ldp, true, 0);
       }
-      if (!split_out) store_tile(p.D, p.ldd, vec_ok, (NTERMS == 1) ? p.accumulate : 0);
+      if (!split_out) {
+        if constexpr (FORM == kFormProduct) store_tile(p.D, p.ldd, vec_ok, (NTERMS == 1) ? p.accumulate : 0);
+        else linear_store_tile(p.ep, p.D, p.ldd, p.M, p.N, S, smem_u32(store_staging + warp * 4096),
+                               tm * kBM + quarter * 32, col_base, lane);
+      }
       SGC_TADD(8, blockIdx.x == 0 && threadIdx.x == 0);
     }
   } else if (warp == kMmaWarp) {
@@ -657,7 +678,7 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
     // ------------------------------------------------------------------ MMA issuer
     if (lane == 0 && leader) {
       constexpr uint32_t idesc =
-          umma_idesc_f16(PAIR ? 2 * kBM : kBM, kBN, /*A MN-major*/ false, /*B MN-major*/ true);
+          umma_idesc_f16(PAIR ? 2 * kBM : kBM, kBN, /*A MN-major*/ A_MN, /*B MN-major*/ B_MN);
       auto mma = [&](uint32_t d, uint64_t da, uint64_t db, uint32_t acc) {
         if (PAIR) umma_f16_ss_pair(d, da, db, idesc, acc);
         else umma_f16_ss(d, da, db, idesc, acc);
@@ -682,8 +703,11 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
           ((a_sbo >> 4) & 0x3FFFu) | (1u << 14) | ((uint32_t)a_swz << 29);
       constexpr uint32_t b_desc_hi =
           ((b_sbo >> 4) & 0x3FFFu) | (1u << 14) | ((uint32_t)b_swz << 29);
-      constexpr uint32_t a_desc_lo0 = ((16u >> 4) & 0x3FFFu) << 16;
-      constexpr uint32_t b_desc_lo0 = ((b_lbo >> 4) & 0x3FFFu) << 16;
+      constexpr uint32_t a_desc_lo0 = (((A_MN ? b_lbo : 16u) >> 4) & 0x3FFFu) << 16;
+      constexpr uint32_t b_desc_lo0 = (((B_MN ? b_lbo : 16u) >> 4) & 0x3FFFu) << 16;
+      // 16-byte units from one k16 step to the next: 32 bytes along a K-major row, or 16 rows of
+      // 128 bytes of an MN-major atom.
+      constexpr uint32_t a_step = A_MN ? 128 : 2, b_step = B_MN ? 128 : 2;
       auto desc = [](uint32_t lo, uint32_t hi) -> uint64_t {
         uint64_t d;
         asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
@@ -734,14 +758,14 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
             for (int j0 = 0; j0 < BK / 16; j0 += G) {
 #pragma unroll
               for (int j = j0; j < j0 + G; ++j) {
-                const uint64_t da = desc(a_lo + 2 * j, a_desc_hi);
-                const uint64_t db = desc(b_hi + 128 * j, b_desc_hi);
+                const uint64_t da = desc(a_lo + a_step * j, a_desc_hi);
+                const uint64_t db = desc(b_hi + b_step * j, b_desc_hi);
                 mma(d_x, da, db, (x_fresh && first_kb && j == 0) ? 0u : 1u);
               }
 #pragma unroll
               for (int j = j0; j < j0 + G; ++j) {
-                const uint64_t da = desc(a_hi + 2 * j, a_desc_hi);
-                const uint64_t db = desc(b_lo + 128 * j, b_desc_hi);
+                const uint64_t da = desc(a_hi + a_step * j, a_desc_hi);
+                const uint64_t db = desc(b_lo + b_step * j, b_desc_hi);
                 mma(d_x, da, db, 1u);
               }
             }
@@ -760,8 +784,8 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
             const uint32_t b_hi = b_desc_lo0 + ((st + Cfg::B_OFF) >> 4);
 #pragma unroll
             for (int j = 0; j < BK / 16; ++j) {
-              const uint64_t da = desc(a_hi + 2 * j, a_desc_hi);
-              const uint64_t db = desc(b_hi + 128 * j, b_desc_hi);
+              const uint64_t da = desc(a_hi + a_step * j, a_desc_hi);
+              const uint64_t db = desc(b_hi + b_step * j, b_desc_hi);
               mma(d_main, da, db, (first_kb && j == 0) ? 0u : 1u);
             }
             // the stage may be refilled once these MMAs retire
@@ -793,11 +817,11 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
                     for (int j0 = 0; j0 < BK / 16; j0 += G) {
 #pragma unroll
                       for (int j = j0; j < j0 + G; ++j)
-                        mma(d, desc(a_lo + 2 * j, a_desc_hi), desc(b_hi + 128 * j, b_desc_hi),
+                        mma(d, desc(a_lo + a_step * j, a_desc_hi), desc(b_hi + b_step * j, b_desc_hi),
                             (l == 0 && j == 0) ? 0u : 1u);
 #pragma unroll
                       for (int j = j0; j < j0 + G; ++j)
-                        mma(d, desc(a_hi + 2 * j, a_desc_hi), desc(b_lo + 128 * j, b_desc_hi), 1u);
+                        mma(d, desc(a_hi + a_step * j, a_desc_hi), desc(b_lo + b_step * j, b_desc_hi), 1u);
                     }
                   }
                 }
@@ -809,8 +833,8 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
                   const uint32_t b_hi = b_desc_lo0 + ((stv[l] + Cfg::B_OFF) >> 4);
 #pragma unroll
                   for (int j = 0; j < BK / 16; ++j) {
-                    const uint64_t da = desc(a_hi + 2 * j, a_desc_hi);
-                    const uint64_t db = desc(b_hi + 128 * j, b_desc_hi);
+                    const uint64_t da = desc(a_hi + a_step * j, a_desc_hi);
+                    const uint64_t db = desc(b_hi + b_step * j, b_desc_hi);
                     if (l == 0 && j == 0) umma_f16_ss_scale_d_rt(scale_exp, d, da, db, idesc, PAIR);
                     else mma(d, da, db, 1u);
                   }
@@ -947,21 +971,31 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
             // The leader announces the bytes of both CTAs' copies; the peer's copies may land first
             // (the phase cannot complete before the leader's arrival).
             if (leader) mbar_arrive_expect_tx(&ring_full[s], Cfg::STAGE_BYTES * (PAIR ? 2 : 1));
-            // A tiles: box {BK (k), 128 rows}.  B tiles: boxes {64 (n), BK (k rows)}.
-            load(st, &tmA0, k0, tm * kBM, &ring_full[s]);
-            uint8_t* bdst = st + Cfg::A_TILE;
-            if (NTERMS == 3) {
-              load(st + Cfg::A_TILE, &tmA1, k0, tm * kBM, &ring_full[s]);
-              bdst = st + 2 * Cfg::A_TILE;
-            }
+            // A tiles: box {BK (k), 128 rows}, or boxes {64 (m), BK (k rows)} where A's rows are
+            // contiguous.  B tiles: boxes {64 (n), BK (k rows)}, or one box {BK (k), columns}.
+            auto load_a = [&](uint8_t* dst, const CUtensorMap* map) {
+              if constexpr (A_MN) {
 #pragma unroll
-            for (int a = 0; a < Cfg::BN_CTA / 64; ++a)
-              load(bdst + a * (BK * 128), &tmB0, n0 + a * 64, k0, &ring_full[s]);
-            if (NTERMS == 3) {
+                for (int a = 0; a < kBM / 64; ++a)
+                  load(dst + a * (BK * 128), map, tm * kBM + a * 64, k0, &ring_full[s]);
+              } else {
+                load(dst, map, k0, tm * kBM, &ring_full[s]);
+              }
+            };
+            auto load_b = [&](uint8_t* dst, const CUtensorMap* map) {
+              if constexpr (B_MN) {
 #pragma unroll
-              for (int a = 0; a < Cfg::BN_CTA / 64; ++a)
-                load(bdst + Cfg::B_TILE + a * (BK * 128), &tmB1, n0 + a * 64, k0, &ring_full[s]);
-            }
+                for (int a = 0; a < Cfg::BN_CTA / 64; ++a)
+                  load(dst + a * (BK * 128), map, n0 + a * 64, k0, &ring_full[s]);
+              } else {
+                load(dst, map, k0, n0, &ring_full[s]);
+              }
+            };
+            load_a(st, &tmA0);
+            if (NTERMS == 3) load_a(st + Cfg::A_TILE, &tmA1);
+            uint8_t* bdst = st + (NTERMS == 3 ? 2 : 1) * Cfg::A_TILE;
+            load_b(bdst, &tmB0);
+            if (NTERMS == 3) load_b(bdst + Cfg::B_TILE, &tmB1);
           }
         }
       }
@@ -1122,25 +1156,6 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
     if (PAIR) tmem_dealloc_pair(tmem_base, kTmemCols);
     else tmem_dealloc(tmem_base, kTmemCols);
   }
-}
-
-// Diagnostic kernel (one CTA): thread 0 waits, with the bounded wait that every role of the
-// kernels above uses, on an mbarrier that nothing ever signals, so the wait runs into its clock
-// limit, publishes kErrProbeWait in the error word and raises the CTA's abort flag; the second
-// warp waits on the same barrier with the full limit and must leave as soon as the flag is up.
-// Lets a test walk the path device wait -> error word -> host status without making any real
-// pipeline fail.  `limit` is a few thousand clocks.
-__global__ void wait_timeout_probe_kernel(unsigned int* err, long long limit) {
-  __shared__ uint64_t bar;
-  __shared__ uint32_t abort_flag;
-  if (threadIdx.x == 0) {
-    mbar_init(&bar, 1);
-    abort_flag = 0u;
-    fence_mbar_init();
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) mbar_wait_bounded(&bar, 0, &abort_flag, err, kErrProbeWait, 0u, limit);
-  if (threadIdx.x == 32) mbar_wait_bounded(&bar, 0, &abort_flag, err, kErrProbeWait + 1, 0u, kWaitLimitClocks);
 }
 
 }  // namespace sgc

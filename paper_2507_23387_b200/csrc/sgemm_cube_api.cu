@@ -10,97 +10,12 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
-#include "../../include/sgemm_cube.h"
+#include "ctx.cuh"
 #include "gemm_tc.cuh"
+#include "probe_kernel.cuh"
 #include "split_kernel.cuh"
 
 namespace {
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = true;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-  }
-  ~DeviceGuard() {
-    if (prev >= 0) cudaSetDevice(prev);
-  }
-};
-
-inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-}  // namespace
-
-struct sgemm_cube_ctx {
-  int device = 0;
-  int sm_count = 0;
-  unsigned int* err_dev = nullptr;   // [0] error word; [4..13] scratch of sgemm_cube_exponent_window;
-                                     // [16..19] clocks and nanoseconds of the last timed tensor-core kernel
-  bool err_dev_has_clock = false;    // false for the static entry point's single error word
-  void* ws = nullptr;          // unfused path: FP16 words of A and B, D_hh, D_x
-  size_t ws_bytes = 0;
-  void* part_ws = nullptr;     // split-K partial sums
-  size_t part_ws_bytes = 0;
-  int split_k = 1;             // 1: split the k range of few-tile problems over idle SMs; 0: never
-  void* host_ws = nullptr;     // host-buffer path: device copies of A, B, C
-  size_t host_ws_bytes = 0;
-  long long launches = 0;
-  int kblock_termwise = 128;
-  int kblock_elementwise = 64;
-  int cta_pair = 2;            // 0/1: never/always 2-CTA clusters (cta_group::2); 2: see use_pair
-  int strategy = 0;            // sgemm_cube: 0 auto, 1 fused kernel, 2 split kernel + 3-product kernel
-  int time_kernel = 0;         // record events around the tensor-core kernel of sgemm_cube
-  static constexpr int kTimedCalls = 128;           // event pairs kept (most recent calls)
-  cudaEvent_t ev_ring[2 * kTimedCalls] = {};
-  long long ev_calls = 0;      // timed calls since timing was switched on or last averaged
-  // host-buffer path: copy streams and events of the panel pipeline (created on first use)
-  static constexpr int kMaxPanels = 32;
-  cudaStream_t s_in = nullptr, s_out = nullptr;
-  cudaEvent_t ev_start = nullptr, ev_b = nullptr, ev_out = nullptr;
-  cudaEvent_t ev_a[kMaxPanels] = {}, ev_c[kMaxPanels] = {};
-  int max_pair_clusters[3] = {0, 0, 0};   // co-resident 2-CTA clusters: <1,false>, <3,false>, <3,true>
-  EncodeTiledFn encode = nullptr;
-  bool attrs_set = false;
-};
-
-namespace {
-
-int grow(void** buf, size_t* have, size_t want) {
-  if (*have >= want) return SGEMM_CUBE_OK;
-  if (*buf) {
-    if (cudaFree(*buf) != cudaSuccess) return SGEMM_CUBE_CUDA_ERROR;
-    *buf = nullptr;
-    *have = 0;
-  }
-  if (cudaMalloc(buf, want) != cudaSuccess) {
-    cudaGetLastError();
-    *buf = nullptr;
-    return SGEMM_CUBE_ALLOC_FAILED;
-  }
-  *have = want;
-  return SGEMM_CUBE_OK;
-}
-
-// 2-D tensor map over a row-major matrix: dims {inner, outer}, row pitch in bytes.
-int make_map(sgemm_cube_ctx* h, CUtensorMap* map, CUtensorMapDataType dt, size_t elem, const void* base,
-             uint64_t inner, uint64_t outer, uint64_t ld_elems, uint32_t box_inner,
-             uint32_t box_outer, CUtensorMapSwizzle swz) {
-  cuuint64_t dims[2] = {inner, outer};
-  cuuint64_t strides[1] = {ld_elems * elem};
-  cuuint32_t box[2] = {box_inner, box_outer};
-  cuuint32_t estr[2] = {1, 1};
-  CUresult r = h->encode(map, dt, 2, const_cast<void*>(base), dims, strides, box, estr,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? SGEMM_CUBE_OK : SGEMM_CUBE_CUDA_ERROR;
-}
 
 int set_kernel_attrs(sgemm_cube_ctx* h) {
   if (h->attrs_set) return SGEMM_CUBE_OK;
