@@ -152,32 +152,40 @@ def _dev(t, dtype):
     return ctypes.c_void_p(t.data_ptr())
 
 
-def _vector(t, n, dtype=torch.float32):
+# The helpers below run several times per call of an operator whose kernel takes a few microseconds, so they ask
+# a tensor for as little as they can.
+def _vector(t, n, device, dtype=torch.float32):
     """Pointer of an optional contiguous vector of n elements."""
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == dtype and t.numel() == n and t.is_contiguous(), "contiguous %s vector" % dtype
+    assert t.dtype is dtype and t.numel() == n and t.get_device() == device and t.is_contiguous(), \
+        "expected a contiguous %s vector of %d elements on cuda:%d" % (dtype, n, device)
     return t.data_ptr()
 
 
-def _matrix(t, rows, cols, dtype=torch.float32):
+def _matrix(t, shape, device, dtype=torch.float32):
     """(pointer, leading dimension) of an optional row-major matrix."""
     if t is None:
         return None, 0
-    assert t.is_cuda and t.dtype == dtype and t.shape == (rows, cols), "expected %s (%d, %d)" % (dtype, rows, cols)
-    return t.data_ptr(), _ld(t)
+    assert t.dtype is dtype and t.shape == shape and t.get_device() == device, \
+        "expected a %s tensor %s on cuda:%d" % (dtype, tuple(shape), device)
+    rows, cols = shape
+    ld, inner = t.stride()
+    assert inner == 1 or cols <= 1, "row-major 2-D tensor expected"
+    return t.data_ptr(), (ld if rows > 1 else max(ld, cols))
 
 
-def _operand(t):
+def _operand(t, device):
     """An FP32 tensor or a PackedMatrix as the C struct."""
     if isinstance(t, PackedMatrix):
         return t.operand
-    assert t.is_cuda and t.dtype == torch.float32, "expected a CUDA tensor of dtype float32 or a PackedMatrix"
-    return _Operand(t.data_ptr(), _ld(t), None, None, 0, None)
+    p, ld = _matrix(t, t.shape, device)
+    return _Operand(p, ld, None, None, 0, None)
 
 
-def _raw_stream(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+def _raw_stream(stream, device):
+    """cudaStream_t of a stream, or of the device's current one."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def sgemm_cube_unfused_static(A, B, C, scale_exp=11, stream=None):
@@ -355,86 +363,97 @@ class Handle:
 
     def sgemm_cube_pack(self, X, packed, stream=None):
         """Scale, split and store X in a PackedMatrix of its shape."""
+        dev = self.device
         rows, cols = X.shape
         assert packed.shape == (rows, cols)
-        x, ldx = _matrix(X, rows, cols)
+        x, ldx = _matrix(X, (rows, cols), dev)
         o = packed.operand
         _check(load().sgemm_cube_pack(self._h, rows, cols, x, ldx, o.hi_dev, o.lo_dev, o.ld16, o.exp_dev,
-                                      _raw_stream(stream)), "sgemm_cube_pack")
+                                      _raw_stream(stream, dev)), "sgemm_cube_pack")
 
     def sgemm_cube_linear(self, X, W, Y, bias=None, residual=None, activation=ACT_NONE, preact=None,
                           weight_layout=WEIGHT_KN, stream=None):
         """Y = act(X W + bias) + residual; X and W are FP32 tensors or PackedMatrix objects."""
+        dev = self.device
         (M, K), (a, b) = X.shape, W.shape
         k2, N = (b, a) if weight_layout == WEIGHT_NK else (a, b)
         assert K == k2, "X and W do not fit"
-        y, ldy = _matrix(Y, M, N)
-        r, ldr = _matrix(residual, M, N)
-        z, ldz = _matrix(preact, M, N)
-        _check(load().sgemm_cube_linear(self._h, M, N, K, _operand(X), _operand(W), weight_layout, _vector(bias, N),
-                                        r, ldr, activation, y, ldy, z, ldz, _raw_stream(stream)),
+        y, ldy = _matrix(Y, (M, N), dev)
+        r, ldr = _matrix(residual, (M, N), dev)
+        z, ldz = _matrix(preact, (M, N), dev)
+        _check(load().sgemm_cube_linear(self._h, M, N, K, _operand(X, dev), _operand(W, dev), weight_layout, _vector(bias, N, dev),
+                                        r, ldr, activation, y, ldy, z, ldz, _raw_stream(stream, dev)),
                "sgemm_cube_linear")
 
     def sgemm_cube_linear_backward(self, dY, X, W, dX=None, dW=None, dbias=None, preact=None,
                                    activation=ACT_NONE, weight_layout=WEIGHT_KN, stream=None):
         """Gradients of sgemm_cube_linear into whichever of dX, dW and dbias are given."""
+        dev = self.device
         (M, K), (a, b) = X.shape, W.shape
         k2, N = (b, a) if weight_layout == WEIGHT_NK else (a, b)
         assert K == k2, "X and W do not fit"
-        g, lddy = _matrix(dY, M, N)
-        z, ldz = _matrix(preact, M, N)
-        dx, lddx = _matrix(dX, M, K)
-        dw, lddw = _matrix(dW, a, b)
-        _check(load().sgemm_cube_linear_backward(self._h, M, N, K, g, lddy, z, ldz, activation, _operand(X),
-                                                 _operand(W), weight_layout, dx, lddx, dw, lddw, _vector(dbias, N),
-                                                 _raw_stream(stream)), "sgemm_cube_linear_backward")
+        g, lddy = _matrix(dY, (M, N), dev)
+        z, ldz = _matrix(preact, (M, N), dev)
+        dx, lddx = _matrix(dX, (M, K), dev)
+        dw, lddw = _matrix(dW, (a, b), dev)
+        _check(load().sgemm_cube_linear_backward(self._h, M, N, K, g, lddy, z, ldz, activation, _operand(X, dev),
+                                                 _operand(W, dev), weight_layout, dx, lddx, dw, lddw, _vector(dbias, N, dev),
+                                                 _raw_stream(stream, dev)), "sgemm_cube_linear_backward")
 
     def sgemm_cube_layer_norm(self, X, Y, weight=None, bias=None, eps=1e-5, mean=None, rstd=None, stream=None):
         """Layer normalisation of the rows of X (float32, float16 or bfloat16) into Y."""
-        rows, cols = X.shape
-        x, ldx = _matrix(X, rows, cols, X.dtype)
-        y, ldy = _matrix(Y, rows, cols, X.dtype)
-        _check(load().sgemm_cube_layer_norm(self._h, rows, cols, _DTYPE[X.dtype], x, ldx, _vector(weight, cols),
-                                            _vector(bias, cols), eps, y, ldy, _vector(mean, rows),
-                                            _vector(rstd, rows), _raw_stream(stream)), "sgemm_cube_layer_norm")
+        dev = self.device
+        shape, dtype = X.shape, X.dtype
+        rows, cols = shape
+        x, ldx = _matrix(X, shape, dev, dtype)
+        y, ldy = _matrix(Y, shape, dev, dtype)
+        _check(load().sgemm_cube_layer_norm(self._h, rows, cols, _DTYPE[dtype], x, ldx, _vector(weight, cols, dev),
+                                            _vector(bias, cols, dev), eps, y, ldy, _vector(mean, rows, dev),
+                                            _vector(rstd, rows, dev), _raw_stream(stream, dev)), "sgemm_cube_layer_norm")
 
     def sgemm_cube_layer_norm_backward(self, dY, X, mean, rstd, dX=None, weight=None, dweight=None, dbias=None,
                                        stream=None):
         """Gradients of sgemm_cube_layer_norm into whichever of dX, dweight and dbias are given."""
-        rows, cols = X.shape
-        g, lddy = _matrix(dY, rows, cols, X.dtype)
-        x, ldx = _matrix(X, rows, cols, X.dtype)
-        dx, lddx = _matrix(dX, rows, cols, X.dtype)
-        _check(load().sgemm_cube_layer_norm_backward(self._h, rows, cols, _DTYPE[X.dtype], g, lddy, x, ldx,
-                                                     _vector(weight, cols), _vector(mean, rows), _vector(rstd, rows),
-                                                     dx, lddx, _vector(dweight, cols), _vector(dbias, cols),
-                                                     _raw_stream(stream)), "sgemm_cube_layer_norm_backward")
+        dev = self.device
+        shape, dtype = X.shape, X.dtype
+        rows, cols = shape
+        g, lddy = _matrix(dY, shape, dev, dtype)
+        x, ldx = _matrix(X, shape, dev, dtype)
+        dx, lddx = _matrix(dX, shape, dev, dtype)
+        _check(load().sgemm_cube_layer_norm_backward(self._h, rows, cols, _DTYPE[dtype], g, lddy, x, ldx,
+                                                     _vector(weight, cols, dev), _vector(mean, rows, dev), _vector(rstd, rows, dev),
+                                                     dx, lddx, _vector(dweight, cols, dev), _vector(dbias, cols, dev),
+                                                     _raw_stream(stream, dev)), "sgemm_cube_layer_norm_backward")
 
     def sgemm_cube_token_logprobs(self, logits, tokens, logp, entropy=None, stats=None, top_logp=None,
                                   top_index=None, scale=1.0, stream=None):
         """Log probabilities of tokens (int64, negative: no target), entropy, softmax statistics (rows, 2)
         and the top_logp.shape[1] most likely alternatives of every row."""
-        rows, vocab = logits.shape
-        x, ld = _matrix(logits, rows, vocab, logits.dtype)
+        dev = self.device
+        shape, dtype = logits.shape, logits.dtype
+        rows, vocab = shape
+        x, ld = _matrix(logits, shape, dev, dtype)
         assert (top_logp is None) == (top_index is None)
         k = 0 if top_logp is None else top_logp.shape[1]
-        _check(load().sgemm_cube_token_logprobs(self._h, rows, vocab, _DTYPE[logits.dtype], x, ld,
-                                                _vector(tokens, rows, torch.int64), scale, _vector(logp, rows),
-                                                _vector(entropy, rows), _vector(stats, 2 * rows), k,
-                                                _vector(top_logp, rows * k), _vector(top_index, rows * k, torch.int64),
-                                                _raw_stream(stream)), "sgemm_cube_token_logprobs")
+        _check(load().sgemm_cube_token_logprobs(self._h, rows, vocab, _DTYPE[dtype], x, ld,
+                                                _vector(tokens, rows, dev, torch.int64), scale, _vector(logp, rows, dev),
+                                                _vector(entropy, rows, dev), _vector(stats, 2 * rows, dev), k,
+                                                _vector(top_logp, rows * k, dev), _vector(top_index, rows * k, dev, torch.int64),
+                                                _raw_stream(stream, dev)), "sgemm_cube_token_logprobs")
 
     def sgemm_cube_token_logprobs_backward(self, logits, tokens, stats, dlogits, dlogp=None, entropy=None,
                                            dentropy=None, scale=1.0, stream=None):
         """Gradient of the logits for the gradients of logp and entropy; dlogits may be logits."""
-        rows, vocab = logits.shape
-        x, ld = _matrix(logits, rows, vocab, logits.dtype)
-        dx, lddl = _matrix(dlogits, rows, vocab, logits.dtype)
-        _check(load().sgemm_cube_token_logprobs_backward(self._h, rows, vocab, _DTYPE[logits.dtype], x, ld,
-                                                         _vector(tokens, rows, torch.int64), scale,
-                                                         _vector(stats, 2 * rows), _vector(entropy, rows),
-                                                         _vector(dlogp, rows), _vector(dentropy, rows), dx, lddl,
-                                                         _raw_stream(stream)), "sgemm_cube_token_logprobs_backward")
+        dev = self.device
+        shape, dtype = logits.shape, logits.dtype
+        rows, vocab = shape
+        x, ld = _matrix(logits, shape, dev, dtype)
+        dx, lddl = _matrix(dlogits, shape, dev, dtype)
+        _check(load().sgemm_cube_token_logprobs_backward(self._h, rows, vocab, _DTYPE[dtype], x, ld,
+                                                         _vector(tokens, rows, dev, torch.int64), scale,
+                                                         _vector(stats, 2 * rows, dev), _vector(entropy, rows, dev),
+                                                         _vector(dlogp, rows, dev), _vector(dentropy, rows, dev), dx, lddl,
+                                                         _raw_stream(stream, dev)), "sgemm_cube_token_logprobs_backward")
 
     def sgemm_cube_launch_count(self) -> int:
         return int(load().sgemm_cube_launch_count(self._h))

@@ -35,13 +35,16 @@ struct sgemm_cube_ctx {
   int sm_count = 0;
   unsigned int* err_dev = nullptr;   // [0] error word; [4..13] scratch of sgemm_cube_exponent_window;
                                      // [16..19] clocks and nanoseconds of the last timed tensor-core kernel;
-                                     // [20..27] ranges and exponents of the linear layer's packing
+                                     // [20..27] ranges and exponents of the linear layer's packing;
+                                     // [32..32 + sm_count) finished slices of its split-K tiles
   bool err_dev_has_clock = false;    // false for the static entry point's single error word
   void* ws = nullptr;          // unfused path: FP16 words of A and B, D_hh, D_x
   size_t ws_bytes = 0;
   void* part_ws = nullptr;     // split-K partial sums
   size_t part_ws_bytes = 0;
   int split_k = 1;             // 1: split the k range of few-tile problems over idle SMs; 0: never
+  void* tile_ws = nullptr;     // linear forms: two 128 x 256 tiles for every block of the tensor-core kernel
+  size_t tile_ws_bytes = 0;
   void* host_ws = nullptr;     // host-buffer path: device copies of A, B, C
   size_t host_ws_bytes = 0;
   long long launches = 0;

@@ -3,6 +3,8 @@
 #pragma once
 
 #include <cstdint>
+#include <type_traits>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -77,31 +79,57 @@ struct Elem<__nv_bfloat16> {
 // Which columns of a row a thread of a group of `threads` holds.  VEC: 16-byte vectors, vector i at
 // (i * threads + t) * kVec; otherwise (rows that are not 16-byte aligned) single elements, element i at
 // i * threads + t.  Either way a warp's accesses are contiguous.  PT elements a thread, columns past
-// `cols` read as `fill`.
+// `cols` read as zero.
+// A row is asked for (fetch) before it is needed (get): the raw words wait in registers.
 template <typename T, int PT, bool VEC>
-__device__ __forceinline__ void load_row(const T* __restrict__ row, int cols, int t, int threads, float fill,
-                                         float (&v)[PT]) {
-  if constexpr (VEC) {
-    constexpr int V = Elem<T>::kVec;
-    uint4 raw[PT / V];
+struct RowRegs {
+  static constexpr int kWords = VEC ? PT / Elem<T>::kVec : PT;
+  typename std::conditional<VEC, uint4, T>::type raw[kWords];
+  __device__ __forceinline__ void fetch(const T* row, int cols, int t, int threads) {
 #pragma unroll
-    for (int i = 0; i < PT / V; ++i) {
-      const int c = (i * threads + t) * V;
-      raw[i] = c < cols ? __ldcs(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (VEC) {
+        const int c = (i * threads + t) * Elem<T>::kVec;
+        raw[i] = c < cols ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0, 0, 0, 0);
+      } else {
+        const int c = i * threads + t;
+        raw[i] = c < cols ? row[c] : Elem<T>::put(0.f);
+      }
     }
+  }
+  __device__ __forceinline__ void get(float (&v)[PT]) const {
 #pragma unroll
-    for (int i = 0; i < PT / V; ++i) {
-      float e[V];
-      Elem<T>::unpack(raw[i], e);
-      const bool in = (i * threads + t) * V < cols;
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (VEC) {
+        constexpr int V = Elem<T>::kVec;
+        float e[V];
+        Elem<T>::unpack(raw[i], e);
 #pragma unroll
-      for (int q = 0; q < V; ++q) v[i * V + q] = in ? e[q] : fill;
+        for (int q = 0; q < V; ++q) v[i * V + q] = e[q];
+      } else {
+        v[i] = Elem<T>::get(raw[i]);
+      }
     }
-  } else {
+  }
+};
+// The thread's entries of a vector of FP32 parameters, `fill` past the end or where there is none.  The vector is
+// read in 16-byte pieces where the rows are and it is aligned itself.
+template <typename T, int PT, bool VEC>
+__device__ __forceinline__ void load_params(const float* p, float fill, int cols, int t, int threads, float (&v)[PT]) {
+  constexpr int V = VEC ? Elem<T>::kVec : 1;
+  const bool vec = VEC && (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
 #pragma unroll
-    for (int i = 0; i < PT; ++i) {
-      const int c = i * threads + t;
-      v[i] = c < cols ? Elem<T>::get(row[c]) : fill;
+  for (int i = 0; i < PT / V; ++i) {
+    const int c = (i * threads + t) * V;
+    if (VEC && p && vec && c < cols) {
+#pragma unroll
+      for (int q = 0; q < V; q += 4) {
+        const float4 f = __ldg(reinterpret_cast<const float4*>(p + c + q));
+        v[i * V + q] = f.x; v[i * V + q + 1] = f.y; v[i * V + q + 2] = f.z; v[i * V + q + 3] = f.w;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < V; ++q) v[i * V + q] = p && c + q < cols ? __ldg(p + c + q) : fill;
     }
   }
 }

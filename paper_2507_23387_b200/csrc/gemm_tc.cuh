@@ -84,6 +84,8 @@ enum : unsigned int {
   kErrConvEmptyWait = 0x106,
   kErrConvFullWait = 0x107,
   kErrRelayWait = 0x108,
+  kErrTileEmptyWait = 0x109,
+  kErrTileFullWait = 0x10A,
   kErrProbeWait = 0x1F0,
 };
 
@@ -305,11 +307,23 @@ struct TcLinearParams : TcGemmParams {
 template <int FORM>
 using TcParams = std::conditional_t<FORM == kFormProduct, TcGemmParams, TcLinearParams>;
 
+// Linear forms: warps 10-15 store.  The accumulate warps hold 128 sums a thread and have no registers left
+// for bias, activation and residual, and while they work on those the tensor core waits; so they put a
+// finished tile into scratch (two tiles of 128 KB a block, which stay in L2) and go on with the next
+// product, and six warps that have nothing else to do carry it to Y.  With split-K the scratch holds every
+// slice's tile, and the block that finishes a tile's last slice adds them up, in slice order.
+constexpr int kFirstStoreWarp = 10;
+constexpr int kNumStoreWarps = 6;
+constexpr int kLinearThreads = (kFirstStoreWarp + kNumStoreWarps) * 32;
+constexpr int kTileFloats = kBM * kBN;
+template <bool FUSED, int FORM>
+constexpr int tc_threads() { return FUSED ? kFusedThreads : (FORM == kFormProduct ? kTcThreads : kLinearThreads); }
+
 // REORD: the reordered elementwise order (p.order == 2) has its own instantiations, so that its
 // accumulate path (two chunk buffers live at once) does not weigh on the register allocation of
 // the termwise / elementwise kernels.
 template <int NTERMS, bool FUSED, bool PAIR, bool REORD = false, int FORM = kFormProduct>
-__global__ void __launch_bounds__(FUSED ? kFusedThreads : kTcThreads, 1)
+__global__ void __launch_bounds__(tc_threads<FUSED, FORM>(), 1)
 tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmA1,
                const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmB1,
                const TcParams<FORM> p) {
@@ -345,12 +359,18 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
   constexpr int kFusedBars = FUSED ? STAGES : 0;
   uint64_t* full32_bar = bars + 2 * STAGES + 5;              // [STAGES]  FUSED: TMA -> converters
   uint64_t* conv_bar = bars + 2 * STAGES + 5 + kFusedBars;   // [STAGES]  FUSED: converters -> relay
-  uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 5 + 2 * kFusedBars);
+  constexpr int kTileBars = FORM == kFormProduct ? 0 : 2;
+  uint64_t* tile_full_bar = bars + 2 * STAGES + 5 + 2 * kFusedBars;   // [2]  accumulate -> store warps
+  uint64_t* tile_empty_bar = tile_full_bar + kTileBars;               // [2]  store -> accumulate warps
+  uint64_t* decided_bar = tile_empty_bar + kTileBars;                 // [2]  split-K: whether this block was last
+  constexpr int kNumBars = 2 * STAGES + 5 + 2 * kFusedBars + 3 * kTileBars;
+  uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
+  volatile uint32_t* was_last = tmem_base_slot + 2;                   // [2]
   volatile uint32_t* abort_flag = tmem_base_slot + 1;
   // PAIR: a wait that gives up also raises the peer's flag (shared::cluster address of the same slot)
   const uint32_t peer_abort =
       PAIR ? mapa_u32(smem_u32(tmem_base_slot + 1), cta_rank ^ 1u) : 0u;
-  static_assert((2 * STAGES + 5 + 2 * kFusedBars) * 8 + 8 <= 256, "barrier block");
+  static_assert(kNumBars * 8 + 16 <= 256, "barrier block");
   uint8_t* store_staging = smem + Cfg::RING_BYTES + 256;   // epilogue transposition buffers
 
   const int warp = threadIdx.x >> 5;
@@ -383,6 +403,11 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
     for (int s = 0; s < kFusedBars; ++s) {
       mbar_init(&full32_bar[s], 1);
       mbar_init(&conv_bar[s], kNumConvWarps);
+    }
+    for (int s = 0; s < kTileBars; ++s) {
+      mbar_init(&tile_full_bar[s], kNumEpiWarps);
+      mbar_init(&tile_empty_bar[s], kNumStoreWarps);
+      mbar_init(&decided_bar[s], 1);
     }
     mbar_init(drain_bar, 1);
     *abort_flag = 0u;
@@ -422,6 +447,10 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
     kb0 = (ksplit > 1) ? slice * p.kslice_blocks : 0;
     kb1 = (ksplit > 1) ? min(num_kb, kb0 + p.kslice_blocks) : num_kb;
   };
+  // Linear forms: where the sums of a unit wait (slice 0 of the tile, for the block that adds the slices).
+  [[maybe_unused]] auto scratch_tile = [&](int unit, int slice, uint32_t t) -> long long {
+    return ksplit > 1 ? (long long)(unit % num_tiles) * ksplit + slice : (long long)blockIdx.x * 2 + t;
+  };
   const int chunk = p.kchunk_blocks;                           // stages per k-block g
   // Reordered elementwise order, fast form: a k-block's value P_x / s_f + P_hh is formed inside one
   // TMEM region (the correction products first, then the first hi*hi MMA scales the accumulator
@@ -437,7 +466,8 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
   // that the code below it is compiled against the new limit.
   if (warp < kNumEpiWarps) {
     if (FUSED) setmaxnreg_inc<SGC_FUSED_EPI_REGS>();
-    else setmaxnreg_inc<208>();       // 384 threads x 168: 256 x 208 + 128 x 56 fits the pool
+    else if (FORM == kFormProduct) setmaxnreg_inc<208>();   // 384 threads x 168: 256 x 208 + 128 x 56 fits the pool
+    else setmaxnreg_inc<168>();       // 512 threads x 128: 256 x 168 + 256 x 88 is the pool
     // ------------------------------------------------------------------ accumulate / epilogue
     const int quarter = warp & 3;                 // TMEM lanes 32*quarter .. +31 (warp id mod 4)
     const int half = warp >> 2;                   // columns [128*half, 128*half + 128)
@@ -445,11 +475,15 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
     const bool vec_ok = ((reinterpret_cast<uintptr_t>(p.D) & 15) == 0) && ((p.ldd & 3) == 0);
     uint32_t drains[2] = {0, 0};
     uint32_t gchunk = 0;
+    [[maybe_unused]] uint32_t tiles_done = 0;
     bool ok = true;
     float S[128];
     // TMEM is read 64 columns at a time (fewer, longer loads: the tensor pipe is held up for as
-    // long as a drain lasts, and the load latency is most of that), 16 where registers are tight.
-    constexpr int GW = FUSED ? SGC_FUSED_GW : 64;
+    // long as a drain lasts, and the load latency is most of that), 16 where registers are tight: in the
+    // linear forms, whose store warps need theirs (with 64 registers instead of 88 they spilled, and
+    // 8192 x 8192 x 1024 with bias, gelu, residual and z took 866 us instead of 531; the shorter loads
+    // cost the plain product nothing that can be measured, 311 and 317 us).
+    constexpr int GW = FUSED ? SGC_FUSED_GW : (FORM == kFormProduct ? 64 : 16);
     // The k-block additions as packed FP32x2 instructions (IEEE per lane: same results, half the
     // issue slots): elementwise 4096^3 338 -> 365 TFLOP/s.  Not in the fused kernel, whose
     // converter warps keep the packed pipe busy (there it measured 279 -> 246).
@@ -634,7 +668,7 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
             store16(base, ld, p.M, p.N, row, col_base + g * 16, &S[g * 16], false, accumulate);
         }
       };
-      const bool split_out = (NTERMS == 3) && !FUSED && (p.Phh != nullptr);
+      const bool split_out = FORM == kFormProduct && (NTERMS == 3) && !FUSED && (p.Phh != nullptr);
       if (split_out) store_tile(p.Phh + (long long)slice * p.pstride, p.ldp, true, 0);
       if (NTERMS == 3 && p.order == 0) {
         // Termwise: the correction stream meets the dominant stream once: here, or (split-K) in
@@ -666,15 +700,52 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
         if (split_out) store_tile(p.Px + (long long)slice * p.pstride, p.ldp, true, 0);
       }
       if (!split_out) {
-        if constexpr (FORM == kFormProduct) store_tile(p.D, p.ldd, vec_ok, (NTERMS == 1) ? p.accumulate : 0);
-        else linear_store_tile(p.ep, p.D, p.ldd, p.M, p.N, S, smem_u32(store_staging + warp * 4096),
-                               tm * kBM + quarter * 32, col_base, lane);
+        if constexpr (FORM == kFormProduct) {
+          store_tile(p.D, p.ldd, vec_ok, (NTERMS == 1) ? p.accumulate : 0);
+        } else {
+          if (p.ep.tiles == nullptr) {
+            const PowerBack back = power_back(p.ep.exp_a, p.ep.exp_b);
+#pragma unroll
+            for (int j = 0; j < 128; ++j) S[j] = back(S[j]);
+            store_tile(p.D, p.ldd, vec_ok, 0);
+          } else {
+            const int t = (int)(tiles_done & 1);
+            if (!mbar_wait_bounded(&tile_empty_bar[t], ((tiles_done >> 1) & 1) ^ 1, abort_flag, p.err,
+                                   kErrTileEmptyWait, peer_abort)) {
+              ok = false;
+              break;
+            }
+            float* tile = p.ep.tiles + scratch_tile(unit, slice, t) * kTileFloats;
+#pragma unroll
+            for (int c = 0; c < 32; ++c)
+              *tile_slot(tile, half * 32 + c, quarter * 32 + lane) =
+                  make_float4(S[4 * c], S[4 * c + 1], S[4 * c + 2], S[4 * c + 3]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&tile_full_bar[t]);
+          }
+          ++tiles_done;
+        }
       }
       SGC_TADD(8, blockIdx.x == 0 && threadIdx.x == 0);
     }
+    if constexpr (FORM != kFormProduct) {
+      if (ok && tiles_done > 0 && p.ep.tiles != nullptr) {
+        const uint32_t it = tiles_done - 1;
+        int tm, tn, kb0, kb1, slice;
+        unit_rc(first_tile + (int)it * tile_stride, tm, tn, kb0, kb1, slice);
+        // the last tile: nothing is left to overlap with, so the accumulate warps lend a hand
+        uint64_t* bar = (ksplit > 1 ? decided_bar : tile_full_bar) + (it & 1);
+        if (mbar_wait_bounded(bar, (it >> 1) & 1, abort_flag, p.err, kErrTileFullWait, peer_abort) &&
+            (ksplit == 1 || was_last[it & 1]))
+          linear_store_blocks(p.ep, p.D, p.ldd, p.M, p.N,
+                              p.ep.tiles + scratch_tile(first_tile + (int)it * tile_stride, 0, it & 1) * kTileFloats,
+                              ksplit, kTileFloats, tm * kBM, tn * kBN, kNumStoreWarps + warp,
+                              kNumStoreWarps + kNumEpiWarps, lane);
+      }
+    }
   } else if (warp == kMmaWarp) {
     if (FUSED) setmaxnreg_dec<SGC_FUSED_OTHER_REGS>();
-    else setmaxnreg_dec<56>();
+    else setmaxnreg_dec<FORM == kFormProduct ? 56 : 88>();
     // ------------------------------------------------------------------ MMA issuer
     if (lane == 0 && leader) {
       constexpr uint32_t idesc =
@@ -925,7 +996,7 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
     }
   } else if (warp == kProducerWarp) {
     if (FUSED) setmaxnreg_dec<SGC_FUSED_OTHER_REGS>();
-    else setmaxnreg_dec<56>();
+    else setmaxnreg_dec<FORM == kFormProduct ? 56 : 88>();
     // ------------------------------------------------------------------ TMA producer
     // not FUSED: FP16 operand tiles, read by the MMA thread.  FUSED: FP32 tiles of A and B, which
     // the converter warps turn into FP16 words in place (this CTA's own rows of A and its own
@@ -1129,7 +1200,40 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
       }
     }
   } else {
-    setmaxnreg_dec<56>();      // idle warps of the last warpgroup
+    setmaxnreg_dec<FORM == kFormProduct ? 56 : 88>();      // idle warps of the last warpgroup; linear forms: store warps
+    if constexpr (FORM != kFormProduct) {
+      if (p.ep.tiles != nullptr) {
+        uint32_t it = 0;
+        for (int unit = first_tile; unit < num_units; unit += tile_stride, ++it) {
+          int tm, tn, kb0, kb1, slice;
+          unit_rc(unit, tm, tn, kb0, kb1, slice);
+          const int t = (int)(it & 1);
+          if (!mbar_wait_bounded(&tile_full_bar[t], (it >> 1) & 1, abort_flag, p.err, kErrTileFullWait, peer_abort)) break;
+          bool store = true;
+          if (ksplit > 1) {
+            // The block's tile is complete: say so, and learn whether the tile's other slices are.  One
+            // thread's fences and atomic stand for the whole block (it has waited for every warp's stores).
+            if (warp == kFirstStoreWarp && lane == 0) {
+              unsigned int* count = p.ep.arrivals + unit % num_tiles;
+              __threadfence();
+              const bool last = atomicAdd(count, 1u) == (unsigned int)ksplit - 1;
+              if (last) *count = 0u;
+              __threadfence();
+              was_last[t] = last;
+              mbar_arrive(&decided_bar[t]);
+            }
+            if (!mbar_wait_bounded(&decided_bar[t], (it >> 1) & 1, abort_flag, p.err, kErrTileFullWait, peer_abort)) break;
+            store = was_last[t] != 0;
+          }
+          if (store)
+            linear_store_blocks(p.ep, p.D, p.ldd, p.M, p.N, p.ep.tiles + scratch_tile(unit, 0, t) * kTileFloats, ksplit,
+                                kTileFloats, tm * kBM, tn * kBN, warp - kFirstStoreWarp,
+                                unit + tile_stride < num_units ? kNumStoreWarps : kNumStoreWarps + kNumEpiWarps, lane);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&tile_empty_bar[t]);
+        }
+      }
+    }
   }
 
   // ---------------------------------------------------------------------- teardown

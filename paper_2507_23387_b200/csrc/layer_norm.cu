@@ -6,14 +6,15 @@
 //
 // Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx, each once.  A row
 // lives in the registers of one group of warps between its load and its store, so the second moment is
-// taken about the mean (no cancellation of squares) without a second read.
+// taken about the mean (no cancellation of squares) without a second read.  Blocks are persistent: a
+// group asks for its next row before it works on the present one, and keeps its columns' weights (forward)
+// or running sums of dw and db (backward) in registers all the way.
 #include "ctx.cuh"
 #include "elements.cuh"
 
 namespace sgc {
 
-constexpr int kFwdPT = 32;      // elements a thread holds, forward
-constexpr int kBwdPT = 16;      // backward: x, dy and two running sums for each
+constexpr int kPT = 16;         // elements of a row a thread holds
 
 // Sums over a row's group of warps.  `slot` alternates between two buffers, so one barrier a sum is enough.
 template <int WARPS, int N>
@@ -60,42 +61,44 @@ struct NormParams {
 
 // WARPS warps a row, 8 / WARPS rows a block (one for WARPS >= 8).
 template <typename T, int WARPS, bool VEC>
-__global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256) norm_forward_kernel(NormParams p) {
+__global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 3) norm_forward_kernel(NormParams p) {
   constexpr int kGroups = WARPS >= 8 ? 1 : 8 / WARPS, kThreads = WARPS * 32;
   __shared__ float buf[2][kGroups * WARPS];
   const int group = threadIdx.x / kThreads, t = threadIdx.x % kThreads, wg = t >> 5;
-  const long long row = (long long)blockIdx.x * kGroups + group;
-  if (row >= p.rows) return;                           // whole groups leave; groups meet at their own barriers
-  const int bar = kGroups == 1 ? 0 : kThreads;
-  float v[kFwdPT];
-  load_row<T, kFwdPT, VEC>(static_cast<const T*>(p.X) + row * p.ldx, p.cols, t, kThreads, 0.f, v);
-  float s[1] = {0.f};
+  const int bar = kGroups == 1 ? 0 : kThreads;         // groups meet at their own barriers
+  const float inv_n = 1.f / (float)p.cols;
+  const long long step = (long long)gridDim.x * kGroups;
+  long long row = (long long)blockIdx.x * kGroups + group;
+  if (row >= p.rows) return;
+  RowRegs<T, kPT, VEC> next;
+  next.fetch(static_cast<const T*>(p.X) + row * p.ldx, p.cols, t, kThreads);
+  float w[kPT], b[kPT];
+  load_params<T, kPT, VEC>(p.weight, 1.f, p.cols, t, kThreads, w);
+  load_params<T, kPT, VEC>(p.bias, 0.f, p.cols, t, kThreads, b);
+  for (; row < p.rows; row += step) {
+    float v[kPT];
+    next.get(v);
+    if (row + step < p.rows) next.fetch(static_cast<const T*>(p.X) + (row + step) * p.ldx, p.cols, t, kThreads);
+    float s[1] = {0.f};
 #pragma unroll
-  for (int i = 0; i < kFwdPT; ++i) s[0] += v[i];
-  group_sum<WARPS>(s, buf[0], group, wg, bar);
-  const float mean = s[0] / (float)p.cols;
-  s[0] = 0.f;
+    for (int i = 0; i < kPT; ++i) s[0] += v[i];
+    group_sum<WARPS>(s, buf[0], group, wg, bar);
+    const float mean = s[0] * inv_n;
+    s[0] = 0.f;
 #pragma unroll
-  for (int i = 0; i < kFwdPT; ++i) {
-    const float d = row_column<T, VEC>(i, t, kThreads) < p.cols ? v[i] - mean : 0.f;
-    s[0] = fmaf(d, d, s[0]);
-  }
-  group_sum<WARPS>(s, buf[1], group, wg, bar);
-  const float rstd = 1.f / sqrtf(s[0] / (float)p.cols + p.eps);
-#pragma unroll
-  for (int i = 0; i < kFwdPT; ++i) {
-    const int c = row_column<T, VEC>(i, t, kThreads);
-    float n = (v[i] - mean) * rstd;
-    if (c < p.cols) {
-      if (p.weight) n *= __ldg(p.weight + c);
-      if (p.bias) n += __ldg(p.bias + c);
+    for (int i = 0; i < kPT; ++i) {
+      v[i] -= mean;
+      s[0] = fmaf(v[i], row_column<T, VEC>(i, t, kThreads) < p.cols ? v[i] : 0.f, s[0]);
     }
-    v[i] = n;
-  }
-  store_row<T, kFwdPT, VEC>(static_cast<T*>(p.out) + row * p.ldo, p.cols, t, kThreads, v);
-  if (t == 0) {
-    if (p.mean) p.mean[row] = mean;
-    if (p.rstd) p.rstd[row] = rstd;
+    group_sum<WARPS>(s, buf[1], group, wg, bar);
+    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_n, p.eps));
+#pragma unroll
+    for (int i = 0; i < kPT; ++i) v[i] = fmaf(v[i] * rstd, w[i], b[i]);
+    store_row<T, kPT, VEC>(static_cast<T*>(p.out) + row * p.ldo, p.cols, t, kThreads, v);
+    if (t == 0) {
+      if (p.mean) p.mean[row] = mean;
+      if (p.rstd) p.rstd[row] = rstd;
+    }
   }
 }
 
@@ -130,57 +133,71 @@ __global__ void __launch_bounds__(1024) norm_forward_long_kernel(NormParams p) {
   }
 }
 
-// A persistent block walks over rows; a thread holds the same columns of every row, so its two running
-// sums for dw and db stay in registers until the end, when the block writes one partial row of each.
+// dx, and the block's partial sums of dw and db: a thread holds the same columns of every row.
 template <typename T, int WARPS, bool VEC>
-__global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256) norm_backward_kernel(NormParams p) {
+__global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 2) norm_backward_kernel(NormParams p) {
   constexpr int kGroups = WARPS >= 8 ? 1 : 8 / WARPS, kThreads = WARPS * 32;
   __shared__ float buf[2][kGroups * WARPS * 2];
   const int group = threadIdx.x / kThreads, t = threadIdx.x % kThreads, wg = t >> 5;
   const int bar = kGroups == 1 ? 0 : kThreads;
   const float inv_n = 1.f / (float)p.cols;
-  float dw[kBwdPT], db[kBwdPT];
+  const long long step = (long long)gridDim.x * kGroups;
+  long long row = (long long)blockIdx.x * kGroups + group;
+  float dw[kPT], db[kPT];
 #pragma unroll
-  for (int i = 0; i < kBwdPT; ++i) dw[i] = db[i] = 0.f;
+  for (int i = 0; i < kPT; ++i) dw[i] = db[i] = 0.f;
+  RowRegs<T, kPT, VEC> next_x, next_g;
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto fetch = [&](long long r) {
+    next_x.fetch(static_cast<const T*>(p.X) + r * p.ldx, p.cols, t, kThreads);
+    next_g.fetch(static_cast<const T*>(p.dY) + r * p.lddy, p.cols, t, kThreads);
+    next_mean = __ldg(p.mean_in + r);
+    next_rstd = __ldg(p.rstd_in + r);
+  };
+  if (row < p.rows) fetch(row);
   int slot = 0;
-  for (long long row = (long long)blockIdx.x * kGroups + group; row < p.rows; row += (long long)gridDim.x * kGroups) {
-    float x[kBwdPT], g[kBwdPT];
-    load_row<T, kBwdPT, VEC>(static_cast<const T*>(p.X) + row * p.ldx, p.cols, t, kThreads, 0.f, x);
-    load_row<T, kBwdPT, VEC>(static_cast<const T*>(p.dY) + row * p.lddy, p.cols, t, kThreads, 0.f, g);
-    const float mean = p.mean_in[row], rstd = p.rstd_in[row];
+  for (; row < p.rows; row += step) {
+    float x[kPT], g[kPT];
+    next_x.get(x);
+    next_g.get(g);
+    const float mean = next_mean, rstd = next_rstd;
+    if (row + step < p.rows) fetch(row + step);
     float s[2] = {0.f, 0.f};
+    {
+      float w[kPT];                                    // from L1: registers are short here
+      load_params<T, kPT, VEC>(p.weight, 1.f, p.cols, t, kThreads, w);
 #pragma unroll
-    for (int i = 0; i < kBwdPT; ++i) {
-      const int c = row_column<T, VEC>(i, t, kThreads);
-      x[i] = (x[i] - mean) * rstd;                     // n; columns past the end have g = 0
-      dw[i] = fmaf(g[i], x[i], dw[i]);
-      db[i] += g[i];
-      if (p.weight) g[i] *= c < p.cols ? __ldg(p.weight + c) : 0.f;
-      s[0] += g[i];
-      s[1] = fmaf(g[i], x[i], s[1]);
+      for (int i = 0; i < kPT; ++i) {
+        x[i] = (x[i] - mean) * rstd;                   // n; columns past the end have g = 0
+        dw[i] = fmaf(g[i], x[i], dw[i]);
+        db[i] += g[i];
+        g[i] *= w[i];
+        s[0] += g[i];
+        s[1] = fmaf(g[i], x[i], s[1]);
+      }
     }
     if (!p.out) continue;
     group_sum<WARPS>(s, buf[slot], group, wg, bar);
     slot ^= 1;
     const float mu = s[0] * inv_n, mun = s[1] * inv_n;
 #pragma unroll
-    for (int i = 0; i < kBwdPT; ++i) g[i] = rstd * (g[i] - mu - x[i] * mun);
-    store_row<T, kBwdPT, VEC>(static_cast<T*>(p.out) + row * p.ldo, p.cols, t, kThreads, g);
+    for (int i = 0; i < kPT; ++i) g[i] = rstd * (g[i] - mu - x[i] * mun);
+    store_row<T, kPT, VEC>(static_cast<T*>(p.out) + row * p.ldo, p.cols, t, kThreads, g);
   }
   if (!p.part) return;
   float* pw = p.part + (long long)blockIdx.x * 2 * p.cols;
   if constexpr (kGroups == 1) {
 #pragma unroll
-    for (int i = 0; i < kBwdPT; ++i) {
+    for (int i = 0; i < kPT; ++i) {
       const int c = row_column<T, VEC>(i, t, kThreads);
       if (c < p.cols) { pw[c] = dw[i]; pw[p.cols + c] = db[i]; }
     }
   } else {                                             // the block's groups first, in order
-    __shared__ float sum[2][kThreads * kBwdPT];
+    __shared__ float sum[2][kThreads * kPT];
     for (int g = 0; g < kGroups; ++g) {
       if (g == group) {
 #pragma unroll
-        for (int i = 0; i < kBwdPT; ++i) {
+        for (int i = 0; i < kPT; ++i) {
           sum[0][i * kThreads + t] = (g ? sum[0][i * kThreads + t] : 0.f) + dw[i];
           sum[1][i * kThreads + t] = (g ? sum[1][i * kThreads + t] : 0.f) + db[i];
         }
@@ -189,7 +206,7 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256) norm_backward_ke
     }
     if (group == 0) {
 #pragma unroll
-      for (int i = 0; i < kBwdPT; ++i) {
+      for (int i = 0; i < kPT; ++i) {
         const int c = row_column<T, VEC>(i, t, kThreads);
         if (c < p.cols) { pw[c] = sum[0][i * kThreads + t]; pw[p.cols + c] = sum[1][i * kThreads + t]; }
       }
@@ -245,22 +262,26 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormParams p, int row
   }
 }
 
-// Adds the blocks' partial rows in a fixed order: 32 columns a block, eight warps over the partial rows.
-// grid (ceil(cols / 32), 2): dw, db.
-__global__ void __launch_bounds__(256)
+// Adds the blocks' partial rows in a fixed order: 32 columns a block, 16 warps over the partial rows, eight
+// loads of a thread in flight.  grid (ceil(cols / 32), 2): dw, db.
+__global__ void __launch_bounds__(512)
 norm_parts_kernel(const float* __restrict__ part, int parts, int cols, float* dweight, float* dbias) {
-  __shared__ float sum[8][32];
+  __shared__ float sum[16][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + lane;
   float* out = blockIdx.y ? dbias : dweight;
   if (!out) return;
   float s = 0.f;
-  if (c < cols)
-    for (int i = warp; i < parts; i += 8) s += part[((long long)i * 2 + blockIdx.y) * cols + c];
+  if (c < cols) {
+    const float* src = part + (long long)blockIdx.y * cols + c;
+    const long long ld = 2ll * cols;
+#pragma unroll 8
+    for (int i = warp; i < parts; i += 16) s += src[i * ld];
+  }
   sum[warp][lane] = s;
   __syncthreads();
   if (warp == 0 && c < cols) {
-    for (int w = 1; w < 8; ++w) s += sum[w][lane];
+    for (int w = 1; w < 16; ++w) s += sum[w][lane];
     out[c] = s;
   }
 }
@@ -276,21 +297,36 @@ int done(sgemm_cube_ctx* h) {
   return cudaGetLastError() == cudaSuccess ? SGEMM_CUBE_OK : SGEMM_CUBE_CUDA_ERROR;
 }
 
+// Blocks of a persistent kernel: one per `groups` rows, at most what is resident at once.
+template <typename K>
+int persistent_blocks(sgemm_cube_ctx* h, K kernel, int threads, int rows, int groups, int* blocks) {
+  int per_sm = 0;
+  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0) != cudaSuccess || per_sm < 1) {
+    cudaGetLastError();
+    return SGEMM_CUBE_CUDA_ERROR;
+  }
+  const long long want = ((long long)rows + groups - 1) / groups, cap = (long long)per_sm * h->sm_count;
+  *blocks = (int)(want < cap ? want : cap);
+  return SGEMM_CUBE_OK;
+}
+
 template <typename T, int WARPS, bool VEC>
 int forward_rows(sgemm_cube_ctx* h, const NormParams& p, cudaStream_t st) {
-  constexpr int groups = WARPS >= 8 ? 1 : 8 / WARPS;
-  sgc::norm_forward_kernel<T, WARPS, VEC>
-      <<<(unsigned)((p.rows + groups - 1) / groups), WARPS > 8 ? WARPS * 32 : 256, 0, st>>>(p);
+  constexpr int groups = WARPS >= 8 ? 1 : 8 / WARPS, threads = WARPS > 8 ? WARPS * 32 : 256;
+  int blocks = 0;
+  const int rc = persistent_blocks(h, sgc::norm_forward_kernel<T, WARPS, VEC>, threads, p.rows, groups, &blocks);
+  if (rc) return rc;
+  sgc::norm_forward_kernel<T, WARPS, VEC><<<(unsigned)blocks, threads, 0, st>>>(p);
   return done(h);
 }
 template <typename T, bool VEC>
 int forward_typed(sgemm_cube_ctx* h, const NormParams& p, cudaStream_t st) {
-  if (p.cols <= 1 * 32 * sgc::kFwdPT) return forward_rows<T, 1, VEC>(h, p, st);
-  if (p.cols <= 2 * 32 * sgc::kFwdPT) return forward_rows<T, 2, VEC>(h, p, st);
-  if (p.cols <= 4 * 32 * sgc::kFwdPT) return forward_rows<T, 4, VEC>(h, p, st);
-  if (p.cols <= 8 * 32 * sgc::kFwdPT) return forward_rows<T, 8, VEC>(h, p, st);
-  if (p.cols <= 16 * 32 * sgc::kFwdPT) return forward_rows<T, 16, VEC>(h, p, st);
-  if (p.cols <= 32 * 32 * sgc::kFwdPT) return forward_rows<T, 32, VEC>(h, p, st);
+  if (p.cols <= 1 * 32 * sgc::kPT) return forward_rows<T, 1, VEC>(h, p, st);
+  if (p.cols <= 2 * 32 * sgc::kPT) return forward_rows<T, 2, VEC>(h, p, st);
+  if (p.cols <= 4 * 32 * sgc::kPT) return forward_rows<T, 4, VEC>(h, p, st);
+  if (p.cols <= 8 * 32 * sgc::kPT) return forward_rows<T, 8, VEC>(h, p, st);
+  if (p.cols <= 16 * 32 * sgc::kPT) return forward_rows<T, 16, VEC>(h, p, st);
+  if (p.cols <= 32 * 32 * sgc::kPT) return forward_rows<T, 32, VEC>(h, p, st);
   sgc::norm_forward_long_kernel<T><<<(unsigned)p.rows, 1024, 0, st>>>(p);
   return done(h);
 }
@@ -298,23 +334,18 @@ int forward_typed(sgemm_cube_ctx* h, const NormParams& p, cudaStream_t st) {
 template <typename T, int WARPS, bool VEC>
 int backward_rows(sgemm_cube_ctx* h, NormParams p, float* dweight, float* dbias, cudaStream_t st) {
   constexpr int groups = WARPS >= 8 ? 1 : 8 / WARPS, threads = WARPS > 8 ? WARPS * 32 : 256;
-  int per_sm = 0;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, sgc::norm_backward_kernel<T, WARPS, VEC>, threads, 0) !=
-      cudaSuccess || per_sm < 1) {
-    cudaGetLastError();
-    return SGEMM_CUBE_CUDA_ERROR;
-  }
-  const long long want = ((long long)p.rows + groups - 1) / groups, cap = (long long)per_sm * h->sm_count;
-  const int blocks = (int)(want < cap ? want : cap);
+  int blocks = 0;
+  int rc = persistent_blocks(h, sgc::norm_backward_kernel<T, WARPS, VEC>, threads, p.rows, groups, &blocks);
+  if (rc) return rc;
   if (dweight || dbias) {
-    int rc = grow(&h->part_ws, &h->part_ws_bytes, (size_t)blocks * 2 * p.cols * 4);
+    rc = grow(&h->part_ws, &h->part_ws_bytes, (size_t)blocks * 2 * p.cols * 4);
     if (rc) return rc;
     p.part = static_cast<float*>(h->part_ws);
   }
   sgc::norm_backward_kernel<T, WARPS, VEC><<<(unsigned)blocks, threads, 0, st>>>(p);
-  int rc = done(h);
+  rc = done(h);
   if (rc || !p.part) return rc;
-  sgc::norm_parts_kernel<<<dim3((unsigned)((p.cols + 31) / 32), 2), 256, 0, st>>>(p.part, blocks, p.cols, dweight, dbias);
+  sgc::norm_parts_kernel<<<dim3((unsigned)((p.cols + 31) / 32), 2), 512, 0, st>>>(p.part, blocks, p.cols, dweight, dbias);
   return done(h);
 }
 template <typename T>
@@ -330,7 +361,7 @@ int backward_long(sgemm_cube_ctx* h, NormParams p, float* dweight, float* dbias,
     p.part = static_cast<float*>(h->part_ws);
     sgc::norm_columns_kernel<T><<<dim3((unsigned)tiles, (unsigned)blocks), 256, 0, st>>>(p, per);
     if ((rc = done(h))) return rc;
-    sgc::norm_parts_kernel<<<dim3((unsigned)tiles, 2), 256, 0, st>>>(p.part, blocks, p.cols, dweight, dbias);
+    sgc::norm_parts_kernel<<<dim3((unsigned)tiles, 2), 512, 0, st>>>(p.part, blocks, p.cols, dweight, dbias);
     if ((rc = done(h))) return rc;
   }
   if (!p.out) return rc;
@@ -339,12 +370,12 @@ int backward_long(sgemm_cube_ctx* h, NormParams p, float* dweight, float* dbias,
 }
 template <typename T, bool VEC>
 int backward_typed(sgemm_cube_ctx* h, const NormParams& p, float* dw, float* db, cudaStream_t st) {
-  if (p.cols <= 1 * 32 * sgc::kBwdPT) return backward_rows<T, 1, VEC>(h, p, dw, db, st);
-  if (p.cols <= 2 * 32 * sgc::kBwdPT) return backward_rows<T, 2, VEC>(h, p, dw, db, st);
-  if (p.cols <= 4 * 32 * sgc::kBwdPT) return backward_rows<T, 4, VEC>(h, p, dw, db, st);
-  if (p.cols <= 8 * 32 * sgc::kBwdPT) return backward_rows<T, 8, VEC>(h, p, dw, db, st);
-  if (p.cols <= 16 * 32 * sgc::kBwdPT) return backward_rows<T, 16, VEC>(h, p, dw, db, st);
-  if (p.cols <= 32 * 32 * sgc::kBwdPT) return backward_rows<T, 32, VEC>(h, p, dw, db, st);
+  if (p.cols <= 1 * 32 * sgc::kPT) return backward_rows<T, 1, VEC>(h, p, dw, db, st);
+  if (p.cols <= 2 * 32 * sgc::kPT) return backward_rows<T, 2, VEC>(h, p, dw, db, st);
+  if (p.cols <= 4 * 32 * sgc::kPT) return backward_rows<T, 4, VEC>(h, p, dw, db, st);
+  if (p.cols <= 8 * 32 * sgc::kPT) return backward_rows<T, 8, VEC>(h, p, dw, db, st);
+  if (p.cols <= 16 * 32 * sgc::kPT) return backward_rows<T, 16, VEC>(h, p, dw, db, st);
+  if (p.cols <= 32 * 32 * sgc::kPT) return backward_rows<T, 32, VEC>(h, p, dw, db, st);
   return backward_long<T>(h, p, dw, db, st);
 }
 

@@ -11,6 +11,8 @@ using sgc::PackJob;
 // Words of the handle's device scratch that the packing kernels use: running maxima and block counts
 // of up to two jobs (left zero by every call), exponents of operands that a call packs itself.
 constexpr int kRangeWords = 20, kExpWords = 24;
+// then one count of finished slices a tile: split-K is taken for at most sm_count / 2 tiles
+constexpr int kArrivalWords = 32;
 
 struct Packed {
   const uint16_t* hi;
@@ -76,7 +78,7 @@ int linear_attrs(sgemm_cube_ctx* h, int* clusters) {
     a.id = cudaLaunchAttributeClusterDimension;
     a.val.clusterDim.x = 2; a.val.clusterDim.y = 1; a.val.clusterDim.z = 1;
     cfg.gridDim = dim3(2 * h->sm_count, 1, 1);
-    cfg.blockDim = dim3(sgc::kTcThreads, 1, 1);
+    cfg.blockDim = dim3(sgc::kLinearThreads, 1, 1);
     cfg.dynamicSmemBytes = Cfg::SMEM_BYTES;
     cfg.attrs = &a;
     cfg.numAttrs = 1;
@@ -119,7 +121,7 @@ int launch_linear_kernel(sgemm_cube_ctx* h, const Packed& A, const Packed& B, co
   }
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
-  cfg.blockDim = dim3(sgc::kTcThreads, 1, 1);
+  cfg.blockDim = dim3(sgc::kLinearThreads, 1, 1);
   cfg.dynamicSmemBytes = Cfg::SMEM_BYTES;
   cfg.stream = st;
   cudaLaunchAttribute attr;
@@ -158,7 +160,6 @@ int linear_slices(const sgemm_cube_ctx* h, int M, int N, int K, int chunk_k) {
   const int per = (chunks + want - 1) / want;
   return (chunks + per - 1) / per;
 }
-size_t slice_stride(int M, int N) { return round_up((size_t)M * round_up((size_t)N, 4), 64); }
 
 // C (M x N) = epilogue of A B on packed operands, termwise.
 template <int FORM>
@@ -184,21 +185,21 @@ int linear_product(sgemm_cube_ctx* h, int M, int N, int K, const Packed& A, cons
   p.ep = ep;
   const int slices = linear_slices(h, M, N, K, p.kchunk_blocks * BK);
   if (slices > 1) {
-    const size_t stride = slice_stride(M, N);
-    rc = grow(&h->part_ws, &h->part_ws_bytes, 2 * (size_t)slices * stride * 4);
+    const size_t tiles = (size_t)((M + sgc::kBM - 1) / sgc::kBM) * ((N + sgc::kBN - 1) / sgc::kBN);
+    rc = grow(&h->part_ws, &h->part_ws_bytes, tiles * slices * sgc::kTileFloats * 4);
     if (rc) return rc;
     const int chunks = (K + p.kchunk_blocks * BK - 1) / (p.kchunk_blocks * BK);
     p.ksplit = slices;
     p.kslice_blocks = (chunks + slices - 1) / slices * p.kchunk_blocks;
-    p.Phh = static_cast<float*>(h->part_ws);
-    p.Px = p.Phh + (size_t)slices * stride;
-    p.pstride = (long long)stride;
-    p.ldp = (long long)round_up((size_t)N, 4);
-    rc = launch_linear_kernel<FORM, false>(h, A, B, p, st);
+    p.ep.tiles = static_cast<float*>(h->part_ws);
+    p.ep.arrivals = h->err_dev + kArrivalWords;
+    return launch_linear_kernel<FORM, false>(h, A, B, p, st);
+  }
+  // Nothing but the way back to do: the accumulate warps store to Y themselves.
+  if (ep.bias || ep.R || ep.Z || ep.act != SGEMM_CUBE_ACT_NONE) {
+    rc = grow(&h->tile_ws, &h->tile_ws_bytes, (size_t)h->sm_count * 2 * sgc::kTileFloats * 4);
     if (rc) return rc;
-    sgc::linear_reduce_kernel<<<blocks_for(h, (long long)M * ((N + 3) / 4)), 256, 0, st>>>(
-        M, N, slices, p.Phh, p.Px, p.pstride, p.ldp, Y, ldy, ep);
-    return launched(h);
+    p.ep.tiles = static_cast<float*>(h->tile_ws);
   }
   const bool pair = (h->cta_pair == 2 ? M > sgc::kBM : h->cta_pair == 1) && h->linear_pair_clusters > 0;
   if (pair) {

@@ -1,5 +1,4 @@
-// What a linear layer does to a finished product element, and how a 32 x 128 register tile of them is
-// stored.  Shared by the tensor-core kernel's epilogue, the split-K reduction and the few-row kernel.
+// What a linear layer does to a finished product element, and how a tile of them is stored.  Shared by the tensor-core kernel's epilogue, the split-K reduction and the few-row kernel.
 //
 //   z = 2^-(p_x + p_w) acc + b[col],   y = act(z) + R[row, col]
 //
@@ -14,41 +13,81 @@ namespace sgc {
 
 enum Activation { kActNone = 0, kActRelu, kActGelu, kActGeluTanh, kActSilu };
 
-// act(z), FP32 throughout.  The library's erff, tanhf and expf (about 2 ulp), not the fast
-// approximations: the product in front is good to 2^-22 and the activation should not be what limits it.
+// exp and 1 / x on the special function unit (2^-22 and one ulp).
+__device__ __forceinline__ float fast_exp(float x) {
+  float e;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(x * 1.4426950408889634f));
+  return e;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// s = 1 / (1 + exp(-z)), and s (1 - s) without the difference (which loses its bits where s is near 1).
+__device__ __forceinline__ float sigmoid(float z, float& slope) {
+  const float e = fast_exp(-fabsf(z));
+  const float r = fast_rcp(1.f + e);
+  slope = e * r * r;
+  return z < 0.f ? e * r : r;
+}
+
+// Phi(z), the normal distribution function, and e = exp(-z^2 / 2).  Hastings' rational form (Abramowitz and
+// Stegun 7.1.26): erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + 0.3275911 x), off by at most 1.5e-7 for
+// x >= 0; the lower tail is taken from it directly, not as a difference from 1.  15 instructions where erff
+// and expf take 45: with those the kernels around the product were bound by arithmetic, not by memory
+// (8192 x 16384: 347 us for the pass that needs 164).
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = fast_rcp(fmaf(0.3275911f, x, 1.f));
+  float q = fmaf(1.061405429f, t, -1.453152027f);
+  q = fmaf(q, t, 1.421413741f);
+  q = fmaf(q, t, -0.284496736f);
+  q = fmaf(q, t, 0.254829592f);
+  e = fast_exp(-x * x);
+  q = 0.5f * q * t * e;
+  return z < 0.f ? q : 1.f - q;
+}
+
+// sigmoid(2u) = (1 + tanh u) / 2 with the tanh form's u = sqrt(2 / pi) (z + 0.044715 z^3)
+__device__ __forceinline__ float gelu_tanh_weight(float z, float& slope) {
+  return sigmoid(1.5957691216057308f * fmaf(0.044715f * z * z, z, z), slope);
+}
+
+// act(z), good to 2^-21 (|z| + 1).
 __device__ __forceinline__ float act_value(int act, float z) {
+  float unused;
   switch (act) {
     case kActRelu: return z < 0.f ? 0.f : z;                            // keeps NaN
-    case kActGelu: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    case kActGeluTanh:
-      return 0.5f * z * (1.f + tanhf(0.79788456080286536f * fmaf(0.044715f * z * z, z, z)));
-    case kActSilu: return z / (1.f + expf(-z));
+    case kActGelu: return z * normal_cdf(z, unused);
+    case kActGeluTanh: return z * gelu_tanh_weight(z, unused);
+    case kActSilu: return z * sigmoid(z, unused);
     default: return z;
   }
 }
 
-// act'(z).  relu'(0) = 0.  For z far below zero the products that vanish are cut off before a factor
-// overflows (z^2 and exp(-z) leave the FP32 range, their products do not), so no 0 * inf appears.
+// act'(z), good to 2^-20.  relu'(0) = 0.  Where a factor overflows while the product vanishes, z is cut off first
+// (no 0 * inf).
 __device__ __forceinline__ float act_slope(int act, float z) {
   switch (act) {
     case kActRelu: return z > 0.f ? 1.f : (z == z ? 0.f : z);
     case kActGelu: {
-      const float phi = 0.5f * (1.f + erff(z * 0.70710678118654752f));
-      const float u = fminf(fabsf(z), 20.f);                            // exp(-200) = 0 in FP32
-      return fmaf(copysignf(u, z) * 0.39894228040143268f, expf(-0.5f * u * u), phi);
+      float e;
+      const float phi = normal_cdf(z, e);
+      return fmaf(copysignf(fminf(fabsf(z), 20.f), z) * 0.39894228040143268f, e, phi);     // e = 0 from 20 on
     }
     case kActGeluTanh: {
-      const float u = copysignf(fminf(fabsf(z), 20.f), z);              // tanh is +-1 from there on
-      const float t = tanhf(0.79788456080286536f * fmaf(0.044715f * u * u, u, u));
-      const float s = 0.5f * (1.f + t) +
-                      0.5f * u * (1.f - t * t) * 0.79788456080286536f * fmaf(0.134145f * u, u, 1.f);
-      return z == z ? s : z;
+      const float u = copysignf(fminf(fabsf(z), 20.f), z);              // the weight is 0 or 1 from there on
+      float ds;
+      const float w = gelu_tanh_weight(u, ds);
+      const float d = 1.5957691216057308f * fmaf(0.134145f * u, u, 1.f);
+      return z == z ? fmaf(u * ds, d, w) : z;
     }
     case kActSilu: {
-      const float p = 1.f / (1.f + expf(-z));
-      const float u = fmaxf(z, -110.f);                                 // p = 0 in FP32 from -104 on
-      const float s = p * fmaf(u, 1.f - p, 1.f);
-      return z == z ? s : z;
+      const float u = copysignf(fminf(fabsf(z), 110.f), z);             // s is 0 or 1 in FP32 from 104 on
+      float ds;
+      const float w = sigmoid(u, ds);
+      return z == z ? fmaf(u, ds, w) : z;
     }
     default: return 1.f;
   }
@@ -64,6 +103,11 @@ struct LinearEpilogue {
   long long ldz;
   int act;
   int vec;                // Y, Z and R take 16-byte accesses
+  // Scratch tiles of 128 x 256 sums: two for every block, or (split-K) `ksplit` for every tile of Y, which the
+  // block that comes last to a tile adds up; `arrivals` counts them, one word a tile, zero between calls.
+  // Null: the accumulate warps store to Y themselves.
+  float* tiles;
+  unsigned int* arrivals;
 };
 
 // 2^-(p_a + p_b) as two FP32 factors (the sum of two exponents can leave the range of one).
@@ -85,78 +129,128 @@ __device__ __forceinline__ float linear_finish(const LinearEpilogue& e, float z,
   return y;
 }
 
-// The 32 rows x 128 columns of one accumulate warp: lane l holds row `row0 + l`, columns col0 .. col0 + 127.
-// 32 x 32 blocks go through the warp's 4 KB staging buffer (16-byte chunks XOR-swizzled by row: no bank
-// conflicts either way), so that bias, residual and stores run along rows.  Aligned matrices: 16 bytes
-// per lane, four rows an instruction.  Others (odd leading dimensions): 4 bytes per lane, a row an
-// instruction, which keeps the accesses of a warp in one or two 128-byte lines.
-__device__ __forceinline__ void linear_store_tile(const LinearEpilogue& e, float* Y, long long ldy, int M, int N,
-                                                  const float (&S)[128], uint32_t stg, int row0, int col0,
-                                                  int lane) {
+// A finished 128 x 256 tile of sums waits in the block's scratch as float4 [64][128]: four columns of a row, the 128
+// rows next to each other, which is how the accumulate warps hold it (a thread has a row).
+__device__ __forceinline__ float4* tile_slot(float* tile, int col4, int row) {
+  return reinterpret_cast<float4*>(tile) + col4 * 128 + row;
+}
+
+template <int ACT>
+__device__ __forceinline__ void act_four(float4& v) {
+  v.x = act_value(ACT, v.x); v.y = act_value(ACT, v.y); v.z = act_value(ACT, v.z); v.w = act_value(ACT, v.w);
+}
+
+// Blocks of 32 rows x 16 columns of such a tile, from `first` on every `step`-th, to Y: lane = every eighth row x four
+// columns, so that a warp reads whole lines and writes 64 bytes of every row.  `slices` tiles `stride` floats
+// apart (split-K) are added in order.  Few warps do this and instructions are what bounds it: bias and addresses
+// are taken once for the four rows of a lane, and a block inside N of aligned matrices tests nothing but rows.
+// (One row at a time with everything tested took 18 us for a tile; the accumulate warps doing it on their
+// 128 registers, with the tensor core waiting, 55 us: 8192 x 16384 x 4096 with gelu 4011 us, without 2388.)
+__device__ __forceinline__ void linear_store_blocks(const LinearEpilogue& e, float* Y, long long ldy, int M, int N,
+                                                    float* tile, int slices, long long stride, int row0, int col0,
+                                                    int first, int step, int lane) {
+  constexpr int U = 4;                                       // rows of a lane, 8 apart
   const PowerBack back = power_back(e.exp_a, e.exp_b);
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-      asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(stg + lane * 128 + ((q ^ (lane & 7)) << 4)),
-                   "f"(S[g * 32 + 4 * q]), "f"(S[g * 32 + 4 * q + 1]), "f"(S[g * 32 + 4 * q + 2]),
-                   "f"(S[g * 32 + 4 * q + 3])
-                   : "memory");
-    __syncwarp();
-    if (e.vec) {
-      const int q = lane & 7;
-      const int col = col0 + g * 32 + q * 4;
-      const bool full = col + 4 <= N;
-      float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (e.bias) {
-        if (col < N) b.x = e.bias[col];
-        if (col + 1 < N) b.y = e.bias[col + 1];
-        if (col + 2 < N) b.z = e.bias[col + 2];
-        if (col + 3 < N) b.w = e.bias[col + 3];
-      }
+  const float back_all = back.f0 * back.f1;
+  const bool one_factor = fabsf(back_all) >= 1.17549435e-38f && fabsf(back_all) <= 1.7e38f;
+  const int lr = lane >> 2, lc = lane & 3;
+  const int blocks = (min(128, M - row0) + 8 * U - 1) / (8 * U) * 16;
 #pragma unroll 1
-      for (int i = 0; i < 8; ++i) {
-        const int r = i * 4 + (lane >> 3);
-        const int row = row0 + r;
-        if (row >= M || col >= N) continue;
-        float4 v;
-        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                     : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                     : "r"(stg + r * 128 + ((q ^ (r & 7)) << 4))
-                     : "memory");
-        v.x = back(v.x) + b.x; v.y = back(v.y) + b.y; v.z = back(v.z) + b.z; v.w = back(v.w) + b.w;
-        if (full) {
-          float4 res = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (e.R) res = *reinterpret_cast<const float4*>(e.R + (long long)row * e.ldr + col);
-          if (e.Z) *reinterpret_cast<float4*>(e.Z + (long long)row * e.ldz + col) = v;
-          if (e.act != kActNone) {
-            v.x = act_value(e.act, v.x); v.y = act_value(e.act, v.y);
-            v.z = act_value(e.act, v.z); v.w = act_value(e.act, v.w);
+  for (int b = first; b < blocks; b += step) {
+    const int r0 = (b >> 4) * (8 * U) + lr;
+    const int col = col0 + (b & 15) * 16 + lc * 4;
+    if (col0 + (b & 15) * 16 >= N) continue;
+    const bool full = e.vec && col0 + (b & 15) * 16 + 16 <= N;
+    const int row = row0 + r0;
+    const float4* src = tile_slot(tile, (b & 15) * 4 + lc, r0);
+    float4 v[U], res[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = __ldcg(src + 8 * u);
+    float4 bias = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (e.bias) {
+      if (col < N) bias.x = __ldg(e.bias + col);
+      if (col + 1 < N) bias.y = __ldg(e.bias + col + 1);
+      if (col + 2 < N) bias.z = __ldg(e.bias + col + 2);
+      if (col + 3 < N) bias.w = __ldg(e.bias + col + 3);
+    }
+    if (e.R) {
+      const float* r = e.R + row * e.ldr + col;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        res[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row + 8 * u < M) {
+          const float* ru = r + 8 * u * e.ldr;
+          if (full) {
+            res[u] = *reinterpret_cast<const float4*>(ru);
+          } else {
+            if (col < N) res[u].x = ru[0];
+            if (col + 1 < N) res[u].y = ru[1];
+            if (col + 2 < N) res[u].z = ru[2];
+            if (col + 3 < N) res[u].w = ru[3];
           }
-          if (e.R) { v.x += res.x; v.y += res.y; v.z += res.z; v.w += res.w; }
-          *reinterpret_cast<float4*>(Y + (long long)row * ldy + col) = v;
-        } else {
-          const float z[4] = {v.x, v.y, v.z, v.w};
-          for (int j = 0; j < 4 && col + j < N; ++j)
-            Y[(long long)row * ldy + col + j] = linear_finish(e, z[j], row, col + j);
         }
       }
-    } else {
-      const int col = col0 + g * 32 + lane;
-      const float b = (e.bias && col < N) ? e.bias[col] : 0.f;
+    }
 #pragma unroll 1
-      for (int r = 0; r < 32; ++r) {
-        const int row = row0 + r;
-        if (row >= M || col >= N) break;
-        float v;
-        asm volatile("ld.shared.f32 %0, [%1];"
-                     : "=f"(v)
-                     : "r"(stg + r * 128 + ((((lane >> 2) ^ (r & 7)) << 4) | ((lane & 3) << 2)))
-                     : "memory");
-        Y[(long long)row * ldy + col] = linear_finish(e, back(v) + b, row, col);
+    for (int s = 1; s < slices; ++s) {
+      const float4* more = src + s * (stride / 4);
+      float4 f[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) f[u] = __ldcg(more + 8 * u);
+#pragma unroll
+      for (int u = 0; u < U; ++u) { v[u].x += f[u].x; v[u].y += f[u].y; v[u].z += f[u].z; v[u].w += f[u].w; }
+    }
+    auto store = [&](float* out, long long ld) {
+      out += row * ld + col;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (row + 8 * u >= M) break;
+        float* o = out + 8 * u * ld;
+        if (full) {
+          *reinterpret_cast<float4*>(o) = v[u];
+        } else {
+          if (col < N) o[0] = v[u].x;
+          if (col + 1 < N) o[1] = v[u].y;
+          if (col + 2 < N) o[2] = v[u].z;
+          if (col + 3 < N) o[3] = v[u].w;
+        }
+      }
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (one_factor) {
+        v[u].x = fmaf(v[u].x, back_all, bias.x); v[u].y = fmaf(v[u].y, back_all, bias.y);
+        v[u].z = fmaf(v[u].z, back_all, bias.z); v[u].w = fmaf(v[u].w, back_all, bias.w);
+      } else {
+        v[u].x = back(v[u].x) + bias.x; v[u].y = back(v[u].y) + bias.y;
+        v[u].z = back(v[u].z) + bias.z; v[u].w = back(v[u].w) + bias.w;
       }
     }
-    __syncwarp();
+    if (e.Z) store(e.Z, e.ldz);
+    switch (e.act) {
+      case kActRelu:
+#pragma unroll
+        for (int u = 0; u < U; ++u) act_four<kActRelu>(v[u]);
+        break;
+      case kActGelu:
+#pragma unroll
+        for (int u = 0; u < U; ++u) act_four<kActGelu>(v[u]);
+        break;
+      case kActGeluTanh:
+#pragma unroll
+        for (int u = 0; u < U; ++u) act_four<kActGeluTanh>(v[u]);
+        break;
+      case kActSilu:
+#pragma unroll
+        for (int u = 0; u < U; ++u) act_four<kActSilu>(v[u]);
+        break;
+      default: break;
+    }
+    if (e.R) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) { v[u].x += res[u].x; v[u].y += res[u].y; v[u].z += res[u].z; v[u].w += res[u].w; }
+    }
+    store(Y, ldy);
   }
 }
 

@@ -1,6 +1,6 @@
 // Kernels around the product of a linear layer: packing an FP32 operand (power-of-two scaling found on
-// the device, then the two-word split), the gradient in front of the activation, the split-K reduction
-// with the layer's epilogue, and the product for a few rows.
+// the device, then the two-word split), the gradient in front of the activation, and the product for a
+// few rows.
 #pragma once
 
 #include <cstdint>
@@ -188,7 +188,9 @@ __device__ __forceinline__ void pack_items(const PackJob& j, long long first, lo
   const float scale = pow2f(kPackScaleExp);
   const int per_row = (j.cols + 7) >> 3;
   const long long total = (long long)j.rows * per_row;
-  for (long long it = first; it < total; it += stride) {
+  // From the end to the start: the range pass before read from start to end, so what it read last is
+  // still in L2.
+  for (long long it = total - 1 - first; it >= 0; it -= stride) {
     const long long r = total < (1ll << 31) ? (long long)((uint32_t)it / (uint32_t)per_row) : it / per_row;
     const int c = (int)(it - r * per_row) << 3;
     const float* src = j.X + r * j.ldx + c;
@@ -255,34 +257,6 @@ dz_split_kernel(PackJob j, unsigned int sum_blocks, const float* __restrict__ pa
     add_column_parts(part, chunks, j.cols, dbias, (blockIdx.x - split_blocks) * 256 + threadIdx.x);
   else
     pack_items<ACT, true>(j, (long long)blockIdx.x * 256 + threadIdx.x, (long long)split_blocks * 256);
-}
-
-// Split-K: the slices' hi*hi sums and correction sums are added among themselves, in slice order, and
-// meet once, then the layer's epilogue.  Four columns a thread; Phh and Px have ldp % 4 == 0.
-__global__ void __launch_bounds__(256)
-linear_reduce_kernel(int M, int N, int slices, const float* __restrict__ Phh, const float* __restrict__ Px,
-                     long long pstride, long long ldp, float* Y, long long ldy, LinearEpilogue e) {
-  const PowerBack back = power_back(e.exp_a, e.exp_b);
-  const int per_row = (N + 3) >> 2;
-  const long long total = (long long)M * per_row;
-  for (long long it = (long long)blockIdx.x * 256 + threadIdx.x; it < total; it += (long long)gridDim.x * 256) {
-    const long long r = total < (1ll << 31) ? (long long)((uint32_t)it / (uint32_t)per_row) : it / per_row;
-    const int c = (int)(it - r * per_row) << 2;
-    const long long off = r * ldp + c;
-    float4 hh = *reinterpret_cast<const float4*>(Phh + off);
-    float4 x = *reinterpret_cast<const float4*>(Px + off);
-    for (int s = 1; s < slices; ++s) {
-      const float4 h1 = *reinterpret_cast<const float4*>(Phh + off + s * pstride);
-      const float4 x1 = *reinterpret_cast<const float4*>(Px + off + s * pstride);
-      hh.x += h1.x; hh.y += h1.y; hh.z += h1.z; hh.w += h1.w;
-      x.x += x1.x; x.y += x1.y; x.z += x1.z; x.w += x1.w;
-    }
-    const float z[4] = {back(fmaf(x.x, kPackInvScale, hh.x)), back(fmaf(x.y, kPackInvScale, hh.y)),
-                        back(fmaf(x.z, kPackInvScale, hh.z)), back(fmaf(x.w, kPackInvScale, hh.w))};
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (c + q < N) Y[r * ldy + c + q] = linear_finish(e, z[q] + (e.bias ? e.bias[c + q] : 0.f), r, c + q);
-  }
 }
 
 // The empty inner dimension: y = act(b) + R.

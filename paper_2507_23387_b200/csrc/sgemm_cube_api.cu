@@ -414,12 +414,15 @@ int sgemm_cube_create(sgemm_cube_handle* out, int device) {
     return SGEMM_CUBE_CUDA_ERROR;
   }
   h->encode = reinterpret_cast<EncodeTiledFn>(fn);
-  if (cudaMalloc(reinterpret_cast<void**>(&h->err_dev), 32 * sizeof(unsigned int)) != cudaSuccess) {
+  const size_t words = 32 + (size_t)h->sm_count;
+  if (cudaMalloc(reinterpret_cast<void**>(&h->err_dev), words * sizeof(unsigned int)) != cudaSuccess) {
     cudaGetLastError();
     delete h;
     return SGEMM_CUBE_ALLOC_FAILED;
   }
-  if (cudaMemset(h->err_dev, 0, 32 * sizeof(unsigned int)) != cudaSuccess) {
+  // (waited for: the caller's streams need not be ordered after the default stream)
+  if (cudaMemset(h->err_dev, 0, words * sizeof(unsigned int)) != cudaSuccess ||
+      cudaStreamSynchronize(nullptr) != cudaSuccess) {
     cudaFree(h->err_dev);
     delete h;
     return SGEMM_CUBE_CUDA_ERROR;
@@ -440,6 +443,7 @@ int sgemm_cube_destroy(sgemm_cube_handle h) {
   if (h->ws) cudaFree(h->ws);
   if (h->host_ws) cudaFree(h->host_ws);
   if (h->part_ws) cudaFree(h->part_ws);
+  if (h->tile_ws) cudaFree(h->tile_ws);
   for (cudaEvent_t e : h->ev_ring)
     if (e) cudaEventDestroy(e);
   if (h->s_in) cudaStreamDestroy(h->s_in);
@@ -781,6 +785,8 @@ int sgemm_cube_check(sgemm_cube_handle h, void* stream, uint32_t* detail_out) {
   if (detail_out) *detail_out = e;
   if (e) {
     cudaMemset(h->err_dev, 0, sizeof(e));
+    // counts that a kernel which gave up has left behind
+    cudaMemset(h->err_dev + 20, 0, (12 + (size_t)h->sm_count) * sizeof(unsigned int));
     return SGEMM_CUBE_DEVICE_TIMEOUT;
   }
   return SGEMM_CUBE_OK;
