@@ -13,15 +13,15 @@ namespace sgc {
 
 enum Activation { kActNone = 0, kActRelu, kActGelu, kActGeluTanh, kActSilu };
 
-// exp and 1 / x on the special function unit (2^-22 and one ulp).
+// exp and 1 / x on the special function unit (2^-22 and one ulp; exponentials below 2^-126 are zero).
 __device__ __forceinline__ float fast_exp(float x) {
   float e;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(x * 1.4426950408889634f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * 1.4426950408889634f));
   return e;
 }
 __device__ __forceinline__ float fast_rcp(float x) {
   float r;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 // s = 1 / (1 + exp(-z)), and s (1 - s) without the difference (which loses its bits where s is near 1).

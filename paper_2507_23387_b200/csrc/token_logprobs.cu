@@ -8,19 +8,29 @@
 // Bound by reading the logits once.  Exponentials run in base 2, t = (x - m) a with a = scale log2 e.  The difference
 // is taken first: one FMA with fl(m a) would save an instruction, but overflows where masked logits hold the
 // type's lowest value, and puts the rounding of m a into every term.
+#include <type_traits>
+
 #include "ctx.cuh"
 #include "elements.cuh"
 
 namespace sgc {
 
-constexpr int kLpThreads = 512;
+constexpr int kLpThreads = 256;
 constexpr int kLpWarps = kLpThreads / 32;
 constexpr int kTopMax = 32;
 constexpr int kCandidates = 256;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kNoWeight = -160.f;      // 2^-160 is zero in FP32: exponents are cut there where they are factors
 
+// 2^t, zero below 2^-126: in a sum such weights are nothing beside the row's largest, which is 1, and keeping them
+// takes three more instructions.
 __device__ __forceinline__ float ex2(float t) {
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+  return e;
+}
+// 2^t down to the subnormal numbers, for the gradient, where each element stands alone.
+__device__ __forceinline__ float ex2_gradual(float t) {
   float e;
   asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(t));
   return e;
@@ -69,25 +79,36 @@ struct LogprobParams {
   long long* top_index;
 };
 
+// Two FP32 values in one register pair: the packed instructions round each like the scalar ones.
+struct Two {
+  uint64_t p;
+};
+__device__ __forceinline__ Two two(float a, float b) {
+  Two t;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(t.p) : "f"(a), "f"(b));
+  return t;
+}
+__device__ __forceinline__ void parts_of(Two t, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(t.p)); }
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+  Two c;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(c.p) : "l"(a.p), "l"(b.p));
+  return c;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  Two c;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(c.p) : "l"(a.p), "l"(b.p));
+  return c;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.p) : "l"(a.p), "l"(b.p), "l"(c.p));
+  return d;
+}
+
 // Running sums of a part of a row; S in base-2 units.
 struct Running {
   float m, Z, S;
 };
-__device__ __forceinline__ void raise(Running& r, float m, float a) {   // m > r.m
-  const float d = (r.m - m) * a;
-  const float f = ex2(d);                      // zero when r.m is -inf
-  r.S = f * fmaf(fmaxf(d, kNoWeight), r.Z, r.S);
-  r.Z *= f;
-  r.m = m;
-}
-// `m` is r.m, or 0 while that is -inf (then x is -inf or NaN)
-__device__ __forceinline__ void add_one(Running& r, float x, float m, float a) {
-  const float t = (x - m) * a;
-  const float e = ex2(t);
-  r.Z += e;
-  r.S = fmaf(e, fmaxf(t, kNoWeight), r.S);
-}
-__device__ __forceinline__ float finite_max(const Running& r) { return r.m == -INFINITY ? 0.f : r.m; }
 __device__ __forceinline__ void join(Running& r, Running o, float a) {
   if (o.m > r.m) { const Running x = r; r = o; o = x; }
   // r has the larger m; an -inf part has empty sums, or NaN ones, which stay
@@ -96,6 +117,56 @@ __device__ __forceinline__ void join(Running& r, Running o, float a) {
   const float f = ex2(d);
   r.Z = fmaf(o.Z, f, r.Z);
   r.S += f * fmaf(fmaxf(d, kNoWeight), o.Z, o.S);
+}
+// join over groups of N neighbouring lanes; the first lane of each ends up with the sum
+template <int N>
+__device__ __forceinline__ void join_lanes(Running& r, float a) {
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) {
+    Running other;
+    other.m = __shfl_down_sync(0xffffffffu, r.m, o);
+    other.Z = __shfl_down_sync(0xffffffffu, r.Z, o);
+    other.S = __shfl_down_sync(0xffffffffu, r.S, o);
+    join(r, other, a);
+  }
+}
+
+// The same for one thread while it goes through its columns: even and odd elements apart, so that the packed
+// instructions apply (half the issue slots: with 16-bit logits those are what is short).
+struct ThreadSums {
+  float m;
+  Two Z, S;
+  __device__ __forceinline__ void raise(float top, float a) {            // top > m
+    const float d = (m - top) * a;
+    const float f = ex2(d);                      // zero when m was -inf
+    const float c = fmaxf(d, kNoWeight);
+    S = fma2(two(c, c), Z, S) * two(f, f);
+    Z = Z * two(f, f);
+    m = top;
+  }
+  // -m, or 0 while m is -inf (then the elements are -inf or NaN)
+  __device__ __forceinline__ float minus_m() const { return m == -INFINITY ? 0.f : -m; }
+  __device__ __forceinline__ void add(float x0, float x1, float minus, float a) {
+    const Two t = (two(x0, x1) + two(minus, minus)) * two(a, a);
+    float t0, t1;
+    parts_of(t, t0, t1);
+    const Two e = two(ex2(t0), ex2(t1));
+    Z = Z + e;
+    S = fma2(e, two(fmaxf(t0, kNoWeight), fmaxf(t1, kNoWeight)), S);
+  }
+  __device__ __forceinline__ Running sum() const {
+    float z0, z1, s0, s1;
+    parts_of(Z, z0, z1);
+    parts_of(S, s0, s1);
+    return Running{m, z0 + z1, s0 + s1};
+  }
+};
+
+// Four 32-bit words of -inf elements.
+template <typename T>
+__device__ __forceinline__ uint4 no_logits() {
+  const uint32_t w = sizeof(T) == 4 ? 0xFF800000u : (std::is_same<T, __half>::value ? 0xFC00FC00u : 0xFF80FF80u);
+  return make_uint4(w, w, w, w);
 }
 
 // Order of the alternatives: larger logit first, then the lower column, as one unsigned number; 0 is none.
@@ -146,24 +217,45 @@ struct Piece {
     tail = n - head - vecs * V;
   }
   __device__ __forceinline__ const uint4* vec(int v) const { return reinterpret_cast<const uint4*>(x + head) + v; }
-  // element e of thread t's own sequence (front, vectors, rest), as a column of the piece; -1 past its end
-  __device__ __forceinline__ int column(int t, int e) const {
-    constexpr int V = Elem<T>::kVec;
-    if (t < head) {
-      if (e == 0) return t;
-      --e;
-    }
-    const int mine = vecs > t ? (vecs - t + kLpThreads - 1) / kLpThreads * V : 0;
-    if (e < mine) return head + (t + e / V * kLpThreads) * V + e % V;
-    return (e == mine && t < tail) ? head + vecs * V + t : -1;
-  }
-  __device__ __forceinline__ int owner(int c) const {
+  __device__ __forceinline__ int owner(int c) const {                     // the thread that takes column c
     constexpr int V = Elem<T>::kVec;
     if (c < head) return c;
     c -= head;
     return c < vecs * V ? c / V % kLpThreads : c - vecs * V;
   }
 };
+
+// Calls f(key) for the columns above `bound` that the owners of the first `count` keys of `list` hold, these keys
+// themselves left out; the work is spread over `threads` threads, which all make the same calls (key 0: nothing
+// there), so that f may use the whole warp.
+template <typename T, typename F>
+__device__ __forceinline__ void for_columns_above(const Piece<T>& piece, int c0, const uint64_t* list, int count,
+                                                  uint64_t bound, int t, int threads, F f) {
+  constexpr int V = Elem<T>::kVec;
+  auto call = [&](float x, int c, uint64_t own, bool in) {
+    const uint64_t k = in ? order_key(x, (uint32_t)(c0 + c)) : 0ull;
+    f(k > bound && k != own ? k : 0ull);
+  };
+  for (int i0 = 0; i0 < 2 * count; i0 += threads) {      // the elements in front and at the end
+    const int i = i0 + t;
+    const uint64_t own = i < 2 * count ? list[i >> 1] : 0ull;
+    const int w = own ? piece.owner((int)key_column(own) - c0) : 0;
+    const int c = (i & 1) ? piece.head + piece.vecs * V + w : w;
+    const bool in = own != 0 && w < ((i & 1) ? piece.tail : piece.head);
+    call(in ? Elem<T>::get(piece.x[c]) : 0.f, c, own, in);
+  }
+  const int each = (piece.vecs + kLpThreads - 1) / kLpThreads;
+  for (int i0 = 0; i0 < count * each; i0 += threads) {
+    const int i = i0 + t, j = i / each;
+    const uint64_t own = j < count ? list[j] : 0ull;
+    const int v = (own ? piece.owner((int)key_column(own) - c0) : 0) + (i - j * each) * kLpThreads;
+    const bool in = own != 0 && v < piece.vecs;
+    float e[V];
+    Elem<T>::unpack(in ? __ldg(piece.vec(v)) : no_logits<T>(), e);
+#pragma unroll
+    for (int q = 0; q < V; ++q) call(e[q], piece.head + v * V + q, own, in);
+  }
+}
 
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(LogprobParams p) {
@@ -172,7 +264,7 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(LogprobParam
   __shared__ Running block_sum;
   __shared__ uint64_t list[TOP ? kLpWarps : 1][32];
   __shared__ uint64_t more[TOP ? kCandidates : 1];
-  __shared__ uint64_t best[TOP ? 32 : 1];
+  __shared__ uint64_t best[32];
   __shared__ int more_count;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const uint32_t ranks = cluster_size(), rank = cluster_rank_x();
@@ -182,161 +274,160 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(LogprobParam
   const int c0 = (int)min((long long)p.vocab, rank * per), c1 = (int)min((long long)p.vocab, c0 + per);
   const Piece<T> piece(x_row + c0, c1 - c0);
 
-  Running r{-INFINITY, 0.f, 0.f};
+  // the target's logit, long before it is needed
+  long long target = -1;
+  float target_logit = 0.f;
+  if (t == 0 && rank == 0 && p.logp) {
+    target = p.tokens[row];
+    if (target >= 0 && target < p.vocab) target_logit = Elem<T>::get(x_row[target]);
+  }
+
+  ThreadSums r{-INFINITY, two(0.f, 0.f), two(0.f, 0.f)};
   int at = -1;                                           // where m was met: -1 nowhere, 0 front, 1 + batch, then the rest
+  const int batches = (piece.vecs + kLpThreads * U - 1) / (kLpThreads * U);
+  uint4 next[U];
+  auto fetch = [&](int b, uint4 (&raw)[U]) {             // the vectors of batch b, -inf past the end
+    const int v0 = b * kLpThreads * U + t;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      raw[u] = v0 + u * kLpThreads < piece.vecs ? __ldg(piece.vec(v0 + u * kLpThreads)) : no_logits<T>();
+  };
+  fetch(0, next);
   if (t < piece.head) {
     const float x = Elem<T>::get(piece.x[t]);
-    if (x > r.m) { raise(r, x, p.a); at = 0; }
-    add_one(r, x, finite_max(r), p.a);
+    if (x > r.m) { r.raise(x, p.a); at = 0; }
+    r.add(x, -INFINITY, r.minus_m(), p.a);
   }
-  const int batches = (piece.vecs + kLpThreads * U - 1) / (kLpThreads * U);
   for (int b = 0; b < batches; ++b) {
-    uint4 raw[U];
-    const int v0 = b * kLpThreads * U + t;
-    const bool whole = (b + 1) * kLpThreads * U <= piece.vecs;
+    float v[U][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u) Elem<T>::unpack(next[u], v[u]);
+    if (b + 1 < batches) fetch(b + 1, next);
+    float top = v[0][0];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (whole || v0 + u * kLpThreads < piece.vecs) raw[u] = __ldg(piece.vec(v0 + u * kLpThreads));
-    float v[U][V];
-    float top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (whole || v0 + u * kLpThreads < piece.vecs) {
-        Elem<T>::unpack(raw[u], v[u]);
-      } else {
-#pragma unroll
-        for (int q = 0; q < V; ++q) v[u][q] = -INFINITY;
-      }
 #pragma unroll
       for (int q = 0; q < V; ++q) top = fmaxf(top, v[u][q]);
-    }
-    if (top > r.m) { raise(r, top, p.a); at = 1 + b; }
-    const float m = finite_max(r);
+    if (top > r.m) { r.raise(top, p.a); at = 1 + b; }
+    const float minus = r.minus_m();
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int q = 0; q < V; ++q) add_one(r, v[u][q], m, p.a);
+      for (int q = 0; q < V; q += 2) r.add(v[u][q], v[u][q + 1], minus, p.a);
   }
   if (t < piece.tail) {
     const float x = Elem<T>::get(piece.x[piece.head + piece.vecs * V + t]);
-    if (x > r.m) { raise(r, x, p.a); at = 1 + batches; }
-    add_one(r, x, finite_max(r), p.a);
+    if (x > r.m) { r.raise(x, p.a); at = 1 + batches; }
+    r.add(x, -INFINITY, r.minus_m(), p.a);
   }
+  Running sum = r.sum();
 
-  if (TOP) {
+  if constexpr (TOP) {
     // The k largest of the threads' maxima bound the k largest elements from below, and hold every thread
     // that owns one of them: an element among the k largest is not above its thread's maximum.
-    uint64_t key = 0;
-    int e0 = 0, e1 = 1;                                  // elements of the own sequence that hold the maximum
-    if (at > 0 && at <= batches) { e0 = (t < piece.head) + (at - 1) * 16; e1 = e0 + 16; }
-    else if (at > batches) { e0 = (t < piece.head) + (piece.vecs > t ? (piece.vecs - t + kLpThreads - 1) / kLpThreads * V : 0); e1 = e0 + 1; }
-    for (int e = e0; e < e1; ++e) {
-      const int c = piece.column(t, e);
-      if (c < 0) break;
-      const uint64_t k = order_key(Elem<T>::get(piece.x[c]), (uint32_t)(c0 + c));
-      if (k > key) key = k;
+    int c = -1;                                          // column of the own maximum, the lowest if it is met again
+    if (at > 0 && at <= batches) {
+      uint4 raw[U];
+      fetch(at - 1, raw);
+#pragma unroll
+      for (int u = U - 1; u >= 0; --u) {
+        float e[V];
+        Elem<T>::unpack(raw[u], e);
+#pragma unroll
+        for (int q = V - 1; q >= 0; --q)
+          if (e[q] == r.m) c = piece.head + ((at - 1) * kLpThreads * U + t + u * kLpThreads) * V + q;
+      }
+    } else if (at > batches) {
+      c = piece.head + piece.vecs * V + t;
+    } else if (t < piece.head) {                         // in front, or nothing above -inf: the first column
+      c = t;
+    } else if (t < piece.vecs) {
+      c = piece.head + t * V;
+    } else if (t < piece.tail) {
+      c = piece.head + piece.vecs * V + t;
     }
     if (t == 0) more_count = 0;
-    list[warp][lane] = sort_lanes(key, lane);
+    list[warp][lane] = sort_lanes(c >= 0 ? order_key(r.m, (uint32_t)(c0 + c)) : 0ull, lane);
     __syncthreads();
-    for (int s = kLpWarps / 2; s > 0; s >>= 1) {
-      uint64_t k = 0;
-      if (warp < s) k = merge_lanes(list[warp][lane], list[warp + s][31 - lane], lane);
-      __syncthreads();
-      if (warp < s) list[warp][lane] = k;
+    for (int s = kLpWarps / 2; s > 0; s >>= 1) {         // warp w takes over list w + s, which nobody else reads
+      if (warp < s) list[warp][lane] = merge_lanes(list[warp][lane], list[warp + s][31 - lane], lane);
       __syncthreads();
     }
     const uint64_t bound = list[0][p.top_k - 1];
     // what else these threads own above the bound
-    for (int j = warp; j < p.top_k; j += kLpWarps) {
-      const uint64_t own = list[0][j];
-      if (own == 0) break;
-      const int w = piece.owner((int)key_column(own) - c0);
-      for (int e = lane;; e += 32) {
-        const int c = piece.column(w, e);
-        if (c >= 0) {
-          const uint64_t k = order_key(Elem<T>::get(piece.x[c]), (uint32_t)(c0 + c));
-          if (k > bound && k != own) {
-            const int at_more = atomicAdd(&more_count, 1);
-            if (at_more < kCandidates) more[at_more] = k;
-          }
-        }
-        if (__all_sync(0xffffffffu, c < 0)) break;
+    for_columns_above(piece, c0, list[0], p.top_k, bound, t, kLpThreads, [&](uint64_t k) {
+      if (k) {
+        const int slot = atomicAdd(&more_count, 1);
+        if (slot < kCandidates) more[slot] = k;
       }
-    }
+    });
     __syncthreads();
     if (warp == 0) {
       uint64_t k = list[0][lane];
+      auto add = [&](uint64_t o) {
+        o = sort_lanes(o, lane);
+        k = merge_lanes(k, __shfl_sync(0xffffffffu, o, 31 - lane), lane);
+      };
       if (more_count <= kCandidates) {
-        for (int i = 0; i < more_count; i += 32) {
-          const uint64_t o = sort_lanes(i + lane < more_count ? more[i + lane] : 0ull, lane);
-          k = merge_lanes(k, __shfl_sync(0xffffffffu, o, 31 - lane), lane);
-        }
+        for (int i = 0; i < more_count; i += 32) add(i + lane < more_count ? more[i + lane] : 0ull);
       } else {                                           // many in a few threads: straight from the row
-        for (int j = 0; j < p.top_k; ++j) {
-          const uint64_t own = list[0][j];
-          if (own == 0) break;
-          const int w = piece.owner((int)key_column(own) - c0);
-          for (int e = lane;; e += 32) {
-            const int c = piece.column(w, e);
-            uint64_t o = 0;
-            if (c >= 0) {
-              o = order_key(Elem<T>::get(piece.x[c]), (uint32_t)(c0 + c));
-              if (o <= bound || o == own) o = 0;
-            }
-            if (__any_sync(0xffffffffu, o != 0)) {
-              o = sort_lanes(o, lane);
-              k = merge_lanes(k, __shfl_sync(0xffffffffu, o, 31 - lane), lane);
-            }
-            if (__all_sync(0xffffffffu, c < 0)) break;
-          }
-        }
+        for_columns_above(piece, c0, list[0], p.top_k, bound, lane, 32, [&](uint64_t o) {
+          if (__any_sync(0xffffffffu, o != 0)) add(o);
+        });
       }
       best[lane] = k;
     }
   }
 
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    Running other;
-    other.m = __shfl_down_sync(0xffffffffu, r.m, o);
-    other.Z = __shfl_down_sync(0xffffffffu, r.Z, o);
-    other.S = __shfl_down_sync(0xffffffffu, r.S, o);
-    join(r, other, p.a);
-  }
-  if (lane == 0) parts[warp] = r;
+  join_lanes<32>(sum, p.a);
+  if (lane == 0) parts[warp] = sum;
   __syncthreads();
-  if (t == 0) {
-    for (int w = 1; w < kLpWarps; ++w) join(r, parts[w], p.a);
-    block_sum = r;
+  if (warp == 0) {
+    sum = lane < kLpWarps ? parts[lane] : Running{-INFINITY, 0.f, 0.f};
+    join_lanes<kLpWarps>(sum, p.a);
+    if (lane == 0) block_sum = sum;
   }
-  if (ranks > 1) cluster_meet();
-  else __syncthreads();
-  if (rank == 0 && warp == 0) {
-    r = block_sum;
-    uint64_t k = TOP ? best[lane] : 0ull;
-    for (uint32_t o = 1; o < ranks; ++o) {
-      const uint32_t a = remote_address(&block_sum, o);
-      Running other;
-      other.m = remote_f32(a); other.Z = remote_f32(a + 4); other.S = remote_f32(a + 8);
-      join(r, other, p.a);
-      if (TOP) k = merge_lanes(k, remote_u64(remote_address(&best[31 - lane], o)), lane);
+  if (ranks > 1) {
+    cluster_meet();
+    if (rank == 0 && warp == 0) {
+      if (lane > 0 && lane < ranks) {
+        const uint32_t a = remote_address(&block_sum, lane);
+        sum = Running{remote_f32(a), remote_f32(a + 4), remote_f32(a + 8)};
+      } else if (lane > 0) {
+        sum = Running{-INFINITY, 0.f, 0.f};
+      }
+      join_lanes<8>(sum, p.a);
+      if constexpr (TOP) {
+        uint64_t k = best[lane], o[7];
+#pragma unroll
+        for (int i = 0; i < 7; ++i) o[i] = i + 1 < (int)ranks ? remote_u64(remote_address(&best[31 - lane], i + 1)) : 0ull;
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+          if (i + 1 < (int)ranks) k = merge_lanes(k, o[i], lane);
+        __syncwarp();
+        best[lane] = k;
+      }
     }
-    const bool none = r.m == -INFINITY && r.Z == 0.f;     // every logit is -inf
-    const float log_z = logf(r.Z);
+  }
+  if (rank == 0 && warp == 0) {
+    sum.m = __shfl_sync(0xffffffffu, sum.m, 0);
+    sum.Z = __shfl_sync(0xffffffffu, sum.Z, 0);
+    sum.S = __shfl_sync(0xffffffffu, sum.S, 0);
+    const bool none = sum.m == -INFINITY && sum.Z == 0.f;  // every logit is -inf
+    const float log_z = logf(sum.Z);
     if (lane == 0) {
-      if (p.stats) { p.stats[2 * row] = r.m; p.stats[2 * row + 1] = r.Z; }
-      if (p.entropy) p.entropy[row] = none ? 0.f : log_z - r.S / r.Z * kLn2;
+      if (p.stats) { p.stats[2 * row] = sum.m; p.stats[2 * row + 1] = sum.Z; }
+      if (p.entropy) p.entropy[row] = none ? 0.f : log_z - sum.S / sum.Z * kLn2;
       if (p.logp) {
-        const long long target = p.tokens[row];
         float lp = 0.f;
         if (target >= p.vocab) lp = NAN;
-        else if (target >= 0) lp = none ? -INFINITY : (Elem<T>::get(x_row[target]) - r.m) * p.scale - log_z;
+        else if (target >= 0) lp = none ? -INFINITY : (target_logit - sum.m) * p.scale - log_z;
         p.logp[row] = lp;
       }
     }
     if (TOP && lane < p.top_k) {
-      p.top_logp[row * p.top_k + lane] = none ? -INFINITY : (k ? (key_logit(k) - r.m) * p.scale - log_z : NAN);
+      const uint64_t k = best[lane];
+      p.top_logp[row * p.top_k + lane] = none ? -INFINITY : (k ? (key_logit(k) - sum.m) * p.scale - log_z : NAN);
       p.top_index[row * p.top_k + lane] = k ? (long long)key_column(k) : lane;
     }
   }
@@ -386,19 +477,25 @@ __global__ void __launch_bounds__(256) token_logprobs_grad_kernel(LogprobGradPar
     const int tc = (target >= c0 && target < c1) ? (int)target : -1;
     auto grad = [&](float v, int col) {
       const float t = (v - base) * p.a;
-      const float d = ex2(t) * fmaf(B, fmaxf(t, kNoWeight), A);
+      const float d = ex2_gradual(t) * fmaf(B, fmaxf(t, kNoWeight), A);
       return col == tc ? d + hit : d;
     };
     if (VEC) {
-      for (int v0 = c0 + threadIdx.x * V; v0 < c1; v0 += 256 * V * U) {
+      // single elements up to the first 16-byte boundary (the same in both rows), vectors, single elements
+      const int off = (int)((reinterpret_cast<uintptr_t>(x + c0) & 15u) / sizeof(T));
+      const int head = min(c1 - c0, (V - off) % V);
+      const int b0 = c0 + head, b1 = b0 + (c1 - b0) / V * V;
+      if ((int)threadIdx.x < head) dx[c0 + threadIdx.x] = Elem<T>::put(grad(Elem<T>::get(x[c0 + threadIdx.x]), c0 + threadIdx.x));
+      if ((int)threadIdx.x < c1 - b1) dx[b1 + threadIdx.x] = Elem<T>::put(grad(Elem<T>::get(x[b1 + threadIdx.x]), b1 + threadIdx.x));
+      for (int v0 = b0 + threadIdx.x * V; v0 < b1; v0 += 256 * V * U) {
         uint4 raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (v0 + u * 256 * V < c1) raw[u] = __ldcs(reinterpret_cast<const uint4*>(x + v0 + u * 256 * V));
+          if (v0 + u * 256 * V < b1) raw[u] = __ldcs(reinterpret_cast<const uint4*>(x + v0 + u * 256 * V));
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int col = v0 + u * 256 * V;
-          if (col >= c1) break;
+          if (col >= b1) break;
           float e[V];
           Elem<T>::unpack(raw[u], e);
 #pragma unroll
@@ -511,7 +608,8 @@ int sgemm_cube_token_logprobs_backward(sgemm_cube_handle h, int rows, int vocab,
   p.dlogp = dlogp; p.dentropy = dentropy;
   p.dX = dlogits; p.lddx = lddl;
   const size_t e = elem_size(dtype);
-  p.vec = sgc::rows_take_vectors(logits, ld, vocab, e) && sgc::rows_take_vectors(dlogits, lddl, vocab, e);
+  // vectors where the two rows meet 16-byte boundaries at the same columns
+  p.vec = (reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(dlogits)) % 16 == 0 && (ld - lddl) * e % 16 == 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (dtype == SGEMM_CUBE_F32) return launch_grad<float>(h, p, st);
   if (dtype == SGEMM_CUBE_F16) return launch_grad<__half>(h, p, st);
