@@ -451,7 +451,7 @@ int sgemm_cube_layer_norm_backward(sgemm_cube_handle h, int rows, int cols, int 
  *                     columns; equal logits are ordered by column (both NULL iff top_k == 0)
  *   logits_dev      rows x vocab of `dtype`, row-major, any alignment; -inf marks a token that is not allowed
  *   tokens_dev      rows int64, or NULL with logp_dev NULL
- * 0 <= top_k <= 32 and <= vocab; vocab >= 1; scale positive and finite.  A row whose every logit is -inf has no
+ * 0 <= top_k <= 32 and <= vocab; vocab >= 1; 2^-30 <= scale <= 2^30.  A row whose every logit is -inf has no
  * distribution: logp and top_logp are -inf, entropy 0, top_index the first columns, stats {-inf, 0}, its
  * gradient zero.  A row that holds NaN or +inf gives NaN (top_index then names valid columns, no more).
  * Errors: INVALID_ARG, CUDA_ERROR. */

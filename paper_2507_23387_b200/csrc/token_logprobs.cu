@@ -5,9 +5,11 @@
 //   Z = sum exp(scale (x - m)),   S = sum exp(scale (x - m)) scale (x - m);
 // when m grows to m' both shrink by r = exp(scale (m - m')) and S also takes r scale (m - m') Z.  Then
 //   lse = scale m + log Z,   log p_t = scale (x_t - m) - log Z,   H = log Z - S / Z.
-// Bound by reading the logits once.  Exponentials run in base 2, t = (x - m) a with a = scale log2 e.  The difference
-// is taken first: one FMA with fl(m a) would save an instruction, but overflows where masked logits hold the
-// type's lowest value, and puts the rounding of m a into every term.
+// Bound by reading the logits once; with 16-bit logits as much by issuing instructions, so these are counted.
+// Exponentials run in base 2, a = scale log2 e: t = x a - M, M = fl(m a), is one FMA; what the rounding of M does to
+// every term alike is taken out of a thread's sums at the end.  Logits are cut at -2^60 (2^-30 <= scale <= 2^30), so
+// that -inf gives a weight of zero and no 0 * inf.  A thread whose largest logit is beyond +-2^59 (masked with the
+// type's lowest value, say) sums its columns again in the form (x - m) a, which neither overflows nor is cut.
 #include <type_traits>
 
 #include "ctx.cuh"
@@ -21,6 +23,8 @@ constexpr int kTopMax = 32;
 constexpr int kCandidates = 256;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kNoWeight = -160.f;      // 2^-160 is zero in FP32: exponents are cut there where they are factors
+constexpr float kLowestLogit = -1152921504606846976.f;    // -2^60
+constexpr float kFarLogit = 576460752303423488.f;         // 2^59
 
 // 2^t, zero below 2^-126: in a sum such weights are nothing beside the row's largest, which is 1, and keeping them
 // takes three more instructions.
@@ -132,35 +136,80 @@ __device__ __forceinline__ void join_lanes(Running& r, float a) {
 }
 
 // The same for one thread while it goes through its columns: even and odd elements apart, so that the packed
-// instructions apply (half the issue slots: with 16-bit logits those are what is short).
+// instructions apply.  M = fl(m a), 0 while m is far from zero: -inf and other cut logits then weigh nothing.
 struct ThreadSums {
-  float m;
+  float m, M;
   Two Z, S;
   __device__ __forceinline__ void raise(float top, float a) {            // top > m
-    const float d = (m - top) * a;
-    const float f = ex2(d);                      // zero when m was -inf
-    const float c = fmaxf(d, kNoWeight);
-    S = fma2(two(c, c), Z, S) * two(f, f);
+    const float to = fabsf(top) < kFarLogit ? top * a : 0.f;
+    const float d = fmaxf(M - to, kNoWeight);
+    const float f = fabsf(m) < kFarLogit ? ex2(d) : 0.f;         // 0 times the sums, not 0: NaN stays
+    S = fma2(two(d, d), Z, S) * two(f, f);
     Z = Z * two(f, f);
     m = top;
+    M = to;
   }
-  // -m, or 0 while m is -inf (then the elements are -inf or NaN)
-  __device__ __forceinline__ float minus_m() const { return m == -INFINITY ? 0.f : -m; }
-  __device__ __forceinline__ void add(float x0, float x1, float minus, float a) {
-    const Two t = (two(x0, x1) + two(minus, minus)) * two(a, a);
+  // x >= kLowestLogit or NaN
+  __device__ __forceinline__ void add(float x0, float x1, Two a, Two minus_m) {
+    const Two t = fma2(two(x0, x1), a, minus_m);
     float t0, t1;
     parts_of(t, t0, t1);
     const Two e = two(ex2(t0), ex2(t1));
     Z = Z + e;
-    S = fma2(e, two(fmaxf(t0, kNoWeight), fmaxf(t1, kNoWeight)), S);
+    S = fma2(e, t, S);
   }
-  __device__ __forceinline__ Running sum() const {
+  // with the rounding of M taken out: t is too large by lo = m a - M
+  __device__ __forceinline__ Running sum(float a) const {
     float z0, z1, s0, s1;
     parts_of(Z, z0, z1);
     parts_of(S, s0, s1);
-    return Running{m, z0 + z1, s0 + s1};
+    const float lo = fabsf(m) < kFarLogit ? fmaf(m, a, -M) : 0.f;
+    const float f = ex2(-lo), z = z0 + z1;
+    return Running{m, z * f, fmaf(-lo, z, s0 + s1) * f};
   }
 };
+// A logit as ThreadSums takes it; NaN stays.
+__device__ __forceinline__ float cut_logit(float x) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(kLowestLogit));
+  return y;
+}
+// The same for a word of elements, where the type allows it (FP16 has no -2^60: its elements are cut one by one).
+template <typename T>
+__device__ __forceinline__ uint32_t cut_word(uint32_t w) {
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+    const uint32_t low = 0xDD80DD80u;                                       // -2^60 twice
+    const __nv_bfloat162 m =
+        __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&w), *reinterpret_cast<const __nv_bfloat162*>(&low));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  }
+  return w;
+}
+
+// The largest of the elements in a word, or of two words element by element; a NaN loses against a number.
+template <typename T>
+__device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b) {
+  if constexpr (sizeof(T) == 4) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  } else if constexpr (std::is_same<T, __half>::value) {
+    const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  } else {
+    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  }
+}
+template <typename T>
+__device__ __forceinline__ float max_of_word(uint32_t w) {
+  if constexpr (sizeof(T) == 4) {
+    return __uint_as_float(w);
+  } else if constexpr (std::is_same<T, __half>::value) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return fmaxf(f.x, f.y);
+  } else {
+    return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  }
+}
 
 // Four 32-bit words of -inf elements.
 template <typename T>
@@ -257,9 +306,31 @@ __device__ __forceinline__ void for_columns_above(const Piece<T>& piece, int c0,
   }
 }
 
+// A thread's sums where its largest logit m is far from zero.
+template <typename T>
+__device__ __forceinline__ Running sum_far(const Piece<T>& piece, int t, float m, float a) {
+  constexpr int V = Elem<T>::kVec;
+  Running r{m, 0.f, 0.f};
+  auto add = [&](float x) {
+    const float d = (x - m) * a;
+    const float e = ex2(d);
+    r.Z += e;
+    r.S = fmaf(e, fmaxf(d, kNoWeight), r.S);
+  };
+  if (t < piece.head) add(Elem<T>::get(piece.x[t]));
+  for (int v = t; v < piece.vecs; v += kLpThreads) {
+    float e[V];
+    Elem<T>::unpack(__ldg(piece.vec(v)), e);
+#pragma unroll
+    for (int q = 0; q < V; ++q) add(e[q]);
+  }
+  if (t < piece.tail) add(Elem<T>::get(piece.x[piece.head + piece.vecs * V + t]));
+  return r;
+}
+
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(LogprobParams p) {
-  constexpr int V = Elem<T>::kVec, U = 16 / V;           // 16 elements of a thread in flight
+  constexpr int V = Elem<T>::kVec, U = 4;                // 64 bytes of a thread are a batch, another is in flight
   __shared__ Running parts[kLpWarps];
   __shared__ Running block_sum;
   __shared__ uint64_t list[TOP ? kLpWarps : 1][32];
@@ -282,7 +353,9 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(LogprobParam
     if (target >= 0 && target < p.vocab) target_logit = Elem<T>::get(x_row[target]);
   }
 
-  ThreadSums r{-INFINITY, two(0.f, 0.f), two(0.f, 0.f)};
+  ThreadSums r{-INFINITY, 0.f, two(0.f, 0.f), two(0.f, 0.f)};
+  const Two a2 = two(p.a, p.a);
+  auto add_single = [&](float x) { r.add(cut_logit(x), kLowestLogit, a2, two(-r.M, -r.M)); };
   int at = -1;                                           // where m was met: -1 nowhere, 0 front, 1 + batch, then the rest
   const int batches = (piece.vecs + kLpThreads * U - 1) / (kLpThreads * U);
   uint4 next[U];
@@ -296,31 +369,39 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(LogprobParam
   if (t < piece.head) {
     const float x = Elem<T>::get(piece.x[t]);
     if (x > r.m) { r.raise(x, p.a); at = 0; }
-    r.add(x, -INFINITY, r.minus_m(), p.a);
+    add_single(x);
   }
   for (int b = 0; b < batches; ++b) {
-    float v[U][V];
+    uint4 raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) Elem<T>::unpack(next[u], v[u]);
+    for (int u = 0; u < U; ++u) raw[u] = next[u];
     if (b + 1 < batches) fetch(b + 1, next);
-    float top = v[0][0];
+    uint32_t w = raw[0].x;
 #pragma unroll
     for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int q = 0; q < V; ++q) top = fmaxf(top, v[u][q]);
+      w = max_words<T>(w, max_words<T>(max_words<T>(raw[u].x, raw[u].y), max_words<T>(raw[u].z, raw[u].w)));
+    const float top = max_of_word<T>(w);
     if (top > r.m) { r.raise(top, p.a); at = 1 + b; }
-    const float minus = r.minus_m();
+    const Two minus = two(-r.M, -r.M);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      float v[V];
+      raw[u].x = cut_word<T>(raw[u].x); raw[u].y = cut_word<T>(raw[u].y);
+      raw[u].z = cut_word<T>(raw[u].z); raw[u].w = cut_word<T>(raw[u].w);
+      Elem<T>::unpack(raw[u], v);
+      constexpr bool cut = std::is_same<T, __nv_bfloat16>::value;
 #pragma unroll
-      for (int q = 0; q < V; q += 2) r.add(v[u][q], v[u][q + 1], minus, p.a);
+      for (int q = 0; q < V; q += 2)
+        r.add(cut ? v[q] : cut_logit(v[q]), cut ? v[q + 1] : cut_logit(v[q + 1]), a2, minus);
+    }
   }
   if (t < piece.tail) {
     const float x = Elem<T>::get(piece.x[piece.head + piece.vecs * V + t]);
     if (x > r.m) { r.raise(x, p.a); at = 1 + batches; }
-    r.add(x, -INFINITY, r.minus_m(), p.a);
+    add_single(x);
   }
-  Running sum = r.sum();
+  Running sum = r.sum(p.a);
+  if (!(fabsf(r.m) < kFarLogit) && r.m != -INFINITY) sum = sum_far(piece, t, r.m, p.a);   // NaN for +inf
 
   if constexpr (TOP) {
     // The k largest of the threads' maxima bound the k largest elements from below, and hold every thread
@@ -515,7 +596,9 @@ namespace {
 
 template <typename T, bool TOP>
 int launch_logprobs(sgemm_cube_ctx* h, const sgc::LogprobParams& p, cudaStream_t st) {
-  // Few rows: a cluster of blocks shares a row, its pieces at least 4096 columns.
+  // Few rows: a cluster of blocks shares a row, its pieces at least 4096 columns.  (Two blocks a row for more rows
+  // than that, or blocks of 128 threads, measured slower: 1000 x 50001 BF16 with eight alternatives 54 and 34 us
+  // against 34, 512 x 131072 45 and 44 against 38.)
   int ranks = 1;
   while (ranks < 8 && (long long)p.rows * ranks < 2 * h->sm_count && p.vocab / (2 * ranks) >= 4096) ranks *= 2;
   cudaLaunchConfig_t cfg;
@@ -550,7 +633,7 @@ int launch_grad(sgemm_cube_ctx* h, sgc::LogprobGradParams p, cudaStream_t st) {
 size_t elem_size(int dtype) { return dtype == SGEMM_CUBE_F32 ? 4 : 2; }
 bool bad_dtype(int dtype) { return dtype < SGEMM_CUBE_F32 || dtype > SGEMM_CUBE_BF16; }
 bool off_elem(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % elem_size(dtype) != 0; }
-bool bad_scale(float s) { return !(s > 0.f && s <= 3.0e38f); }
+bool bad_scale(float s) { return !(s >= 0x1p-30f && s <= 0x1p30f); }
 
 }  // namespace
 
