@@ -66,6 +66,7 @@ struct sgemm_cube_ctx {
   bool attrs_set = false;
   bool linear_ready = false;   // linear forms: kernel attributes set, co-resident 2-CTA clusters known
   int linear_pair_clusters = 0;
+  int pack_once_blocks = 0, dz_once_blocks[5] = {0, 0, 0, 0, 0};   // resident blocks of the one-launch packing kernels
 };
 
 inline int grow(void** buf, size_t* have, size_t want) {

@@ -74,21 +74,6 @@ constexpr int kNumConvWarps = SGC_CONV_WARPS;      // a multiple of 4 (see the c
 constexpr int kFusedThreads = ((kNumEpiWarps + kNumConvWarps + 4 + 3) / 4) * 128;
 constexpr uint32_t kTmemCols = 512;
 
-// error codes written to the device error word (which wait gave up)
-enum : unsigned int {
-  kErrProducerEmptyWait = 0x101,
-  kErrMmaFullWait = 0x102,
-  kErrMmaTmemEmptyWait = 0x103,
-  kErrEpiTmemFullWait = 0x104,
-  kErrDrainWait = 0x105,
-  kErrConvEmptyWait = 0x106,
-  kErrConvFullWait = 0x107,
-  kErrRelayWait = 0x108,
-  kErrTileEmptyWait = 0x109,
-  kErrTileFullWait = 0x10A,
-  kErrProbeWait = 0x1F0,
-};
-
 // Optional role timing (compile with -DSGC_ROLE_TIMING): CTA 0 adds the clocks each role spends in
 // its phases to a global table; used only for performance investigations.
 #ifdef SGC_ROLE_TIMING

@@ -9,7 +9,8 @@ namespace {
 using sgc::PackJob;
 
 // Words of the handle's device scratch that the packing kernels use: running maxima and block counts
-// of up to two jobs (left zero by every call), exponents of operands that a call packs itself.
+// of up to two jobs (left zero by every call; the cooperative kernels have theirs apart), exponents of operands
+// that a call packs itself.
 constexpr int kRangeWords = 20, kExpWords = 24;
 // then one count of finished slices a tile: split-K is taken for at most sm_count / 2 tiles
 constexpr int kArrivalWords = 32;
@@ -42,10 +43,59 @@ PackJob pack_job(int rows, int cols, const float* X, int64_t ldx, uint16_t* hi, 
 }
 long long elements(const PackJob& j) { return (long long)j.rows * j.cols; }
 
+sgc::GridWords* grid_words(sgemm_cube_ctx* h) { return reinterpret_cast<sgc::GridWords*>(h->err_dev + kRangeWords); }
+
+template <typename K>
+int resident_blocks(sgemm_cube_ctx* h, K kernel, int* cached) {
+  if (*cached == 0) {
+    int per_sm = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, 256, 0) != cudaSuccess) { cudaGetLastError(); per_sm = 0; }
+    *cached = per_sm > 0 ? per_sm * h->sm_count : -1;
+  }
+  return *cached;
+}
+template <typename... P, typename... A>
+int launch_cooperative(sgemm_cube_ctx* h, void (*kernel)(P...), dim3 grid, cudaStream_t st, A... args) {
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.stream = st;
+  cudaLaunchAttribute a;
+  a.id = cudaLaunchAttributeCooperative;
+  a.val.cooperative = 1;
+  cfg.attrs = &a;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) {
+    cudaGetLastError();
+    return SGEMM_CUBE_CUDA_ERROR;
+  }
+  h->launches++;
+  return SGEMM_CUBE_OK;
+}
+
 // Range and split of one job, or of two in the same launches (the blocks in proportion to the elements).
 int launch_pack(sgemm_cube_ctx* h, const PackJob* jobs, int n, cudaStream_t st) {
   const long long ea = elements(jobs[0]), eb = n == 2 ? elements(jobs[1]) : 0;
   const PackJob& b = jobs[n == 2 ? 1 : 0];
+  // one cooperative launch where the blocks that are resident at once hold everything
+  const long long items_a = (long long)jobs[0].rows * ((jobs[0].cols + 7) / 8);
+  const long long items_b = n == 2 ? (long long)b.rows * ((b.cols + 7) / 8) : 0;
+  const int resident = resident_blocks(h, sgc::pack_once_kernel, &h->pack_once_blocks);
+  long long once_a = (items_a + 255) / 256, once_b = (items_b + 255) / 256;
+  if (once_a + once_b > resident && n == 2) {            // fewer blocks with more items each, in proportion
+    once_b = (long long)((double)resident * (double)items_b / (double)(items_a + items_b) + 0.5);
+    once_b = once_b < 1 ? 1 : (once_b > resident - 1 ? resident - 1 : once_b);
+    once_a = resident - once_b;
+  } else if (once_a > resident) {
+    once_a = resident;
+  }
+  const long long held = 256ll * sgc::kOnceItems;
+  if (resident >= 2 && items_a <= once_a * held && items_b <= once_b * held) {
+    const int rc = launch_cooperative(h, sgc::pack_once_kernel, dim3((unsigned)(once_a + once_b), 1, 1), st, jobs[0], b,
+                                      (unsigned)once_a, grid_words(h), h->err_dev);
+    if (rc == SGEMM_CUBE_OK) return rc;                  // else: a device that is partly occupied by others
+  }
   for (int phase = 0; phase < 2; ++phase) {
     int blocks = blocks_for(h, (ea + eb) / (phase == 0 ? 16 : 8) + 1), blocks_a = blocks;
     if (n == 2) {
@@ -300,6 +350,11 @@ Packed words_of(const sgemm_cube_operand* o, int rows, int cols, Carve& c, int* 
 template <int ACT>
 int launch_dz(sgemm_cube_ctx* h, const PackJob& j, bool split, float* col_part, int chunks, int rows_per_chunk,
               float* dbias, cudaStream_t st) {
+  const dim3 once((unsigned)((j.cols + 127) / 128), (unsigned)((j.rows + sgc::kOnceRows - 1) / sgc::kOnceRows), 1);
+  if (split && (long long)once.x * once.y <= resident_blocks(h, sgc::dz_once_kernel<ACT>, &h->dz_once_blocks[ACT]) &&
+      launch_cooperative(h, sgc::dz_once_kernel<ACT>, once, st, j, col_part, dbias, grid_words(h), h->err_dev) ==
+          SGEMM_CUBE_OK)
+    return SGEMM_CUBE_OK;
   const dim3 grid((unsigned)((j.cols + 127) / 128), (unsigned)chunks, 1);
   sgc::dz_range_kernel<ACT><<<grid, 256, 0, st>>>(j, col_part, rows_per_chunk, split ? h->err_dev + kRangeWords : nullptr);
   int rc = launched(h);
@@ -427,11 +482,13 @@ int sgemm_cube_linear_backward(sgemm_cube_handle h, int M, int N, int K, const f
   if (K == 0) dX = dW = nullptr;                 // no elements
   const bool split = dX || dW;
   if (!split && !dbias) return SGEMM_CUBE_OK;
-  // Row chunks of the column sums: about eight blocks an SM in all, at least 32 rows a chunk.
+  // Row chunks of the column sums: about eight blocks an SM in all, at least kOnceRows rows a chunk.  That is what
+  // they have where the one-launch form fits (at most four blocks an SM), so both forms add in the same order.
   const int col_blocks = (N + 127) / 128;
   int chunks = (8 * h->sm_count + col_blocks - 1) / col_blocks;
-  if (chunks > (M + 31) / 32) chunks = (M + 31) / 32;
-  const int rows_per_chunk = (int)round_up((size_t)((M + chunks - 1) / chunks), 32);
+  const int most = (M + sgc::kOnceRows - 1) / sgc::kOnceRows;
+  if (chunks > most) chunks = most;
+  const int rows_per_chunk = (int)round_up((size_t)((M + chunks - 1) / chunks), sgc::kOnceRows);
   chunks = (M + rows_per_chunk - 1) / rows_per_chunk;
   PackJob jobs[2];
   int n_jobs = 0;

@@ -8,6 +8,7 @@
 #include <cuda_runtime.h>
 
 #include "linear_epilogue.cuh"
+#include "ptx_sm100.cuh"
 #include "split_math.cuh"
 
 namespace sgc {
@@ -257,6 +258,190 @@ dz_split_kernel(PackJob j, unsigned int sum_blocks, const float* __restrict__ pa
     add_column_parts(part, chunks, j.cols, dbias, (blockIdx.x - split_blocks) * 256 + threadIdx.x);
   else
     pack_items<ACT, true>(j, (long long)blockIdx.x * 256 + threadIdx.x, (long long)split_blocks * 256);
+}
+
+// ---------------------------------------------------------------------------------- one launch for both
+// Matrices that fit the registers of the blocks that are resident at once (32 elements a thread, 4.8 million in
+// all) are packed in one cooperative launch: every block reads its part once, the blocks agree on the largest
+// magnitude, and each splits what it holds.  Two launches and a second read take twice as long there
+// (777 x 1001 and 1001 x 2049 together 16 us).
+struct GridWords {             // zero between calls
+  unsigned int amax[2];        // of up to two jobs
+  unsigned int arrived, left;
+};
+
+// Publishes a block's largest magnitude for its job and waits for all blocks; returns the job's.  The last block to
+// leave clears the words.  The launch is cooperative, so all blocks run; the wait is bounded all the same.
+__device__ __forceinline__ bool agree_on_amax(uint32_t m, int job, GridWords* words, unsigned int* err, uint32_t& amax) {
+  __shared__ uint32_t warp_max[32];
+  __shared__ uint32_t result[2];
+  m = __reduce_max_sync(0xffffffffu, m);
+  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < (int)(blockDim.x >> 5); ++w) m = max(m, warp_max[w]);
+    const unsigned int blocks = gridDim.x * gridDim.y;
+    atomicMax(&words->amax[job], m);
+    __threadfence();
+    atomicAdd(&words->arrived, 1u);
+    const long long t0 = clock64();
+    unsigned int seen = 0;
+    bool ok = true;
+    while (true) {
+      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(&words->arrived) : "memory");
+      if (seen >= blocks) break;
+      if (clock64() - t0 > kWaitLimitClocks) { ok = false; break; }
+    }
+    if (ok) {
+      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(result[0]) : "l"(&words->amax[job]) : "memory");
+      __threadfence();
+      if (atomicAdd(&words->left, 1u) == blocks - 1) {
+        words->amax[0] = words->amax[1] = 0u;
+        words->arrived = words->left = 0u;
+      }
+    } else {
+      atomicExch(err, (unsigned int)kErrPackWait);
+    }
+    result[1] = ok;
+  }
+  __syncthreads();
+  amax = result[0];
+  return result[1] != 0;
+}
+
+constexpr int kOnceItems = 4;  // of 8 elements, a thread
+
+// The first `blocks_a` blocks take job a.
+__global__ void __launch_bounds__(256, 4)
+pack_once_kernel(PackJob a, PackJob b, unsigned int blocks_a, GridWords* words, unsigned int* err) {
+  const bool second = blockIdx.x >= blocks_a;
+  const PackJob& j = second ? b : a;
+  const unsigned int nblk = second ? gridDim.x - blocks_a : blocks_a;
+  const unsigned int blk = second ? blockIdx.x - blocks_a : blockIdx.x;
+  constexpr int U = kOnceItems;
+  const int per_row = (j.cols + 7) >> 3;
+  const int total = j.rows * per_row;                    // within 32 bits: the matrix is small
+  float v[U][8];
+  int row[U], col[U];
+  uint32_t m = 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int it = ((int)blk + u * (int)nblk) * 256 + (int)threadIdx.x;
+    row[u] = it < total ? it / per_row : -1;
+    col[u] = (it - row[u] * per_row) << 3;
+    if (row[u] < 0) col[u] = j.cols;
+    const float* src = j.X + (long long)max(row[u], 0) * j.ldx + col[u];
+    if (j.vec && col[u] + 8 <= j.cols) {
+      const float4 f = *reinterpret_cast<const float4*>(src);
+      const float4 g = *reinterpret_cast<const float4*>(src + 4);
+      v[u][0] = f.x; v[u][1] = f.y; v[u][2] = f.z; v[u][3] = f.w;
+      v[u][4] = g.x; v[u][5] = g.y; v[u][6] = g.z; v[u][7] = g.w;
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[u][q] = col[u] + q < j.cols ? src[q] : 0.f;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int q = 0; q < 8; ++q) m = max(m, finite_bits(v[u][q]));
+  uint32_t amax;
+  if (!agree_on_amax(m, second ? 1 : 0, words, err, amax)) return;
+  const int p = pack_exponent(amax);
+  if (blk == 0 && threadIdx.x == 0) *j.exp = p;
+  const float pre = pow2f(p), scale = pow2f(kPackScaleExp);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (row[u] < 0) continue;
+    uint4 h, l;
+    split_two(v[u][0] * pre, v[u][1] * pre, scale, h.x, l.x);
+    split_two(v[u][2] * pre, v[u][3] * pre, scale, h.y, l.y);
+    split_two(v[u][4] * pre, v[u][5] * pre, scale, h.z, l.z);
+    split_two(v[u][6] * pre, v[u][7] * pre, scale, h.w, l.w);
+    *reinterpret_cast<uint4*>(j.hi + row[u] * j.ldh + col[u]) = h;
+    *reinterpret_cast<uint4*>(j.lo + row[u] * j.ldh + col[u]) = l;
+  }
+}
+
+// The same for dz with its column sums: a block holds 128 columns x 64 rows, a thread four columns of eight rows.
+// grid (ceil(cols / 128), ceil(rows / 64)); the first row of blocks adds up the bias gradient.
+constexpr int kOnceRows = 64;
+template <int ACT>
+__global__ void __launch_bounds__(256, 4)
+dz_once_kernel(PackJob j, float* col_part, float* dbias, GridWords* words, unsigned int* err) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c0 = blockIdx.x * 128 + lane * 4;
+  constexpr int U = kOnceRows / 8;
+  float v[U][4];
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  uint32_t m = 0;
+  float z[U][4];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int r = blockIdx.y * kOnceRows + warp + 8 * u;
+    const float* x = j.X + (long long)r * j.ldx + c0;
+    const float* zp = ACT != kActNone ? j.Z + (long long)r * j.ldz + c0 : nullptr;
+    if (j.vec && r < j.rows && c0 < j.cols) {            // cols % 4 == 0: a lane has all four or none
+      const float4 f = *reinterpret_cast<const float4*>(x);
+      v[u][0] = f.x; v[u][1] = f.y; v[u][2] = f.z; v[u][3] = f.w;
+      if (ACT != kActNone) {
+        const float4 g = *reinterpret_cast<const float4*>(zp);
+        z[u][0] = g.x; z[u][1] = g.y; z[u][2] = g.z; z[u][3] = g.w;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const bool in = r < j.rows && c0 + q < j.cols;
+        v[u][q] = in ? x[q] : 0.f;
+        if (ACT != kActNone) z[u][q] = in ? zp[q] : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (ACT != kActNone) v[u][q] *= act_slope(ACT, z[u][q]);
+      m = max(m, finite_bits(v[u][q]));
+      sum[q] += v[u][q];
+    }
+  if (dbias) {
+    __shared__ float part[8][128];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) part[warp][lane * 4 + q] = sum[q];
+    __syncthreads();
+    const int t = threadIdx.x, c = blockIdx.x * 128 + t;
+    if (t < 128 && c < j.cols) {
+      float s = part[0][t];
+      for (int w = 1; w < 8; ++w) s += part[w][t];
+      col_part[(long long)blockIdx.y * j.cols + c] = s;
+    }
+    __threadfence();                                     // the partial rows, before the block arrives
+    __syncthreads();
+  }
+  uint32_t amax;
+  if (!agree_on_amax(m, 0, words, err, amax)) return;
+  const int p = pack_exponent(amax);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *j.exp = p;
+  const float pre = pow2f(p), scale = pow2f(kPackScaleExp);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int r = blockIdx.y * kOnceRows + warp + 8 * u;
+    if (r >= j.rows || c0 >= ((j.cols + 7) & ~7)) continue;
+    uint2 h, l;
+    split_two(v[u][0] * pre, v[u][1] * pre, scale, h.x, l.x);
+    split_two(v[u][2] * pre, v[u][3] * pre, scale, h.y, l.y);
+    *reinterpret_cast<uint2*>(j.hi + r * j.ldh + c0) = h;
+    *reinterpret_cast<uint2*>(j.lo + r * j.ldh + c0) = l;
+  }
+  if (dbias && blockIdx.y == 0 && threadIdx.x < 128) {
+    const int c = blockIdx.x * 128 + threadIdx.x;
+    if (c < j.cols) {
+      float s = __ldcg(col_part + c);
+      for (int k = 1; k < (int)gridDim.y; ++k) s += __ldcg(col_part + (long long)k * j.cols + c);
+      dbias[c] = s;
+    }
+  }
 }
 
 // The empty inner dimension: y = act(b) + R.

@@ -10,6 +10,22 @@
 
 namespace sgc {
 
+// error codes written to the device error word (which wait gave up)
+enum : unsigned int {
+  kErrProducerEmptyWait = 0x101,
+  kErrMmaFullWait = 0x102,
+  kErrMmaTmemEmptyWait = 0x103,
+  kErrEpiTmemFullWait = 0x104,
+  kErrDrainWait = 0x105,
+  kErrConvEmptyWait = 0x106,
+  kErrConvFullWait = 0x107,
+  kErrRelayWait = 0x108,
+  kErrTileEmptyWait = 0x109,
+  kErrTileFullWait = 0x10A,
+  kErrPackWait = 0x10B,
+  kErrProbeWait = 0x1F0,
+};
+
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }
