@@ -35,8 +35,7 @@ struct sgemm_cube_ctx {
   int sm_count = 0;
   unsigned int* err_dev = nullptr;   // [0] error word; [4..13] scratch of sgemm_cube_exponent_window;
                                      // [16..19] clocks and nanoseconds of the last timed tensor-core kernel;
-                                     // [20..27] ranges and exponents of the linear layer's packing;
-                                     // [32..32 + sm_count) finished slices of its split-K tiles
+                                     // [20..27] ranges and exponents of the linear layer's packing
   bool err_dev_has_clock = false;    // false for the static entry point's single error word
   void* ws = nullptr;          // unfused path: FP16 words of A and B, D_hh, D_x
   size_t ws_bytes = 0;
@@ -65,7 +64,7 @@ struct sgemm_cube_ctx {
   EncodeTiledFn encode = nullptr;
   bool attrs_set = false;
   bool linear_ready = false;   // linear forms: kernel attributes set, co-resident 2-CTA clusters known
-  int linear_pair_clusters = 0;
+  int linear_pair_clusters = 0, linear_slice_clusters[9] = {0};
   int pack_once_blocks = 0, dz_once_blocks[5] = {0, 0, 0, 0, 0};   // resident blocks of the one-launch packing kernels
 };
 

@@ -295,8 +295,9 @@ using TcParams = std::conditional_t<FORM == kFormProduct, TcGemmParams, TcLinear
 // Linear forms: warps 10-15 store.  The accumulate warps hold 128 sums a thread and have no registers left
 // for bias, activation and residual, and while they work on those the tensor core waits; so they put a
 // finished tile into scratch (two tiles of 128 KB a block, which stay in L2) and go on with the next
-// product, and six warps that have nothing else to do carry it to Y.  With split-K the scratch holds every
-// slice's tile, and the block that finishes a tile's last slice adds them up, in slice order.
+// product, and six warps that have nothing else to do carry it to Y.  With split-K the slices of a tile are the
+// blocks of a cluster: the scratch holds every slice's tile, and when all are there each block adds the slices, in
+// order, for its share of the tile.
 constexpr int kFirstStoreWarp = 10;
 constexpr int kNumStoreWarps = 6;
 constexpr int kLinearThreads = (kFirstStoreWarp + kNumStoreWarps) * 32;
@@ -347,15 +348,14 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
   constexpr int kTileBars = FORM == kFormProduct ? 0 : 2;
   uint64_t* tile_full_bar = bars + 2 * STAGES + 5 + 2 * kFusedBars;   // [2]  accumulate -> store warps
   uint64_t* tile_empty_bar = tile_full_bar + kTileBars;               // [2]  store -> accumulate warps
-  uint64_t* decided_bar = tile_empty_bar + kTileBars;                 // [2]  split-K: whether this block was last
+  uint64_t* slices_bar = tile_empty_bar + kTileBars;                 // [2]  split-K: every slice of the tile is there
   constexpr int kNumBars = 2 * STAGES + 5 + 2 * kFusedBars + 3 * kTileBars;
   uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
-  volatile uint32_t* was_last = tmem_base_slot + 2;                   // [2]
   volatile uint32_t* abort_flag = tmem_base_slot + 1;
   // PAIR: a wait that gives up also raises the peer's flag (shared::cluster address of the same slot)
   const uint32_t peer_abort =
       PAIR ? mapa_u32(smem_u32(tmem_base_slot + 1), cta_rank ^ 1u) : 0u;
-  static_assert(kNumBars * 8 + 16 <= 256, "barrier block");
+  static_assert(kNumBars * 8 + 8 <= 256, "barrier block");
   uint8_t* store_staging = smem + Cfg::RING_BYTES + 256;   // epilogue transposition buffers
 
   const int warp = threadIdx.x >> 5;
@@ -392,7 +392,7 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
     for (int s = 0; s < kTileBars; ++s) {
       mbar_init(&tile_full_bar[s], kNumEpiWarps);
       mbar_init(&tile_empty_bar[s], kNumStoreWarps);
-      mbar_init(&decided_bar[s], 1);
+      mbar_init(&slices_bar[s], FORM == kFormProduct ? 1 : max(1, p.ksplit));
     }
     mbar_init(drain_bar, 1);
     *abort_flag = 0u;
@@ -408,7 +408,8 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
   }
   tc_fence_before_sync();
   __syncthreads();
-  if (PAIR) cluster_sync_all();      // the peer's barriers are initialised before anyone signals them
+  // the peers' barriers are initialised before anyone signals them
+  if (PAIR || (FORM != kFormProduct && p.ksplit > 1)) cluster_sync_all();
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_base_slot;
 
@@ -416,25 +417,40 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
   const int num_m = PAIR ? (p.M + 2 * kBM - 1) / (2 * kBM) : (p.M + kBM - 1) / kBM;
   const int num_n = (p.N + kBN - 1) / kBN;
   const int num_tiles = num_m * num_n;
-  const int first_tile = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
-  const int tile_stride = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+  const int ksplit = FUSED ? 1 : p.ksplit;
+  // Linear forms with split-K: a cluster of `ksplit` blocks works on one tile, block `slice_rank` on its slice.
+  const bool in_cluster = FORM != kFormProduct && ksplit > 1;
+  const int blocks_per_tile = PAIR ? 2 : (in_cluster ? ksplit : 1);
+  const int slice_rank = in_cluster ? (int)cluster_ctarank() : 0;
+  const int first_tile = (int)blockIdx.x / blocks_per_tile;
+  const int tile_stride = (int)gridDim.x / blocks_per_tile;
   auto tile_rc = [&](int tile, int& tm, int& tn) {     // tm in units of 128 rows, tn of 256 columns
     tile_coords(tile, num_m, num_n, tm, tn, PAIR ? SGC_PAIR_GROUP : 16);
     if (PAIR) tm = tm * 2 + (int)cta_rank;
   };
   const int num_kb = (p.K + BK - 1) / BK;                      // pipeline stages per tile
-  const int ksplit = FUSED ? 1 : p.ksplit;
-  const int num_units = num_tiles * ksplit;
+  const int num_units = in_cluster ? num_tiles : num_tiles * ksplit;
   // Work unit -> tile coordinates and its range of stages [kb0, kb1).
   auto unit_rc = [&](int unit, int& tm, int& tn, int& kb0, int& kb1, int& slice) {
-    slice = unit / num_tiles;
-    tile_rc(unit - slice * num_tiles, tm, tn);
+    slice = in_cluster ? slice_rank : unit / num_tiles;
+    tile_rc(in_cluster ? unit : unit - slice * num_tiles, tm, tn);
     kb0 = (ksplit > 1) ? slice * p.kslice_blocks : 0;
     kb1 = (ksplit > 1) ? min(num_kb, kb0 + p.kslice_blocks) : num_kb;
   };
-  // Linear forms: where the sums of a unit wait (slice 0 of the tile, for the block that adds the slices).
-  [[maybe_unused]] auto scratch_tile = [&](int unit, int slice, uint32_t t) -> long long {
-    return ksplit > 1 ? (long long)(unit % num_tiles) * ksplit + slice : (long long)blockIdx.x * 2 + t;
+  // Linear forms: where the sums of a unit wait (with split-K: slice 0 of its tile, the others behind it).
+  [[maybe_unused]] auto scratch_tile = [&](int unit, uint32_t t) -> long long {
+    return in_cluster ? (long long)unit * ksplit : (long long)blockIdx.x * 2 + t;
+  };
+  // A block's share of a tile: worker w of `workers` is one of this many in the whole cluster.
+  [[maybe_unused]] auto carry_tile = [&](int unit, uint32_t t, int tm, int tn, int w, int workers) {
+    if constexpr (FORM != kFormProduct) {
+      float* tile = p.ep.tiles + scratch_tile(unit, t) * kTileFloats;
+      const int first = slice_rank * workers + w, step = ksplit * workers;
+      if (p.ep.vec)
+        linear_store_blocks(p.ep, p.D, p.ldd, p.M, p.N, tile, ksplit, kTileFloats, tm * kBM, tn * kBN, first, step, lane);
+      else
+        linear_store_rows(p.ep, p.D, p.ldd, p.M, p.N, tile, ksplit, kTileFloats, tm * kBM, tn * kBN, first, step, lane);
+    }
   };
   const int chunk = p.kchunk_blocks;                           // stages per k-block g
   // Reordered elementwise order, fast form: a k-block's value P_x / s_f + P_hh is formed inside one
@@ -688,26 +704,35 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
         if constexpr (FORM == kFormProduct) {
           store_tile(p.D, p.ldd, vec_ok, (NTERMS == 1) ? p.accumulate : 0);
         } else {
-          if (p.ep.tiles == nullptr) {
-            const PowerBack back = power_back(p.ep.exp_a, p.ep.exp_b);
-#pragma unroll
-            for (int j = 0; j < 128; ++j) S[j] = back(S[j]);
-            store_tile(p.D, p.ldd, vec_ok, 0);
-          } else {
-            const int t = (int)(tiles_done & 1);
+          const bool direct = p.ep.tiles == nullptr;
+          const int t = (int)(tiles_done & 1);
+          float* tile = p.D;
+          if (!direct) {
             if (!mbar_wait_bounded(&tile_empty_bar[t], ((tiles_done >> 1) & 1) ^ 1, abort_flag, p.err,
                                    kErrTileEmptyWait, peer_abort)) {
               ok = false;
               break;
             }
-            float* tile = p.ep.tiles + scratch_tile(unit, slice, t) * kTileFloats;
+            tile = p.ep.tiles + (scratch_tile(unit, t) + slice_rank) * kTileFloats;
+          }
+          if (direct || !p.ep.vec) {
+            // Straight to Y, with the way back; or along rows to the scratch of unaligned matrices, whose origin
+            // is set back by the row and column that store_tile addresses.
+            if (direct) {
+              const PowerBack back = power_back(p.ep.exp_a, p.ep.exp_b);
+#pragma unroll
+              for (int j = 0; j < 128; ++j) S[j] = back(S[j]);
+            }
+            store_tile(direct ? tile : tile - ((long long)tm * kBM * kBN + tn * kBN), direct ? p.ldd : (long long)kBN,
+                       direct ? vec_ok : true, 0);
+          } else {
 #pragma unroll
             for (int c = 0; c < 32; ++c)
               *tile_slot(tile, half * 32 + c, quarter * 32 + lane) =
                   make_float4(S[4 * c], S[4 * c + 1], S[4 * c + 2], S[4 * c + 3]);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&tile_full_bar[t]);
           }
+          __syncwarp();
+          if (!direct && lane == 0) mbar_arrive(&tile_full_bar[t]);
           ++tiles_done;
         }
       }
@@ -719,13 +744,12 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
         int tm, tn, kb0, kb1, slice;
         unit_rc(first_tile + (int)it * tile_stride, tm, tn, kb0, kb1, slice);
         // the last tile: nothing is left to overlap with, so the accumulate warps lend a hand
-        uint64_t* bar = (ksplit > 1 ? decided_bar : tile_full_bar) + (it & 1);
-        if (mbar_wait_bounded(bar, (it >> 1) & 1, abort_flag, p.err, kErrTileFullWait, peer_abort) &&
-            (ksplit == 1 || was_last[it & 1]))
-          linear_store_blocks(p.ep, p.D, p.ldd, p.M, p.N,
-                              p.ep.tiles + scratch_tile(first_tile + (int)it * tile_stride, 0, it & 1) * kTileFloats,
-                              ksplit, kTileFloats, tm * kBM, tn * kBN, kNumStoreWarps + warp,
-                              kNumStoreWarps + kNumEpiWarps, lane);
+        const int unit = first_tile + (int)it * tile_stride;
+        const bool there = in_cluster ? mbar_wait_bounded_cluster(&slices_bar[it & 1], (it >> 1) & 1, abort_flag, p.err,
+                                                                  kErrTileFullWait, peer_abort)
+                                      : mbar_wait_bounded(&tile_full_bar[it & 1], (it >> 1) & 1, abort_flag, p.err,
+                                                          kErrTileFullWait, peer_abort);
+        if (there) carry_tile(unit, it & 1, tm, tn, kNumStoreWarps + warp, kNumStoreWarps + kNumEpiWarps);
       }
     }
   } else if (warp == kMmaWarp) {
@@ -794,6 +818,8 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
             SGC_TADD(4, blockIdx.x == 0);
             tc_fence_after_sync();
             st = smem_u32(smem + s * Cfg::STAGE_BYTES);
+            // (in a cluster the address carries the CTA's rank, which would reach into the descriptor's next field)
+            if (FORM != kFormProduct) st &= 0x3FFFFu;
             return true;
           };
           // lo_A hi_B and hi_A lo_B of one stage into the correction accumulator.
@@ -1194,26 +1220,18 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
           unit_rc(unit, tm, tn, kb0, kb1, slice);
           const int t = (int)(it & 1);
           if (!mbar_wait_bounded(&tile_full_bar[t], (it >> 1) & 1, abort_flag, p.err, kErrTileFullWait, peer_abort)) break;
-          bool store = true;
-          if (ksplit > 1) {
-            // The block's tile is complete: say so, and learn whether the tile's other slices are.  One
-            // thread's fences and atomic stand for the whole block (it has waited for every warp's stores).
-            if (warp == kFirstStoreWarp && lane == 0) {
-              unsigned int* count = p.ep.arrivals + unit % num_tiles;
+          if (in_cluster) {
+            // This block's slice is complete (every warp's stores have been waited for): say so to every block of the
+            // cluster, then wait for theirs.  The fence makes the slice visible before the arrivals are.
+            if (warp == kFirstStoreWarp) {
               __threadfence();
-              const bool last = atomicAdd(count, 1u) == (unsigned int)ksplit - 1;
-              if (last) *count = 0u;
-              __threadfence();
-              was_last[t] = last;
-              mbar_arrive(&decided_bar[t]);
+              if (lane < ksplit) mbar_arrive_cluster_relaxed(mapa_u32(smem_u32(&slices_bar[t]), (uint32_t)lane));
             }
-            if (!mbar_wait_bounded(&decided_bar[t], (it >> 1) & 1, abort_flag, p.err, kErrTileFullWait, peer_abort)) break;
-            store = was_last[t] != 0;
+            if (!mbar_wait_bounded_cluster(&slices_bar[t], (it >> 1) & 1, abort_flag, p.err, kErrTileFullWait, peer_abort))
+              break;
           }
-          if (store)
-            linear_store_blocks(p.ep, p.D, p.ldd, p.M, p.N, p.ep.tiles + scratch_tile(unit, 0, t) * kTileFloats, ksplit,
-                                kTileFloats, tm * kBM, tn * kBN, warp - kFirstStoreWarp,
-                                unit + tile_stride < num_units ? kNumStoreWarps : kNumStoreWarps + kNumEpiWarps, lane);
+          const bool last = unit + tile_stride >= num_units;
+          carry_tile(unit, t, tm, tn, warp - kFirstStoreWarp, last ? kNumStoreWarps + kNumEpiWarps : kNumStoreWarps);
           __syncwarp();
           if (lane == 0) mbar_arrive(&tile_empty_bar[t]);
         }
@@ -1238,7 +1256,7 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
     atomicAdd(&g_role_timing[10], ns1 - sgc_k_ns0);
   }
 #endif
-  if (PAIR) cluster_sync_all();      // neither CTA exits (or frees TMEM) while its peer still runs
+  if (PAIR || in_cluster) cluster_sync_all();   // no CTA exits (or frees TMEM) while a peer still runs
   if (warp == kMmaWarp) {
     __syncwarp();
     tc_fence_after_sync();

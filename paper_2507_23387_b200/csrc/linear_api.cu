@@ -12,8 +12,7 @@ using sgc::PackJob;
 // of up to two jobs (left zero by every call; the cooperative kernels have theirs apart), exponents of operands
 // that a call packs itself.
 constexpr int kRangeWords = 20, kExpWords = 24;
-// then one count of finished slices a tile: split-K is taken for at most sm_count / 2 tiles
-constexpr int kArrivalWords = 32;
+constexpr int kMaxSlices = 8;          // blocks of a portable cluster
 
 struct Packed {
   const uint16_t* hi;
@@ -113,40 +112,50 @@ int launch_pack(sgemm_cube_ctx* h, const PackJob* jobs, int n, cudaStream_t st) 
   return SGEMM_CUBE_OK;
 }
 
+cudaLaunchConfig_t linear_config(size_t smem, unsigned cluster, cudaLaunchAttribute* attr, cudaStream_t st) {
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.blockDim = dim3(sgc::kLinearThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  if (cluster > 1) {
+    attr->id = cudaLaunchAttributeClusterDimension;
+    attr->val.clusterDim.x = cluster; attr->val.clusterDim.y = 1; attr->val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+  }
+  return cfg;
+}
+// Kernel attributes, and how many clusters of pairs and of 2 to 8 split-K blocks are resident at once (the fewest
+// over the forms).
 template <int FORM, bool PAIR>
-int linear_attrs(sgemm_cube_ctx* h, int* clusters) {
+int linear_attrs(sgemm_cube_ctx* h) {
   auto kernel = sgc::tc_gemm_kernel<3, false, PAIR, false, FORM>;
-  using Cfg = sgc::TcCfg<3, PAIR, false>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::SMEM_BYTES) != cudaSuccess) {
+  constexpr size_t smem = sgc::TcCfg<3, PAIR, false>::SMEM_BYTES;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
     cudaGetLastError();
     return SGEMM_CUBE_CUDA_ERROR;
   }
-  if (PAIR) {
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
+  for (int c = 2; c <= (PAIR ? 2 : kMaxSlices); ++c) {
     cudaLaunchAttribute a;
-    a.id = cudaLaunchAttributeClusterDimension;
-    a.val.clusterDim.x = 2; a.val.clusterDim.y = 1; a.val.clusterDim.z = 1;
-    cfg.gridDim = dim3(2 * h->sm_count, 1, 1);
-    cfg.blockDim = dim3(sgc::kLinearThreads, 1, 1);
-    cfg.dynamicSmemBytes = Cfg::SMEM_BYTES;
-    cfg.attrs = &a;
-    cfg.numAttrs = 1;
+    cudaLaunchConfig_t cfg = linear_config(smem, (unsigned)c, &a, nullptr);
+    cfg.gridDim = dim3((unsigned)(c * h->sm_count), 1, 1);
     int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
-    *clusters = n;
+    int& least = PAIR ? h->linear_pair_clusters : h->linear_slice_clusters[c];
+    if (n < least) least = n;
   }
   return SGEMM_CUBE_OK;
 }
 int linear_setup(sgemm_cube_ctx* h) {
   if (h->linear_ready) return SGEMM_CUBE_OK;
-  int rc, c[3] = {0, 0, 0};
-  if ((rc = linear_attrs<sgc::kFormKM, false>(h, nullptr)) || (rc = linear_attrs<sgc::kFormKK, false>(h, nullptr)) ||
-      (rc = linear_attrs<sgc::kFormMM, false>(h, nullptr)) || (rc = linear_attrs<sgc::kFormKM, true>(h, c)) ||
-      (rc = linear_attrs<sgc::kFormKK, true>(h, c + 1)) || (rc = linear_attrs<sgc::kFormMM, true>(h, c + 2)))
+  h->linear_pair_clusters = h->sm_count;
+  for (int& n : h->linear_slice_clusters) n = h->sm_count;
+  int rc;
+  if ((rc = linear_attrs<sgc::kFormKM, false>(h)) || (rc = linear_attrs<sgc::kFormKK, false>(h)) ||
+      (rc = linear_attrs<sgc::kFormMM, false>(h)) || (rc = linear_attrs<sgc::kFormKM, true>(h)) ||
+      (rc = linear_attrs<sgc::kFormKK, true>(h)) || (rc = linear_attrs<sgc::kFormMM, true>(h)))
     return rc;
-  h->linear_pair_clusters = c[0] < c[1] ? c[0] : c[1];
-  if (c[2] < h->linear_pair_clusters) h->linear_pair_clusters = c[2];
   h->linear_ready = true;
   return SGEMM_CUBE_OK;
 }
@@ -169,25 +178,13 @@ int launch_linear_kernel(sgemm_cube_ctx* h, const Packed& A, const Packed& B, co
               : make_map(h, &tm[2 + w], t, 2, b, p.K, p.N, B.ld, Cfg::BK, Cfg::BN_CTA, z);
     if (rc) return rc;
   }
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.blockDim = dim3(sgc::kLinearThreads, 1, 1);
-  cfg.dynamicSmemBytes = Cfg::SMEM_BYTES;
-  cfg.stream = st;
   cudaLaunchAttribute attr;
-  const int tiles_n = (p.N + sgc::kBN - 1) / sgc::kBN;
-  if (PAIR) {
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    const long long units = (long long)((p.M + 2 * sgc::kBM - 1) / (2 * sgc::kBM)) * tiles_n;
-    const int cap = h->linear_pair_clusters;
-    cfg.gridDim = dim3(2 * (unsigned)(units < cap ? units : cap), 1, 1);
-  } else {
-    const long long units = (long long)((p.M + sgc::kBM - 1) / sgc::kBM) * tiles_n * p.ksplit;
-    cfg.gridDim = dim3((unsigned)(units < h->sm_count ? units : h->sm_count), 1, 1);
-  }
+  const unsigned cluster = PAIR ? 2u : (unsigned)p.ksplit;
+  cudaLaunchConfig_t cfg = linear_config(Cfg::SMEM_BYTES, cluster, &attr, st);
+  const long long tiles = (long long)((p.M + (PAIR ? 2 : 1) * sgc::kBM - 1) / ((PAIR ? 2 : 1) * sgc::kBM)) *
+                          ((p.N + sgc::kBN - 1) / sgc::kBN);
+  const int cap = PAIR ? h->linear_pair_clusters : (cluster > 1 ? h->linear_slice_clusters[cluster] : h->sm_count);
+  cfg.gridDim = dim3(cluster * (unsigned)(tiles < cap ? tiles : cap), 1, 1);
   h->launches++;
   if (cudaLaunchKernelEx(&cfg, sgc::tc_gemm_kernel<3, false, PAIR, false, FORM>, tm[0], tm[1], tm[2], tm[3], p) !=
       cudaSuccess) {
@@ -197,18 +194,23 @@ int launch_linear_kernel(sgemm_cube_ctx* h, const Packed& A, const Packed& B, co
   return SGEMM_CUBE_OK;
 }
 
-// How many k slices: enough units to give most SMs one, when the 128 x 256 tiles leave half of them idle.
+// How many k slices, when the 128 x 256 tiles leave half of the SMs idle: the clusters that are resident at once go
+// through the tiles in turns, and a turn takes as long as its slice; the fewest slices among those that take the
+// least time.  A slice is at least two k-blocks.
 int linear_slices(const sgemm_cube_ctx* h, int M, int N, int K, int chunk_k) {
   if (!h->split_k) return 1;
   const long long tiles = (long long)((M + sgc::kBM - 1) / sgc::kBM) * ((N + sgc::kBN - 1) / sgc::kBN);
   if (tiles * 2 > h->sm_count) return 1;
   const int chunks = (K + chunk_k - 1) / chunk_k;
-  int want = (int)(h->sm_count / tiles);
-  if (want > 16) want = 16;
-  if (want > chunks / 2) want = chunks / 2;
-  if (want < 2) return 1;
-  const int per = (chunks + want - 1) / want;
-  return (chunks + per - 1) / per;
+  int best = 1;
+  long long best_time = chunks;
+  for (int s = 2; s <= kMaxSlices && 2 * s <= chunks; ++s) {
+    const int per = (chunks + s - 1) / s, clusters = h->linear_slice_clusters[s];
+    if (clusters < 1 || (chunks + per - 1) / per != s) continue;      // the last slice would be empty
+    const long long time = (tiles + clusters - 1) / clusters * per;
+    if (time < best_time) { best_time = time; best = s; }
+  }
+  return best;
 }
 
 // C (M x N) = epilogue of A B on packed operands, termwise.
@@ -242,8 +244,11 @@ int linear_product(sgemm_cube_ctx* h, int M, int N, int K, const Packed& A, cons
     p.ksplit = slices;
     p.kslice_blocks = (chunks + slices - 1) / slices * p.kchunk_blocks;
     p.ep.tiles = static_cast<float*>(h->part_ws);
-    p.ep.arrivals = h->err_dev + kArrivalWords;
-    return launch_linear_kernel<FORM, false>(h, A, B, p, st);
+    rc = launch_linear_kernel<FORM, false>(h, A, B, p, st);
+    if (rc != SGEMM_CUBE_CUDA_ERROR) return rc;
+    p.ksplit = 1;                                        // clusters that cannot be scheduled: whole k
+    p.kslice_blocks = 0;
+    p.ep.tiles = nullptr;
   }
   // Nothing but the way back to do: the accumulate warps store to Y themselves.
   if (ep.bias || ep.R || ep.Z || ep.act != SGEMM_CUBE_ACT_NONE) {

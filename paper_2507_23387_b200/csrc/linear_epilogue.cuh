@@ -103,11 +103,9 @@ struct LinearEpilogue {
   long long ldz;
   int act;
   int vec;                // Y, Z and R take 16-byte accesses
-  // Scratch tiles of 128 x 256 sums: two for every block, or (split-K) `ksplit` for every tile of Y, which the
-  // block that comes last to a tile adds up; `arrivals` counts them, one word a tile, zero between calls.
-  // Null: the accumulate warps store to Y themselves.
+  // Scratch tiles of 128 x 256 sums: two for every block, or (split-K) `ksplit` for every tile of Y.  Null: the
+  // accumulate warps store to Y themselves.
   float* tiles;
-  unsigned int* arrivals;
 };
 
 // 2^-(p_a + p_b) as two FP32 factors (the sum of two exponents can leave the range of one).
@@ -135,6 +133,11 @@ __device__ __forceinline__ float4* tile_slot(float* tile, int col4, int row) {
   return reinterpret_cast<float4*>(tile) + col4 * 128 + row;
 }
 
+template <int ACT, int N>
+__device__ __forceinline__ void act_each(float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = act_value(ACT, v[i]);
+}
 template <int ACT>
 __device__ __forceinline__ void act_four(float4& v) {
   v.x = act_value(ACT, v.x); v.y = act_value(ACT, v.y); v.z = act_value(ACT, v.z); v.w = act_value(ACT, v.w);
@@ -249,6 +252,60 @@ __device__ __forceinline__ void linear_store_blocks(const LinearEpilogue& e, flo
     if (e.R) {
 #pragma unroll
       for (int u = 0; u < U; ++u) { v[u].x += res[u].x; v[u].y += res[u].y; v[u].z += res[u].z; v[u].w += res[u].w; }
+    }
+    store(Y, ldy);
+  }
+}
+
+// The same where Y, Z or R cannot be met with 16 bytes: the scratch tile is row-major, 256 columns, and a warp takes half
+// of two rows at a time, lane = one column in 32, so that its accesses stay in one or two lines.
+__device__ __forceinline__ void linear_store_rows(const LinearEpilogue& e, float* Y, long long ldy, int M, int N,
+                                                  const float* tile, int slices, long long stride, int row0, int col0,
+                                                  int first, int step, int lane) {
+  constexpr int U = 2, C = 4;                                // rows, and columns of a lane
+  const PowerBack back = power_back(e.exp_a, e.exp_b);
+  const int blocks = (min(128, M - row0) + U - 1) / U * 2;
+#pragma unroll 1
+  for (int b = first; b < blocks; b += step) {
+    const int r = (b >> 1) * U, row = row0 + r, c = (b & 1) * 128 + lane, col = col0 + c;
+    if (col0 + (b & 1) * 128 >= N) continue;
+    const float* src = tile + r * 256 + c;
+    float v[U * C], res[U * C], bias[C];
+#pragma unroll
+    for (int i = 0; i < U * C; ++i) v[i] = __ldcg(src + (i / C) * 256 + (i % C) * 32);
+#pragma unroll
+    for (int q = 0; q < C; ++q) bias[q] = e.bias && col + q * 32 < N ? __ldg(e.bias + col + q * 32) : 0.f;
+    if (e.R) {
+#pragma unroll
+      for (int i = 0; i < U * C; ++i)
+        res[i] = row + i / C < M && col + (i % C) * 32 < N ? e.R[(row + i / C) * e.ldr + col + (i % C) * 32] : 0.f;
+    }
+#pragma unroll 1
+    for (int s = 1; s < slices; ++s) {
+      float f[U * C];
+#pragma unroll
+      for (int i = 0; i < U * C; ++i) f[i] = __ldcg(src + s * stride + (i / C) * 256 + (i % C) * 32);
+#pragma unroll
+      for (int i = 0; i < U * C; ++i) v[i] += f[i];
+    }
+    auto store = [&](float* out, long long ld) {
+#pragma unroll
+      for (int i = 0; i < U * C; ++i)
+        if (row + i / C < M && col + (i % C) * 32 < N) out[(row + i / C) * ld + col + (i % C) * 32] = v[i];
+    };
+#pragma unroll
+    for (int i = 0; i < U * C; ++i) v[i] = back(v[i]) + bias[i % C];
+    if (e.Z) store(e.Z, e.ldz);
+    switch (e.act) {
+      case kActRelu: act_each<kActRelu>(v); break;
+      case kActGelu: act_each<kActGelu>(v); break;
+      case kActGeluTanh: act_each<kActGeluTanh>(v); break;
+      case kActSilu: act_each<kActSilu>(v); break;
+      default: break;
+    }
+    if (e.R) {
+#pragma unroll
+      for (int i = 0; i < U * C; ++i) v[i] += res[i];
     }
     store(Y, ldy);
   }

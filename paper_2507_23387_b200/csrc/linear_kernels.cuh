@@ -290,6 +290,7 @@ __device__ __forceinline__ bool agree_on_amax(uint32_t m, int job, GridWords* wo
     while (true) {
       asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(&words->arrived) : "memory");
       if (seen >= blocks) break;
+      __nanosleep(32);                                   // the arrivals need the line, too
       if (clock64() - t0 > kWaitLimitClocks) { ok = false; break; }
     }
     if (ok) {

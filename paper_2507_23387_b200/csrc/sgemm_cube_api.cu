@@ -414,14 +414,13 @@ int sgemm_cube_create(sgemm_cube_handle* out, int device) {
     return SGEMM_CUBE_CUDA_ERROR;
   }
   h->encode = reinterpret_cast<EncodeTiledFn>(fn);
-  const size_t words = 32 + (size_t)h->sm_count;
-  if (cudaMalloc(reinterpret_cast<void**>(&h->err_dev), words * sizeof(unsigned int)) != cudaSuccess) {
+  if (cudaMalloc(reinterpret_cast<void**>(&h->err_dev), 32 * sizeof(unsigned int)) != cudaSuccess) {
     cudaGetLastError();
     delete h;
     return SGEMM_CUBE_ALLOC_FAILED;
   }
   // (waited for: the caller's streams need not be ordered after the default stream)
-  if (cudaMemset(h->err_dev, 0, words * sizeof(unsigned int)) != cudaSuccess ||
+  if (cudaMemset(h->err_dev, 0, 32 * sizeof(unsigned int)) != cudaSuccess ||
       cudaStreamSynchronize(nullptr) != cudaSuccess) {
     cudaFree(h->err_dev);
     delete h;
@@ -786,7 +785,7 @@ int sgemm_cube_check(sgemm_cube_handle h, void* stream, uint32_t* detail_out) {
   if (e) {
     cudaMemset(h->err_dev, 0, sizeof(e));
     // counts that a kernel which gave up has left behind
-    cudaMemset(h->err_dev + 20, 0, (12 + (size_t)h->sm_count) * sizeof(unsigned int));
+    cudaMemset(h->err_dev + 20, 0, 4 * sizeof(unsigned int));
     return SGEMM_CUBE_DEVICE_TIMEOUT;
   }
   return SGEMM_CUBE_OK;
