@@ -112,6 +112,38 @@ struct RowRegs {
     }
   }
 };
+// The same through shared memory, for vectors: a thread's own 16-byte slots, filled by asynchronous copies of the
+// thread itself, so nobody else has to be waited for, rows can be asked for several ahead, and the copies are under
+// way whatever the compiler does with the loads around them (it moved the loads into registers behind the arithmetic,
+// where registers were short).  `slots` is the thread's first of kWords, `pitch` uint4 apart.
+template <typename T, int PT>
+struct RowSlots {
+  static constexpr int kWords = PT / Elem<T>::kVec;
+  static __device__ __forceinline__ void ask(uint4* slots, int pitch, const T* row, int cols, int t, int threads) {
+    constexpr int V = Elem<T>::kVec;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const int c = (i * threads + t) * V;
+      const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(slots + i * pitch));
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"        // 0 bytes read: zeros
+                   ::"r"(dst), "l"(row + (c < cols ? c : 0)), "r"(c < cols ? 16 : 0) : "memory");
+    }
+  }
+  static __device__ __forceinline__ void get(const uint4* slots, int pitch, float (&v)[PT]) {
+    constexpr int V = Elem<T>::kVec;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      float e[V];
+      Elem<T>::unpack(slots[i * pitch], e);
+#pragma unroll
+      for (int q = 0; q < V; ++q) v[i * V + q] = e[q];
+    }
+  }
+};
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // The thread's entries of a vector of FP32 parameters, `fill` past the end or where there is none.  The vector is
 // read in 16-byte pieces where the rows are and it is aligned itself.
 template <typename T, int PT, bool VEC>

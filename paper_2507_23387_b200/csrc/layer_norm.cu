@@ -7,7 +7,7 @@
 // Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx, each once.  A row
 // lives in the registers of one group of warps between its load and its store, so the second moment is
 // taken about the mean (no cancellation of squares) without a second read.  Blocks are persistent: a
-// group asks for its next row before it works on the present one, and keeps its columns' weights (forward)
+// group asks for its next rows before it works on the present one, and keeps its columns' weights (forward)
 // or running sums of dw and db (backward) in registers all the way.
 #include "ctx.cuh"
 #include "elements.cuh"
@@ -15,6 +15,18 @@
 namespace sgc {
 
 constexpr int kPT = 16;         // elements of a row a thread holds
+
+// Aligned rows pass through shared memory: this many rows of a block's groups have slots there (three where they fit,
+// so that two are under way beside the present one).
+template <typename T, int WARPS>
+constexpr int slot_stages(int tensors) {
+  const size_t row = (size_t)tensors * kPT * sizeof(T) * (WARPS > 8 ? WARPS * 32 : 256);
+  return 3 * row <= 200 * 1024 ? 3 : (2 * row <= 200 * 1024 ? 2 : 1);
+}
+template <typename T, int WARPS, bool VEC, int TENSORS>
+constexpr int kStages = VEC ? slot_stages<T, WARPS>(TENSORS) : 0;
+template <typename T, int WARPS, bool VEC, int TENSORS>
+constexpr size_t kSlotBytes = (size_t)kStages<T, WARPS, VEC, TENSORS> * TENSORS * kPT * sizeof(T) * (WARPS > 8 ? WARPS * 32 : 256);
 
 // Sums over a row's group of warps.  `slot` alternates between two buffers, so one barrier a sum is enough.
 template <int WARPS, int N>
@@ -70,15 +82,37 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
   const long long step = (long long)gridDim.x * kGroups;
   long long row = (long long)blockIdx.x * kGroups + group;
   if (row >= p.rows) return;
+  constexpr int kBlock = WARPS > 8 ? WARPS * 32 : 256, kWords = VEC ? kPT / Elem<T>::kVec : 1;
+  constexpr int kRing = kStages<T, WARPS, VEC, 1>, kAhead = kRing - 1;
+  static_assert(!VEC || kRing == 3, "forward rows always fit three times");
+  extern __shared__ uint4 ring[];                      // [kRing][kWords][kBlock]
   RowRegs<T, kPT, VEC> next;
-  next.fetch(static_cast<const T*>(p.X) + row * p.ldx, p.cols, t, kThreads);
+  auto ask = [&](long long r, int s) {                 // an empty group past the end
+    if (r < p.rows)
+      RowSlots<T, kPT>::ask(ring + s * kWords * kBlock + threadIdx.x, kBlock, static_cast<const T*>(p.X) + r * p.ldx,
+                            p.cols, t, kThreads);
+    async_commit();
+  };
+  int stage = 0;
+  if constexpr (VEC) {
+    for (int a = 0; a < kAhead; ++a) ask(row + a * step, a);
+  } else {
+    next.fetch(static_cast<const T*>(p.X) + row * p.ldx, p.cols, t, kThreads);
+  }
   float w[kPT], b[kPT];
   load_params<T, kPT, VEC>(p.weight, 1.f, p.cols, t, kThreads, w);
   load_params<T, kPT, VEC>(p.bias, 0.f, p.cols, t, kThreads, b);
   for (; row < p.rows; row += step) {
     float v[kPT];
-    next.get(v);
-    if (row + step < p.rows) next.fetch(static_cast<const T*>(p.X) + (row + step) * p.ldx, p.cols, t, kThreads);
+    if constexpr (VEC) {
+      ask(row + kAhead * step, stage == 0 ? kAhead : stage - 1);
+      async_wait<kAhead>();
+      RowSlots<T, kPT>::get(ring + stage * kWords * kBlock + threadIdx.x, kBlock, v);
+      stage = stage == kAhead ? 0 : stage + 1;
+    } else {
+      next.get(v);
+      if (row + step < p.rows) next.fetch(static_cast<const T*>(p.X) + (row + step) * p.ldx, p.cols, t, kThreads);
+    }
     float s[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < kPT; ++i) s[0] += v[i];
@@ -133,7 +167,10 @@ __global__ void __launch_bounds__(1024) norm_forward_long_kernel(NormParams p) {
   }
 }
 
-// dx, and the block's partial sums of dw and db: a thread holds the same columns of every row.
+// dx, and the block's partial sums of dw and db: a thread holds the same columns of every row.  The longest aligned
+// rows (1024 threads, 64 registers each) stay in their slots and are read twice from there, for the sums and for dx;
+// shorter ones are held in registers with the weights (2048 x 16384 FP32 260 us held, 110 read twice; 8192 x 4096
+// 81 held, 90 read twice).
 template <typename T, int WARPS, bool VEC>
 __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 2) norm_backward_kernel(NormParams p) {
   constexpr int kGroups = WARPS >= 8 ? 1 : 8 / WARPS, kThreads = WARPS * 32;
@@ -146,43 +183,137 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
   float dw[kPT], db[kPT];
 #pragma unroll
   for (int i = 0; i < kPT; ++i) dw[i] = db[i] = 0.f;
-  RowRegs<T, kPT, VEC> next_x, next_g;
+  int slot = 0;
   float next_mean = 0.f, next_rstd = 0.f;
-  auto fetch = [&](long long r) {
-    next_x.fetch(static_cast<const T*>(p.X) + r * p.ldx, p.cols, t, kThreads);
-    next_g.fetch(static_cast<const T*>(p.dY) + r * p.lddy, p.cols, t, kThreads);
+  auto fetch_stats = [&](long long r) {
     next_mean = __ldg(p.mean_in + r);
     next_rstd = __ldg(p.rstd_in + r);
   };
-  if (row < p.rows) fetch(row);
-  int slot = 0;
-  for (; row < p.rows; row += step) {
-    float x[kPT], g[kPT];
-    next_x.get(x);
-    next_g.get(g);
-    const float mean = next_mean, rstd = next_rstd;
-    if (row + step < p.rows) fetch(row + step);
-    float s[2] = {0.f, 0.f};
-    {
-      float w[kPT];                                    // from L1: registers are short here
-      load_params<T, kPT, VEC>(p.weight, 1.f, p.cols, t, kThreads, w);
-#pragma unroll
-      for (int i = 0; i < kPT; ++i) {
-        x[i] = (x[i] - mean) * rstd;                   // n; columns past the end have g = 0
-        dw[i] = fmaf(g[i], x[i], dw[i]);
-        db[i] += g[i];
-        g[i] *= w[i];
-        s[0] += g[i];
-        s[1] = fmaf(g[i], x[i], s[1]);
+  if (row < p.rows) fetch_stats(row);
+  if constexpr (VEC) {
+    constexpr int V = Elem<T>::kVec, kWords = kPT / V, kBlock = WARPS > 8 ? WARPS * 32 : 256;
+    constexpr int kRing = kStages<T, WARPS, VEC, 2>;
+    extern __shared__ uint4 ring[];                    // [kRing][2][kWords][kBlock]
+    auto ask = [&](long long r, int s) {               // an empty group past the end
+      if (r < p.rows) {
+        uint4* to = ring + s * 2 * kWords * kBlock + threadIdx.x;
+        RowSlots<T, kPT>::ask(to, kBlock, static_cast<const T*>(p.X) + r * p.ldx, p.cols, t, kThreads);
+        RowSlots<T, kPT>::ask(to + kWords * kBlock, kBlock, static_cast<const T*>(p.dY) + r * p.lddy, p.cols, t, kThreads);
       }
-    }
-    if (!p.out) continue;
-    group_sum<WARPS>(s, buf[slot], group, wg, bar);
-    slot ^= 1;
-    const float mu = s[0] * inv_n, mun = s[1] * inv_n;
+      async_commit();
+    };
+    constexpr bool kHold = WARPS <= 16;
+    const bool wvec = (reinterpret_cast<uintptr_t>(p.weight) & 15u) == 0;
+    float w[kHold ? kPT : 1];
+    if constexpr (kHold) load_params<T, kPT, VEC>(p.weight, 1.f, p.cols, t, kThreads, w);
+    // n, dy and u = dy w of vector i of a row
+    auto vector_of = [&](const uint4* from, int i, float mean, float rstd, float (&n)[V], float (&g)[V], float (&u)[V]) {
+      Elem<T>::unpack(from[i * kBlock], n);
+      Elem<T>::unpack(from[(kWords + i) * kBlock], g);
+      const int c = (i * kThreads + t) * V;
 #pragma unroll
-    for (int i = 0; i < kPT; ++i) g[i] = rstd * (g[i] - mu - x[i] * mun);
-    store_row<T, kPT, VEC>(static_cast<T*>(p.out) + row * p.ldo, p.cols, t, kThreads, g);
+      for (int q = 0; q < V; ++q) n[q] = (n[q] - mean) * rstd;
+      if constexpr (kHold) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) u[q] = g[q] * w[i * V + q];
+      } else if (p.weight && c < p.cols) {
+        if (wvec) {
+#pragma unroll
+          for (int q = 0; q < V; q += 4) {
+            const float4 w = __ldg(reinterpret_cast<const float4*>(p.weight + c + q));
+            u[q] = g[q] * w.x; u[q + 1] = g[q + 1] * w.y; u[q + 2] = g[q + 2] * w.z; u[q + 3] = g[q + 3] * w.w;
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < V; ++q) u[q] = g[q] * __ldg(p.weight + c + q);
+        }
+      } else {
+#pragma unroll
+        for (int q = 0; q < V; ++q) u[q] = g[q];       // columns past the end: g = 0
+      }
+    };
+    int stage = 0;
+    for (int a = 0; a < (kRing > 1 ? kRing - 1 : 1); ++a) ask(row + a * step, a);
+    for (; row < p.rows; row += step) {
+      const float mean = next_mean, rstd = next_rstd;
+      if (kRing > 1) ask(row + (kRing - 1) * step, stage == 0 ? kRing - 1 : stage - 1);
+      if (row + step < p.rows) fetch_stats(row + step);
+      async_wait<(kRing > 1 ? kRing - 1 : 0)>();
+      const uint4* from = ring + stage * 2 * kWords * kBlock + threadIdx.x;
+      float s[2] = {0.f, 0.f};
+      float held_n[kHold ? kWords : 1][V], held_u[kHold ? kWords : 1][V];
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        float lone_n[V], lone_u[V], g[V];
+        float (&n)[V] = kHold ? held_n[kHold ? i : 0] : lone_n;
+        float (&u)[V] = kHold ? held_u[kHold ? i : 0] : lone_u;
+        vector_of(from, i, mean, rstd, n, g, u);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          dw[i * V + q] = fmaf(g[q], n[q], dw[i * V + q]);
+          db[i * V + q] += g[q];
+          s[0] += u[q];
+          s[1] = fmaf(u[q], n[q], s[1]);
+        }
+      }
+      if (p.out) {
+        group_sum<WARPS>(s, buf[slot], group, wg, bar);
+        slot ^= 1;
+        const float mu = s[0] * inv_n, mun = s[1] * inv_n;
+        T* out = static_cast<T*>(p.out) + row * p.ldo;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+          float lone_n[V], lone_u[V], g[V];
+          float (&n)[V] = kHold ? held_n[kHold ? i : 0] : lone_n;
+          float (&u)[V] = kHold ? held_u[kHold ? i : 0] : lone_u;
+          if (!kHold) vector_of(from, i, mean, rstd, n, g, u);
+#pragma unroll
+          for (int q = 0; q < V; ++q) u[q] = rstd * (u[q] - mu - n[q] * mun);
+          const int c = (i * kThreads + t) * V;
+          if (c < p.cols) *reinterpret_cast<uint4*>(out + c) = Elem<T>::pack(u);
+        }
+      }
+      if (kRing == 1) ask(row + step, 0);              // the thread has read its slots for the last time
+      stage = stage + 1 >= kRing ? 0 : stage + 1;
+    }
+  } else {
+    RowRegs<T, kPT, VEC> next_x, next_g;
+    auto fetch = [&](long long r) {
+      next_x.fetch(static_cast<const T*>(p.X) + r * p.ldx, p.cols, t, kThreads);
+      next_g.fetch(static_cast<const T*>(p.dY) + r * p.lddy, p.cols, t, kThreads);
+    };
+    if (row < p.rows) fetch(row);
+    for (; row < p.rows; row += step) {
+      float x[kPT], g[kPT];
+      next_x.get(x);
+      next_g.get(g);
+      const float mean = next_mean, rstd = next_rstd;
+      if (row + step < p.rows) {
+        fetch(row + step);
+        fetch_stats(row + step);
+      }
+      float s[2] = {0.f, 0.f};
+      {
+        float w[kPT];                                  // from L1: registers are short here
+        load_params<T, kPT, VEC>(p.weight, 1.f, p.cols, t, kThreads, w);
+#pragma unroll
+        for (int i = 0; i < kPT; ++i) {
+          x[i] = (x[i] - mean) * rstd;                 // n; columns past the end have g = 0
+          dw[i] = fmaf(g[i], x[i], dw[i]);
+          db[i] += g[i];
+          g[i] *= w[i];
+          s[0] += g[i];
+          s[1] = fmaf(g[i], x[i], s[1]);
+        }
+      }
+      if (!p.out) continue;
+      group_sum<WARPS>(s, buf[slot], group, wg, bar);
+      slot ^= 1;
+      const float mu = s[0] * inv_n, mun = s[1] * inv_n;
+#pragma unroll
+      for (int i = 0; i < kPT; ++i) g[i] = rstd * (g[i] - mu - x[i] * mun);
+      store_row<T, kPT, VEC>(static_cast<T*>(p.out) + row * p.ldo, p.cols, t, kThreads, g);
+    }
   }
   if (!p.part) return;
   float* pw = p.part + (long long)blockIdx.x * 2 * p.cols;
@@ -299,9 +430,11 @@ int done(sgemm_cube_ctx* h) {
 
 // Blocks of a persistent kernel: one per `groups` rows, at most what is resident at once.
 template <typename K>
-int persistent_blocks(sgemm_cube_ctx* h, K kernel, int threads, int rows, int groups, int* blocks) {
+int persistent_blocks(sgemm_cube_ctx* h, K kernel, int threads, size_t smem, int rows, int groups, int* blocks) {
   int per_sm = 0;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0) != cudaSuccess || per_sm < 1) {
+  if ((smem > 32 * 1024 &&                              // (48 KB with the static arrays is where the limit starts)
+       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) ||
+      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess || per_sm < 1) {
     cudaGetLastError();
     return SGEMM_CUBE_CUDA_ERROR;
   }
@@ -314,9 +447,10 @@ template <typename T, int WARPS, bool VEC>
 int forward_rows(sgemm_cube_ctx* h, const NormParams& p, cudaStream_t st) {
   constexpr int groups = WARPS >= 8 ? 1 : 8 / WARPS, threads = WARPS > 8 ? WARPS * 32 : 256;
   int blocks = 0;
-  const int rc = persistent_blocks(h, sgc::norm_forward_kernel<T, WARPS, VEC>, threads, p.rows, groups, &blocks);
+  constexpr size_t smem = sgc::kSlotBytes<T, WARPS, VEC, 1>;
+  const int rc = persistent_blocks(h, sgc::norm_forward_kernel<T, WARPS, VEC>, threads, smem, p.rows, groups, &blocks);
   if (rc) return rc;
-  sgc::norm_forward_kernel<T, WARPS, VEC><<<(unsigned)blocks, threads, 0, st>>>(p);
+  sgc::norm_forward_kernel<T, WARPS, VEC><<<(unsigned)blocks, threads, smem, st>>>(p);
   return done(h);
 }
 template <typename T, bool VEC>
@@ -335,14 +469,15 @@ template <typename T, int WARPS, bool VEC>
 int backward_rows(sgemm_cube_ctx* h, NormParams p, float* dweight, float* dbias, cudaStream_t st) {
   constexpr int groups = WARPS >= 8 ? 1 : 8 / WARPS, threads = WARPS > 8 ? WARPS * 32 : 256;
   int blocks = 0;
-  int rc = persistent_blocks(h, sgc::norm_backward_kernel<T, WARPS, VEC>, threads, p.rows, groups, &blocks);
+  constexpr size_t smem = sgc::kSlotBytes<T, WARPS, VEC, 2>;
+  int rc = persistent_blocks(h, sgc::norm_backward_kernel<T, WARPS, VEC>, threads, smem, p.rows, groups, &blocks);
   if (rc) return rc;
   if (dweight || dbias) {
     rc = grow(&h->part_ws, &h->part_ws_bytes, (size_t)blocks * 2 * p.cols * 4);
     if (rc) return rc;
     p.part = static_cast<float*>(h->part_ws);
   }
-  sgc::norm_backward_kernel<T, WARPS, VEC><<<(unsigned)blocks, threads, 0, st>>>(p);
+  sgc::norm_backward_kernel<T, WARPS, VEC><<<(unsigned)blocks, threads, smem, st>>>(p);
   rc = done(h);
   if (rc || !p.part) return rc;
   sgc::norm_parts_kernel<<<dim3((unsigned)((p.cols + 31) / 32), 2), 512, 0, st>>>(p.part, blocks, p.cols, dweight, dbias);

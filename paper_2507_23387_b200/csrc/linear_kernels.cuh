@@ -240,6 +240,7 @@ __global__ void __launch_bounds__(256) pack_split_kernel(PackJob a, PackJob b, u
 __device__ __forceinline__ void add_column_parts(const float* part, int chunks, int cols, float* out, int col) {
   if (col >= cols) return;
   float s = part[col];
+#pragma unroll 8
   for (int c = 1; c < chunks; ++c) s += part[(long long)c * cols + col];
   out[col] = s;
 }
@@ -439,6 +440,7 @@ dz_once_kernel(PackJob j, float* col_part, float* dbias, GridWords* words, unsig
     const int c = blockIdx.x * 128 + threadIdx.x;
     if (c < j.cols) {
       float s = __ldcg(col_part + c);
+#pragma unroll 8
       for (int k = 1; k < (int)gridDim.y; ++k) s += __ldcg(col_part + (long long)k * j.cols + c);
       dbias[c] = s;
     }
