@@ -9,6 +9,8 @@
 // taken about the mean (no cancellation of squares) without a second read.  Blocks are persistent: a
 // group asks for its next rows before it works on the present one, and keeps its columns' weights (forward)
 // or running sums of dw and db (backward) in registers all the way.
+#include <atomic>
+
 #include "ctx.cuh"
 #include "elements.cuh"
 
@@ -21,6 +23,7 @@ constexpr int kPT = 16;         // elements of a row a thread holds
 template <typename T, int WARPS>
 constexpr int slot_stages(int tensors) {
   const size_t row = (size_t)tensors * kPT * sizeof(T) * (WARPS > 8 ? WARPS * 32 : 256);
+  if (tensors == 1 && WARPS == 8 && sizeof(T) == 4) return 2;      // 8192 x 4096 forward 46 us, 52 with three
   return 3 * row <= 200 * 1024 ? 3 : (2 * row <= 200 * 1024 ? 2 : 1);
 }
 template <typename T, int WARPS, bool VEC, int TENSORS>
@@ -84,7 +87,7 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
   if (row >= p.rows) return;
   constexpr int kBlock = WARPS > 8 ? WARPS * 32 : 256, kWords = VEC ? kPT / Elem<T>::kVec : 1;
   constexpr int kRing = kStages<T, WARPS, VEC, 1>, kAhead = kRing - 1;
-  static_assert(!VEC || kRing == 3, "forward rows always fit three times");
+  static_assert(!VEC || kRing >= 2, "forward rows always fit twice");
   extern __shared__ uint4 ring[];                      // [kRing][kWords][kBlock]
   RowRegs<T, kPT, VEC> next;
   auto ask = [&](long long r, int s) {                 // an empty group past the end
@@ -428,16 +431,21 @@ int done(sgemm_cube_ctx* h) {
   return cudaGetLastError() == cudaSuccess ? SGEMM_CUBE_OK : SGEMM_CUBE_CUDA_ERROR;
 }
 
-// Blocks of a persistent kernel: one per `groups` rows, at most what is resident at once.
-template <typename K>
-int persistent_blocks(sgemm_cube_ctx* h, K kernel, int threads, size_t smem, int rows, int groups, int* blocks) {
-  int per_sm = 0;
-  if ((smem > 32 * 1024 &&                              // (48 KB with the static arrays is where the limit starts)
+// Blocks of a persistent kernel: one per `groups` rows, at most what is resident at once.  `KERNEL` is asked for its
+// occupancy once a device.
+template <auto KERNEL>
+int persistent_blocks(sgemm_cube_ctx* h, int threads, size_t smem, int rows, int groups, int* blocks) {
+  static std::atomic<int> known[64];                   // blocks an SM, per device; 0: not asked yet
+  std::atomic<int>* entry = h->device < 64 ? &known[h->device] : nullptr;
+  auto kernel = KERNEL;
+  int per_sm = entry ? entry->load(std::memory_order_relaxed) : 0;
+  if (per_sm == 0 && ((smem > 32 * 1024 &&                              // (48 KB with the static arrays is where the limit starts)
        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) ||
-      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess || per_sm < 1) {
+      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess || per_sm < 1)) {
     cudaGetLastError();
     return SGEMM_CUBE_CUDA_ERROR;
   }
+  if (entry) entry->store(per_sm, std::memory_order_relaxed);
   const long long want = ((long long)rows + groups - 1) / groups, cap = (long long)per_sm * h->sm_count;
   *blocks = (int)(want < cap ? want : cap);
   return SGEMM_CUBE_OK;
@@ -448,7 +456,7 @@ int forward_rows(sgemm_cube_ctx* h, const NormParams& p, cudaStream_t st) {
   constexpr int groups = WARPS >= 8 ? 1 : 8 / WARPS, threads = WARPS > 8 ? WARPS * 32 : 256;
   int blocks = 0;
   constexpr size_t smem = sgc::kSlotBytes<T, WARPS, VEC, 1>;
-  const int rc = persistent_blocks(h, sgc::norm_forward_kernel<T, WARPS, VEC>, threads, smem, p.rows, groups, &blocks);
+  const int rc = persistent_blocks<sgc::norm_forward_kernel<T, WARPS, VEC>>(h, threads, smem, p.rows, groups, &blocks);
   if (rc) return rc;
   sgc::norm_forward_kernel<T, WARPS, VEC><<<(unsigned)blocks, threads, smem, st>>>(p);
   return done(h);
@@ -470,7 +478,7 @@ int backward_rows(sgemm_cube_ctx* h, NormParams p, float* dweight, float* dbias,
   constexpr int groups = WARPS >= 8 ? 1 : 8 / WARPS, threads = WARPS > 8 ? WARPS * 32 : 256;
   int blocks = 0;
   constexpr size_t smem = sgc::kSlotBytes<T, WARPS, VEC, 2>;
-  int rc = persistent_blocks(h, sgc::norm_backward_kernel<T, WARPS, VEC>, threads, smem, p.rows, groups, &blocks);
+  int rc = persistent_blocks<sgc::norm_backward_kernel<T, WARPS, VEC>>(h, threads, smem, p.rows, groups, &blocks);
   if (rc) return rc;
   if (dweight || dbias) {
     rc = grow(&h->part_ws, &h->part_ws_bytes, (size_t)blocks * 2 * p.cols * 4);

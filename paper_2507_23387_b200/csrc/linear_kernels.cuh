@@ -525,6 +525,11 @@ few_rows_nk_kernel(FewRowsParams p, int ksplit) {
   for (int i = 0; i < NR; ++i)
 #pragma unroll
     for (int m = 0; m < MR; ++m) acc[i][m] = 0.f;
+  // what the last step needs, asked for now: this thread's output, and the way back
+  const int out_n = (blockIdx.x * groups + threadIdx.x / (NR * MR)) * NR + threadIdx.x % (NR * MR) / MR;
+  const bool out_in = threadIdx.x < groups * NR * MR && out_n < p.N && threadIdx.x % MR < p.M;
+  const float out_bias = out_in && p.ep.bias ? __ldg(p.ep.bias + out_n) : 0.f;
+  const PowerBack back = power_back(p.ep.exp_a, p.ep.exp_b);
   // element e of the lane's step at k0: k0 + lane * 8 + e, or k0 + lane + 32 e where loads are single words
   constexpr int LS = LOAD == kLoadF32 ? 1 : E, ES = LOAD == kLoadF32 ? 32 : 1;
   for (int k0 = slice * 32 * E; k0 < p.K; k0 += ksplit * 32 * E) {
@@ -597,16 +602,15 @@ few_rows_nk_kernel(FewRowsParams p, int ksplit) {
       for (int m = 0; m < MR; ++m) part[warp][i * MR + m] = acc[i][m];
   }
   __syncthreads();
-  // thread t of the block: output t / MR of the block's groups * NR, row t % MR
-  const PowerBack back = power_back(p.ep.exp_a, p.ep.exp_b);
-  for (int t = threadIdx.x; t < groups * NR * MR; t += 256) {
+  // thread t of the block: output t / MR of the block's groups * NR, row t % MR (at most 8 * 16 of them)
+  static_assert(8 * NR * MR <= 256, "one output a thread");
+  if (out_in) {
+    const int t = threadIdx.x, n = out_n;
     const int g = t / (NR * MR), i = t % (NR * MR) / MR, m = t % MR;
-    const int n = (blockIdx.x * groups + g) * NR + i;
-    if (n >= p.N || m >= p.M) continue;
     float z = part[g * ksplit][i * MR + m];
     for (int s = 1; s < ksplit; ++s) z += part[g * ksplit + s][i * MR + m];
     z = z != 0.f && fabsf(z) < kTinySum ? few_rows_tiny<LOAD>(p, m, n, true) : back(z);
-    z += p.ep.bias ? p.ep.bias[n] : 0.f;
+    z += out_bias;
     p.Y[(long long)m * p.ldy + n] = linear_finish(p.ep, z, m, n);
   }
 }
