@@ -7,9 +7,10 @@
 //   lse = scale m + log Z,   log p_t = scale (x_t - m) - log Z,   H = log Z - S / Z.
 // Bound by reading the logits once; with 16-bit logits as much by issuing instructions, so these are counted.
 // Exponentials run in base 2, a = scale log2 e: t = x a - M, M = fl(m a), is one FMA; what the rounding of M does to
-// every term alike is taken out of a thread's sums at the end.  Logits are cut at -2^60 (2^-30 <= scale <= 2^30), so
-// that -inf gives a weight of zero and no 0 * inf.  A thread whose largest logit is beyond +-2^59 (masked with the
-// type's lowest value, say) sums its columns again in the form (x - m) a, which neither overflows nor is cut.
+// every term alike (at most 1 while |M| < 2^25) is taken out of a thread's sums at the end.  Logits are cut at -2^60
+// (2^-30 <= scale <= 2^30), so that -inf gives a weight of zero and no 0 * inf.  A thread whose largest logit has
+// |m a| >= 2^25 (masked with the type's lowest value, or a large scale) sums its columns again in the form (x - m) a,
+// which neither overflows nor is cut.
 #include <type_traits>
 
 #include "ctx.cuh"
@@ -24,7 +25,7 @@ constexpr int kCandidates = 256;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kNoWeight = -160.f;      // 2^-160 is zero in FP32: exponents are cut there where they are factors
 constexpr float kLowestLogit = -1152921504606846976.f;    // -2^60
-constexpr float kFarLogit = 576460752303423488.f;         // 2^59
+constexpr float kFarTerm = 33554432.f;                    // 2^25, so near logits lie within 2^55 of zero, well above the cut
 
 // 2^t, zero below 2^-126: in a sum such weights are nothing beside the row's largest, which is 1, and keeping them
 // takes three more instructions.
@@ -140,10 +141,11 @@ __device__ __forceinline__ void join_lanes(Running& r, float a) {
 struct ThreadSums {
   float m, M;
   Two Z, S;
+  static __device__ __forceinline__ bool near(float m, float a) { return fabsf(m * a) < kFarTerm; }
   __device__ __forceinline__ void raise(float top, float a) {            // top > m
-    const float to = fabsf(top) < kFarLogit ? top * a : 0.f;
+    const float to = near(top, a) ? top * a : 0.f;
     const float d = fmaxf(M - to, kNoWeight);
-    const float f = fabsf(m) < kFarLogit ? ex2(d) : 0.f;         // 0 times the sums, not 0: NaN stays
+    const float f = near(m, a) ? ex2(d) : 0.f;         // 0 times the sums, not 0: NaN stays
     S = fma2(two(d, d), Z, S) * two(f, f);
     Z = Z * two(f, f);
     m = top;
@@ -163,7 +165,7 @@ struct ThreadSums {
     float z0, z1, s0, s1;
     parts_of(Z, z0, z1);
     parts_of(S, s0, s1);
-    const float lo = fabsf(m) < kFarLogit ? fmaf(m, a, -M) : 0.f;
+    const float lo = near(m, a) ? fmaf(m, a, -M) : 0.f;
     const float f = ex2(-lo), z = z0 + z1;
     return Running{m, z * f, fmaf(-lo, z, s0 + s1) * f};
   }
@@ -401,7 +403,7 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(LogprobParam
     add_single(x);
   }
   Running sum = r.sum(p.a);
-  if (!(fabsf(r.m) < kFarLogit) && r.m != -INFINITY) sum = sum_far(piece, t, r.m, p.a);   // NaN for +inf
+  if (!ThreadSums::near(r.m, p.a) && r.m != -INFINITY) sum = sum_far(piece, t, r.m, p.a);   // NaN for +inf
 
   if constexpr (TOP) {
     // The k largest of the threads' maxima bound the k largest elements from below, and hold every thread
