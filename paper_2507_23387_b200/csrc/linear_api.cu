@@ -3,6 +3,7 @@
 #include "ctx.cuh"
 #include "gemm_tc.cuh"
 #include "linear_kernels.cuh"
+#include "short_batch.cuh"
 
 namespace {
 
@@ -147,6 +148,16 @@ int linear_attrs(sgemm_cube_ctx* h) {
   }
   return SGEMM_CUBE_OK;
 }
+template <int NT>
+int short_batch_attrs() {
+  constexpr int smem = (int)sgc::ShortBatchCfg<NT>::SMEM_BYTES;
+  if (cudaFuncSetAttribute(sgc::short_batch_kernel<NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+      cudaFuncSetAttribute(sgc::short_batch_kernel<NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+    cudaGetLastError();
+    return SGEMM_CUBE_CUDA_ERROR;
+  }
+  return SGEMM_CUBE_OK;
+}
 int linear_setup(sgemm_cube_ctx* h) {
   if (h->linear_ready) return SGEMM_CUBE_OK;
   h->linear_pair_clusters = h->sm_count;
@@ -156,6 +167,7 @@ int linear_setup(sgemm_cube_ctx* h) {
       (rc = linear_attrs<sgc::kFormMM, false>(h)) || (rc = linear_attrs<sgc::kFormKM, true>(h)) ||
       (rc = linear_attrs<sgc::kFormKK, true>(h)) || (rc = linear_attrs<sgc::kFormMM, true>(h)))
     return rc;
+  if ((rc = short_batch_attrs<16>()) || (rc = short_batch_attrs<32>()) || (rc = short_batch_attrs<64>())) return rc;
   h->linear_ready = true;
   return SGEMM_CUBE_OK;
 }
@@ -194,12 +206,11 @@ int launch_linear_kernel(sgemm_cube_ctx* h, const Packed& A, const Packed& B, co
   return SGEMM_CUBE_OK;
 }
 
-// How many k slices, when the 128 x 256 tiles leave half of the SMs idle: the clusters that are resident at once go
+// How many k slices, when the tiles leave half of the SMs idle: the clusters that are resident at once go
 // through the tiles in turns, and a turn takes as long as its slice; the fewest slices among those that take the
 // least time.  A slice is at least two k-blocks.
-int linear_slices(const sgemm_cube_ctx* h, int M, int N, int K, int chunk_k) {
+int linear_slices(const sgemm_cube_ctx* h, long long tiles, int K, int chunk_k) {
   if (!h->split_k) return 1;
-  const long long tiles = (long long)((M + sgc::kBM - 1) / sgc::kBM) * ((N + sgc::kBN - 1) / sgc::kBN);
   if (tiles * 2 > h->sm_count) return 1;
   const int chunks = (K + chunk_k - 1) / chunk_k;
   int best = 1;
@@ -235,9 +246,9 @@ int linear_product(sgemm_cube_ctx* h, int M, int N, int K, const Packed& A, cons
   p.err = h->err_dev;
   p.ksplit = 1;
   p.ep = ep;
-  const int slices = linear_slices(h, M, N, K, p.kchunk_blocks * BK);
+  const size_t tiles = (size_t)((M + sgc::kBM - 1) / sgc::kBM) * ((N + sgc::kBN - 1) / sgc::kBN);
+  const int slices = linear_slices(h, (long long)tiles, K, p.kchunk_blocks * BK);
   if (slices > 1) {
-    const size_t tiles = (size_t)((M + sgc::kBM - 1) / sgc::kBM) * ((N + sgc::kBN - 1) / sgc::kBN);
     rc = grow(&h->part_ws, &h->part_ws_bytes, tiles * slices * sgc::kTileFloats * 4);
     if (rc) return rc;
     const int chunks = (K + p.kchunk_blocks * BK - 1) / (p.kchunk_blocks * BK);
@@ -272,7 +283,15 @@ int linear_product_any(int form, sgemm_cube_ctx* h, int M, int N, int K, const P
 }
 
 // ------------------------------------------------------------------------------------------ few rows
+// Up to 8 rows of an FP32 weight.  Of a packed one the tensor cores are the faster way (16384 x 4096 with 8 rows 65 us,
+// 172 here), except for what a launch of theirs costs more: one row (outputs x inputs: 57 us, 65 there; 1024 x 1024 10
+// and 14), and up to four of a weight below 8 million elements (2048 x 2048 16 and 18; 4096 x 4096 29 and 27).
 constexpr int kFewRows = 8;
+
+bool use_few_rows(int M, int N, int K, bool packed, bool nk) {
+  if (!packed) return M <= kFewRows;
+  return nk && (M == 1 || (M <= 4 && (long long)N * K < (1ll << 23)));
+}
 
 template <int MR, int LOAD>
 int launch_few_nk(sgemm_cube_ctx* h, const sgc::FewRowsParams& p, cudaStream_t st) {
@@ -310,10 +329,65 @@ int launch_few_kn(sgemm_cube_ctx* h, const sgc::FewRowsParams& p, cudaStream_t s
 }
 template <int LOAD>
 int launch_few(sgemm_cube_ctx* h, const sgc::FewRowsParams& p, bool nk, cudaStream_t st) {
+  if constexpr (LOAD == sgc::kLoadPacked) {
+    if (p.M == 1) return launch_few_nk<1, LOAD>(h, p, st);
+    return p.M == 2 ? launch_few_nk<2, LOAD>(h, p, st) : launch_few_nk<4, LOAD>(h, p, st);
+  } else {
   if (p.M == 1) return nk ? launch_few_nk<1, LOAD>(h, p, st) : launch_few_kn<1, LOAD>(h, p, st);
   if (p.M == 2) return nk ? launch_few_nk<2, LOAD>(h, p, st) : launch_few_kn<2, LOAD>(h, p, st);
   if (p.M <= 4) return nk ? launch_few_nk<4, LOAD>(h, p, st) : launch_few_kn<4, LOAD>(h, p, st);
   return nk ? launch_few_nk<8, LOAD>(h, p, st) : launch_few_kn<8, LOAD>(h, p, st);
+  }
+}
+
+// ------------------------------------------------------------------------------------------ short batches
+// Rows and blocks of 64 k for which the short-batch kernel is the faster one (cold cache, times with the launches' own):
+//   up to 64 rows always: 4096 x 4096 with 16 rows 29 us, 50 on the 128-row tiles; 16384 x 4096 with 64 rows 70 and 89;
+//   up to 256 where its 64-row tiles fit the SMs at once and have little to do each: 128 rows of 4096 x 4096 (32 blocks)
+//   43 and 52, 256 of 4096 x 1024 (16 blocks) 27 and 38; but 160 of 4096 x 4096 (64 blocks) 70 and 58, 65 of
+//   16384 x 4096 (two turns of tiles) 129 and 89.
+constexpr int kShortRows = 64, kShortMoreRows = 256, kShortMoreBlocks = 32;
+
+bool use_short_batch(const sgemm_cube_ctx* h, int M, int N, int K, int* slices) {
+  const int nt = M <= 16 ? 16 : (M <= 32 ? 32 : 64);
+  const long long tiles = (long long)((N + sgc::kShortN - 1) / sgc::kShortN) * ((M + nt - 1) / nt);
+  *slices = linear_slices(h, tiles, K, 2 * sgc::kShortK);
+  if (M <= kShortRows) return true;
+  const int blocks = (K + sgc::kShortK - 1) / sgc::kShortK;
+  return M <= kShortMoreRows && tiles <= h->sm_count && (blocks + *slices - 1) / *slices <= kShortMoreBlocks;
+}
+
+template <int NT, bool W_MN>
+int launch_short(sgemm_cube_ctx* h, const Packed& W, sgc::ShortBatchParams p, int slices, cudaStream_t st) {
+  CUtensorMap tm[2];
+  for (int w = 0; w < 2; ++w) {
+    const uint16_t* words = w ? W.lo : W.hi;
+    const int rc = W_MN ? make_map(h, &tm[w], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, words, p.N, p.K, W.ld, 64, sgc::kShortK,
+                                   CU_TENSOR_MAP_SWIZZLE_128B)
+                        : make_map(h, &tm[w], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, words, p.K, p.N, W.ld, sgc::kShortK,
+                                   sgc::kShortN, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc) return rc;
+  }
+  const int blocks = (p.K + sgc::kShortK - 1) / sgc::kShortK;
+  p.kslice_blocks = (blocks + slices - 1) / slices;
+  p.ksplit = (blocks + p.kslice_blocks - 1) / p.kslice_blocks;       // no slice is empty
+  cudaLaunchAttribute attr;
+  cudaLaunchConfig_t cfg = linear_config(sgc::ShortBatchCfg<NT>::SMEM_BYTES, (unsigned)p.ksplit, &attr, st);
+  cfg.blockDim = dim3(sgc::kShortThreads, 1, 1);
+  cfg.gridDim = dim3((unsigned)((p.N + sgc::kShortN - 1) / sgc::kShortN * p.row_tiles * p.ksplit), 1, 1);
+  h->launches++;
+  if (cudaLaunchKernelEx(&cfg, sgc::short_batch_kernel<NT, W_MN>, tm[0], tm[1], p) != cudaSuccess) {
+    cudaGetLastError();
+    return SGEMM_CUBE_CUDA_ERROR;
+  }
+  return SGEMM_CUBE_OK;
+}
+template <int NT>
+int launch_short(sgemm_cube_ctx* h, const Packed& W, sgc::ShortBatchParams p, bool nk, int slices, cudaStream_t st) {
+  p.row_tiles = (p.M + NT - 1) / NT;
+  const int rc = nk ? launch_short<NT, false>(h, W, p, slices, st) : launch_short<NT, true>(h, W, p, slices, st);
+  if (rc != SGEMM_CUBE_CUDA_ERROR || slices == 1) return rc;         // clusters that cannot be scheduled: whole k
+  return nk ? launch_short<NT, false>(h, W, p, 1, st) : launch_short<NT, true>(h, W, p, 1, st);
 }
 
 // ------------------------------------------------------------------------------------------ arguments
@@ -427,7 +501,7 @@ int sgemm_cube_linear(sgemm_cube_handle h, int M, int N, int K, const sgemm_cube
     sgc::linear_empty_kernel<<<blocks_for(h, (long long)M * N), 256, 0, st>>>(M, N, Y, ldy, ep);
     return launched(h);
   }
-  if (M <= kFewRows && !is_packed(X)) {
+  if (!is_packed(X) && use_few_rows(M, N, K, is_packed(W), nk)) {
     sgc::FewRowsParams p;
     memset(&p, 0, sizeof(p));
     p.M = M; p.N = N; p.K = K;
@@ -445,19 +519,35 @@ int sgemm_cube_linear(sgemm_cube_handle h, int M, int N, int K, const sgemm_cube
     return launch_few<sgc::kLoadF32>(h, p, nk, st);
   }
   PackJob jobs[2];
-  int n_jobs = 0;
+  int n_jobs = 0, slices = 1;
   int* exps = reinterpret_cast<int*>(h->err_dev + kExpWords);
   const int w_rows = nk ? N : K, w_cols = nk ? K : N;
+  const bool short_batch = !is_packed(X) && use_short_batch(h, M, N, K, &slices);
+  if ((rc = linear_setup(h))) return rc;
   Carve size;
-  words_of(X, M, K, size, exps, jobs, &n_jobs);
+  if (!short_batch) words_of(X, M, K, size, exps, jobs, &n_jobs);
   words_of(W, w_rows, w_cols, size, exps + 1, jobs, &n_jobs);
   if ((rc = grow(&h->ws, &h->ws_bytes, size.used))) return rc;
   Carve c;
   c.base = static_cast<uint8_t*>(h->ws);
   n_jobs = 0;
-  const Packed px = words_of(X, M, K, c, exps, jobs, &n_jobs);
+  Packed px;
+  if (!short_batch) px = words_of(X, M, K, c, exps, jobs, &n_jobs);
   const Packed pw = words_of(W, w_rows, w_cols, c, exps + 1, jobs, &n_jobs);
   if (n_jobs && (rc = launch_pack(h, jobs, n_jobs, st))) return rc;
+  if (short_batch) {
+    sgc::ShortBatchParams p;
+    memset(&p, 0, sizeof(p));
+    p.M = M; p.N = N; p.K = K;
+    p.X = X->f32_dev; p.ldx = X->ld;
+    p.xvec = aligned16(p.X) && p.ldx % 4 == 0;
+    p.Y = Y; p.ldy = ldy;
+    p.err = h->err_dev;
+    p.ep = ep;
+    p.ep.exp_b = pw.exp;
+    if (M <= 16) return launch_short<16>(h, pw, p, nk, slices, st);
+    return M <= 32 ? launch_short<32>(h, pw, p, nk, slices, st) : launch_short<64>(h, pw, p, nk, slices, st);
+  }
   return linear_product_any(nk ? sgc::kFormKK : sgc::kFormKM, h, M, N, K, px, pw, Y, ldy, ep, st);
 }
 

@@ -113,10 +113,12 @@ struct PowerBack {
   float f0, f1;
   __device__ __forceinline__ float operator()(float v) const { return v * f0 * f1; }
 };
-__device__ __forceinline__ PowerBack power_back(const int* pa, const int* pb) {
-  const int t = -((pa ? *pa : 0) + (pb ? *pb : 0));
+__device__ __forceinline__ PowerBack power_back_of(int t) {       // 2^t
   const int t0 = t > 127 ? 127 : (t < -126 ? -126 : t);
   return PowerBack{__int_as_float((127 + t0) << 23), __int_as_float((127 + t - t0) << 23)};
+}
+__device__ __forceinline__ PowerBack power_back(const int* pa, const int* pb) {
+  return power_back_of(-((pa ? *pa : 0) + (pb ? *pb : 0)));
 }
 
 // One element whose z is known: stores z, returns y.

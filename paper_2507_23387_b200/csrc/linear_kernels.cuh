@@ -621,6 +621,7 @@ few_rows_nk_kernel(FewRowsParams p, int ksplit) {
 template <int MR, int LOAD>
 __global__ void __launch_bounds__(256)
 few_rows_kn_kernel(FewRowsParams p, int k_per_block) {
+  static_assert(LOAD != kLoadPacked, "packed weights of this layout go to the tensor cores");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int n0 = blockIdx.x * 128;
   const int k_begin = blockIdx.y * k_per_block, k_end = min(p.K, k_begin + k_per_block);
@@ -635,21 +636,7 @@ few_rows_kn_kernel(FewRowsParams p, int k_per_block) {
   constexpr int U = 4;                                 // k in flight per warp
   for (int k0 = k_begin + warp; k0 < k_end; k0 += 8 * U) {
     float w[U][4];
-    if (LOAD == kLoadPacked) {                         // ldw % 8 == 0 and zeros past N: a lane has all four words
-      uint2 h[U], l[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const bool in = k0 + 8 * u < k_end && n < p.N;
-        const long long off = (long long)(k0 + 8 * u) * p.ldw + n;
-        h[u] = in ? __ldcs(reinterpret_cast<const uint2*>(p.Whi + off)) : make_uint2(0, 0);
-        l[u] = in ? __ldcs(reinterpret_cast<const uint2*>(p.Wlo + off)) : make_uint2(0, 0);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        join_words(h[u].x, l[u].x, w[u][0], w[u][1]);
-        join_words(h[u].y, l[u].y, w[u][2], w[u][3]);
-      }
-    } else if (LOAD == kLoadF32Vec) {                  // N % 4 == 0
+    if (LOAD == kLoadF32Vec) {                         // N % 4 == 0
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const bool in = k0 + 8 * u < k_end && n < p.N;

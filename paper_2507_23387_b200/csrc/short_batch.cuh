@@ -1,0 +1,325 @@
+// The linear layer for a batch of 16 to 64 rows with packed weights: Y^T = W X^T on the tensor cores, one launch.
+//
+// The weight's 4 bytes per element are what bounds it, so the weight takes the 128-row side of the tile and the few rows
+// of X the narrow one (16, 32 or 64 columns): a stage holds 32 KB of the weight and little else, and four to six of
+// them are in flight in every SM.  X is not packed by a launch of its own: warps of this kernel turn 64 columns of it
+// into words as they are needed, each such block with an exponent of its own (15 - e_max, as in packing; the more
+// local scale keeps at least as many bits).  The warps that take the sums of a block out of TMEM bring them to the
+// smallest exponent so far, like the running maximum of a softmax: all factors are powers of two, and what they push
+// below FP32's range is nothing beside the block that caused it.
+//
+// A cluster of up to eight blocks shares a tile's k range where there are fewer tiles than SMs; their sums meet
+// in shared memory, added in the order of the slices.
+#pragma once
+
+#include <cstdint>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "linear_epilogue.cuh"
+#include "linear_kernels.cuh"
+#include "ptx_sm100.cuh"
+#include "split_math.cuh"
+
+namespace sgc {
+
+constexpr int kShortThreads = 512;
+constexpr int kShortK = 64;                  // k of a stage, of an exponent and of a stay in TMEM
+constexpr int kShortN = 128;                 // outputs of a tile
+
+struct ShortBatchParams {
+  int M, N, K;
+  int row_tiles;                             // of NT rows; neighbouring blocks take the same part of the weight
+  const float* X;
+  long long ldx;
+  int xvec;
+  float* Y;
+  long long ldy;
+  int ksplit, kslice_blocks;
+  unsigned int* err;
+  LinearEpilogue ep;                         // exp_b: the weight's exponent
+};
+
+template <int NT>
+struct ShortBatchCfg {
+  static constexpr uint32_t W_TILE = kShortN * kShortK * 2, X_TILE = NT * kShortK * 2;
+  static constexpr uint32_t STAGE_BYTES = 2 * (W_TILE + X_TILE);
+  static constexpr int STAGES = 221184 / STAGE_BYTES;
+  static constexpr uint32_t RING_BYTES = STAGES * STAGE_BYTES;
+  static constexpr uint32_t SMEM_BYTES = RING_BYTES + 1024 /*align*/ + 512 /*barriers, exponents*/;
+  static_assert(STAGES <= 6, "the ring of 16 exponents covers what is under way: STAGES + 2 blocks");
+  static_assert(NT * kShortN * 4 <= RING_BYTES, "the sums lie where the stages were");
+};
+
+// 2^d for d <= 0, zero where FP32 has no normal number for it.
+__device__ __forceinline__ float pow2_down(int d) { return d < -126 ? 0.f : pow2f(d); }
+
+template <int NT, bool W_MN>
+__global__ void __launch_bounds__(kShortThreads, 1)
+short_batch_kernel(const __grid_constant__ CUtensorMap tm_hi, const __grid_constant__ CUtensorMap tm_lo,
+                   const ShortBatchParams p) {
+  using Cfg = ShortBatchCfg<NT>;
+  constexpr int STAGES = Cfg::STAGES, kRing = 16, kGroups = 4;
+  constexpr uint32_t kTmem = 4 * NT < 32 ? 32 : 4 * NT;      // two regions of hi*hi and of cross sums
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + Cfg::RING_BYTES);    // TMA and converters -> MMA
+  uint64_t* empty_bar = full_bar + STAGES;                                     // MMA -> TMA and converters
+  uint64_t* tfull_bar = empty_bar + STAGES;                                    // [2] MMA -> accumulate warps
+  uint64_t* tempty_bar = tfull_bar + 2;                                        // [2] accumulate warps -> MMA
+  uint64_t* pair_bar = tempty_bar + 2;                                         // [kGroups] between two converter warps
+  int* block_exp = reinterpret_cast<int*>(pair_bar + kGroups);                 // [kRing]
+  uint32_t* part_max = reinterpret_cast<uint32_t*>(block_exp + kRing);         // [2][kGroups][2]
+  int* slice_exp = reinterpret_cast<int*>(part_max + 4 * kGroups);             // [8] of the cluster's blocks
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(slice_exp + 8);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  static_assert((2 * STAGES + 4 + kGroups) * 8 + (kRing + 4 * kGroups + 8 + 2) * 4 <= 512, "barrier block");
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int ranks = p.ksplit, rank = ranks > 1 ? (int)cluster_ctarank() : 0;
+  const int tile = (int)(blockIdx.x / (unsigned)ranks);
+  const int n0 = tile / p.row_tiles * kShortN, m0 = tile % p.row_tiles * NT, rows = min(NT, p.M - m0);
+  const int num_kb = (p.K + kShortK - 1) / kShortK;
+  const int kb0 = rank * p.kslice_blocks, count = min(num_kb, kb0 + p.kslice_blocks) - kb0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&full_bar[s], 3);                            // the TMA thread and two converter warps
+      mbar_init(&empty_bar[s], 1);
+    }
+    for (int r = 0; r < 2; ++r) {
+      mbar_init(&tfull_bar[r], 1);
+      mbar_init(&tempty_bar[r], 4);
+    }
+    for (int g = 0; g < kGroups; ++g) mbar_init(&pair_bar[g], 2);
+    *abort_flag = 0u;
+    fence_mbar_init();
+    tma_prefetch_desc(&tm_hi);
+    tma_prefetch_desc(&tm_lo);
+  }
+  if (warp == 1) { tmem_alloc(tmem_slot, kTmem); tmem_relinquish(); }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (ranks > 1) cluster_sync_all();                         // the peers run before anyone writes to them
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA: the weight's words
+    if (lane == 0) {
+      bool ok = true;
+      for (int i = 0; i < count; ++i) {
+        const int s = i % STAGES;
+        if (!mbar_wait_bounded(&empty_bar[s], ((i / STAGES) & 1) ^ 1, abort_flag, p.err, kErrProducerEmptyWait)) {
+          ok = false;
+          break;
+        }
+        uint8_t* st = smem + s * Cfg::STAGE_BYTES;
+        const int k0 = (kb0 + i) * kShortK;
+        mbar_arrive_expect_tx(&full_bar[s], 2 * Cfg::W_TILE);
+        if constexpr (W_MN) {                                // boxes of 64 outputs x 64 k rows
+          for (int a = 0; a < 2; ++a) {
+            tma_load_2d(st + a * 8192, &tm_hi, n0 + a * 64, k0, &full_bar[s]);
+            tma_load_2d(st + Cfg::W_TILE + a * 8192, &tm_lo, n0 + a * 64, k0, &full_bar[s]);
+          }
+        } else {                                             // one box of 64 k x 128 outputs
+          tma_load_2d(st, &tm_hi, k0, n0, &full_bar[s]);
+          tma_load_2d(st + Cfg::W_TILE, &tm_lo, k0, n0, &full_bar[s]);
+        }
+      }
+      if (!ok) {                                             // copies may be under way: let them land
+        const long long t0 = clock64();
+        while (clock64() - t0 < kAbortDrainClocks) {}
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer
+    if (lane == 0) {
+      constexpr uint32_t idesc = umma_idesc_f16(kShortN, NT, W_MN, false);
+      constexpr uint32_t w_step = W_MN ? 2048 : 32;          // bytes from one k16 step to the next
+      for (int i = 0; i < count; ++i) {
+        const int s = i % STAGES, r = i & 1;
+        if (!mbar_wait_bounded(&full_bar[s], (i / STAGES) & 1, abort_flag, p.err, kErrMmaFullWait)) break;
+        if (!mbar_wait_bounded(&tempty_bar[r], ((i >> 1) & 1) ^ 1, abort_flag, p.err, kErrMmaTmemEmptyWait)) break;
+        tc_fence_after_sync();
+        const uint32_t w = smem_u32(smem + s * Cfg::STAGE_BYTES), x = w + 2 * Cfg::W_TILE;
+        const uint32_t d = tmem + r * 2 * NT;
+        auto w_desc = [&](uint32_t a) { return umma_smem_desc(a, W_MN ? 8192 : 16, 1024, kSwizzle128); };
+        auto x_desc = [&](uint32_t a) { return umma_smem_desc(a, 16, 1024, kSwizzle128); };
+#pragma unroll
+        for (int j = 0; j < kShortK / 16; ++j)
+          umma_f16_ss(d, w_desc(w + j * w_step), x_desc(x + j * 32), idesc, j != 0);
+#pragma unroll
+        for (int j = 0; j < kShortK / 16; ++j) {
+          umma_f16_ss(d + NT, w_desc(w + Cfg::W_TILE + j * w_step), x_desc(x + j * 32), idesc, j != 0);
+          umma_f16_ss(d + NT, w_desc(w + j * w_step), x_desc(x + Cfg::X_TILE + j * 32), idesc, 1);
+        }
+        umma_commit(&empty_bar[s]);
+        umma_commit(&tfull_bar[r]);
+      }
+    }
+  } else if (warp >= 8) {
+    // ------------------------------------------------------------------ converters: X to words
+    // Two warps take every fourth block of 64 columns; a thread has eight neighbouring elements of NT / 8 rows.
+    constexpr int U = NT / 8;
+    const int group = (warp - 8) >> 1, t = threadIdx.x & 63;
+    const int chunk = t & 7, row0 = t >> 3;
+    for (int i = group; i < count; i += kGroups) {
+      const int s = i % STAGES, k = (kb0 + i) * kShortK + chunk * 8;
+      float v[U][8];
+      uint32_t m = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int row = row0 + 8 * u;
+        const float* src = p.X + (m0 + row) * p.ldx + k;
+        if (row < rows && p.xvec && k + 8 <= p.K) {
+          const float4 f = __ldg(reinterpret_cast<const float4*>(src)), g = __ldg(reinterpret_cast<const float4*>(src) + 1);
+          v[u][0] = f.x; v[u][1] = f.y; v[u][2] = f.z; v[u][3] = f.w;
+          v[u][4] = g.x; v[u][5] = g.y; v[u][6] = g.z; v[u][7] = g.w;
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[u][q] = row < rows && k + q < p.K ? __ldg(src + q) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) m = max(m, finite_bits(v[u][q]));
+      m = __reduce_max_sync(0xffffffffu, m);
+      uint32_t* both = part_max + ((i / kGroups) & 1) * 2 * kGroups + group * 2;
+      if (lane == 0) {
+        both[warp & 1] = m;
+        mbar_arrive(&pair_bar[group]);
+      }
+      bool ok = mbar_wait_bounded(&pair_bar[group], (i / kGroups) & 1, abort_flag, p.err, kErrConvFullWait);
+      m = max(both[0], both[1]);
+      const int e = m == 0 ? 126 : pack_exponent(m);         // nothing but zeros: no reason to rescale
+      const float pre = pow2f(e), scale = pow2f(kPackScaleExp);
+      ok = ok && mbar_wait_bounded(&empty_bar[s], ((i / STAGES) & 1) ^ 1, abort_flag, p.err, kErrConvEmptyWait);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      if (t == 0) block_exp[i % kRing] = e;
+      uint8_t* words = smem + s * Cfg::STAGE_BYTES + 2 * Cfg::W_TILE;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int row = row0 + 8 * u;
+        uint4 hi, lo;
+        split_two(v[u][0] * pre, v[u][1] * pre, scale, hi.x, lo.x);
+        split_two(v[u][2] * pre, v[u][3] * pre, scale, hi.y, lo.y);
+        split_two(v[u][4] * pre, v[u][5] * pre, scale, hi.z, lo.z);
+        split_two(v[u][6] * pre, v[u][7] * pre, scale, hi.w, lo.w);
+        uint8_t* at = words + row * 128 + ((chunk ^ (row & 7)) << 4);        // 128-byte swizzle
+        *reinterpret_cast<uint4*>(at) = hi;
+        *reinterpret_cast<uint4*>(at + Cfg::X_TILE) = lo;
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&full_bar[s]);
+    }
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------------ accumulate: one output a thread
+    const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    float S[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) S[j] = 0.f;
+    int e = 126;
+    for (int i = 0; i < count; ++i) {
+      const int r = i & 1;
+      const bool ok = mbar_wait_bounded(&tfull_bar[r], (i >> 1) & 1, abort_flag, p.err, kErrEpiTmemFullWait);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      tc_fence_after_sync();
+      const int now = block_exp[i % kRing];
+      if (now < e) {
+        const float down = pow2_down(now - e);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) S[j] *= down;
+        e = now;
+      }
+      const float f = pow2_down(e - now);
+#pragma unroll
+      for (int g = 0; g < NT / 16; ++g) {
+        uint32_t vh[16], vx[16];
+        tmem_ld_32x32b_x16(mine + r * 2 * NT + g * 16, vh);
+        tmem_ld_32x32b_x16(mine + r * 2 * NT + NT + g * 16, vx);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          S[g * 16 + j] = fmaf(fmaf(__uint_as_float(vx[j]), kPackInvScale, __uint_as_float(vh[j])), f, S[g * 16 + j]);
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&tempty_bar[r]);
+    }
+    // every stage has been multiplied: the sums go where the first of them was
+    float* sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) sums[j * kShortN + (warp & 3) * 32 + lane] = S[j];
+    if (warp == 4 && lane < ranks)
+      asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(ranks > 1 ? mapa_u32(smem_u32(slice_exp + rank), (uint32_t)lane)
+                                                                      : smem_u32(slice_exp)), "r"(e) : "memory");
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (ranks > 1) cluster_sync_all();
+
+  // ---------------------------------------------------------------------- all warps: rows rank, rank + ranks, ... of Y
+  {
+    constexpr int U = 4;
+    const int f = (warp & 3) * 32 + lane, n = n0 + f;
+    const bool in = n < p.N;
+    int least = slice_exp[0];
+    for (int s = 1; s < ranks; ++s) least = min(least, slice_exp[s]);
+    const PowerBack back = power_back_of(-(least + *p.ep.exp_b));
+    const float bias = p.ep.bias && in ? __ldg(p.ep.bias + n) : 0.f;
+    const uint32_t sums = smem_u32(smem) + f * 4;
+#pragma unroll 1
+    for (int i = warp >> 2; rank + ranks * i < rows; i += 4 * U) {
+      float v[U], res[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int row = rank + ranks * (i + 4 * u);
+        v[u] = 0.f;
+        res[u] = p.ep.R && in && row < rows ? p.ep.R[(m0 + row) * p.ep.ldr + n] : 0.f;
+      }
+#pragma unroll 1
+      for (int s = 0; s < ranks; ++s) {
+        const float scale = pow2_down(least - slice_exp[s]);
+        const uint32_t from = ranks > 1 ? mapa_u32(sums, (uint32_t)s) : sums;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int row = min(rank + ranks * (i + 4 * u), rows - 1);
+          float x;
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(from + row * (kShortN * 4)) : "memory");
+          v[u] = fmaf(x, scale, v[u]);
+        }
+      }
+      auto store = [&](float* out, long long ld) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int row = rank + ranks * (i + 4 * u);
+          if (in && row < rows) out[(m0 + row) * ld + n] = v[u];
+        }
+      };
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = back(v[u]) + bias;
+      if (p.ep.Z) store(p.ep.Z, p.ep.ldz);
+      switch (p.ep.act) {
+        case kActRelu: act_each<kActRelu>(v); break;
+        case kActGelu: act_each<kActGelu>(v); break;
+        case kActGeluTanh: act_each<kActGeluTanh>(v); break;
+        case kActSilu: act_each<kActSilu>(v); break;
+        default: break;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) if (p.ep.R) v[u] += res[u];
+      store(p.Y, p.ldy);
+    }
+  }
+  if (ranks > 1) cluster_sync_all();                         // a block's sums stay until every other has read them
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, kTmem);
+  }
+}
+
+}  // namespace sgc
