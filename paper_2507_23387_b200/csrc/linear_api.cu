@@ -148,11 +148,12 @@ int linear_attrs(sgemm_cube_ctx* h) {
   }
   return SGEMM_CUBE_OK;
 }
-template <int NT>
+template <int NT, bool W_F32>
 int short_batch_attrs() {
-  constexpr int smem = (int)sgc::ShortBatchCfg<NT>::SMEM_BYTES;
-  if (cudaFuncSetAttribute(sgc::short_batch_kernel<NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
-      cudaFuncSetAttribute(sgc::short_batch_kernel<NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+  constexpr int smem = (int)sgc::ShortBatchCfg<NT, W_F32>::SMEM_BYTES;
+  constexpr cudaFuncAttribute a = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  if (cudaFuncSetAttribute(sgc::short_batch_kernel<NT, false, W_F32>, a, smem) != cudaSuccess ||
+      cudaFuncSetAttribute(sgc::short_batch_kernel<NT, true, W_F32>, a, smem) != cudaSuccess) {
     cudaGetLastError();
     return SGEMM_CUBE_CUDA_ERROR;
   }
@@ -167,7 +168,9 @@ int linear_setup(sgemm_cube_ctx* h) {
       (rc = linear_attrs<sgc::kFormMM, false>(h)) || (rc = linear_attrs<sgc::kFormKM, true>(h)) ||
       (rc = linear_attrs<sgc::kFormKK, true>(h)) || (rc = linear_attrs<sgc::kFormMM, true>(h)))
     return rc;
-  if ((rc = short_batch_attrs<16>()) || (rc = short_batch_attrs<32>()) || (rc = short_batch_attrs<64>())) return rc;
+  if ((rc = short_batch_attrs<16, false>()) || (rc = short_batch_attrs<32, false>()) || (rc = short_batch_attrs<64, false>()) ||
+      (rc = short_batch_attrs<16, true>()) || (rc = short_batch_attrs<32, true>()) || (rc = short_batch_attrs<64, true>()))
+    return rc;
   h->linear_ready = true;
   return SGEMM_CUBE_OK;
 }
@@ -283,14 +286,19 @@ int linear_product_any(int form, sgemm_cube_ctx* h, int M, int N, int K, const P
 }
 
 // ------------------------------------------------------------------------------------------ few rows
-// Up to 8 rows of an FP32 weight.  Of a packed one the tensor cores are the faster way (16384 x 4096 with 8 rows 65 us,
-// 172 here), except for what a launch of theirs costs more: one row (outputs x inputs: 57 us, 65 there; 1024 x 1024 10
-// and 14), and up to four of a weight below 8 million elements (2048 x 2048 16 and 18; 4096 x 4096 29 and 27).
+// Which calls the FMA kernels take: their arithmetic grows with the rows, the tensor cores' costs a longer start
+// (cold cache, times with the launches' own).
+//   packed, outputs x inputs: one row (16384 x 4096 57 us, 65 on the tensor cores; 1024 x 1024 10 and 14), and up to four
+//   of a weight below 8 million elements (2048 x 2048 16 and 18; but 4096 x 4096 29 and 27); inputs x outputs: never
+//   (one row of 1024 x 4096 33 and 18)
+//   FP32: up to four rows (4096 x 4096 31 and 34), up to eight below 2 million elements (1024 x 1024 12 and 18; but 8 rows
+//   of 2048 x 2048 28 and 23, of 16384 x 4096 164 and 86)
 constexpr int kFewRows = 8;
 
 bool use_few_rows(int M, int N, int K, bool packed, bool nk) {
-  if (!packed) return M <= kFewRows;
-  return nk && (M == 1 || (M <= 4 && (long long)N * K < (1ll << 23)));
+  const long long weights = (long long)N * K;
+  if (!packed) return M <= 4 || (M <= kFewRows && weights < (1ll << 21));
+  return nk && (M == 1 || (M <= 4 && weights < (1ll << 23)));
 }
 
 template <int MR, int LOAD>
@@ -357,37 +365,42 @@ bool use_short_batch(const sgemm_cube_ctx* h, int M, int N, int K, int* slices) 
   return M <= kShortMoreRows && tiles <= h->sm_count && (blocks + *slices - 1) / *slices <= kShortMoreBlocks;
 }
 
-template <int NT, bool W_MN>
-int launch_short(sgemm_cube_ctx* h, const Packed& W, sgc::ShortBatchParams p, int slices, cudaStream_t st) {
+template <int NT, bool W_MN, bool W_F32>
+int launch_short(sgemm_cube_ctx* h, const sgemm_cube_operand& W, sgc::ShortBatchParams p, int slices, cudaStream_t st) {
+  using Cfg = sgc::ShortBatchCfg<NT, W_F32>;
+  constexpr CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16, f32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+  constexpr CUtensorMapSwizzle swizzle = W_F32 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
   CUtensorMap tm[2];
-  for (int w = 0; w < 2; ++w) {
-    const uint16_t* words = w ? W.lo : W.hi;
-    const int rc = W_MN ? make_map(h, &tm[w], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, words, p.N, p.K, W.ld, 64, sgc::kShortK,
-                                   CU_TENSOR_MAP_SWIZZLE_128B)
-                        : make_map(h, &tm[w], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, words, p.K, p.N, W.ld, sgc::kShortK,
-                                   sgc::kShortN, CU_TENSOR_MAP_SWIZZLE_128B);
+  for (int w = 0; w < (W_F32 ? 1 : 2); ++w) {
+    const void* words = W_F32 ? static_cast<const void*>(W.f32_dev) : (w ? W.lo_dev : W.hi_dev);
+    const int64_t ld = W_F32 ? W.ld : W.ld16;
+    const size_t size = W_F32 ? 4 : 2;
+    const int rc = W_MN ? make_map(h, &tm[w], W_F32 ? f32 : f16, size, words, p.N, p.K, ld, W_F32 ? sgc::kShortN : 64, sgc::kShortK, swizzle)
+                        : make_map(h, &tm[w], W_F32 ? f32 : f16, size, words, p.K, p.N, ld, sgc::kShortK, sgc::kShortN, swizzle);
     if (rc) return rc;
   }
+  if (W_F32) tm[1] = tm[0];
   const int blocks = (p.K + sgc::kShortK - 1) / sgc::kShortK;
-  p.kslice_blocks = (blocks + slices - 1) / slices;
-  p.ksplit = (blocks + p.kslice_blocks - 1) / p.kslice_blocks;       // no slice is empty
-  cudaLaunchAttribute attr;
-  cudaLaunchConfig_t cfg = linear_config(sgc::ShortBatchCfg<NT>::SMEM_BYTES, (unsigned)p.ksplit, &attr, st);
-  cfg.blockDim = dim3(sgc::kShortThreads, 1, 1);
-  cfg.gridDim = dim3((unsigned)((p.N + sgc::kShortN - 1) / sgc::kShortN * p.row_tiles * p.ksplit), 1, 1);
-  h->launches++;
-  if (cudaLaunchKernelEx(&cfg, sgc::short_batch_kernel<NT, W_MN>, tm[0], tm[1], p) != cudaSuccess) {
+  p.row_tiles = (p.M + NT - 1) / NT;
+  for (;; slices = 1) {                                              // clusters that cannot be scheduled: whole k
+    p.kslice_blocks = (blocks + slices - 1) / slices;
+    p.ksplit = (blocks + p.kslice_blocks - 1) / p.kslice_blocks;     // no slice is empty
+    cudaLaunchAttribute attr;
+    cudaLaunchConfig_t cfg = linear_config(Cfg::SMEM_BYTES, (unsigned)p.ksplit, &attr, st);
+    cfg.blockDim = dim3(sgc::kShortThreads, 1, 1);
+    cfg.gridDim = dim3((unsigned)((p.N + sgc::kShortN - 1) / sgc::kShortN * p.row_tiles * p.ksplit), 1, 1);
+    if (cudaLaunchKernelEx(&cfg, sgc::short_batch_kernel<NT, W_MN, W_F32>, tm[0], tm[1], p) == cudaSuccess) break;
     cudaGetLastError();
-    return SGEMM_CUBE_CUDA_ERROR;
+    if (slices == 1) return SGEMM_CUBE_CUDA_ERROR;
   }
+  h->launches++;
   return SGEMM_CUBE_OK;
 }
 template <int NT>
-int launch_short(sgemm_cube_ctx* h, const Packed& W, sgc::ShortBatchParams p, bool nk, int slices, cudaStream_t st) {
-  p.row_tiles = (p.M + NT - 1) / NT;
-  const int rc = nk ? launch_short<NT, false>(h, W, p, slices, st) : launch_short<NT, true>(h, W, p, slices, st);
-  if (rc != SGEMM_CUBE_CUDA_ERROR || slices == 1) return rc;         // clusters that cannot be scheduled: whole k
-  return nk ? launch_short<NT, false>(h, W, p, 1, st) : launch_short<NT, true>(h, W, p, 1, st);
+int launch_short(sgemm_cube_ctx* h, const sgemm_cube_operand& W, const sgc::ShortBatchParams& p, bool nk, int slices, cudaStream_t st) {
+  if (W.f32_dev)
+    return nk ? launch_short<NT, false, true>(h, W, p, slices, st) : launch_short<NT, true, true>(h, W, p, slices, st);
+  return nk ? launch_short<NT, false, false>(h, W, p, slices, st) : launch_short<NT, true, false>(h, W, p, slices, st);
 }
 
 // ------------------------------------------------------------------------------------------ arguments
@@ -522,18 +535,21 @@ int sgemm_cube_linear(sgemm_cube_handle h, int M, int N, int K, const sgemm_cube
   int n_jobs = 0, slices = 1;
   int* exps = reinterpret_cast<int*>(h->err_dev + kExpWords);
   const int w_rows = nk ? N : K, w_cols = nk ? K : N;
+  if ((rc = linear_setup(h))) return rc;                 // clusters that are resident: the choices below look at them
   const bool short_batch = !is_packed(X) && use_short_batch(h, M, N, K, &slices);
-  if ((rc = linear_setup(h))) return rc;
   Carve size;
   if (!short_batch) words_of(X, M, K, size, exps, jobs, &n_jobs);
-  words_of(W, w_rows, w_cols, size, exps + 1, jobs, &n_jobs);
-  if ((rc = grow(&h->ws, &h->ws_bytes, size.used))) return rc;
+  // An FP32 weight that TMA can read is split inside the kernel, by every tile of rows for itself: 128 rows of
+  // 2048 x 2048 29 us, 34 with packing first; 256 rows of 1024 x 1024 21 and 26, of 4096 x 1024 43 and 40.
+  const bool direct = short_batch && W->f32_dev && aligned16(W->f32_dev) && W->ld % 4 == 0;
+  if (!direct) words_of(W, w_rows, w_cols, size, exps + 1, jobs, &n_jobs);
+  if (size.used && (rc = grow(&h->ws, &h->ws_bytes, size.used))) return rc;
   Carve c;
   c.base = static_cast<uint8_t*>(h->ws);
   n_jobs = 0;
-  Packed px;
+  Packed px, pw;
   if (!short_batch) px = words_of(X, M, K, c, exps, jobs, &n_jobs);
-  const Packed pw = words_of(W, w_rows, w_cols, c, exps + 1, jobs, &n_jobs);
+  if (!direct) pw = words_of(W, w_rows, w_cols, c, exps + 1, jobs, &n_jobs);
   if (n_jobs && (rc = launch_pack(h, jobs, n_jobs, st))) return rc;
   if (short_batch) {
     sgc::ShortBatchParams p;
@@ -545,8 +561,10 @@ int sgemm_cube_linear(sgemm_cube_handle h, int M, int N, int K, const sgemm_cube
     p.err = h->err_dev;
     p.ep = ep;
     p.ep.exp_b = pw.exp;
-    if (M <= 16) return launch_short<16>(h, pw, p, nk, slices, st);
-    return M <= 32 ? launch_short<32>(h, pw, p, nk, slices, st) : launch_short<64>(h, pw, p, nk, slices, st);
+    sgemm_cube_operand w = *W;
+    if (!direct) w = sgemm_cube_operand{nullptr, 0, pw.hi, pw.lo, pw.ld, pw.exp};
+    if (M <= 16) return launch_short<16>(h, w, p, nk, slices, st);
+    return M <= 32 ? launch_short<32>(h, w, p, nk, slices, st) : launch_short<64>(h, w, p, nk, slices, st);
   }
   return linear_product_any(nk ? sgc::kFormKK : sgc::kFormKM, h, M, N, K, px, pw, Y, ldy, ep, st);
 }
