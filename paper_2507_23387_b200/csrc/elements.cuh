@@ -140,6 +140,47 @@ struct RowSlots {
     }
   }
 };
+// Vectors of rows that start `shift` elements behind a 16-byte boundary, laid on the boundaries: vector i of a thread at
+// i * threads * kVec + first, first = t * kVec - shift.  The first and the last may reach outside the row, where the
+// elements are zero.  What the first one brings from the row before is put to zero on the way out; row 0 has none
+// before it (`lead`), and there the thread copies the elements itself.
+template <typename T, int PT>
+struct ShiftedSlots {
+  static constexpr int V = Elem<T>::kVec, kWords = PT / V;
+  static __device__ __forceinline__ void ask(uint4* slots, int pitch, const T* row, int cols, int first, int threads, bool lead) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const int c = i * threads * V + first;
+      if (i == 0 && c < 0 && lead) {
+        T e[V];
+#pragma unroll
+        for (int q = 0; q < V; ++q) e[q] = c + q >= 0 ? row[c + q] : Elem<T>::put(0.f);
+        *slots = *reinterpret_cast<const uint4*>(e);
+        continue;
+      }
+      const int bytes = min(16, max(0, (cols - c) * (int)sizeof(T)));     // the rest of the slot becomes zero
+      const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(slots + i * pitch));
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                   ::"r"(dst), "l"(row + (bytes > 0 ? c : first % V)), "r"(bytes) : "memory");
+    }
+  }
+  static __device__ __forceinline__ void vector(const uint4* slots, int pitch, int i, int first, float (&e)[V]) {
+    Elem<T>::unpack(slots[i * pitch], e);
+    if (i == 0 && first < 0) {
+#pragma unroll
+      for (int q = 0; q < V; ++q) e[q] = first + q >= 0 ? e[q] : 0.f;
+    }
+  }
+  static __device__ __forceinline__ void store(T* row, int cols, int c, const float (&e)[V]) {
+    if (c >= 0 && c + V <= cols) {
+      *reinterpret_cast<uint4*>(row + c) = Elem<T>::pack(e);
+    } else if (c < cols) {
+#pragma unroll
+      for (int q = 0; q < V; ++q)
+        if ((unsigned)(c + q) < (unsigned)cols) row[c + q] = Elem<T>::put(e[q]);
+    }
+  }
+};
 __device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }

@@ -9,6 +9,12 @@
 // taken about the mean (no cancellation of squares) without a second read.  Blocks are persistent: a
 // group asks for its next rows before it works on the present one, and keeps its columns' weights (forward)
 // or running sums of dw and db (backward) in registers all the way.
+//
+// Rows of an odd length start anywhere between two 16-byte boundaries and are read element by element, except by the
+// backward kernel where all tensors agree in where a row starts: then the vectors are laid on the boundaries
+// (kShifted), and a group's rows are a multiple of 8 (FP32: 4) apart, so that they all start equally far behind one
+// and a thread's columns stay the same (4000 x 7001 BF16 58 us, 83 by elements; the forward kernel gained 2 of 41
+// and lost as much on aligned rows).
 #include <atomic>
 
 #include "ctx.cuh"
@@ -72,6 +78,7 @@ struct NormParams {
   const float* mean_in;
   const float* rstd_in;
   float* part;             // backward: [blocks][2][cols] partial sums of dw and db, or null
+  int period;              // backward: rows this far apart start equally far behind a 16-byte boundary
 };
 
 // WARPS warps a row, 8 / WARPS rows a block (one for WARPS >= 8).
@@ -174,8 +181,11 @@ __global__ void __launch_bounds__(1024) norm_forward_long_kernel(NormParams p) {
 // rows (1024 threads, 64 registers each) stay in their slots and are read twice from there, for the sums and for dx;
 // shorter ones are held in registers with the weights (2048 x 16384 FP32 260 us held, 110 read twice; 8192 x 4096
 // 81 held, 90 read twice).
-template <typename T, int WARPS, bool VEC>
+enum RowAccess { kElements = 0, kAligned, kShifted };
+
+template <typename T, int WARPS, RowAccess ACCESS>
 __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 2) norm_backward_kernel(NormParams p) {
+  constexpr bool VEC = ACCESS != kElements, SHIFT = ACCESS == kShifted;
   constexpr int kGroups = WARPS >= 8 ? 1 : 8 / WARPS, kThreads = WARPS * 32;
   __shared__ float buf[2][kGroups * WARPS * 2];
   const int group = threadIdx.x / kThreads, t = threadIdx.x % kThreads, wg = t >> 5;
@@ -193,6 +203,15 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
     next_rstd = __ldg(p.rstd_in + r);
   };
   if (row < p.rows) fetch_stats(row);
+  // the thread's first column, and the column of its element i
+  int first = VEC ? t * Elem<T>::kVec : t;
+  if constexpr (SHIFT)
+    first -= (int)((reinterpret_cast<uintptr_t>(static_cast<const T*>(p.X) + row * p.ldx) & 15u) / sizeof(T));
+  auto column = [&](int i) {
+    constexpr int V = VEC ? Elem<T>::kVec : 1;
+    return i / V * kThreads * V + first + i % V;
+  };
+  auto inside = [&](int c) { return (unsigned)c < (unsigned)p.cols; };
   if constexpr (VEC) {
     constexpr int V = Elem<T>::kVec, kWords = kPT / V, kBlock = WARPS > 8 ? WARPS * 32 : 256;
     constexpr int kRing = kStages<T, WARPS, VEC, 2>;
@@ -200,20 +219,37 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
     auto ask = [&](long long r, int s) {               // an empty group past the end
       if (r < p.rows) {
         uint4* to = ring + s * 2 * kWords * kBlock + threadIdx.x;
-        RowSlots<T, kPT>::ask(to, kBlock, static_cast<const T*>(p.X) + r * p.ldx, p.cols, t, kThreads);
-        RowSlots<T, kPT>::ask(to + kWords * kBlock, kBlock, static_cast<const T*>(p.dY) + r * p.lddy, p.cols, t, kThreads);
+        const T* x = static_cast<const T*>(p.X) + r * p.ldx;
+        const T* g = static_cast<const T*>(p.dY) + r * p.lddy;
+        if constexpr (SHIFT) {
+          ShiftedSlots<T, kPT>::ask(to, kBlock, x, p.cols, first, kThreads, r == 0);
+          ShiftedSlots<T, kPT>::ask(to + kWords * kBlock, kBlock, g, p.cols, first, kThreads, r == 0);
+        } else {
+          RowSlots<T, kPT>::ask(to, kBlock, x, p.cols, t, kThreads);
+          RowSlots<T, kPT>::ask(to + kWords * kBlock, kBlock, g, p.cols, t, kThreads);
+        }
       }
       async_commit();
     };
     constexpr bool kHold = WARPS <= 16;
-    const bool wvec = (reinterpret_cast<uintptr_t>(p.weight) & 15u) == 0;
+    const bool wvec = !SHIFT && (reinterpret_cast<uintptr_t>(p.weight) & 15u) == 0;
     float w[kHold ? kPT : 1];
-    if constexpr (kHold) load_params<T, kPT, VEC>(p.weight, 1.f, p.cols, t, kThreads, w);
+    if constexpr (kHold && SHIFT) {
+#pragma unroll
+      for (int i = 0; i < kPT; ++i) w[i] = p.weight && inside(column(i)) ? __ldg(p.weight + column(i)) : 1.f;
+    } else if constexpr (kHold) {
+      load_params<T, kPT, VEC>(p.weight, 1.f, p.cols, t, kThreads, w);
+    }
     // n, dy and u = dy w of vector i of a row
     auto vector_of = [&](const uint4* from, int i, float mean, float rstd, float (&n)[V], float (&g)[V], float (&u)[V]) {
-      Elem<T>::unpack(from[i * kBlock], n);
-      Elem<T>::unpack(from[(kWords + i) * kBlock], g);
-      const int c = (i * kThreads + t) * V;
+      if constexpr (SHIFT) {
+        ShiftedSlots<T, kPT>::vector(from, kBlock, i, first, n);
+        ShiftedSlots<T, kPT>::vector(from + kWords * kBlock, kBlock, i, first, g);
+      } else {
+        Elem<T>::unpack(from[i * kBlock], n);
+        Elem<T>::unpack(from[(kWords + i) * kBlock], g);
+      }
+      const int c = column(i * V);
 #pragma unroll
       for (int q = 0; q < V; ++q) n[q] = (n[q] - mean) * rstd;
       if constexpr (kHold) {
@@ -228,7 +264,7 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
           }
         } else {
 #pragma unroll
-          for (int q = 0; q < V; ++q) u[q] = g[q] * __ldg(p.weight + c + q);
+          for (int q = 0; q < V; ++q) u[q] = !SHIFT || inside(c + q) ? g[q] * __ldg(p.weight + c + q) : 0.f;
         }
       } else {
 #pragma unroll
@@ -272,8 +308,9 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
           if (!kHold) vector_of(from, i, mean, rstd, n, g, u);
 #pragma unroll
           for (int q = 0; q < V; ++q) u[q] = rstd * (u[q] - mu - n[q] * mun);
-          const int c = (i * kThreads + t) * V;
-          if (c < p.cols) *reinterpret_cast<uint4*>(out + c) = Elem<T>::pack(u);
+          const int c = column(i * V);
+          if constexpr (SHIFT) ShiftedSlots<T, kPT>::store(out, p.cols, c, u);
+          else if (c < p.cols) *reinterpret_cast<uint4*>(out + c) = Elem<T>::pack(u);
         }
       }
       if (kRing == 1) ask(row + step, 0);              // the thread has read its slots for the last time
@@ -323,8 +360,8 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
   if constexpr (kGroups == 1) {
 #pragma unroll
     for (int i = 0; i < kPT; ++i) {
-      const int c = row_column<T, VEC>(i, t, kThreads);
-      if (c < p.cols) { pw[c] = dw[i]; pw[p.cols + c] = db[i]; }
+      const int c = column(i);
+      if (inside(c)) { pw[c] = dw[i]; pw[p.cols + c] = db[i]; }
     }
   } else {                                             // the block's groups first, in order
     __shared__ float sum[2][kThreads * kPT];
@@ -332,8 +369,10 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
       if (g == group) {
 #pragma unroll
         for (int i = 0; i < kPT; ++i) {
-          sum[0][i * kThreads + t] = (g ? sum[0][i * kThreads + t] : 0.f) + dw[i];
-          sum[1][i * kThreads + t] = (g ? sum[1][i * kThreads + t] : 0.f) + db[i];
+          const int at = SHIFT ? column(i) : i * kThreads + t;       // shifted groups hold their columns elsewhere
+          if (SHIFT && !inside(at)) continue;
+          sum[0][at] = (g ? sum[0][at] : 0.f) + dw[i];
+          sum[1][at] = (g ? sum[1][at] : 0.f) + db[i];
         }
       }
       __syncthreads();
@@ -341,8 +380,8 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
     if (group == 0) {
 #pragma unroll
       for (int i = 0; i < kPT; ++i) {
-        const int c = row_column<T, VEC>(i, t, kThreads);
-        if (c < p.cols) { pw[c] = sum[0][i * kThreads + t]; pw[p.cols + c] = sum[1][i * kThreads + t]; }
+        const int c = column(i), at = SHIFT ? c : i * kThreads + t;
+        if (inside(c)) { pw[c] = sum[0][at]; pw[p.cols + c] = sum[1][at]; }
       }
     }
   }
@@ -434,7 +473,7 @@ int done(sgemm_cube_ctx* h) {
 // Blocks of a persistent kernel: one per `groups` rows, at most what is resident at once.  `KERNEL` is asked for its
 // occupancy once a device.
 template <auto KERNEL>
-int persistent_blocks(sgemm_cube_ctx* h, int threads, size_t smem, int rows, int groups, int* blocks) {
+int persistent_blocks(sgemm_cube_ctx* h, int threads, size_t smem, int rows, int period, int groups, int* blocks) {
   static std::atomic<int> known[64];                   // blocks an SM, per device; 0: not asked yet
   std::atomic<int>* entry = h->device < 64 ? &known[h->device] : nullptr;
   auto kernel = KERNEL;
@@ -447,7 +486,8 @@ int persistent_blocks(sgemm_cube_ctx* h, int threads, size_t smem, int rows, int
   }
   if (entry) entry->store(per_sm, std::memory_order_relaxed);
   const long long want = ((long long)rows + groups - 1) / groups, cap = (long long)per_sm * h->sm_count;
-  *blocks = (int)(want < cap ? want : cap);
+  const long long turn = period > groups ? period / groups : 1;      // blocks that take `period` rows, or more
+  *blocks = (int)(want <= cap ? want : (cap > turn ? cap / turn * turn : turn));
   return SGEMM_CUBE_OK;
 }
 
@@ -456,7 +496,7 @@ int forward_rows(sgemm_cube_ctx* h, const NormParams& p, cudaStream_t st) {
   constexpr int groups = WARPS >= 8 ? 1 : 8 / WARPS, threads = WARPS > 8 ? WARPS * 32 : 256;
   int blocks = 0;
   constexpr size_t smem = sgc::kSlotBytes<T, WARPS, VEC, 1>;
-  const int rc = persistent_blocks<sgc::norm_forward_kernel<T, WARPS, VEC>>(h, threads, smem, p.rows, groups, &blocks);
+  const int rc = persistent_blocks<sgc::norm_forward_kernel<T, WARPS, VEC>>(h, threads, smem, p.rows, 1, groups, &blocks);
   if (rc) return rc;
   sgc::norm_forward_kernel<T, WARPS, VEC><<<(unsigned)blocks, threads, smem, st>>>(p);
   return done(h);
@@ -473,19 +513,19 @@ int forward_typed(sgemm_cube_ctx* h, const NormParams& p, cudaStream_t st) {
   return done(h);
 }
 
-template <typename T, int WARPS, bool VEC>
+template <typename T, int WARPS, sgc::RowAccess ACCESS>
 int backward_rows(sgemm_cube_ctx* h, NormParams p, float* dweight, float* dbias, cudaStream_t st) {
   constexpr int groups = WARPS >= 8 ? 1 : 8 / WARPS, threads = WARPS > 8 ? WARPS * 32 : 256;
   int blocks = 0;
-  constexpr size_t smem = sgc::kSlotBytes<T, WARPS, VEC, 2>;
-  int rc = persistent_blocks<sgc::norm_backward_kernel<T, WARPS, VEC>>(h, threads, smem, p.rows, groups, &blocks);
+  constexpr size_t smem = sgc::kSlotBytes<T, WARPS, ACCESS != sgc::kElements, 2>;
+  int rc = persistent_blocks<sgc::norm_backward_kernel<T, WARPS, ACCESS>>(h, threads, smem, p.rows, p.period, groups, &blocks);
   if (rc) return rc;
   if (dweight || dbias) {
     rc = grow(&h->part_ws, &h->part_ws_bytes, (size_t)blocks * 2 * p.cols * 4);
     if (rc) return rc;
     p.part = static_cast<float*>(h->part_ws);
   }
-  sgc::norm_backward_kernel<T, WARPS, VEC><<<(unsigned)blocks, threads, smem, st>>>(p);
+  sgc::norm_backward_kernel<T, WARPS, ACCESS><<<(unsigned)blocks, threads, smem, st>>>(p);
   rc = done(h);
   if (rc || !p.part) return rc;
   sgc::norm_parts_kernel<<<dim3((unsigned)((p.cols + 31) / 32), 2), 512, 0, st>>>(p.part, blocks, p.cols, dweight, dbias);
@@ -511,15 +551,35 @@ int backward_long(sgemm_cube_ctx* h, NormParams p, float* dweight, float* dbias,
   sgc::norm_backward_long_kernel<T><<<(unsigned)p.rows, 1024, 0, st>>>(p);
   return done(h);
 }
-template <typename T, bool VEC>
-int backward_typed(sgemm_cube_ctx* h, const NormParams& p, float* dw, float* db, cudaStream_t st) {
-  if (p.cols <= 1 * 32 * sgc::kPT) return backward_rows<T, 1, VEC>(h, p, dw, db, st);
-  if (p.cols <= 2 * 32 * sgc::kPT) return backward_rows<T, 2, VEC>(h, p, dw, db, st);
-  if (p.cols <= 4 * 32 * sgc::kPT) return backward_rows<T, 4, VEC>(h, p, dw, db, st);
-  if (p.cols <= 8 * 32 * sgc::kPT) return backward_rows<T, 8, VEC>(h, p, dw, db, st);
-  if (p.cols <= 16 * 32 * sgc::kPT) return backward_rows<T, 16, VEC>(h, p, dw, db, st);
-  if (p.cols <= 32 * 32 * sgc::kPT) return backward_rows<T, 32, VEC>(h, p, dw, db, st);
+template <typename T, sgc::RowAccess ACCESS>
+int backward_as(sgemm_cube_ctx* h, const NormParams& p, float* dw, float* db, cudaStream_t st) {
+  if (p.cols <= 1 * 32 * sgc::kPT) return backward_rows<T, 1, ACCESS>(h, p, dw, db, st);
+  if (p.cols <= 2 * 32 * sgc::kPT) return backward_rows<T, 2, ACCESS>(h, p, dw, db, st);
+  if (p.cols <= 4 * 32 * sgc::kPT) return backward_rows<T, 4, ACCESS>(h, p, dw, db, st);
+  if (p.cols <= 8 * 32 * sgc::kPT) return backward_rows<T, 8, ACCESS>(h, p, dw, db, st);
+  if (p.cols <= 16 * 32 * sgc::kPT) return backward_rows<T, 16, ACCESS>(h, p, dw, db, st);
+  if (p.cols <= 32 * 32 * sgc::kPT) return backward_rows<T, 32, ACCESS>(h, p, dw, db, st);
   return backward_long<T>(h, p, dw, db, st);
+}
+
+template <typename T>
+int backward_typed(sgemm_cube_ctx* h, NormParams p, float* dw, float* db, cudaStream_t st) {
+  constexpr int v = sgc::Elem<T>::kVec;
+  p.period = 1;
+  if (sgc::rows_take_vectors(p.X, p.ldx, p.cols, sizeof(T)) && sgc::rows_take_vectors(p.dY, p.lddy, p.cols, sizeof(T)) &&
+      (!p.out || sgc::rows_take_vectors(p.out, p.ldo, p.cols, sizeof(T))))
+    return backward_as<T, sgc::kAligned>(h, p, dw, db, st);
+  // All rows start alike, and what the first vector lays in front costs no more warps a row.
+  const auto start = [](const void* q) { return reinterpret_cast<uintptr_t>(q) % 16; };
+  bool alike = start(p.X) == start(p.dY) && (p.ldx - p.lddy) % v == 0;
+  if (p.out) alike = alike && start(p.X) == start(p.out) && (p.ldx - p.ldo) % v == 0;
+  int limit = 32 * sgc::kPT;
+  while (limit < p.cols) limit *= 2;
+  if (alike && p.cols >= v && p.cols + v - 1 <= limit && limit <= 32 * 32 * sgc::kPT) {
+    if (p.ldx % v) p.period = v;
+    return backward_as<T, sgc::kShifted>(h, p, dw, db, st);
+  }
+  return backward_as<T, sgc::kElements>(h, p, dw, db, st);
 }
 
 size_t elem_size(int dtype) { return dtype == SGEMM_CUBE_F32 ? 4 : 2; }
@@ -582,15 +642,9 @@ int sgemm_cube_layer_norm_backward(sgemm_cube_handle h, int rows, int cols, int 
   p.out = dX; p.ldo = lddx;
   p.weight = weight;
   p.mean_in = mean; p.rstd_in = rstd;
-  const size_t e = elem_size(dtype);
-  const bool vec = sgc::rows_take_vectors(X, ldx, cols, e) && sgc::rows_take_vectors(dY, lddy, cols, e) &&
-                   (!dX || sgc::rows_take_vectors(dX, lddx, cols, e));
-  if (dtype == SGEMM_CUBE_F32)
-    return vec ? backward_typed<float, true>(h, p, dweight, dbias, st) : backward_typed<float, false>(h, p, dweight, dbias, st);
-  if (dtype == SGEMM_CUBE_F16)
-    return vec ? backward_typed<__half, true>(h, p, dweight, dbias, st) : backward_typed<__half, false>(h, p, dweight, dbias, st);
-  return vec ? backward_typed<__nv_bfloat16, true>(h, p, dweight, dbias, st)
-             : backward_typed<__nv_bfloat16, false>(h, p, dweight, dbias, st);
+  if (dtype == SGEMM_CUBE_F32) return backward_typed<float>(h, p, dweight, dbias, st);
+  if (dtype == SGEMM_CUBE_F16) return backward_typed<__half>(h, p, dweight, dbias, st);
+  return backward_typed<__nv_bfloat16>(h, p, dweight, dbias, st);
 }
 
 }  // extern "C"
