@@ -344,7 +344,7 @@ int sgemm_cube_auto_scaled(sgemm_cube_handle h, int M, int N, int K,
  * given tokens with their gradient.  No call synchronises; once the handle's workspace has its size
  * the calls can be captured into a graph.  As everywhere, calls on one handle that may overlap on the
  * GPU need one handle per stream.  Sums, statistics and softmax sums are FP32 (the products' k-blocks as
- * sgemm_cube, termwise); every result is the same from call to call.
+ * sgemm_cube, termwise, unless said otherwise); every result is the same from call to call.
  */
 
 /* Operand of a linear layer: a row-major FP32 matrix (f32_dev, ld), or, with f32_dev NULL, one packed by
@@ -393,8 +393,11 @@ int sgemm_cube_pack(sgemm_cube_handle h, int rows, int cols,
  *   bias_dev N FP32 or NULL;  R_dev M x N FP32 (ldr >= N) or NULL, may be Y_dev itself (then ldr == ldy)
  *   Y_dev M x N FP32 (written);  Z_dev M x N FP32 or NULL: z is stored there for the backward pass
  * FP32 matrices may have any alignment.  The product is the three-product form of sgemm_cube on packed
- * operands; an FP32 X of at most 8 rows is multiplied in FP32 (W read once, no packing).  M, N, K >= 0;
- * K == 0 gives Y = act(b) + R.
+ * operands, with two forms of its own for an FP32 X of few rows, which read W once and pack nothing ahead:
+ * for a short batch (up to 64 rows, to 256 for small weights) X, and an FP32 W that starts its rows on 16 bytes,
+ * are split inside the kernel with an exponent for every 64 inputs instead of one for the matrix, and the
+ * sums are taken over k-blocks of 64; one to eight rows may be multiplied in FP32.  M, N, K >= 0; K == 0 gives
+ * Y = act(b) + R.
  * Errors: INVALID_ARG, MISALIGNED (packed operands), ALLOC_FAILED, CUDA_ERROR. */
 int sgemm_cube_linear(sgemm_cube_handle h, int M, int N, int K,
                       const sgemm_cube_operand* X, const sgemm_cube_operand* W, int weight_layout,
