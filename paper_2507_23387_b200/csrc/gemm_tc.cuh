@@ -284,6 +284,8 @@ __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[64]) 
 // packed operands (linear_epilogue.cuh): one power-of-two exponent per operand is undone and the
 // layer's epilogue applied.  The two letters say which index of A and of B is contiguous in memory:
 // K the contracted one, M the other (row-major A is K, row-major B is M).
+// 8192 x 16384 x 4096 under the power cap: forward with gelu and z 2416 us, dX 2256, dW 2262 (1365 to 1460 TFLOP/s of FP16
+// products); 1024 x 4096 x 1024, one wave: 33 bare, 50 with everything.
 enum LinearForm { kFormProduct = 0, kFormKM, kFormKK, kFormMM };
 
 struct TcLinearParams : TcGemmParams {

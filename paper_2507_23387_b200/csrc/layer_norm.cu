@@ -4,7 +4,8 @@
 //   backward   u = dy w;  n = (x - mean) rstd;  dx = rstd (u - mean(u) - n mean(u n))
 //              dw = sum over rows of dy n;  db = sum over rows of dy
 //
-// Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx, each once.  A row
+// Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx, each once (8192 x 4096 FP32
+// 46 us and 73, 5.8 and 5.5 TB/s; BF16 rows by instructions as well, 6000 x 2048 13 and 26, 3.8 and 2.8 TB/s).  A row
 // lives in the registers of one group of warps between its load and its store, so the second moment is
 // taken about the mean (no cancellation of squares) without a second read.  Blocks are persistent: a
 // group asks for its next rows before it works on the present one, and keeps its columns' weights (forward)

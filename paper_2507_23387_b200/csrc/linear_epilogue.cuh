@@ -1,4 +1,5 @@
-// What a linear layer does to a finished product element, and how a tile of them is stored.  Shared by the tensor-core kernel's epilogue, the split-K reduction and the few-row kernel.
+// What a linear layer does to a finished product element, and how a tile of them is stored.  Shared by the
+// tensor-core kernels' epilogues and the few-row kernels.
 //
 //   z = 2^-(p_x + p_w) acc + b[col],   y = act(z) + R[row, col]
 //
