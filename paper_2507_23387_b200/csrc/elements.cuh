@@ -80,36 +80,20 @@ struct Elem<__nv_bfloat16> {
 // (i * threads + t) * kVec; otherwise (rows that are not 16-byte aligned) single elements, element i at
 // i * threads + t.  Either way a warp's accesses are contiguous.  PT elements a thread, columns past
 // `cols` read as zero.
-// A row is asked for (fetch) before it is needed (get): the raw words wait in registers.
-template <typename T, int PT, bool VEC>
+// Single elements of a row that is asked for (fetch) before it is needed (get): they wait in registers.
+template <typename T, int PT>
 struct RowRegs {
-  static constexpr int kWords = VEC ? PT / Elem<T>::kVec : PT;
-  typename std::conditional<VEC, uint4, T>::type raw[kWords];
+  T raw[PT];
   __device__ __forceinline__ void fetch(const T* row, int cols, int t, int threads) {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-      if constexpr (VEC) {
-        const int c = (i * threads + t) * Elem<T>::kVec;
-        raw[i] = c < cols ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0, 0, 0, 0);
-      } else {
-        const int c = i * threads + t;
-        raw[i] = c < cols ? row[c] : Elem<T>::put(0.f);
-      }
+    for (int i = 0; i < PT; ++i) {
+      const int c = i * threads + t;
+      raw[i] = c < cols ? row[c] : Elem<T>::put(0.f);
     }
   }
   __device__ __forceinline__ void get(float (&v)[PT]) const {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-      if constexpr (VEC) {
-        constexpr int V = Elem<T>::kVec;
-        float e[V];
-        Elem<T>::unpack(raw[i], e);
-#pragma unroll
-        for (int q = 0; q < V; ++q) v[i * V + q] = e[q];
-      } else {
-        v[i] = Elem<T>::get(raw[i]);
-      }
-    }
+    for (int i = 0; i < PT; ++i) v[i] = Elem<T>::get(raw[i]);
   }
 };
 // The same through shared memory, for vectors: a thread's own 16-byte slots, filled by asynchronous copies of the

@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
   constexpr int kRing = kStages<T, WARPS, VEC, 1>, kAhead = kRing - 1;
   static_assert(!VEC || kRing >= 2, "forward rows always fit twice");
   extern __shared__ uint4 ring[];                      // [kRing][kWords][kBlock]
-  RowRegs<T, kPT, VEC> next;
+  RowRegs<T, VEC ? 1 : kPT> next;                      // (not for vectors)
   auto ask = [&](long long r, int s) {                 // an empty group past the end
     if (r < p.rows)
       RowSlots<T, kPT>::ask(ring + s * kWords * kBlock + threadIdx.x, kBlock, static_cast<const T*>(p.X) + r * p.ldx,
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
       stage = stage + 1 >= kRing ? 0 : stage + 1;
     }
   } else {
-    RowRegs<T, kPT, VEC> next_x, next_g;
+    RowRegs<T, kPT> next_x, next_g;
     auto fetch = [&](long long r) {
       next_x.fetch(static_cast<const T*>(p.X) + r * p.ldx, p.cols, t, kThreads);
       next_g.fetch(static_cast<const T*>(p.dY) + r * p.lddy, p.cols, t, kThreads);
