@@ -203,27 +203,40 @@ short_batch_kernel(const __grid_constant__ CUtensorMap tm_hi, const __grid_const
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
     if (lane == 0) {
-      constexpr uint32_t idesc = umma_idesc_f16(kShortN, NT, W_MN, false);
-      constexpr uint32_t w_step = W_MN ? 2048 : 32;          // bytes from one k16 step to the next
+      // An MMA of 128 rows and 16 k takes about 120 clocks however few columns it has, so hi and lo words of X, which lie
+      // one behind the other, are the columns of one: hi*hi and hi*lo next to each other, lo*hi onto the second.  (With
+      // three MMAs a k16 step they bound the kernel: 1440 clocks a block.)
+      constexpr uint32_t idesc_both = umma_idesc_f16(kShortN, 2 * NT, W_MN, false), idesc = umma_idesc_f16(kShortN, NT, W_MN, false);
+      // Descriptors: everything but the address (low word, 16-byte units) is constant, and an MMA's costs one addition.
+      // A single lane issues them all.
+      constexpr uint32_t desc_hi = (1024u >> 4) | (1u << 14) | ((uint32_t)kSwizzle128 << 29);
+      constexpr uint32_t w_lo0 = ((W_MN ? 8192u : 16u) >> 4) << 16, x_lo0 = (16u >> 4) << 16;
+      constexpr uint32_t w_step = (W_MN ? 2048u : 32u) >> 4, x_step = 32u >> 4;    // from one k16 step to the next
+      constexpr uint32_t w_words = Cfg::W_TILE >> 4;   // from hi to lo words
+      const uint32_t ring = (smem_u32(smem) & 0x3FFFFu) >> 4;                      // (a cluster's rank bits cut off)
+      auto desc = [](uint32_t lo) {
+        uint64_t d;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(desc_hi));
+        return d;
+      };
+      int s = 0;
+      uint32_t phase = 0;
       for (int i = 0; i < count; ++i) {
-        const int s = i % STAGES, r = i & 1;
-        if (!mbar_wait_bounded(&full_bar[s], (i / STAGES) & 1, abort_flag, p.err, kErrMmaFullWait)) break;
+        const int r = i & 1;
+        if (!mbar_wait_bounded(&full_bar[s], phase, abort_flag, p.err, kErrMmaFullWait)) break;
         if (!mbar_wait_bounded(&tempty_bar[r], ((i >> 1) & 1) ^ 1, abort_flag, p.err, kErrMmaTmemEmptyWait)) break;
         tc_fence_after_sync();
-        const uint32_t w = smem_u32(smem + s * Cfg::STAGE_BYTES), x = w + 2 * Cfg::W_TILE;
+        const uint32_t w = ring + s * (Cfg::STAGE_BYTES >> 4) + w_lo0;
+        const uint32_t x = ring + s * (Cfg::STAGE_BYTES >> 4) + 2 * w_words + x_lo0;
         const uint32_t d = tmem + r * 2 * NT;
-        auto w_desc = [&](uint32_t a) { return umma_smem_desc(a, W_MN ? 8192 : 16, 1024, kSwizzle128); };
-        auto x_desc = [&](uint32_t a) { return umma_smem_desc(a, 16, 1024, kSwizzle128); };
-#pragma unroll
-        for (int j = 0; j < kShortK / 16; ++j)
-          umma_f16_ss(d, w_desc(w + j * w_step), x_desc(x + j * 32), idesc, j != 0);
 #pragma unroll
         for (int j = 0; j < kShortK / 16; ++j) {
-          umma_f16_ss(d + NT, w_desc(w + Cfg::W_TILE + j * w_step), x_desc(x + j * 32), idesc, j != 0);
-          umma_f16_ss(d + NT, w_desc(w + j * w_step), x_desc(x + Cfg::X_TILE + j * 32), idesc, 1);
+          umma_f16_ss(d, desc(w + j * w_step), desc(x + j * x_step), idesc_both, j != 0);
+          umma_f16_ss(d + NT, desc(w + w_words + j * w_step), desc(x + j * x_step), idesc, 1);
         }
         umma_commit(&empty_bar[s]);
         umma_commit(&tfull_bar[r]);
+        if (++s == STAGES) { s = 0; phase ^= 1; }
       }
     }
   } else if (W_F32 && warp >= 8) {
