@@ -109,7 +109,8 @@ short_batch_kernel(const __grid_constant__ CUtensorMap tm_hi, const __grid_const
                    const ShortBatchParams p) {
   using Cfg = ShortBatchCfg<NT, W_F32>;
   constexpr int STAGES = Cfg::STAGES, F32_STAGES = Cfg::F32_STAGES, kRing = 16, kGroups = 4;
-  constexpr uint32_t kTmem = 4 * NT < 32 ? 32 : 4 * NT;      // two regions of hi*hi and of cross sums
+  // two TMEM regions: hi*hi and hi*lo sums (2 NT columns), lo*hi sums (NT columns, at 2 NT)
+  constexpr uint32_t kRegion = 4 * NT, kTmem = 2 * kRegion;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + Cfg::RING_BYTES);    // TMA and converters -> MMA
@@ -204,8 +205,9 @@ short_batch_kernel(const __grid_constant__ CUtensorMap tm_hi, const __grid_const
     // ------------------------------------------------------------------ MMA issuer
     if (lane == 0) {
       // An MMA of 128 rows and 16 k takes about 120 clocks however few columns it has, so hi and lo words of X, which lie
-      // one behind the other, are the columns of one: hi*hi and hi*lo next to each other, lo*hi onto the second.  (With
-      // three MMAs a k16 step they bound the kernel: 1440 clocks a block.)
+      // one behind the other, are the columns of one: hi*hi and hi*lo next to each other.  lo*hi has columns of its own,
+      // since only MMAs of the same shape are sure to follow one another on the same sums.  (With three MMAs a k16 step
+      // they bound the kernel: 1440 clocks a block.)
       constexpr uint32_t idesc_both = umma_idesc_f16(kShortN, 2 * NT, W_MN, false), idesc = umma_idesc_f16(kShortN, NT, W_MN, false);
       // Descriptors: everything but the address (low word, 16-byte units) is constant, and an MMA's costs one addition.
       // A single lane issues them all.
@@ -228,11 +230,11 @@ short_batch_kernel(const __grid_constant__ CUtensorMap tm_hi, const __grid_const
         tc_fence_after_sync();
         const uint32_t w = ring + s * (Cfg::STAGE_BYTES >> 4) + w_lo0;
         const uint32_t x = ring + s * (Cfg::STAGE_BYTES >> 4) + 2 * w_words + x_lo0;
-        const uint32_t d = tmem + r * 2 * NT;
+        const uint32_t d = tmem + r * kRegion;
 #pragma unroll
         for (int j = 0; j < kShortK / 16; ++j) {
           umma_f16_ss(d, desc(w + j * w_step), desc(x + j * x_step), idesc_both, j != 0);
-          umma_f16_ss(d + NT, desc(w + w_words + j * w_step), desc(x + j * x_step), idesc, 1);
+          umma_f16_ss(d + 2 * NT, desc(w + w_words + j * w_step), desc(x + j * x_step), idesc, j != 0);
         }
         umma_commit(&empty_bar[s]);
         umma_commit(&tfull_bar[r]);
@@ -388,13 +390,15 @@ short_batch_kernel(const __grid_constant__ CUtensorMap tm_hi, const __grid_const
       const float f = pow2_down(e - now);
 #pragma unroll
       for (int g = 0; g < NT / 16; ++g) {
-        uint32_t vh[16], vx[16];
-        tmem_ld_32x32b_x16(mine + r * 2 * NT + g * 16, vh);
-        tmem_ld_32x32b_x16(mine + r * 2 * NT + NT + g * 16, vx);
+        uint32_t v[3][16];
+#pragma unroll
+        for (int a = 0; a < 3; ++a) tmem_ld_32x32b_x16(mine + r * kRegion + a * NT + g * 16, v[a]);
         tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          S[g * 16 + j] = fmaf(fmaf(__uint_as_float(vx[j]), kPackInvScale, __uint_as_float(vh[j])), f, S[g * 16 + j]);
+        for (int j = 0; j < 16; ++j) {
+          const float cross = __uint_as_float(v[1][j]) + __uint_as_float(v[2][j]);
+          S[g * 16 + j] = fmaf(fmaf(cross, kPackInvScale, __uint_as_float(v[0][j])), f, S[g * 16 + j]);
+        }
       }
       tc_fence_before_sync();
       __syncwarp();
