@@ -2,7 +2,8 @@
 //
 // The weight's 4 bytes per element are what bounds it, so the weight takes the 128-row side of the tile and the few rows
 // of X the narrow one (16, 32 or 64 columns): a stage holds 32 KB of the weight and little else, and four to six of
-// them are in flight in every SM (16384 x 4096 packed, 24 rows: 52 us, 5.2 TB/s; its 128 tiles leave 20 SMs idle).  An
+// them are in flight in every SM (16384 x 4096 packed, 24 rows: 50 us, 5.4 TB/s; its 128 tiles leave 20 SMs idle, and
+// the MMA thread needs 1100 clocks of the 1500 that a block of 64 k takes).  An
 // FP32 weight comes in FP32 and is split here too, by eight warps, which then bound the kernel (86 us where packing and
 // the product on packed words took 200).  X is not packed by a launch of its own: warps of this kernel turn 64 columns of it
 // into words as they are needed, each such block with an exponent of its own (15 - e_max, as in packing; the more
@@ -120,12 +121,13 @@ short_batch_kernel(const __grid_constant__ CUtensorMap tm_hi, const __grid_const
   uint64_t* pair_bar = tempty_bar + 2;                                         // [kGroups] between two converter warps
   uint64_t* full32_bar = pair_bar + kGroups;                                   // FP32 weights: TMA -> converters
   uint64_t* empty32_bar = full32_bar + F32_STAGES;                             // and back
-  int* block_exp = reinterpret_cast<int*>(empty32_bar + F32_STAGES);           // [kRing]
+  uint64_t* drain_bar = empty32_bar + F32_STAGES;                              // the MMA thread's last wait
+  int* block_exp = reinterpret_cast<int*>(drain_bar + 1);                      // [kRing]
   uint32_t* part_max = reinterpret_cast<uint32_t*>(block_exp + kRing);         // [2][8 warps][X, weight]
   int* slice_exp = reinterpret_cast<int*>(part_max + 32);                      // [8] of the cluster's blocks
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(slice_exp + 8);
   volatile uint32_t* abort_flag = tmem_slot + 1;
-  static_assert((2 * STAGES + 4 + kGroups + 2 * F32_STAGES) * 8 + (kRing + 32 + 8 + 2) * 4 <= 1024, "barrier block");
+  static_assert((2 * STAGES + 5 + kGroups + 2 * F32_STAGES) * 8 + (kRing + 32 + 8 + 2) * 4 <= 1024, "barrier block");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int ranks = p.ksplit, rank = ranks > 1 ? (int)cluster_ctarank() : 0;
@@ -143,6 +145,7 @@ short_batch_kernel(const __grid_constant__ CUtensorMap tm_hi, const __grid_const
       mbar_init(&tfull_bar[r], 1);
       mbar_init(&tempty_bar[r], 4);
     }
+    mbar_init(drain_bar, 1);
     for (int g = 0; g < kGroups; ++g) mbar_init(&pair_bar[g], W_F32 ? 8 : 2);
     for (int s = 0; s < F32_STAGES; ++s) {
       mbar_init(&full32_bar[s], 1);
@@ -240,6 +243,9 @@ short_batch_kernel(const __grid_constant__ CUtensorMap tm_hi, const __grid_const
         umma_commit(&tfull_bar[r]);
         if (++s == STAGES) { s = 0; phase ^= 1; }
       }
+      // whether the loop came to its end or not: everything issued has been done before TMEM is freed
+      umma_commit(drain_bar);
+      mbar_wait_bounded(drain_bar, 0, nullptr, p.err, kErrDrainWait);
     }
   } else if (W_F32 && warp >= 8) {
     // ------------------------------------------------------------------ converters: weight and X to words
