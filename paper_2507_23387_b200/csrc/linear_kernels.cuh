@@ -463,7 +463,8 @@ linear_empty_kernel(int M, int N, float* Y, long long ldy, LinearEpilogue e) {
 // ------------------------------------------------------------------------------------------ few rows
 // Up to eight rows of X: the product is bound by the bytes of W (4 per weight, FP32 or two words), so W
 // streams past the rows once and FP32 FMAs on the ordinary cores keep up; no tile is padded to 128 rows
-// and an FP32 W needs no packing.  A packed weight is put together again as hi + 2^-11 lo (22 bits).
+// and an FP32 W needs no packing.  A packed weight is put together again as 2^-p (hi + 2^-11 lo) (22 bits), so that the
+// products and the partial sums have the size of the result's own terms and not 2^p times that.
 // One row of 4096 x 1024 packed 6.7 us, of 16384 x 4096 about 50 (5.4 TB/s); with more rows the loads of X and the FMAs
 // take over (FP32 weight, 4 rows 75, 8 rows 155), which is where the tensor cores are asked instead.
 struct FewRowsParams {
@@ -480,6 +481,9 @@ struct FewRowsParams {
   LinearEpilogue ep;         // exp_a null; exp_b for a packed W
 };
 enum FewRowsLoad { kLoadPacked = 0, kLoadF32Vec, kLoadF32 };
+// Blocks an SM that their loads in flight leave registers for (one packed row of 16384 x 4096: four 46 us, three 57; and
+// below, four FP32 rows of 4096 x 4096: 64 registers 25 us, the 48 of five blocks 37).
+constexpr int few_rows_blocks(int rows) { return rows == 1 ? 4 : (rows == 4 ? 2 : 3); }
 
 __device__ __forceinline__ uint4 ldg_stream(const void* p) {
   uint4 v;
@@ -488,37 +492,62 @@ __device__ __forceinline__ uint4 ldg_stream(const void* p) {
                : "l"(p));
   return v;
 }
-__device__ __forceinline__ void join_words(uint32_t h2, uint32_t l2, float& w0, float& w1) {
+// Two weights from their words: up = 2^-p, up_lo = 2^(-11-p), each twice in a register pair.
+__device__ __forceinline__ void join_words(uint32_t h2, uint32_t l2, uint64_t up, uint64_t up_lo, float& w0, float& w1) {
   const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&h2));
   const float2 l = __half22float2(*reinterpret_cast<const __half2*>(&l2));
-  w0 = fmaf(l.x, kPackInvScale, h.x);
-  w1 = fmaf(l.y, kPackInvScale, h.y);
+  uint64_t a, b;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(a) : "f"(h.x), "f"(h.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(b) : "f"(l.x), "f"(l.y));
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(a) : "l"(a), "l"(up));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(a) : "l"(b), "l"(up_lo), "l"(a));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(w0), "=f"(w1) : "l"(a));
 }
 
-// A sum at the lower end of the FP32 range, where every product has lost bits to underflow (K of them, 2^-150 each):
-// once more in FP64.  Sums that small are not met in a working model; nothing else is slowed by this.
+// Sums that FP32 may have got wrong at the ends of its range are taken once more in FP64, by the whole warp for one
+// output after the other: at the lower end, where products have lost bits to underflow (2^-150 each), and those
+// that are not finite, since products or partial sums can overflow where the sum does not (what is infinite or NaN
+// in FP64 too stays so).  A sum of exactly zero is kept: rows of zeros are common, and products that all vanish
+// add up to less than K 2^-150, which is below the smallest normal number.
+// Sums like that are not met in a working model; nothing else is slowed by this.
 constexpr float kTinySum = 7.5e-37f;                   // 2^-120
+constexpr float kLargestFloat = 3.402823466e38f;
 template <int LOAD>
-__device__ __noinline__ float few_rows_tiny(const FewRowsParams& p, int m, int n, bool nk) {
-  double s = 0.0;
-  for (int k = 0; k < p.K; ++k) {
-    const long long off = nk ? n * p.ldw + k : k * p.ldw + n;
-    double w;
-    if (LOAD == kLoadPacked)
-      w = (double)__half2float(__ushort_as_half(p.Whi[off])) +
-          (double)kPackInvScale * (double)__half2float(__ushort_as_half(p.Wlo[off]));
-    else
-      w = (double)p.W[off];
-    s += (double)p.X[m * p.ldx + k] * w;
+__device__ __noinline__ float few_rows_again(const FewRowsParams& p, unsigned int todo, float z, int m, int n, bool nk) {
+  const int lane = threadIdx.x & 31;
+  for (; todo; todo &= todo - 1) {
+    const int who = __ffs(todo) - 1;
+    const int row = __shfl_sync(0xffffffffu, m, who), col = __shfl_sync(0xffffffffu, n, who);
+    double s = 0.0;
+    for (int k = lane; k < p.K; k += 32) {
+      const long long off = nk ? col * p.ldw + k : k * p.ldw + col;
+      double w;
+      if (LOAD == kLoadPacked)
+        w = (double)__half2float(__ushort_as_half(p.Whi[off])) +
+            (double)kPackInvScale * (double)__half2float(__ushort_as_half(p.Wlo[off]));
+      else
+        w = (double)p.W[off];
+      s += (double)p.X[row * p.ldx + k] * w;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == who) z = (float)ldexp(s, LOAD == kLoadPacked ? -*p.ep.exp_b : 0);
   }
-  return (float)ldexp(s, p.ep.exp_b ? -*p.ep.exp_b : 0);
+  return z;
+}
+// z, or what FP64 makes of it; the whole warp calls, `in` says whose z is an output.
+template <int LOAD>
+__device__ __forceinline__ float few_rows_checked(const FewRowsParams& p, bool in, float z, int m, int n, bool nk) {
+  const bool sure = z == 0.f || (fabsf(z) >= kTinySum && fabsf(z) <= kLargestFloat);
+  const unsigned int todo = __ballot_sync(0xffffffffu, in && !sure);
+  return todo ? few_rows_again<LOAD>(p, todo, z, m, n, nk) : z;
 }
 
 // W stored outputs x inputs (rows contiguous along k).  A group of `ksplit` warps owns NR outputs; lanes
 // run along k, eight weights of every output a step; the lanes' sums meet in shuffles and the warps' in
 // shared memory, always in the same order.  MR: rows computed (>= M; rows past M repeat the last).
 template <int MR, int NR, int LOAD>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, few_rows_blocks(MR))
 few_rows_nk_kernel(FewRowsParams p, int ksplit) {
   constexpr int E = 8;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -529,11 +558,16 @@ few_rows_nk_kernel(FewRowsParams p, int ksplit) {
   for (int i = 0; i < NR; ++i)
 #pragma unroll
     for (int m = 0; m < MR; ++m) acc[i][m] = 0.f;
-  // what the last step needs, asked for now: this thread's output, and the way back
+  // what the last step needs, asked for now: this thread's output
   const int out_n = (blockIdx.x * groups + threadIdx.x / (NR * MR)) * NR + threadIdx.x % (NR * MR) / MR;
   const bool out_in = threadIdx.x < groups * NR * MR && out_n < p.N && threadIdx.x % MR < p.M;
   const float out_bias = out_in && p.ep.bias ? __ldg(p.ep.bias + out_n) : 0.f;
-  const PowerBack back = power_back(p.ep.exp_a, p.ep.exp_b);
+  uint64_t up = 0, up_lo = 0;
+  if constexpr (LOAD == kLoadPacked) {
+    const float f = pow2f(-__ldg(p.ep.exp_b)), f_lo = f * kPackInvScale;   // (2^-137 at the least: subnormal, not lost)
+    asm("mov.b64 %0, {%1, %1};" : "=l"(up) : "f"(f));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(up_lo) : "f"(f_lo));
+  }
   // element e of the lane's step at k0: k0 + lane * 8 + e, or k0 + lane + 32 e where loads are single words
   constexpr int LS = LOAD == kLoadF32 ? 1 : E, ES = LOAD == kLoadF32 ? 32 : 1;
   for (int k0 = slice * 32 * E; k0 < p.K; k0 += ksplit * 32 * E) {
@@ -550,10 +584,10 @@ few_rows_nk_kernel(FewRowsParams p, int ksplit) {
       }
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
-        join_words(h[i].x, l[i].x, w[i][0], w[i][1]);
-        join_words(h[i].y, l[i].y, w[i][2], w[i][3]);
-        join_words(h[i].z, l[i].z, w[i][4], w[i][5]);
-        join_words(h[i].w, l[i].w, w[i][6], w[i][7]);
+        join_words(h[i].x, l[i].x, up, up_lo, w[i][0], w[i][1]);
+        join_words(h[i].y, l[i].y, up, up_lo, w[i][2], w[i][3]);
+        join_words(h[i].z, l[i].z, up, up_lo, w[i][4], w[i][5]);
+        join_words(h[i].w, l[i].w, up, up_lo, w[i][6], w[i][7]);
       }
     } else if (LOAD == kLoadF32Vec) {
 #pragma unroll
@@ -608,22 +642,22 @@ few_rows_nk_kernel(FewRowsParams p, int ksplit) {
   __syncthreads();
   // thread t of the block: output t / MR of the block's groups * NR, row t % MR (at most 8 * 16 of them)
   static_assert(8 * NR * MR <= 256, "one output a thread");
+  const int t = threadIdx.x, n = out_n, m = t % MR;
+  float z = 0.f;
   if (out_in) {
-    const int t = threadIdx.x, n = out_n;
-    const int g = t / (NR * MR), i = t % (NR * MR) / MR, m = t % MR;
-    float z = part[g * ksplit][i * MR + m];
+    const int g = t / (NR * MR), i = t % (NR * MR) / MR;
+    z = part[g * ksplit][i * MR + m];
     for (int s = 1; s < ksplit; ++s) z += part[g * ksplit + s][i * MR + m];
-    z = z != 0.f && fabsf(z) < kTinySum ? few_rows_tiny<LOAD>(p, m, n, true) : back(z);
-    z += out_bias;
-    p.Y[(long long)m * p.ldy + n] = linear_finish(p.ep, z, m, n);
   }
+  z = few_rows_checked<LOAD>(p, out_in, z, m, n, true);
+  if (out_in) p.Y[(long long)m * p.ldy + n] = linear_finish(p.ep, z + out_bias, m, n);
 }
 
 // W stored inputs x outputs (rows contiguous along n).  A block owns 128 outputs, four a lane, and its
 // eight warps take every eighth k of the block's k range; the grid's y dimension cuts k into slices of a
 // cluster, whose sums meet in the first block's shared memory, warps and blocks in order.
 template <int MR, int LOAD>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, MR <= 4 ? 4 : 1)
 few_rows_kn_kernel(FewRowsParams p, int k_per_block) {
   static_assert(LOAD != kLoadPacked, "packed weights of this layout go to the tensor cores");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -684,22 +718,23 @@ few_rows_kn_kernel(FewRowsParams p, int k_per_block) {
     __syncthreads();
   }
   if (blockIdx.y == 0) {
-    const PowerBack back = power_back(p.ep.exp_a, p.ep.exp_b);
     const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(sums));
-    for (int t = threadIdx.x; t < MR * 128; t += 256) {
+    for (int t = threadIdx.x; t < MR * 128; t += 256) {  // (whole warps)
       const int m = t >> 7, c = n0 + (t & 127);
-      if (m >= p.M || c >= p.N) continue;
-      float z = sums[t];
-      for (uint32_t s = 1; s < slices; ++s) {
-        uint32_t remote;
-        float v;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(base + t * 4), "r"(s));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
-        z += v;
+      const bool in = m < p.M && c < p.N;
+      float z = 0.f;
+      if (in) {
+        z = sums[t];
+        for (uint32_t s = 1; s < slices; ++s) {
+          uint32_t remote;
+          float v;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(base + t * 4), "r"(s));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+          z += v;
+        }
       }
-      z = z != 0.f && fabsf(z) < kTinySum ? few_rows_tiny<LOAD>(p, m, c, false) : back(z);
-      z += p.ep.bias ? p.ep.bias[c] : 0.f;
-      p.Y[(long long)m * p.ldy + c] = linear_finish(p.ep, z, m, c);
+      z = few_rows_checked<LOAD>(p, in, z, m, c, false);
+      if (in) p.Y[(long long)m * p.ldy + c] = linear_finish(p.ep, z + (p.ep.bias ? p.ep.bias[c] : 0.f), m, c);
     }
   }
   if (slices > 1)                                      // a block's sums stay until the first has read them
