@@ -165,7 +165,8 @@ int sgemm_cube_split(sgemm_cube_handle h, int rows, int cols,
  * K == 0 stores C = 0 (the empty sum; left alone by sgemm_cube_hgemm with accumulate != 0); an
  * operand without elements may be a null pointer.
  * Once the workspace for a problem size exists (after the first call at that size or a larger
- * one) the call only enqueues work on `stream`: it can be captured into a CUDA graph and replayed.
+ * one) the call only enqueues work on `stream`: it can be captured into a CUDA graph and replayed, also
+ * after larger calls (a workspace that a captured call has used is kept until the handle is destroyed).
  * A handle's workspace is shared by its calls, so calls that may overlap on the GPU need one
  * handle per stream.
  * Errors: INVALID_ARG, MISALIGNED, CUDA_ERROR (ALLOC_FAILED only with the TWO_PHASE strategy
@@ -342,8 +343,9 @@ int sgemm_cube_auto_scaled(sgemm_cube_handle h, int M, int N, int K,
  *
  * A linear layer with its gradients, layer normalisation with its gradients, and log probabilities of
  * given tokens with their gradient.  No call synchronises; once the handle's workspace has its size
- * the calls can be captured into a graph.  As everywhere, calls on one handle that may overlap on the
- * GPU need one handle per stream.  Sums, statistics and softmax sums are FP32 (the products' k-blocks as
+ * the calls can be captured into a graph.  A graph keeps the workspace that its calls were captured with: a larger
+ * call may follow, and the graph can be replayed until the handle is destroyed.  As everywhere, calls on one handle
+ * that may overlap on the GPU, replays among them, need one handle per stream.  Sums, statistics and softmax sums are FP32 (the products' k-blocks as
  * sgemm_cube, termwise, unless said otherwise); every result is the same from call to call.
  */
 

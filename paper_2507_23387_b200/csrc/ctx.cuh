@@ -4,6 +4,7 @@
 
 #include <cstdint>
 #include <cstring>
+#include <vector>
 
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -48,6 +49,7 @@ struct sgemm_cube_ctx {
   size_t tile_ws_bytes = 0;
   void* host_ws = nullptr;     // host-buffer path: device copies of A, B, C
   size_t host_ws_bytes = 0;
+  std::vector<void*> graph_ws; // buffers that captured calls have used, outgrown ones among them
   long long launches = 0;
   int kblock_termwise = 128;
   int kblock_elementwise = 64;
@@ -70,20 +72,47 @@ struct sgemm_cube_ctx {
   int pack_once_blocks = 0, dz_once_blocks[5] = {0, 0, 0, 0, 0};   // resident blocks of the one-launch packing kernels
 };
 
-inline int grow(void** buf, size_t* have, size_t want) {
-  if (*have >= want) return SGEMM_CUBE_OK;
-  if (*buf) {
-    if (cudaFree(*buf) != cudaSuccess) return SGEMM_CUBE_CUDA_ERROR;
-    *buf = nullptr;
-    *have = 0;
+// Room of at least `want` bytes in one of the handle's buffers, for a call on `st`.  A buffer that grows is freed and
+// allocated anew, unless a call that was captured has had it: the graph goes on using it whenever it is replayed, so
+// such a buffer stays until the handle is destroyed.
+inline int grow(sgemm_cube_ctx* h, void** buf, size_t* have, size_t want, cudaStream_t st) {
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  // (an error: the legacy stream while another one is captured; this call is not part of that)
+  if (cudaStreamIsCapturing(st, &status) != cudaSuccess) { cudaGetLastError(); status = cudaStreamCaptureStatusNone; }
+  const bool capturing = status != cudaStreamCaptureStatusNone;
+  const auto in_graph = [&](void* p) {
+    for (void* q : h->graph_ws)
+      if (q == p) return true;
+    return false;
+  };
+  if (*have < want) {
+    const bool keep = *buf && (capturing || in_graph(*buf));
+    if (*buf && !keep) {
+      if (cudaFree(*buf) != cudaSuccess) return SGEMM_CUBE_CUDA_ERROR;
+      *buf = nullptr;
+      *have = 0;
+    }
+    void* fresh = nullptr;
+    if (cudaMalloc(&fresh, want) != cudaSuccess) {
+      cudaGetLastError();
+      return SGEMM_CUBE_ALLOC_FAILED;
+    }
+    if (keep && !in_graph(*buf)) h->graph_ws.push_back(*buf);
+    *buf = fresh;
+    *have = want;
   }
-  if (cudaMalloc(buf, want) != cudaSuccess) {
-    cudaGetLastError();
-    *buf = nullptr;
-    return SGEMM_CUBE_ALLOC_FAILED;
-  }
-  *have = want;
+  if (capturing && !in_graph(*buf)) h->graph_ws.push_back(*buf);
   return SGEMM_CUBE_OK;
+}
+inline void free_workspaces(sgemm_cube_ctx* h) {
+  void* const current[] = {h->ws, h->part_ws, h->tile_ws, h->host_ws};
+  for (void* p : h->graph_ws) {
+    bool also = false;
+    for (void* q : current) also = also || q == p;
+    if (!also) cudaFree(p);
+  }
+  for (void* p : current)
+    if (p) cudaFree(p);
 }
 
 // 2-D tensor map over a row-major matrix: dims {inner, outer}, row pitch in bytes.

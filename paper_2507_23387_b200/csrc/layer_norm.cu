@@ -522,7 +522,7 @@ int backward_rows(sgemm_cube_ctx* h, NormParams p, float* dweight, float* dbias,
   int rc = persistent_blocks<sgc::norm_backward_kernel<T, WARPS, ACCESS>>(h, threads, smem, p.rows, p.period, groups, &blocks);
   if (rc) return rc;
   if (dweight || dbias) {
-    rc = grow(&h->part_ws, &h->part_ws_bytes, (size_t)blocks * 2 * p.cols * 4);
+    rc = grow(h, &h->part_ws, &h->part_ws_bytes, (size_t)blocks * 2 * p.cols * 4, st);
     if (rc) return rc;
     p.part = static_cast<float*>(h->part_ws);
   }
@@ -541,7 +541,7 @@ int backward_long(sgemm_cube_ctx* h, NormParams p, float* dweight, float* dbias,
     if (blocks > (p.rows + 31) / 32) blocks = (p.rows + 31) / 32;
     const int per = (p.rows + blocks - 1) / blocks;
     blocks = (p.rows + per - 1) / per;
-    if ((rc = grow(&h->part_ws, &h->part_ws_bytes, (size_t)blocks * 2 * p.cols * 4))) return rc;
+    if ((rc = grow(h, &h->part_ws, &h->part_ws_bytes, (size_t)blocks * 2 * p.cols * 4, st))) return rc;
     p.part = static_cast<float*>(h->part_ws);
     sgc::norm_columns_kernel<T><<<dim3((unsigned)tiles, (unsigned)blocks), 256, 0, st>>>(p, per);
     if ((rc = done(h))) return rc;

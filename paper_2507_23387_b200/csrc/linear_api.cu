@@ -252,7 +252,7 @@ int linear_product(sgemm_cube_ctx* h, int M, int N, int K, const Packed& A, cons
   const size_t tiles = (size_t)((M + sgc::kBM - 1) / sgc::kBM) * ((N + sgc::kBN - 1) / sgc::kBN);
   const int slices = linear_slices(h, (long long)tiles, K, p.kchunk_blocks * BK);
   if (slices > 1) {
-    rc = grow(&h->part_ws, &h->part_ws_bytes, tiles * slices * sgc::kTileFloats * 4);
+    rc = grow(h, &h->part_ws, &h->part_ws_bytes, tiles * slices * sgc::kTileFloats * 4, st);
     if (rc) return rc;
     const int chunks = (K + p.kchunk_blocks * BK - 1) / (p.kchunk_blocks * BK);
     p.ksplit = slices;
@@ -266,7 +266,7 @@ int linear_product(sgemm_cube_ctx* h, int M, int N, int K, const Packed& A, cons
   }
   // Nothing but the way back to do: the accumulate warps store to Y themselves.
   if (ep.bias || ep.R || ep.Z || ep.act != SGEMM_CUBE_ACT_NONE) {
-    rc = grow(&h->tile_ws, &h->tile_ws_bytes, (size_t)h->sm_count * 2 * sgc::kTileFloats * 4);
+    rc = grow(h, &h->tile_ws, &h->tile_ws_bytes, (size_t)h->sm_count * 2 * sgc::kTileFloats * 4, st);
     if (rc) return rc;
     p.ep.tiles = static_cast<float*>(h->tile_ws);
   }
@@ -543,7 +543,7 @@ int sgemm_cube_linear(sgemm_cube_handle h, int M, int N, int K, const sgemm_cube
   // 2048 x 2048 29 us, 34 with packing first; 256 rows of 1024 x 1024 21 and 26, of 4096 x 1024 43 and 40.
   const bool direct = short_batch && W->f32_dev && aligned16(W->f32_dev) && W->ld % 4 == 0;
   if (!direct) words_of(W, w_rows, w_cols, size, exps + 1, jobs, &n_jobs);
-  if (size.used && (rc = grow(&h->ws, &h->ws_bytes, size.used))) return rc;
+  if (size.used && (rc = grow(h, &h->ws, &h->ws_bytes, size.used, st))) return rc;
   Carve c;
   c.base = static_cast<uint8_t*>(h->ws);
   n_jobs = 0;
@@ -621,7 +621,7 @@ int sgemm_cube_linear_backward(sgemm_cube_handle h, int M, int N, int K, const f
       glo = c.take<uint16_t>((size_t)M * ldg);
     }
     if (dbias) col_part = c.take<float>((size_t)chunks * N);
-    if (!pass && (rc = grow(&h->ws, &h->ws_bytes, c.used))) return rc;
+    if (!pass && (rc = grow(h, &h->ws, &h->ws_bytes, c.used, st))) return rc;
   }
   if (n_jobs && (rc = launch_pack(h, jobs, n_jobs, st))) return rc;
   PackJob j = pack_job(M, N, dY, lddy, ghi, glo, ldg, exps + 2);

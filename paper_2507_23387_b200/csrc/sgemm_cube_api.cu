@@ -238,7 +238,7 @@ int launch_tc_gemm(sgemm_cube_ctx* h, int M, int N, int K, const uint16_t* Ahi, 
       const size_t ldp = round_up((size_t)N, 4);
       const size_t pstride = round_up((size_t)M * ldp, 64);
       const size_t need = (size_t)slices * pstride * 4 * (order == SGEMM_CUBE_TERMWISE ? 2 : 1);
-      if (slices >= 2 && grow(&h->part_ws, &h->part_ws_bytes, need) == SGEMM_CUBE_OK) {
+      if (slices >= 2 && grow(h, &h->part_ws, &h->part_ws_bytes, need, st) == SGEMM_CUBE_OK) {
         pair = false;
         p.ksplit = slices;
         p.kslice_blocks = chunks_per_slice * p.kchunk_blocks;
@@ -252,7 +252,7 @@ int launch_tc_gemm(sgemm_cube_ctx* h, int M, int N, int K, const uint16_t* Ahi, 
   if (Dll && !p.Phh) {
     const size_t ldp = round_up((size_t)N, 4);
     const size_t pstride = round_up((size_t)M * ldp, 64);
-    if ((rc = grow(&h->part_ws, &h->part_ws_bytes, 2 * pstride * 4))) return rc;
+    if ((rc = grow(h, &h->part_ws, &h->part_ws_bytes, 2 * pstride * 4, st))) return rc;
     p.Phh = static_cast<float*>(h->part_ws);
     p.Px = p.Phh + pstride;
     p.pstride = (long long)pstride;
@@ -327,7 +327,7 @@ int launch_two_phase(sgemm_cube_ctx* h, int M, int N, int K, const float* A, int
                      float pre_a = 1.0f, float pre_b = 1.0f) {
   const size_t ldA16 = round_up((size_t)K, 8), ldB16 = round_up((size_t)N, 8);
   const size_t szA = round_up((size_t)M * ldA16 * 2, 256), szB = round_up((size_t)K * ldB16 * 2, 256);
-  int rc = grow(&h->ws, &h->ws_bytes, 2 * szA + 2 * szB);
+  int rc = grow(h, &h->ws, &h->ws_bytes, 2 * szA + 2 * szB, st);
   if (rc) return rc;
   uint8_t* w = static_cast<uint8_t*>(h->ws);
   uint16_t* Ahi = reinterpret_cast<uint16_t*>(w);
@@ -439,10 +439,7 @@ int sgemm_cube_destroy(sgemm_cube_handle h) {
   unsigned int e = 0;
   if (rc == SGEMM_CUBE_OK && cudaMemcpy(&e, h->err_dev, sizeof(e), cudaMemcpyDeviceToHost) == cudaSuccess && e)
     rc = SGEMM_CUBE_DEVICE_TIMEOUT;
-  if (h->ws) cudaFree(h->ws);
-  if (h->host_ws) cudaFree(h->host_ws);
-  if (h->part_ws) cudaFree(h->part_ws);
-  if (h->tile_ws) cudaFree(h->tile_ws);
+  free_workspaces(h);
   for (cudaEvent_t e : h->ev_ring)
     if (e) cudaEventDestroy(e);
   if (h->s_in) cudaStreamDestroy(h->s_in);
@@ -584,7 +581,7 @@ int sgemm_cube_unfused(sgemm_cube_handle h, int M, int N, int K, const float* A,
   const size_t ldD = round_up((size_t)N, 4);
   const size_t szA = round_up((size_t)M * ldA16 * 2, 256), szB = round_up((size_t)K * ldB16 * 2, 256);
   const size_t szD = round_up((size_t)M * ldD * 4, 256);
-  rc = grow(&h->ws, &h->ws_bytes, 2 * szA + 2 * szB + 2 * szD);
+  rc = grow(h, &h->ws, &h->ws_bytes, 2 * szA + 2 * szB + 2 * szD, st);
   if (rc) return rc;
   uint8_t* w = static_cast<uint8_t*>(h->ws);
   uint16_t* Ahi = reinterpret_cast<uint16_t*>(w);
@@ -627,7 +624,7 @@ int sgemm_cube_four_term(sgemm_cube_handle h, int M, int N, int K, const float* 
   const size_t ldD = round_up((size_t)N, 4);
   const size_t szA = round_up((size_t)M * ldA16 * 2, 256), szB = round_up((size_t)K * ldB16 * 2, 256);
   const size_t szD = round_up((size_t)M * ldD * 4, 256);
-  rc = grow(&h->ws, &h->ws_bytes, 2 * szA + 2 * szB + szD);
+  rc = grow(h, &h->ws, &h->ws_bytes, 2 * szA + 2 * szB + szD, st);
   if (rc) return rc;
   uint8_t* w = static_cast<uint8_t*>(h->ws);
   uint16_t* Ahi = reinterpret_cast<uint16_t*>(w);
@@ -661,7 +658,7 @@ int sgemm_cube_host(sgemm_cube_handle h, int M, int N, int K, const float* A_hos
   const size_t ldA = round_up((size_t)K, 4), ldB = round_up((size_t)N, 4), ldC = ldB;
   const size_t szA = round_up((size_t)M * ldA * 4, 256), szB = round_up((size_t)K * ldB * 4, 256);
   const size_t szC = round_up((size_t)M * ldC * 4, 256);
-  rc = grow(&h->host_ws, &h->host_ws_bytes, szA + szB + szC);
+  rc = grow(h, &h->host_ws, &h->host_ws_bytes, szA + szB + szC, st);
   if (rc) return rc;
   uint8_t* w = static_cast<uint8_t*>(h->host_ws);
   float* dA = reinterpret_cast<float*>(w);
@@ -718,7 +715,7 @@ int host_pipelined(sgemm_cube_ctx* h, int M, int N, int K, const float* A_host, 
   if (rc) return rc;
   const size_t ldA16 = round_up((size_t)K, 8), ldB16 = round_up((size_t)N, 8);
   const size_t szA = round_up((size_t)M * ldA16 * 2, 256), szB = round_up((size_t)K * ldB16 * 2, 256);
-  rc = grow(&h->ws, &h->ws_bytes, 2 * szA + 2 * szB);
+  rc = grow(h, &h->ws, &h->ws_bytes, 2 * szA + 2 * szB, st);
   if (rc) return rc;
   uint8_t* w = static_cast<uint8_t*>(h->ws);
   uint16_t* Ahi = reinterpret_cast<uint16_t*>(w);
