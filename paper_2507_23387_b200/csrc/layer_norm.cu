@@ -1,13 +1,16 @@
 // Layer normalisation and its gradients (contracts: include/sgemm_cube.h).
 //
 //   forward    mean = sum x / n;  var = sum (x - mean)^2 / n;  y = (x - mean) rstd w + b
+//              The sum and its division leave mean off by some units in its last place, which is much where the
+//              spread is small beside it.  So what the first mean m0 is off by is found as well:
+//              c = sum (x - m0) / n,  mean = m0 + c,  var = sum (x - m0)^2 / n - c^2,  y = (x - m0 - c) rstd w + b
 //   backward   u = dy w;  n = (x - mean) rstd;  dx = rstd (u - mean(u) - n mean(u n))
 //              dw = sum over rows of dy n;  db = sum over rows of dy
 //
 // Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx, each once (8192 x 4096 FP32
 // 46 us and 73, 5.8 and 5.5 TB/s; BF16 rows by instructions as well, 6000 x 2048 13 and 26, 3.8 and 2.8 TB/s).  A row
 // lives in the registers of one group of warps between its load and its store, so the second moment is
-// taken about the mean (no cancellation of squares) without a second read.  Blocks are persistent: a
+// taken about the first mean (no cancellation of squares) without a second read.  Blocks are persistent: a
 // group asks for its next rows before it works on the present one, and keeps its columns' weights (forward)
 // or running sums of dw and db (backward) in registers all the way.
 //
@@ -39,12 +42,13 @@ template <typename T, int WARPS, bool VEC, int TENSORS>
 constexpr size_t kSlotBytes = (size_t)kStages<T, WARPS, VEC, TENSORS> * TENSORS * kPT * sizeof(T) * (WARPS > 8 ? WARPS * 32 : 256);
 
 // Sums over a row's group of warps.  `slot` alternates between two buffers, so one barrier a sum is enough.
+__device__ __forceinline__ float warp_sum(float s) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s;
+}
 template <int WARPS, int N>
-__device__ __forceinline__ void group_sum(float (&s)[N], float* buf, int group, int warp_in_group, int bar_threads) {
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+__device__ __forceinline__ void join_warps(float (&s)[N], float* buf, int group, int warp_in_group, int bar_threads) {
   if constexpr (WARPS > 1) {
     float* b = buf + group * WARPS * N;
     if ((threadIdx.x & 31) == 0) {
@@ -55,12 +59,24 @@ __device__ __forceinline__ void group_sum(float (&s)[N], float* buf, int group, 
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(bar_threads) : "memory");
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      float t = b[i];
+      if constexpr (WARPS >= 16) {                       // a warp's sum a lane
+        s[i] = b[(threadIdx.x & (WARPS - 1)) * N + i];
 #pragma unroll
-      for (int w = 1; w < WARPS; ++w) t += b[w * N + i];
-      s[i] = t;
+        for (int o = WARPS / 2; o > 0; o >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+      } else {
+        float t = b[i];
+#pragma unroll
+        for (int w = 1; w < WARPS; ++w) t += b[w * N + i];
+        s[i] = t;
+      }
     }
   }
+}
+template <int WARPS, int N>
+__device__ __forceinline__ void group_sum(float (&s)[N], float* buf, int group, int warp_in_group, int bar_threads) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] = warp_sum(s[i]);
+  join_warps<WARPS>(s, buf, group, warp_in_group, bar_threads);
 }
 
 struct NormParams {
@@ -82,11 +98,24 @@ struct NormParams {
   int period;              // backward: rows this far apart start equally far behind a 16-byte boundary
 };
 
+// rstd from the mean square about the first mean and that mean's correction; the difference of the two may fall below
+// zero by rounding (a NaN stays).  1 / sqrt as the approximate one (2^-22) with a Newton step, good to 2 units; the step is
+// left out where it would multiply 0 by infinity.
+__device__ __forceinline__ float norm_rstd(float square, float c, float eps) {
+  const float var = fmaf(-c, c, square), v = (var < 0.f ? 0.f : var) + eps;
+  const float r = rsqrtf(v), e = fmaf(-v * r, r, 1.f);
+  return fabsf(e) < 1.f ? fmaf(0.5f * r, e, r) : r;
+}
+
+// Blocks an SM the registers are cut for: with three, single elements and groups that meet at barriers of their own run
+// out of them (6001 x 2047 BF16 21.4 us, 14.5 with two; 6000 x 2048 13.8 and 12.1; but 8192 x 4096 26.5 and 27.5).
+constexpr int forward_blocks(int warps, bool vec) { return warps > 8 ? 1 : (vec && warps == 8 ? 3 : 2); }
+
 // WARPS warps a row, 8 / WARPS rows a block (one for WARPS >= 8).
 template <typename T, int WARPS, bool VEC>
-__global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 3) norm_forward_kernel(NormParams p) {
+__global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, forward_blocks(WARPS, VEC)) norm_forward_kernel(NormParams p) {
   constexpr int kGroups = WARPS >= 8 ? 1 : 8 / WARPS, kThreads = WARPS * 32;
-  __shared__ float buf[2][kGroups * WARPS];
+  __shared__ float buf[kGroups * WARPS], buf2[kGroups * WARPS * 2];
   const int group = threadIdx.x / kThreads, t = threadIdx.x % kThreads, wg = t >> 5;
   const int bar = kGroups == 1 ? 0 : kThreads;         // groups meet at their own barriers
   const float inv_n = 1.f / (float)p.cols;
@@ -113,6 +142,13 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
   float w[kPT], b[kPT];
   load_params<T, kPT, VEC>(p.weight, 1.f, p.cols, t, kThreads, w);
   load_params<T, kPT, VEC>(p.bias, 0.f, p.cols, t, kThreads, b);
+  // FP32 rows are summed a second time for the correction.  A warp's 512 elements of a 16-bit type have so few bits
+  // that their sum loses next to nothing in FP32; there its difference to count * mean serves.
+  constexpr bool kTwice = sizeof(T) == 4;
+  int columns = 0;                                     // of this warp
+#pragma unroll
+  for (int i = 0; i < kPT; ++i) columns += row_column<T, VEC>(i, t, kThreads) < p.cols;
+  [[maybe_unused]] const float count = (float)__reduce_add_sync(0xffffffffu, columns);
   for (; row < p.rows; row += step) {
     float v[kPT];
     if constexpr (VEC) {
@@ -124,24 +160,28 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
       next.get(v);
       if (row + step < p.rows) next.fetch(static_cast<const T*>(p.X) + (row + step) * p.ldx, p.cols, t, kThreads);
     }
-    float s[1] = {0.f};
+    float s[1] = {0.f}, d[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kPT; ++i) s[0] += v[i];
-    group_sum<WARPS>(s, buf[0], group, wg, bar);
+    const float own = s[0] = warp_sum(s[0]);
+    join_warps<WARPS>(s, buf, group, wg, bar);
     const float mean = s[0] * inv_n;
-    s[0] = 0.f;
 #pragma unroll
     for (int i = 0; i < kPT; ++i) {
       v[i] -= mean;
-      s[0] = fmaf(v[i], row_column<T, VEC>(i, t, kThreads) < p.cols ? v[i] : 0.f, s[0]);
+      const float in = row_column<T, VEC>(i, t, kThreads) < p.cols ? v[i] : 0.f;
+      d[0] = fmaf(v[i], in, d[0]);
+      if constexpr (kTwice) d[1] += in;
     }
-    group_sum<WARPS>(s, buf[1], group, wg, bar);
-    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_n, p.eps));
+    d[0] = warp_sum(d[0]);
+    d[1] = kTwice ? warp_sum(d[1]) : fmaf(-mean, count, own);
+    join_warps<WARPS>(d, buf2, group, wg, bar);
+    const float c = d[1] * inv_n, rstd = norm_rstd(d[0] * inv_n, c, p.eps), shift = -c * rstd;
 #pragma unroll
-    for (int i = 0; i < kPT; ++i) v[i] = fmaf(v[i] * rstd, w[i], b[i]);
+    for (int i = 0; i < kPT; ++i) v[i] = fmaf(fmaf(v[i], rstd, shift), w[i], b[i]);
     store_row<T, kPT, VEC>(static_cast<T*>(p.out) + row * p.ldo, p.cols, t, kThreads, v);
     if (t == 0) {
-      if (p.mean) p.mean[row] = mean;
+      if (p.mean) p.mean[row] = mean + c;
       if (p.rstd) p.rstd[row] = rstd;
     }
   }
@@ -150,30 +190,31 @@ __global__ void __launch_bounds__(WARPS > 8 ? WARPS * 32 : 256, WARPS > 8 ? 1 : 
 // Rows too long for the registers of one block: three passes, the later ones from L2.
 template <typename T>
 __global__ void __launch_bounds__(1024) norm_forward_long_kernel(NormParams p) {
-  __shared__ float buf[2][32];
+  __shared__ float buf[32], buf2[64];
   const long long row = blockIdx.x;
   const T* x = static_cast<const T*>(p.X) + row * p.ldx;
   T* y = static_cast<T*>(p.out) + row * p.ldo;
   const int t = threadIdx.x;
   float s[1] = {0.f};
   for (int c = t; c < p.cols; c += 1024) s[0] += Elem<T>::get(x[c]);
-  group_sum<32>(s, buf[0], 0, t >> 5, 0);
+  group_sum<32>(s, buf, 0, t >> 5, 0);
   const float mean = s[0] / (float)p.cols;
-  s[0] = 0.f;
+  float sd[2] = {0.f, 0.f};
   for (int c = t; c < p.cols; c += 1024) {
     const float d = Elem<T>::get(x[c]) - mean;
-    s[0] = fmaf(d, d, s[0]);
+    sd[0] = fmaf(d, d, sd[0]);
+    sd[1] += d;
   }
-  group_sum<32>(s, buf[1], 0, t >> 5, 0);
-  const float rstd = 1.f / sqrtf(s[0] / (float)p.cols + p.eps);
+  group_sum<32>(sd, buf2, 0, t >> 5, 0);
+  const float more = sd[1] / (float)p.cols, rstd = norm_rstd(sd[0] / (float)p.cols, more, p.eps), shift = -more * rstd;
   for (int c = t; c < p.cols; c += 1024) {
-    float n = (Elem<T>::get(x[c]) - mean) * rstd;
+    float n = fmaf(Elem<T>::get(x[c]) - mean, rstd, shift);
     if (p.weight) n *= p.weight[c];
     if (p.bias) n += p.bias[c];
     y[c] = Elem<T>::put(n);
   }
   if (t == 0) {
-    if (p.mean) p.mean[row] = mean;
+    if (p.mean) p.mean[row] = mean + more;
     if (p.rstd) p.rstd[row] = rstd;
   }
 }
