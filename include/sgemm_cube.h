@@ -347,6 +347,8 @@ int sgemm_cube_auto_scaled(sgemm_cube_handle h, int M, int N, int K,
  * call may follow, and the graph can be replayed until the handle is destroyed.  As everywhere, calls on one handle
  * that may overlap on the GPU, replays among them, need one handle per stream.  Sums, statistics and softmax sums are FP32 (the products' k-blocks as
  * sgemm_cube, termwise, unless said otherwise); every result is the same from call to call.
+ * "Any alignment" below means any multiple of the element's size: a pointer that is not one, to a matrix or a vector,
+ * is refused with INVALID_ARG, and so is a result in the place of an operand with another leading dimension.
  */
 
 /* Operand of a linear layer: a row-major FP32 matrix (f32_dev, ld), or, with f32_dev NULL, one packed by
@@ -394,6 +396,7 @@ int sgemm_cube_pack(sgemm_cube_handle h, int rows, int cols,
  *   X  M x K;  W  K inputs, N outputs in weight_layout;  either may be FP32 or packed
  *   bias_dev N FP32 or NULL;  R_dev M x N FP32 (ldr >= N) or NULL, may be Y_dev itself (then ldr == ldy)
  *   Y_dev M x N FP32 (written);  Z_dev M x N FP32 or NULL: z is stored there for the backward pass
+ *     (neither Y_dev nor R_dev)
  * FP32 matrices may have any alignment.  The product is the three-product form of sgemm_cube on packed
  * operands, with two forms of its own for an FP32 X of few rows, which read W once and pack nothing ahead:
  * for a short batch (up to 64 rows, to 256 for small weights) X, and an FP32 W that starts its rows on 16 bytes,

@@ -31,6 +31,9 @@ struct DeviceGuard {
 };
 
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+// Whether one of the pointers (null ones aside) is not a multiple of `size` bytes.
+template <typename... P>
+inline bool misplaced(size_t size, P... p) { return ((reinterpret_cast<uintptr_t>(p) % size != 0) || ...); }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 struct sgemm_cube_ctx {

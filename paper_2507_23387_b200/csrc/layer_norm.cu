@@ -626,7 +626,6 @@ int backward_typed(sgemm_cube_ctx* h, NormParams p, float* dw, float* db, cudaSt
 
 size_t elem_size(int dtype) { return dtype == SGEMM_CUBE_F32 ? 4 : 2; }
 bool bad_dtype(int dtype) { return dtype < SGEMM_CUBE_F32 || dtype > SGEMM_CUBE_BF16; }
-bool off_elem(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % elem_size(dtype) != 0; }
 
 }  // namespace
 
@@ -638,7 +637,8 @@ int sgemm_cube_layer_norm(sgemm_cube_handle h, int rows, int cols, int dtype, co
   if (!h || rows < 0 || cols < 1 || bad_dtype(dtype) || !(eps >= 0.f) || ldx < cols || ldy < cols)
     return SGEMM_CUBE_INVALID_ARG;
   if (rows == 0) return SGEMM_CUBE_OK;
-  if (!X || !Y || off_elem(X, dtype) || off_elem(Y, dtype)) return SGEMM_CUBE_INVALID_ARG;
+  if (!X || !Y || misplaced(elem_size(dtype), X, Y) || misplaced(4, weight, bias, mean, rstd)) return SGEMM_CUBE_INVALID_ARG;
+  if (X == Y && ldx != ldy && rows > 1) return SGEMM_CUBE_INVALID_ARG;
   DeviceGuard g(h->device);
   if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;
   NormParams p;
@@ -662,8 +662,9 @@ int sgemm_cube_layer_norm_backward(sgemm_cube_handle h, int rows, int cols, int 
                                    void* stream) {
   if (!h || rows < 0 || cols < 1 || bad_dtype(dtype) || ldx < cols || lddy < cols || (dX && lddx < cols))
     return SGEMM_CUBE_INVALID_ARG;
-  if (rows > 0 && (!dY || !X || !mean || !rstd || off_elem(dY, dtype) || off_elem(X, dtype) || off_elem(dX, dtype)))
-    return SGEMM_CUBE_INVALID_ARG;
+  if (rows > 0 && (!dY || !X || !mean || !rstd)) return SGEMM_CUBE_INVALID_ARG;
+  if (misplaced(elem_size(dtype), dY, X, dX) || misplaced(4, weight, mean, rstd, dweight, dbias)) return SGEMM_CUBE_INVALID_ARG;
+  if (dX == dY && lddx != lddy && rows > 1) return SGEMM_CUBE_INVALID_ARG;
   if (!dX && !dweight && !dbias) return SGEMM_CUBE_OK;
   DeviceGuard g(h->device);
   if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;

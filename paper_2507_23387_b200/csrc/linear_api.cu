@@ -409,8 +409,8 @@ bool is_packed(const sgemm_cube_operand* o) { return o->f32_dev == nullptr && o-
 int check_operand(const sgemm_cube_operand* o, int rows, int cols) {
   if (!o) return SGEMM_CUBE_INVALID_ARG;
   if (rows == 0 || cols == 0) return SGEMM_CUBE_OK;              // an empty operand is not looked at
-  if (o->f32_dev) return o->ld >= cols ? SGEMM_CUBE_OK : SGEMM_CUBE_INVALID_ARG;
-  if (!o->hi_dev || !o->lo_dev || !o->exp_dev || o->ld16 < cols) return SGEMM_CUBE_INVALID_ARG;
+  if (o->f32_dev) return o->ld >= cols && !misplaced(4, o->f32_dev) ? SGEMM_CUBE_OK : SGEMM_CUBE_INVALID_ARG;
+  if (!o->hi_dev || !o->lo_dev || !o->exp_dev || o->ld16 < cols || misplaced(4, o->exp_dev)) return SGEMM_CUBE_INVALID_ARG;
   if (!aligned16(o->hi_dev) || !aligned16(o->lo_dev) || o->ld16 % 8) return SGEMM_CUBE_MISALIGNED;
   return SGEMM_CUBE_OK;
 }
@@ -482,7 +482,7 @@ int sgemm_cube_pack(sgemm_cube_handle h, int rows, int cols, const float* X, int
   if (!h) return SGEMM_CUBE_INVALID_ARG;
   if (rows < 0 || cols < 0 || ldx < cols || ld16 < cols) return SGEMM_CUBE_INVALID_ARG;
   if (rows == 0 || cols == 0) return SGEMM_CUBE_OK;
-  if (!X || !hi || !lo || !exp) return SGEMM_CUBE_INVALID_ARG;
+  if (!X || !hi || !lo || !exp || misplaced(4, X, exp)) return SGEMM_CUBE_INVALID_ARG;
   if (!aligned16(hi) || !aligned16(lo) || ld16 % 8) return SGEMM_CUBE_MISALIGNED;
   DeviceGuard g(h->device);
   if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;
@@ -500,7 +500,9 @@ int sgemm_cube_linear(sgemm_cube_handle h, int M, int N, int K, const sgemm_cube
   if ((rc = nk ? check_operand(W, N, K) : check_operand(W, K, N))) return rc;
   if (M == 0 || N == 0) return SGEMM_CUBE_OK;
   if (!Y || ldy < N || (R && ldr < N) || (Z && ldz < N)) return SGEMM_CUBE_INVALID_ARG;
-  if (Z && Z == Y) return SGEMM_CUBE_INVALID_ARG;
+  if (misplaced(4, bias, R, Y, Z)) return SGEMM_CUBE_INVALID_ARG;
+  if (Z && (Z == Y || Z == R)) return SGEMM_CUBE_INVALID_ARG;
+  if (R == Y && ldr != ldy && M > 1) return SGEMM_CUBE_INVALID_ARG;
   DeviceGuard g(h->device);
   if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -579,10 +581,10 @@ int sgemm_cube_linear_backward(sgemm_cube_handle h, int M, int N, int K, const f
   int rc;
   if (dW && (rc = check_operand(X, M, K))) return rc;
   if (dX && (rc = check_operand(W, w_rows, w_cols))) return rc;
-  if ((dX && lddx < K) || (dW && lddw < w_cols)) return SGEMM_CUBE_INVALID_ARG;
+  if ((dX && lddx < K) || (dW && lddw < w_cols) || misplaced(4, dX, dW, dbias)) return SGEMM_CUBE_INVALID_ARG;
   if (M > 0 && N > 0) {
-    if (!dY || lddy < N) return SGEMM_CUBE_INVALID_ARG;
-    if (activation != SGEMM_CUBE_ACT_NONE && (!Z || ldz < N)) return SGEMM_CUBE_INVALID_ARG;
+    if (!dY || lddy < N || misplaced(4, dY)) return SGEMM_CUBE_INVALID_ARG;
+    if (activation != SGEMM_CUBE_ACT_NONE && (!Z || ldz < N || misplaced(4, Z))) return SGEMM_CUBE_INVALID_ARG;
   }
   DeviceGuard g(h->device);
   if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;

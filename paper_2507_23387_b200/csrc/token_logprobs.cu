@@ -635,7 +635,6 @@ int launch_grad(sgemm_cube_ctx* h, sgc::LogprobGradParams p, cudaStream_t st) {
 
 size_t elem_size(int dtype) { return dtype == SGEMM_CUBE_F32 ? 4 : 2; }
 bool bad_dtype(int dtype) { return dtype < SGEMM_CUBE_F32 || dtype > SGEMM_CUBE_BF16; }
-bool off_elem(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % elem_size(dtype) != 0; }
 bool bad_scale(float s) { return !(s >= 0x1p-30f && s <= 0x1p30f); }
 
 }  // namespace
@@ -648,7 +647,8 @@ int sgemm_cube_token_logprobs(sgemm_cube_handle h, int rows, int vocab, int dtyp
   if (!h || rows < 0 || vocab < 1 || ld < vocab || bad_dtype(dtype) || bad_scale(scale)) return SGEMM_CUBE_INVALID_ARG;
   if (top_k < 0 || top_k > sgc::kTopMax || top_k > vocab) return SGEMM_CUBE_INVALID_ARG;
   if (rows == 0) return SGEMM_CUBE_OK;
-  if (!logits || off_elem(logits, dtype)) return SGEMM_CUBE_INVALID_ARG;
+  if (!logits || misplaced(elem_size(dtype), logits)) return SGEMM_CUBE_INVALID_ARG;
+  if (misplaced(4, logp, entropy, stats, top_logp) || misplaced(8, tokens, top_index)) return SGEMM_CUBE_INVALID_ARG;
   if ((logp != nullptr) != (tokens != nullptr)) return SGEMM_CUBE_INVALID_ARG;
   if ((top_k > 0) != (top_logp != nullptr) || (top_k > 0) != (top_index != nullptr)) return SGEMM_CUBE_INVALID_ARG;
   DeviceGuard g(h->device);
@@ -679,7 +679,9 @@ int sgemm_cube_token_logprobs_backward(sgemm_cube_handle h, int rows, int vocab,
     return SGEMM_CUBE_INVALID_ARG;
   if (!dlogp && !dentropy) return SGEMM_CUBE_INVALID_ARG;
   if (rows == 0) return SGEMM_CUBE_OK;
-  if (!logits || !dlogits || !stats || off_elem(logits, dtype) || off_elem(dlogits, dtype)) return SGEMM_CUBE_INVALID_ARG;
+  if (!logits || !dlogits || !stats || misplaced(elem_size(dtype), logits, dlogits)) return SGEMM_CUBE_INVALID_ARG;
+  if (misplaced(4, stats, entropy, dlogp, dentropy) || misplaced(8, tokens)) return SGEMM_CUBE_INVALID_ARG;
+  if (logits == dlogits && ld != lddl && rows > 1) return SGEMM_CUBE_INVALID_ARG;
   if ((dlogp && !tokens) || (dentropy && !entropy)) return SGEMM_CUBE_INVALID_ARG;
   DeviceGuard g(h->device);
   if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;
