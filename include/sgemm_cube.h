@@ -349,6 +349,7 @@ int sgemm_cube_auto_scaled(sgemm_cube_handle h, int M, int N, int K,
  * sgemm_cube, termwise, unless said otherwise); every result is the same from call to call.
  * "Any alignment" below means any multiple of the element's size: a pointer that is not one, to a matrix or a vector,
  * is refused with INVALID_ARG, and so is a result in the place of an operand with another leading dimension.
+ * Dimensions go to 2^31 - 2^16; above, INVALID_ARG.  Leading dimensions and byte offsets have 64 bits.
  */
 
 /* Operand of a linear layer: a row-major FP32 matrix (f32_dev, ld), or, with f32_dev NULL, one packed by

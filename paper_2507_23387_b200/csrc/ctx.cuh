@@ -34,6 +34,10 @@ inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // Whether one of the pointers (null ones aside) is not a multiple of `size` bytes.
 template <typename... P>
 inline bool misplaced(size_t size, P... p) { return ((reinterpret_cast<uintptr_t>(p) % size != 0) || ...); }
+// Whether one of an operator's dimensions is outside [0, 2^31 - 2^16]: the kernels count rows and columns in 32 bits and
+// step past the end by a block's stride.
+template <typename... D>
+inline bool bad_dims(D... d) { return ((d < 0 || d > 0x7FFF0000) || ...); }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 struct sgemm_cube_ctx {

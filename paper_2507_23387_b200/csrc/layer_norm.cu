@@ -634,7 +634,7 @@ extern "C" {
 int sgemm_cube_layer_norm(sgemm_cube_handle h, int rows, int cols, int dtype, const void* X, int64_t ldx,
                           const float* weight, const float* bias, float eps, void* Y, int64_t ldy, float* mean,
                           float* rstd, void* stream) {
-  if (!h || rows < 0 || cols < 1 || bad_dtype(dtype) || !(eps >= 0.f) || ldx < cols || ldy < cols)
+  if (!h || bad_dims(rows, cols) || cols < 1 || bad_dtype(dtype) || !(eps >= 0.f) || ldx < cols || ldy < cols)
     return SGEMM_CUBE_INVALID_ARG;
   if (rows == 0) return SGEMM_CUBE_OK;
   if (!X || !Y || misplaced(elem_size(dtype), X, Y) || misplaced(4, weight, bias, mean, rstd)) return SGEMM_CUBE_INVALID_ARG;
@@ -660,7 +660,7 @@ int sgemm_cube_layer_norm_backward(sgemm_cube_handle h, int rows, int cols, int 
                                    const void* X, int64_t ldx, const float* weight, const float* mean,
                                    const float* rstd, void* dX, int64_t lddx, float* dweight, float* dbias,
                                    void* stream) {
-  if (!h || rows < 0 || cols < 1 || bad_dtype(dtype) || ldx < cols || lddy < cols || (dX && lddx < cols))
+  if (!h || bad_dims(rows, cols) || cols < 1 || bad_dtype(dtype) || ldx < cols || lddy < cols || (dX && lddx < cols))
     return SGEMM_CUBE_INVALID_ARG;
   if (rows > 0 && (!dY || !X || !mean || !rstd)) return SGEMM_CUBE_INVALID_ARG;
   if (misplaced(elem_size(dtype), dY, X, dX) || misplaced(4, weight, mean, rstd, dweight, dbias)) return SGEMM_CUBE_INVALID_ARG;

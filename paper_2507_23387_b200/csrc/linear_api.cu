@@ -480,7 +480,7 @@ extern "C" {
 int sgemm_cube_pack(sgemm_cube_handle h, int rows, int cols, const float* X, int64_t ldx, uint16_t* hi, uint16_t* lo,
                     int64_t ld16, int32_t* exp, void* stream) {
   if (!h) return SGEMM_CUBE_INVALID_ARG;
-  if (rows < 0 || cols < 0 || ldx < cols || ld16 < cols) return SGEMM_CUBE_INVALID_ARG;
+  if (bad_dims(rows, cols) || ldx < cols || ld16 < cols) return SGEMM_CUBE_INVALID_ARG;
   if (rows == 0 || cols == 0) return SGEMM_CUBE_OK;
   if (!X || !hi || !lo || !exp || misplaced(4, X, exp)) return SGEMM_CUBE_INVALID_ARG;
   if (!aligned16(hi) || !aligned16(lo) || ld16 % 8) return SGEMM_CUBE_MISALIGNED;
@@ -493,7 +493,7 @@ int sgemm_cube_pack(sgemm_cube_handle h, int rows, int cols, const float* X, int
 int sgemm_cube_linear(sgemm_cube_handle h, int M, int N, int K, const sgemm_cube_operand* X,
                       const sgemm_cube_operand* W, int weight_layout, const float* bias, const float* R, int64_t ldr,
                       int activation, float* Y, int64_t ldy, float* Z, int64_t ldz, void* stream) {
-  if (!h || M < 0 || N < 0 || K < 0 || bad_layout(weight_layout) || bad_act(activation)) return SGEMM_CUBE_INVALID_ARG;
+  if (!h || bad_dims(M, N, K) || bad_layout(weight_layout) || bad_act(activation)) return SGEMM_CUBE_INVALID_ARG;
   const bool nk = weight_layout == SGEMM_CUBE_WEIGHT_NK;
   int rc = check_operand(X, M, K);
   if (rc) return rc;
@@ -575,7 +575,7 @@ int sgemm_cube_linear_backward(sgemm_cube_handle h, int M, int N, int K, const f
                                int64_t ldz, int activation, const sgemm_cube_operand* X, const sgemm_cube_operand* W,
                                int weight_layout, float* dX, int64_t lddx, float* dW, int64_t lddw, float* dbias,
                                void* stream) {
-  if (!h || M < 0 || N < 0 || K < 0 || bad_layout(weight_layout) || bad_act(activation)) return SGEMM_CUBE_INVALID_ARG;
+  if (!h || bad_dims(M, N, K) || bad_layout(weight_layout) || bad_act(activation)) return SGEMM_CUBE_INVALID_ARG;
   const bool nk = weight_layout == SGEMM_CUBE_WEIGHT_NK;
   const int w_rows = nk ? N : K, w_cols = nk ? K : N;
   int rc;

@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(256)
 dz_range_kernel(PackJob j, float* __restrict__ col_part, int rows_per_chunk, unsigned int* words) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c0 = blockIdx.x * 128;
-  const int r_end = min(j.rows, (int)(blockIdx.y + 1) * rows_per_chunk);
+  const int r_end = (int)min((long long)j.rows, (long long)(blockIdx.y + 1) * rows_per_chunk);
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
   uint32_t m = 0;
   int col[4];

@@ -644,7 +644,7 @@ extern "C" {
 int sgemm_cube_token_logprobs(sgemm_cube_handle h, int rows, int vocab, int dtype, const void* logits, int64_t ld,
                               const int64_t* tokens, float scale, float* logp, float* entropy, float* stats,
                               int top_k, float* top_logp, int64_t* top_index, void* stream) {
-  if (!h || rows < 0 || vocab < 1 || ld < vocab || bad_dtype(dtype) || bad_scale(scale)) return SGEMM_CUBE_INVALID_ARG;
+  if (!h || bad_dims(rows, vocab) || vocab < 1 || ld < vocab || bad_dtype(dtype) || bad_scale(scale)) return SGEMM_CUBE_INVALID_ARG;
   if (top_k < 0 || top_k > sgc::kTopMax || top_k > vocab) return SGEMM_CUBE_INVALID_ARG;
   if (rows == 0) return SGEMM_CUBE_OK;
   if (!logits || misplaced(elem_size(dtype), logits)) return SGEMM_CUBE_INVALID_ARG;
@@ -675,7 +675,7 @@ int sgemm_cube_token_logprobs_backward(sgemm_cube_handle h, int rows, int vocab,
                                        int64_t ld, const int64_t* tokens, float scale, const float* stats,
                                        const float* entropy, const float* dlogp, const float* dentropy,
                                        void* dlogits, int64_t lddl, void* stream) {
-  if (!h || rows < 0 || vocab < 1 || ld < vocab || lddl < vocab || bad_dtype(dtype) || bad_scale(scale))
+  if (!h || bad_dims(rows, vocab) || vocab < 1 || ld < vocab || lddl < vocab || bad_dtype(dtype) || bad_scale(scale))
     return SGEMM_CUBE_INVALID_ARG;
   if (!dlogp && !dentropy) return SGEMM_CUBE_INVALID_ARG;
   if (rows == 0) return SGEMM_CUBE_OK;
