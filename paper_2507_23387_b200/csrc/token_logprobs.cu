@@ -10,8 +10,8 @@
 // Exponentials run in base 2, a = scale log2 e: t = x a - M, M = fl(m a), is one FMA; what the rounding of M does to
 // every term alike (at most 1 while |M| < 2^25) is taken out of a thread's sums at the end.  Logits are cut at -2^60
 // (2^-30 <= scale <= 2^30), so that -inf gives a weight of zero and no 0 * inf.  A thread whose largest logit has
-// |m a| >= 2^25 (masked with the type's lowest value, or a large scale) sums its columns again in the form (x - m) a,
-// which neither overflows nor is cut.
+// |m a| >= 2^25 (masked with the type's lowest value, or a large scale), or had one before that m does not dwarf, sums its
+// columns again in the form (x - m) a, which neither overflows nor is cut.
 #include <type_traits>
 
 #include "ctx.cuh"
@@ -142,11 +142,13 @@ __device__ __forceinline__ void join_lanes(Running& r, float a) {
 struct ThreadSums {
   float m, M;
   Two Z, S;
+  bool lost;               // a largest logit far from zero was followed by a near one that does not dwarf it
   static __device__ __forceinline__ bool near(float m, float a) { return fabsf(m * a) < kFarTerm; }
   __device__ __forceinline__ void raise(float top, float a) {            // top > m
     const float to = near(top, a) ? top * a : 0.f;
     const float d = fmaxf(M - to, kNoWeight);
     const float f = near(m, a) ? ex2(d) : 0.f;         // 0 times the sums, not 0: NaN stays
+    lost = lost || (!near(m, a) && (m - top) * a > kNoWeight);
     S = fma2(two(d, d), Z, S) * two(f, f);
     Z = Z * two(f, f);
     m = top;
@@ -309,7 +311,7 @@ __device__ __forceinline__ void for_columns_above(const Piece<T>& piece, int c0,
   }
 }
 
-// A thread's sums where its largest logit m is far from zero.
+// A thread's sums where its largest logit m, or an earlier one that still counts, is far from zero.
 template <typename T>
 __device__ __forceinline__ Running sum_far(const Piece<T>& piece, int t, float m, float a) {
   constexpr int V = Elem<T>::kVec;
@@ -356,7 +358,7 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(LogprobParam
     if (target >= 0 && target < p.vocab) target_logit = Elem<T>::get(x_row[target]);
   }
 
-  ThreadSums r{-INFINITY, 0.f, two(0.f, 0.f), two(0.f, 0.f)};
+  ThreadSums r{-INFINITY, 0.f, two(0.f, 0.f), two(0.f, 0.f), false};
   const Two a2 = two(p.a, p.a);
   auto add_single = [&](float x) { r.add(cut_logit(x), kLowestLogit, a2, two(-r.M, -r.M)); };
   int at = -1;                                           // where m was met: -1 nowhere, 0 front, 1 + batch, then the rest
@@ -404,7 +406,7 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(LogprobParam
     add_single(x);
   }
   Running sum = r.sum(p.a);
-  if (!ThreadSums::near(r.m, p.a) && r.m != -INFINITY) sum = sum_far(piece, t, r.m, p.a);   // NaN for +inf
+  if ((r.lost || !ThreadSums::near(r.m, p.a)) && r.m != -INFINITY) sum = sum_far(piece, t, r.m, p.a);   // NaN for +inf
 
   if constexpr (TOP) {
     // The k largest of the threads' maxima bound the k largest elements from below, and hold every thread
