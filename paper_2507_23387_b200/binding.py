@@ -59,6 +59,8 @@ class PackedMatrix:
         self.lo = torch.empty_like(self.hi)
         self.exp = torch.empty(1, dtype=torch.int32, device=device)
         self.operand = _Operand(None, 0, self.hi.data_ptr(), self.lo.data_ptr(), ld, self.exp.data_ptr())
+        self.device = self.hi.get_device()
+        self.packed = False                              # until Handle.sgemm_cube_pack has written it
 
 
 def load():
@@ -178,6 +180,8 @@ def _matrix(t, shape, device, dtype=torch.float32):
 def _operand(t, device):
     """An FP32 tensor or a PackedMatrix as the C struct."""
     if isinstance(t, PackedMatrix):
+        assert t.device == device, "expected a PackedMatrix on cuda:%d" % device
+        assert t.packed, "nothing has been packed into this PackedMatrix"
         return t.operand
     p, ld = _matrix(t, t.shape, device)
     return _Operand(p, ld, None, None, 0, None)
@@ -365,11 +369,13 @@ class Handle:
         """Scale, split and store X in a PackedMatrix of its shape."""
         dev = self.device
         rows, cols = X.shape
-        assert packed.shape == (rows, cols)
+        assert packed.shape == (rows, cols) and packed.device == dev, \
+            "expected a PackedMatrix %s on cuda:%d" % ((rows, cols), dev)
         x, ldx = _matrix(X, (rows, cols), dev)
         o = packed.operand
         _check(load().sgemm_cube_pack(self._h, rows, cols, x, ldx, o.hi_dev, o.lo_dev, o.ld16, o.exp_dev,
                                       _raw_stream(stream, dev)), "sgemm_cube_pack")
+        packed.packed = True
 
     def sgemm_cube_linear(self, X, W, Y, bias=None, residual=None, activation=ACT_NONE, preact=None,
                           weight_layout=WEIGHT_KN, stream=None):
