@@ -549,7 +549,7 @@ int sgemm_cube_linear(sgemm_cube_handle h, int M, int N, int K, const sgemm_cube
   Carve c;
   c.base = static_cast<uint8_t*>(h->ws);
   n_jobs = 0;
-  Packed px, pw;
+  Packed px{}, pw{};                                    // (what a form does not pack has no exponent)
   if (!short_batch) px = words_of(X, M, K, c, exps, jobs, &n_jobs);
   if (!direct) pw = words_of(W, w_rows, w_cols, c, exps + 1, jobs, &n_jobs);
   if (n_jobs && (rc = launch_pack(h, jobs, n_jobs, st))) return rc;
