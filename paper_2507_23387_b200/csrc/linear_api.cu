@@ -316,23 +316,23 @@ int launch_few_kn(sgemm_cube_ctx* h, const sgc::FewRowsParams& p, cudaStream_t s
   const int cols = (p.N + 127) / 128;
   int slices = 1;
   while (slices < 8 && (long long)cols * slices < 2 * h->sm_count && p.K / (slices * 2) >= 64) slices *= 2;
-  int k_per = (p.K + slices - 1) / slices;
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cudaLaunchAttribute a;
-  a.id = cudaLaunchAttributeClusterDimension;
-  a.val.clusterDim.x = 1; a.val.clusterDim.y = (unsigned)slices; a.val.clusterDim.z = 1;
-  cfg.gridDim = dim3((unsigned)cols, (unsigned)slices, 1);
-  cfg.blockDim = dim3(256, 1, 1);
-  cfg.dynamicSmemBytes = 8 * MR * 128 * sizeof(float);
-  cfg.stream = st;
-  cfg.attrs = &a;
-  cfg.numAttrs = 1;
-  h->launches++;
-  if (cudaLaunchKernelEx(&cfg, sgc::few_rows_kn_kernel<MR, LOAD>, p, k_per) != cudaSuccess) {
+  for (;; slices = 1) {                                              // clusters that cannot be scheduled: whole k
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute a;
+    a.id = cudaLaunchAttributeClusterDimension;
+    a.val.clusterDim.x = 1; a.val.clusterDim.y = (unsigned)slices; a.val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)cols, (unsigned)slices, 1);
+    cfg.blockDim = dim3(256, 1, 1);
+    cfg.dynamicSmemBytes = 8 * MR * 128 * sizeof(float);
+    cfg.stream = st;
+    cfg.attrs = &a;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, sgc::few_rows_kn_kernel<MR, LOAD>, p, (p.K + slices - 1) / slices) == cudaSuccess) break;
     cudaGetLastError();
-    return SGEMM_CUBE_CUDA_ERROR;
+    if (slices == 1) return SGEMM_CUBE_CUDA_ERROR;
   }
+  h->launches++;
   return SGEMM_CUBE_OK;
 }
 template <int LOAD>

@@ -606,21 +606,22 @@ int launch_logprobs(sgemm_cube_ctx* h, const sgc::LogprobParams& p, cudaStream_t
   // against 34, 512 x 131072 45 and 44 against 38.)
   int ranks = 1;
   while (ranks < 8 && (long long)p.rows * ranks < 2 * h->sm_count && p.vocab / (2 * ranks) >= 4096) ranks *= 2;
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cudaLaunchAttribute a;
-  a.id = cudaLaunchAttributeClusterDimension;
-  a.val.clusterDim.x = (unsigned)ranks; a.val.clusterDim.y = 1; a.val.clusterDim.z = 1;
-  cfg.gridDim = dim3((unsigned)(p.rows * ranks), 1, 1);
-  cfg.blockDim = dim3(sgc::kLpThreads, 1, 1);
-  cfg.stream = st;
-  cfg.attrs = &a;
-  cfg.numAttrs = 1;
-  h->launches++;
-  if (cudaLaunchKernelEx(&cfg, sgc::token_logprobs_kernel<T, TOP>, p) != cudaSuccess) {
+  for (;; ranks = 1) {                                    // clusters that cannot be scheduled: one block a row
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute a;
+    a.id = cudaLaunchAttributeClusterDimension;
+    a.val.clusterDim.x = (unsigned)ranks; a.val.clusterDim.y = 1; a.val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(p.rows * ranks), 1, 1);
+    cfg.blockDim = dim3(sgc::kLpThreads, 1, 1);
+    cfg.stream = st;
+    cfg.attrs = &a;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, sgc::token_logprobs_kernel<T, TOP>, p) == cudaSuccess) break;
     cudaGetLastError();
-    return SGEMM_CUBE_CUDA_ERROR;
+    if (ranks == 1) return SGEMM_CUBE_CUDA_ERROR;
   }
+  h->launches++;
   return SGEMM_CUBE_OK;
 }
 
