@@ -378,6 +378,9 @@ enum {
   SGEMM_CUBE_ACT_GELU_TANH = 3,  /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
   SGEMM_CUBE_ACT_SILU = 4        /* z / (1 + exp(-z)) */
 };
+/* Errors of activations and slopes in units u = 2^-24 of their terms (value: z times a weight; slope: that weight plus z
+ * times its derivative), A the argument of the exponential:  GELU 24 + 5 A, A = z^2 / 2;  GELU_TANH and SILU 12 + 3 A, A = 1.6
+ * (|z| + 0.045 |z|^3) and |z|.  Exponentials below 2^-126 are zero. */
 
 /* Scaling exponent and two-word split of a matrix, all on the device:
  *   p = 15 - e_max, clamped to [-126, 126]; e_max as in sgemm_cube_hi_exponent_range (p = 0 if every
