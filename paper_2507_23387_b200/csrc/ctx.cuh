@@ -45,7 +45,7 @@ struct sgemm_cube_ctx {
   int sm_count = 0;
   unsigned int* err_dev = nullptr;   // [0] error word; [4..13] scratch of sgemm_cube_exponent_window;
                                      // [16..19] clocks and nanoseconds of the last timed tensor-core kernel;
-                                     // [20..27] ranges and exponents of the linear layer's packing
+                                     // [20..31] ranges, exponents and meeting words of the linear layer's packing
   bool err_dev_has_clock = false;    // false for the static entry point's single error word
   void* ws = nullptr;          // unfused path: FP16 words of A and B, D_hh, D_x
   size_t ws_bytes = 0;

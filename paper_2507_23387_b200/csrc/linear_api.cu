@@ -9,10 +9,10 @@ namespace {
 
 using sgc::PackJob;
 
-// Words of the handle's device scratch that the packing kernels use: running maxima and block counts
-// of up to two jobs (left zero by every call; the cooperative kernels have theirs apart), exponents of operands
-// that a call packs itself.
-constexpr int kRangeWords = 20, kExpWords = 24;
+// Words of the handle's device scratch that the packing kernels use: running maxima and block counts of up to two jobs,
+// exponents of operands that a call packs itself, and the words in which the blocks of the one-launch kernels meet.
+// Every call leaves the first and the last four zero; after a kernel that gave up sgemm_cube_check does.
+constexpr int kRangeWords = 20, kExpWords = 24, kGridWords = 28;
 constexpr int kMaxSlices = 8;          // blocks of a portable cluster
 
 struct Packed {
@@ -43,7 +43,7 @@ PackJob pack_job(int rows, int cols, const float* X, int64_t ldx, uint16_t* hi, 
 }
 long long elements(const PackJob& j) { return (long long)j.rows * j.cols; }
 
-sgc::GridWords* grid_words(sgemm_cube_ctx* h) { return reinterpret_cast<sgc::GridWords*>(h->err_dev + kRangeWords); }
+sgc::GridWords* grid_words(sgemm_cube_ctx* h) { return reinterpret_cast<sgc::GridWords*>(h->err_dev + kGridWords); }
 
 template <typename K>
 int resident_blocks(sgemm_cube_ctx* h, K kernel, int* cached) {

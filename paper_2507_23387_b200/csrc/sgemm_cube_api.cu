@@ -783,6 +783,7 @@ int sgemm_cube_check(sgemm_cube_handle h, void* stream, uint32_t* detail_out) {
     cudaMemset(h->err_dev, 0, sizeof(e));
     // counts that a kernel which gave up has left behind
     cudaMemset(h->err_dev + 20, 0, 4 * sizeof(unsigned int));
+    cudaMemset(h->err_dev + 28, 0, 4 * sizeof(unsigned int));
     return SGEMM_CUBE_DEVICE_TIMEOUT;
   }
   return SGEMM_CUBE_OK;
