@@ -784,6 +784,8 @@ int sgemm_cube_check(sgemm_cube_handle h, void* stream, uint32_t* detail_out) {
     // counts that a kernel which gave up has left behind
     cudaMemset(h->err_dev + 20, 0, 4 * sizeof(unsigned int));
     cudaMemset(h->err_dev + 28, 0, 4 * sizeof(unsigned int));
+    // (waited for: the caller's streams need not be ordered after the default stream)
+    if (cudaStreamSynchronize(nullptr) != cudaSuccess) { cudaGetLastError(); return SGEMM_CUBE_CUDA_ERROR; }
     return SGEMM_CUBE_DEVICE_TIMEOUT;
   }
   return SGEMM_CUBE_OK;
