@@ -400,7 +400,7 @@ int sgemm_cube_pack(sgemm_cube_handle h, int rows, int cols,
  *   X  M x K;  W  K inputs, N outputs in weight_layout;  either may be FP32 or packed
  *   bias_dev N FP32 or NULL;  R_dev M x N FP32 (ldr >= N) or NULL, may be Y_dev itself (then ldr == ldy)
  *   Y_dev M x N FP32 (written);  Z_dev M x N FP32 or NULL: z is stored there for the backward pass
- *     (neither Y_dev nor R_dev)
+ *     (neither Y_dev nor R_dev).  Y and Z must not overlap X, W, bias or each other.
  * FP32 matrices may have any alignment.  The product is the three-product form of sgemm_cube on packed
  * operands, with two forms of its own for an FP32 X of few rows, which read W once and pack nothing ahead:
  * for a short batch (up to 64 rows, to 256 for small weights) X, and an FP32 W that starts its rows on 16 bytes,
@@ -446,7 +446,8 @@ int sgemm_cube_layer_norm(sgemm_cube_handle h, int rows, int cols, int dtype,
 /* Its gradients for dY:  with u = dY w and n = (x - mean) rstd,
  *   dX = rstd (u - mean(u) - n mean(u n)),  dweight = sum over rows of dY n,  dbias = sum over rows of dY.
  * dX_dev rows x cols of `dtype` or NULL (may be dY_dev with lddx == lddy); dweight_dev, dbias_dev cols FP32
- * or NULL (zero when rows == 0).  mean_dev and rstd_dev are the forward call's.
+ * or NULL (zero when rows == 0).  mean_dev and rstd_dev are the forward call's; mean rstd has to be an FP32 number
+ * (it is not in a constant row of 1e36 or more with eps = 1e-5: dX may be NaN there).
  * Errors: INVALID_ARG, ALLOC_FAILED, CUDA_ERROR. */
 int sgemm_cube_layer_norm_backward(sgemm_cube_handle h, int rows, int cols, int dtype,
                                    const void* dY_dev, int64_t lddy, const void* X_dev, int64_t ldx,

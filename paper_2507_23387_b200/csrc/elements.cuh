@@ -76,10 +76,9 @@ struct Elem<__nv_bfloat16> {
   static __device__ __forceinline__ __nv_bfloat16 put(float x) { return __float2bfloat16_rn(x); }
 };
 
-// Which columns of a row a thread of a group of `threads` holds.  VEC: 16-byte vectors, vector i at
-// (i * threads + t) * kVec; otherwise (rows that are not 16-byte aligned) single elements, element i at
-// i * threads + t.  Either way a warp's accesses are contiguous.  PT elements a thread, columns past
-// `cols` read as zero.
+// A thread of a group of `threads` holds PT elements of a row: 16-byte vectors, vector i at (i * threads + t) * kVec, or
+// (rows that are not 16-byte aligned) single elements, element i at i * threads + t.  Either way a warp's accesses are
+// contiguous, and columns past `cols` read as zero.
 // Single elements of a row that is asked for (fetch) before it is needed (get): they wait in registers.
 template <typename T, int PT>
 struct RowRegs {

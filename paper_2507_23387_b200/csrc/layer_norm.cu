@@ -8,7 +8,7 @@
 //              dw = sum over rows of dy n;  db = sum over rows of dy
 //
 // Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx, each once (8192 x 4096 FP32
-// 46 us and 73, 5.8 and 5.5 TB/s; BF16 rows by instructions as well, 6000 x 2048 13 and 26, 3.8 and 2.8 TB/s).  A row
+// 44 us and 69, 6.1 and 5.9 TB/s; BF16 rows by instructions as well, 6000 x 2048 12 and 23, 4.1 and 3.2 TB/s).  A row
 // lives in the registers of one group of warps between its load and its store, so the second moment is
 // taken about the first mean (no cancellation of squares) without a second read.  Blocks are persistent: a
 // group asks for its next rows before it works on the present one, and keeps its columns' weights (forward)
@@ -17,8 +17,7 @@
 // Rows of an odd length start anywhere between two 16-byte boundaries and are read element by element, except by the
 // backward kernel where all tensors agree in where a row starts: then the vectors are laid on the boundaries
 // (kShifted), and a group's rows are a multiple of 8 (FP32: 4) apart, so that they all start equally far behind one
-// and a thread's columns stay the same (4000 x 7001 BF16 58 us, 83 by elements; the forward kernel gained 2 of 41
-// and lost as much on aligned rows).
+// and a thread's columns stay the same (4000 x 7001 BF16 51 us, 83 by elements).
 #include <atomic>
 
 #include "ctx.cuh"
@@ -33,7 +32,10 @@ constexpr int kPT = 16;         // elements of a row a thread holds
 template <typename T, int WARPS>
 constexpr int slot_stages(int tensors) {
   const size_t row = (size_t)tensors * kPT * sizeof(T) * (WARPS > 8 ? WARPS * 32 : 256);
-  if (tensors == 1 && WARPS == 8 && sizeof(T) == 4) return 2;      // 8192 x 4096 forward 46 us, 52 with three
+  // FP32 rows of 8 warps (2049 to 4096 columns, three blocks an SM) come two deep, which is the faster over their whole
+  // range (2 and 3 deep: 8192 x 2052 29.9 and 31.6 us, x 2560 29.8 and 30.9, x 3584 37.9 and 40.3, x 4096 45.9 and
+  // 48.8; 1000 x 4096 7.8 and 8.3).
+  if (tensors == 1 && WARPS == 8 && sizeof(T) == 4) return 2;
   return 3 * row <= 200 * 1024 ? 3 : (2 * row <= 200 * 1024 ? 2 : 1);
 }
 template <typename T, int WARPS, bool VEC, int TENSORS>
@@ -41,12 +43,13 @@ constexpr int kStages = VEC ? slot_stages<T, WARPS>(TENSORS) : 0;
 template <typename T, int WARPS, bool VEC, int TENSORS>
 constexpr size_t kSlotBytes = (size_t)kStages<T, WARPS, VEC, TENSORS> * TENSORS * kPT * sizeof(T) * (WARPS > 8 ? WARPS * 32 : 256);
 
-// Sums over a row's group of warps.  `slot` alternates between two buffers, so one barrier a sum is enough.
 __device__ __forceinline__ float warp_sum(float s) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   return s;
 }
+// Warps' sums added over a row's group of warps.  The caller takes two buffers in turn, so one barrier a sum is enough.
+// (16 and 32 warps by shuffles: 2048 x 16384 BF16 32 us, 34.5 with every thread adding up; 4 and 8 are faster that way.)
 template <int WARPS, int N>
 __device__ __forceinline__ void join_warps(float (&s)[N], float* buf, int group, int warp_in_group, int bar_threads) {
   if constexpr (WARPS > 1) {

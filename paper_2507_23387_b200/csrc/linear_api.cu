@@ -341,10 +341,10 @@ int launch_few(sgemm_cube_ctx* h, const sgc::FewRowsParams& p, bool nk, cudaStre
     if (p.M == 1) return launch_few_nk<1, LOAD>(h, p, st);
     return p.M == 2 ? launch_few_nk<2, LOAD>(h, p, st) : launch_few_nk<4, LOAD>(h, p, st);
   } else {
-  if (p.M == 1) return nk ? launch_few_nk<1, LOAD>(h, p, st) : launch_few_kn<1, LOAD>(h, p, st);
-  if (p.M == 2) return nk ? launch_few_nk<2, LOAD>(h, p, st) : launch_few_kn<2, LOAD>(h, p, st);
-  if (p.M <= 4) return nk ? launch_few_nk<4, LOAD>(h, p, st) : launch_few_kn<4, LOAD>(h, p, st);
-  return nk ? launch_few_nk<8, LOAD>(h, p, st) : launch_few_kn<8, LOAD>(h, p, st);
+    if (p.M == 1) return nk ? launch_few_nk<1, LOAD>(h, p, st) : launch_few_kn<1, LOAD>(h, p, st);
+    if (p.M == 2) return nk ? launch_few_nk<2, LOAD>(h, p, st) : launch_few_kn<2, LOAD>(h, p, st);
+    if (p.M <= 4) return nk ? launch_few_nk<4, LOAD>(h, p, st) : launch_few_kn<4, LOAD>(h, p, st);
+    return nk ? launch_few_nk<8, LOAD>(h, p, st) : launch_few_kn<8, LOAD>(h, p, st);
   }
 }
 

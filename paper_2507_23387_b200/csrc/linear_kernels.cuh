@@ -465,7 +465,7 @@ linear_empty_kernel(int M, int N, float* Y, long long ldy, LinearEpilogue e) {
 // streams past the rows once and FP32 FMAs on the ordinary cores keep up; no tile is padded to 128 rows
 // and an FP32 W needs no packing.  A packed weight is put together again as 2^-p (hi + 2^-11 lo) (22 bits), so that the
 // products and the partial sums have the size of the result's own terms and not 2^p times that.
-// One row of 4096 x 1024 packed 6.7 us, of 16384 x 4096 about 50 (5.4 TB/s); with more rows the loads of X and the FMAs
+// One row of 4096 x 1024 packed 6.7 us, of 16384 x 4096 47 (5.7 TB/s); with more rows the loads of X and the FMAs
 // take over (FP32 weight, 4 rows 75, 8 rows 155), which is where the tensor cores are asked instead.
 struct FewRowsParams {
   int M, N, K;

@@ -2,8 +2,9 @@
 //
 // The weight's 4 bytes per element are what bounds it, so the weight takes the 128-row side of the tile and the few rows
 // of X the narrow one (16, 32 or 64 columns): a stage holds 32 KB of the weight and little else, and four to six of
-// them are in flight in every SM (16384 x 4096 packed, 24 rows: 50 us, 5.4 TB/s; its 128 tiles leave 20 SMs idle, and
-// the MMA thread needs 1100 clocks of the 1500 that a block of 64 k takes).  An
+// them are in flight in every SM (16384 x 4096 packed, 24 rows: 48 to 50 us in a chain of launches, 5.4 TB/s, 54 called
+// one by one; its 128 tiles leave 20 SMs idle, and the MMA thread needs 1100 clocks of the 1500 that a block of 64 k
+// takes).  A block takes one tile, so other widths fit worse: 86 tiles leave 62 SMs idle, 149 take two turns.  An
 // FP32 weight comes in FP32 and is split here too, by eight warps, which then bound the kernel (86 us where packing and
 // the product on packed words took 200).  X is not packed by a launch of its own: warps of this kernel turn 64 columns of it
 // into words as they are needed, each such block with an exponent of its own (15 - e_max, as in packing; the more

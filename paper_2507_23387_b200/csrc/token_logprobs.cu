@@ -5,8 +5,9 @@
 //   Z = sum exp(scale (x - m)),   S = sum exp(scale (x - m)) scale (x - m);
 // when m grows to m' both shrink by r = exp(scale (m - m')) and S also takes r scale (m - m') Z.  Then
 //   lse = scale m + log Z,   log p_t = scale (x_t - m) - log Z,   H = log Z - S / Z.
-// Bound by reading the logits once (2048 x 65536 FP32 87 us, 6.2 TB/s); with 16-bit logits by issuing instructions, so
-// these are counted (1000 x 50001 BF16 25 us, 4.0 TB/s at 2.4 instructions a clock; 34 with eight alternatives).
+// Bound by reading the logits once (2048 x 65536 FP32 85 us, 6.3 TB/s); with 16-bit logits by the instructions as much as
+// by waiting for the loads, so the instructions are counted (1000 x 50001 BF16 24 us, 4.2 TB/s; 31 with eight
+// alternatives, half of the issue slots used).
 // Exponentials run in base 2, a = scale log2 e: t = x a - M, M = fl(m a), is one FMA; what the rounding of M does to
 // every term alike (at most 1 while |M| < 2^25) is taken out of a thread's sums at the end.  Logits are cut at -2^60
 // (2^-30 <= scale <= 2^30), so that -inf gives a weight of zero and no 0 * inf.  A thread whose largest logit has
@@ -538,7 +539,7 @@ struct LogprobGradParams {
 // dx_j = e_j (A + B t_j) + [j == target] scale g with e_j = exp2(t_j), t_j = (x_j - m) a:
 //   p_j = e_j / Z,  log p_j = ln2 t_j - log Z,
 //   A = -scale (g + h (H - log Z)) / Z,  B = -scale h ln2 / Z      (g, h the two incoming gradients)
-// Reads and writes every logit once (4096 x 65536 FP32 321 us, 6.7 TB/s).  A block takes chunk `blockIdx % chunks` of a row, then the same of the
+// Reads and writes every logit once (4096 x 65536 FP32 323 us, 6.6 TB/s; BF16 163 us, 6.6 TB/s).  A block takes chunk `blockIdx % chunks` of a row, then the same of the
 // row `gridDim / chunks` further.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) token_logprobs_grad_kernel(LogprobGradParams p) {
