@@ -15,11 +15,12 @@ namespace sgc {
 enum Activation { kActNone = 0, kActRelu, kActGelu, kActGeluTanh, kActSilu };
 
 // exp and 1 / x on the special function unit (2^-22 and one ulp; exponentials below 2^-126 are zero).
-__device__ __forceinline__ float fast_exp(float x) {
+__device__ __forceinline__ float fast_exp2(float x) {
   float e;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * 1.4426950408889634f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
   return e;
 }
+__device__ __forceinline__ float fast_exp(float x) { return fast_exp2(x * 1.4426950408889634f); }
 __device__ __forceinline__ float fast_rcp(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -35,13 +36,12 @@ __device__ __forceinline__ float sigmoid(float z, float& slope) {
 
 // Phi(z), the normal distribution function, and e = exp(-z^2 / 2):  erfc(x) / 2 = t Q(t) exp(-x^2) with
 // t = 1 / (1 + 0.3 x) and Q of degree 8, fitted to exp(x^2) erfc(x) / t over 0 <= x <= 9.5 for the least relative error
-// (2e-8).  The lower tail is taken from it directly, not as a difference from 1, so it keeps its digits: in FP32 off by
-// 4e-7 of itself at z = 0, 1.5e-6 at -3, 3e-6 at -5 (the rounding of x^2 in the exponent).  18 instructions where erff and
-// expf take 45: with those the kernels around the product were bound by arithmetic, not by memory
+// (2e-8), x = |z| / sqrt(2).  The lower tail is taken from it directly, not as a difference from 1, so it keeps its digits: in
+// FP32 off by 4e-7 of itself at z = 0, 1.5e-6 at -3, 3e-6 at -5 (the rounding of z^2 in the exponent).  16 instructions where
+// erff and expf take 45: with those the kernels around the product were bound by arithmetic, not by memory
 // (8192 x 16384: 347 us for the pass that needs 164).
 __device__ __forceinline__ float normal_cdf(float z, float& e) {
-  const float x = fabsf(z) * 0.70710678118654752f;
-  const float t = fast_rcp(fmaf(0.3f, x, 1.f));
+  const float t = fast_rcp(fmaf(0.3f * 0.70710678118654752f, fabsf(z), 1.f));
   float q = fmaf(-0.0647170395f, t, 0.242548227f);
   q = fmaf(q, t, -0.255613238f);
   q = fmaf(q, t, 0.273197532f);
@@ -50,7 +50,7 @@ __device__ __forceinline__ float normal_cdf(float z, float& e) {
   q = fmaf(q, t, 0.0742412135f);
   q = fmaf(q, t, 0.0853459686f);
   q = fmaf(q, t, 0.0845948085f);
-  e = fast_exp(-x * x);
+  e = fast_exp2(-0.5f * 1.4426950408889634f * z * z);
   q = q * t * e;
   return z < 0.f ? q : 1.f - q;
 }
