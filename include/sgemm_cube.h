@@ -341,8 +341,9 @@ int sgemm_cube_auto_scaled(sgemm_cube_handle h, int M, int N, int K,
 
 /* ---- Language-model operators on and around the split product.
  *
- * A linear layer with its gradients, layer normalisation with its gradients, and log probabilities of
- * given tokens with their gradient.  No call synchronises; once the handle's workspace has its size
+ * A linear layer with its gradients, layer normalisation with its gradients, log probabilities of
+ * given tokens with their gradient, embedding with the table's gradient, softmax cross entropy over a vocabulary with its
+ * gradients, and orthogonalised updates.  No call synchronises; once the handle's workspace has its size
  * the calls can be captured into a graph.  A graph keeps the workspace that its calls were captured with: a larger
  * call may follow, and the graph can be replayed until the handle is destroyed.  As everywhere, calls on one handle
  * that may overlap on the GPU, replays among them, need one handle per stream.  Sums, statistics and softmax sums are FP32 (the products' k-blocks as
@@ -483,6 +484,71 @@ int sgemm_cube_token_logprobs_backward(sgemm_cube_handle h, int rows, int vocab,
                                        float scale, const float* stats_dev, const float* entropy_dev,
                                        const float* dlogp_dev, const float* dentropy_dev,
                                        void* dlogits_dev, int64_t lddl, void* stream);
+
+/* Embedding: row t = tokens_dev[i] of a table times a scale,  Y[i] = scale table[t];  zeros where t < 0 (padding), NaN where
+ * t >= vocab.  Computed in FP32, rounded once to the element type.
+ *   tokens_dev  rows int64;  table_dev  vocab x cols, Y_dev  rows x cols, both of `dtype`, row-major, any alignment
+ * rows >= 0, vocab >= 1, cols >= 1; the scale is finite.  Y must not overlap the table.
+ * Errors: INVALID_ARG, CUDA_ERROR. */
+int sgemm_cube_embedding(sgemm_cube_handle h, int rows, int vocab, int cols, int dtype,
+                         const int64_t* tokens_dev, const void* table_dev, int64_t ld, float scale,
+                         void* Y_dev, int64_t ldy, void* stream);
+
+/* Gradient of the table for dY:  dtable[v] = scale * sum of dY[i] over the rows with tokens_dev[i] == v, for all
+ * v of the vocabulary (accumulate == 0: rows that no token names become zero), or that added to what dtable holds
+ * (accumulate == 1: such rows are left alone).  Tokens outside [0, vocab) have no row and take no part.
+ * The sums are FP32 over rows in their order, in pieces of at least 32 of the sorted rows: the same from call to call.
+ *   dY_dev  rows x cols of `dtype`;  dtable_dev  vocab x cols FP32, ldd >= cols.  Any alignment, no overlap.
+ * Workspace: 16 bytes a row, 1 byte a token of the vocabulary, 8192 rows of cols FP32 at most.
+ * Errors: INVALID_ARG, ALLOC_FAILED, CUDA_ERROR. */
+int sgemm_cube_embedding_backward(sgemm_cube_handle h, int rows, int vocab, int cols, int dtype,
+                                  const int64_t* tokens_dev, const void* dY_dev, int64_t lddy, float scale,
+                                  int accumulate, float* dtable_dev, int64_t ldd, void* stream);
+
+/* Softmax cross entropy of a linear layer over a vocabulary of N tokens, without the logits z = X W + b:
+ *   lse_dev[r]  = log sum_j exp(z[r, j])
+ *   loss_dev[r] = lse[r] - z[r, t], t = targets_dev[r]; 0 where t < 0 (no target), NaN where t >= N
+ * Either may be NULL, not both.  X, W, weight_layout and bias as in sgemm_cube_linear, whose products these are (its forms for few rows
+ * among them); a bias of -inf takes a token out.  A row whose every logit is -inf has lse -inf and, with a target, loss +inf.
+ * M >= 0, N >= 1, K >= 1.  Workspace: what sgemm_cube_linear takes to pack its operands, and M N / 8 bytes.
+ * Errors: INVALID_ARG, MISALIGNED (packed operands), ALLOC_FAILED, CUDA_ERROR. */
+int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K,
+                             const sgemm_cube_operand* X, const sgemm_cube_operand* W, int weight_layout,
+                             const float* bias_dev, const int64_t* targets_dev, float* loss_dev, float* lse_dev,
+                             void* stream);
+
+/* The same with its gradients for dloss (M FP32): with dz[r, j] = dloss[r] (exp(z[r, j] - lse[r]) - 1[j == t]), 0 where t < 0,
+ *   dX = dz W^T (M x K),  dW = X^T dz (in weight_layout),  dbias = column sums of dz (N).
+ * It forms the logits itself and needs no call before it: loss_dev and lse_dev are written as above.  Every output
+ * may be NULL and is then not computed.  A row whose every logit is -inf has no gradient.  dz is packed with one exponent, from the largest
+ * |dloss| of a row with a target, as sgemm_cube_linear_backward packs its dz.  Outputs must not overlap inputs or each
+ * other.  M == 0: dW and dbias are zero.
+ * Workspace: as above, and 2 GiB or 8 bytes for every logit, whichever is less (256 rows at the least): more rows are taken
+ * in pieces, whose dW are added up.
+ * Errors: INVALID_ARG, MISALIGNED (packed operands), ALLOC_FAILED, CUDA_ERROR. */
+int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K,
+                                      const sgemm_cube_operand* X, const sgemm_cube_operand* W, int weight_layout,
+                                      const float* bias_dev, const int64_t* targets_dev, const float* dloss_dev,
+                                      float* loss_dev, float* lse_dev, float* dX_dev, int64_t lddx,
+                                      float* dW_dev, int64_t lddw, float* dbias_dev, void* stream);
+
+/* An update brought near the closest matrix with orthonormal rows (columns, where rows > cols) by Newton-Schulz products:
+ *   X = G / (|G|_F + eps);   steps times:  X <- a X + b (X X^T) X + c (X X^T)^2 X;   O = scale X + beta R
+ * The polynomial acts on the singular values alone: x -> a x + b x^3 + c x^5.
+ *   G_dev  rows x cols of `dtype`, any alignment
+ *   coefficients  3 * steps floats (HOST): a, b, c of every step; NULL: 3.4445, -4.7750, 2.0315 in all of them
+ *   R_dev  rows x cols FP32 (ldr >= cols) or NULL (no second term): the weight that is updated, with beta = 1 - rate * decay and a scale
+ *     of -rate times what the sizes ask for; may be O_dev itself (then ldr == ldo)
+ *   O_dev  rows x cols FP32 (written); may be G_dev where that is FP32 (G is read before O is written)
+ * All matrices of the iteration are kept as two FP16 words (22 bits) with exponents that follow from the coefficients:
+ * entries of X keep 22 bits down to 2^-29 of the largest singular value.  The products are those of sgemm_cube, termwise; the sum of
+ * squares is FP64, so G may have any FP32 size.  An infinite or NaN entry makes every entry of X NaN.  Zeros give zeros.
+ * rows, cols >= 0; 1 <= steps <= 64; eps >= 0; singular values must stay in [2^-20, 2^20] at their largest after every step.
+ * Workspace: 8 bytes an entry, 8 bytes for every entry of the smaller Gram matrix.
+ * Errors: INVALID_ARG, ALLOC_FAILED, CUDA_ERROR. */
+int sgemm_cube_orthogonalize(sgemm_cube_handle h, int rows, int cols, int dtype, const void* G_dev, int64_t ldg,
+                             int steps, const float* coefficients, float eps, float scale,
+                             const float* R_dev, int64_t ldr, float beta, float* O_dev, int64_t ldo, void* stream);
 
 /* Size in bytes of the fixed device scratch area used by sgemm_cube_unfused_static. */
 #define SGEMM_CUBE_STATIC_SCRATCH_BYTES (32u << 20)

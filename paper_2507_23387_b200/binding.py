@@ -32,6 +32,8 @@ EXPORTS = ["sgemm_cube_create", "sgemm_cube_destroy", "sgemm_cube_set_option", "
            "sgemm_cube_pack", "sgemm_cube_linear", "sgemm_cube_linear_backward",
            "sgemm_cube_layer_norm", "sgemm_cube_layer_norm_backward",
            "sgemm_cube_token_logprobs", "sgemm_cube_token_logprobs_backward",
+           "sgemm_cube_embedding", "sgemm_cube_embedding_backward",
+           "sgemm_cube_cross_entropy", "sgemm_cube_cross_entropy_backward", "sgemm_cube_orthogonalize",
            "sgemm_cube_status_string", "sgemm_cube_version"]
 
 _lib = None
@@ -102,6 +104,13 @@ def load():
     lib.sgemm_cube_token_logprobs.argtypes = [vp, i32, i32, i32, vp, i64, vp, f32, vp, vp, vp, i32, vp, vp, vp]
     lib.sgemm_cube_token_logprobs_backward.argtypes = [vp, i32, i32, i32, vp, i64, vp, f32, vp, vp, vp, vp, vp,
                                                        i64, vp]
+    lib.sgemm_cube_embedding.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, f32, vp, i64, vp]
+    lib.sgemm_cube_embedding_backward.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, f32, i32, vp, i64, vp]
+    lib.sgemm_cube_cross_entropy.argtypes = [vp, i32, i32, i32, pop, pop, i32, vp, vp, vp, vp, vp]
+    lib.sgemm_cube_cross_entropy_backward.argtypes = [vp, i32, i32, i32, pop, pop, i32, vp, vp, vp, vp, vp, vp, i64, vp,
+                                                      i64, vp, vp]
+    lib.sgemm_cube_orthogonalize.argtypes = [vp, i32, i32, i32, vp, i64, i32, ctypes.POINTER(f32), f32, f32, vp, i64, f32,
+                                             vp, i64, vp]
     lib.sgemm_cube_check.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_uint32)]
     lib.sgemm_cube_last_kernel_ms.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
     lib.sgemm_cube_mean_kernel_ms.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i32)]
@@ -460,6 +469,71 @@ class Handle:
                                                          _vector(stats, 2 * rows, dev), _vector(entropy, rows, dev),
                                                          _vector(dlogp, rows, dev), _vector(dentropy, rows, dev), dx, lddl,
                                                          _raw_stream(stream, dev)), "sgemm_cube_token_logprobs_backward")
+
+    def sgemm_cube_embedding(self, tokens, table, Y, scale=1.0, stream=None):
+        """Y[i] = scale table[tokens[i]] (tokens int64; negative: zeros) for a float32, float16 or bfloat16 table."""
+        dev = self.device
+        (vocab, cols), dtype = table.shape, table.dtype
+        rows = tokens.numel()
+        t, ld = _matrix(table, table.shape, dev, dtype)
+        y, ldy = _matrix(Y, (rows, cols), dev, dtype)
+        _check(load().sgemm_cube_embedding(self._h, rows, vocab, cols, _DTYPE[dtype], _vector(tokens, rows, dev, torch.int64), t, ld,
+                                           scale, y, ldy, _raw_stream(stream, dev)), "sgemm_cube_embedding")
+
+    def sgemm_cube_embedding_backward(self, tokens, dY, dtable, scale=1.0, accumulate=False, stream=None):
+        """Gradient of the table (float32) for dY (float32, float16 or bfloat16), stored or added to dtable."""
+        dev = self.device
+        (vocab, cols), dtype = dtable.shape, dY.dtype
+        rows = tokens.numel()
+        g, lddy = _matrix(dY, (rows, cols), dev, dtype)
+        d, ldd = _matrix(dtable, dtable.shape, dev)
+        _check(load().sgemm_cube_embedding_backward(self._h, rows, vocab, cols, _DTYPE[dtype], _vector(tokens, rows, dev, torch.int64),
+                                                    g, lddy, scale, int(bool(accumulate)), d, ldd, _raw_stream(stream, dev)),
+               "sgemm_cube_embedding_backward")
+
+    def sgemm_cube_cross_entropy(self, X, W, targets, loss=None, bias=None, lse=None, weight_layout=WEIGHT_KN, stream=None):
+        """loss[r] = log sum exp(z[r]) - z[r, targets[r]] (negative: no target) and that log-sum lse, z = X W + bias; X and W
+        are FP32 tensors or PackedMatrix objects."""
+        dev = self.device
+        (M, K), (a, b) = X.shape, W.shape
+        k2, N = (b, a) if weight_layout == WEIGHT_NK else (a, b)
+        assert K == k2, "X and W do not fit"
+        _check(load().sgemm_cube_cross_entropy(self._h, M, N, K, _operand(X, dev), _operand(W, dev), weight_layout,
+                                               _vector(bias, N, dev), _vector(targets, M, dev, torch.int64),
+                                               _vector(loss, M, dev), _vector(lse, M, dev), _raw_stream(stream, dev)),
+               "sgemm_cube_cross_entropy")
+
+    def sgemm_cube_cross_entropy_backward(self, X, W, targets, dloss, dX=None, dW=None, dbias=None, bias=None, loss=None,
+                                          lse=None, weight_layout=WEIGHT_KN, stream=None):
+        """sgemm_cube_cross_entropy and its gradients for dloss, into whichever of the outputs are given."""
+        dev = self.device
+        (M, K), (a, b) = X.shape, W.shape
+        k2, N = (b, a) if weight_layout == WEIGHT_NK else (a, b)
+        assert K == k2, "X and W do not fit"
+        dx, lddx = _matrix(dX, (M, K), dev)
+        dw, lddw = _matrix(dW, (a, b), dev)
+        _check(load().sgemm_cube_cross_entropy_backward(self._h, M, N, K, _operand(X, dev), _operand(W, dev), weight_layout,
+                                                        _vector(bias, N, dev), _vector(targets, M, dev, torch.int64),
+                                                        _vector(dloss, M, dev), _vector(loss, M, dev), _vector(lse, M, dev),
+                                                        dx, lddx, dw, lddw, _vector(dbias, N, dev), _raw_stream(stream, dev)),
+               "sgemm_cube_cross_entropy_backward")
+
+    def sgemm_cube_orthogonalize(self, G, O, steps=5, coefficients=None, eps=1e-7, scale=1.0, residual=None, beta=1.0, stream=None):
+        """O = scale X + beta residual, X what `steps` Newton-Schulz steps make of G (float32, float16 or bfloat16).
+        coefficients: (a, b, c) of every step, or one such triple a step."""
+        dev = self.device
+        shape, dtype = G.shape, G.dtype
+        g, ldg = _matrix(G, shape, dev, dtype)
+        o, ldo = _matrix(O, shape, dev)
+        r, ldr = _matrix(residual, shape, dev)
+        k = None
+        if coefficients is not None:
+            flat = [float(v) for row in coefficients for v in row] if not isinstance(coefficients[0], (int, float)) \
+                else [float(v) for v in coefficients] * steps
+            assert len(flat) == 3 * steps, "expected three coefficients a step"
+            k = (ctypes.c_float * len(flat))(*flat)
+        _check(load().sgemm_cube_orthogonalize(self._h, shape[0], shape[1], _DTYPE[dtype], g, ldg, steps, k, eps, scale, r, ldr,
+                                               beta, o, ldo, _raw_stream(stream, dev)), "sgemm_cube_orthogonalize")
 
     def sgemm_cube_launch_count(self) -> int:
         return int(load().sgemm_cube_launch_count(self._h))

@@ -9,7 +9,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsgemm_cube.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("sgemm_cube_api.cu", "linear_api.cu", "layer_norm.cu", "token_logprobs.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("sgemm_cube_api.cu", "linear_api.cu", "layer_norm.cu", "token_logprobs.cu",
+                                          "embedding.cu", "cross_entropy.cu", "orthogonalize.cu")]
 DEPS = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + \
        [os.path.join(os.path.dirname(HERE), "include", "sgemm_cube.h")]
 

@@ -40,6 +40,14 @@ template <typename... D>
 inline bool bad_dims(D... d) { return ((d < 0 || d > 0x7FFF0000) || ...); }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+namespace sgc {
+// How many clusters of a family of product kernels are resident at once: pairs, and 2 to 8 blocks with a k slice each.
+struct ResidentClusters {
+  bool ready = false;          // kernel attributes set, the counts below known
+  int pairs = 0, slices[9] = {0};
+};
+}  // namespace sgc
+
 struct sgemm_cube_ctx {
   int device = 0;
   int sm_count = 0;
@@ -54,6 +62,12 @@ struct sgemm_cube_ctx {
   int split_k = 1;             // 1: split the k range of few-tile problems over idle SMs; 0: never
   void* tile_ws = nullptr;     // linear forms: two 128 x 256 tiles for every block of the tensor-core kernel
   size_t tile_ws_bytes = 0;
+  void* loss_ws = nullptr;     // cross entropy: logits of a piece of rows, words of their gradient, pairs
+  size_t loss_ws_bytes = 0;
+  void* poly_ws = nullptr;     // orthogonalised updates: words of X, of its Gram matrix and of the polynomial
+  size_t poly_ws_bytes = 0;
+  void* sort_ws = nullptr;     // embedding gradients: sorted tokens and their rows, partial sums
+  size_t sort_ws_bytes = 0;
   void* host_ws = nullptr;     // host-buffer path: device copies of A, B, C
   size_t host_ws_bytes = 0;
   std::vector<void*> graph_ws; // buffers that captured calls have used, outgrown ones among them
@@ -74,8 +88,7 @@ struct sgemm_cube_ctx {
   int max_pair_clusters[3] = {0, 0, 0};   // co-resident 2-CTA clusters: <1,false>, <3,false>, <3,true>
   EncodeTiledFn encode = nullptr;
   bool attrs_set = false;
-  bool linear_ready = false;   // linear forms: kernel attributes set, co-resident 2-CTA clusters known
-  int linear_pair_clusters = 0, linear_slice_clusters[9] = {0};
+  sgc::ResidentClusters linear_clusters, polynomial_clusters, loss_clusters;
   int pack_once_blocks = 0, dz_once_blocks[5] = {0, 0, 0, 0, 0};   // resident blocks of the one-launch packing kernels
 };
 
@@ -112,7 +125,7 @@ inline int grow(sgemm_cube_ctx* h, void** buf, size_t* have, size_t want, cudaSt
   return SGEMM_CUBE_OK;
 }
 inline void free_workspaces(sgemm_cube_ctx* h) {
-  void* const current[] = {h->ws, h->part_ws, h->tile_ws, h->host_ws};
+  void* const current[] = {h->ws, h->part_ws, h->tile_ws, h->loss_ws, h->poly_ws, h->sort_ws, h->host_ws};
   for (void* p : h->graph_ws) {
     bool also = false;
     for (void* q : current) also = also || q == p;

@@ -1,0 +1,529 @@
+// Embedding lookup with a scale, and the gradient of the table by sorted tokens (contracts: include/sgemm_cube.h).
+//
+//   Y[i] = scale E[t_i];   dE[v] = scale sum over i with t_i = v of dY[i]  (+ dE[v])
+//
+// Both only move memory.  The gradient sorts the tokens (stable, so a token's rows are added in their order and the result
+// is the same every time), cuts the sorted list into pieces of equal length, and adds the rows of each piece, a run of equal
+// tokens at a time: a frequent token's rows are shared by many blocks, and a run that leaves a piece goes through partial sums.
+#include <cmath>
+
+#include "ctx.cuh"
+#include "elements.cuh"
+#include "product_host.cuh"
+
+namespace sgc {
+
+// ------------------------------------------------------------------------------------------ lookup
+struct LookupParams {
+  long long rows;
+  int vocab, cols, pieces;       // pieces of a row
+  const long long* tokens;
+  const void* table;
+  long long ld;
+  float scale;
+  void* Y;
+  long long ldy;
+};
+constexpr int kLookupThreads = 128, kLookupItems = 4;
+
+// A block copies a piece of a row: 16-byte vectors or (rows that are not on 16-byte boundaries) single elements.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kLookupThreads) embedding_kernel(LookupParams p) {
+  constexpr int V = VEC ? Elem<T>::kVec : 1, U = kLookupItems;
+  for (long long unit = blockIdx.x; unit < p.rows * p.pieces; unit += gridDim.x) {
+    const long long row = p.pieces == 1 ? unit : unit / p.pieces;
+    const int c0 = (int)(unit - row * p.pieces) * (kLookupThreads * V * U) + threadIdx.x * V;
+    const long long t = __ldg(p.tokens + row);
+    const bool inside = t >= 0 && t < p.vocab;
+    const T* src = static_cast<const T*>(p.table) + (inside ? t : 0) * p.ld;
+    T* dst = static_cast<T*>(p.Y) + row * p.ldy;
+    const float none = t < 0 ? 0.f : NAN;
+    if constexpr (VEC) {
+      uint4 raw[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * kLookupThreads * V;
+        if (inside && c < p.cols) raw[u] = __ldg(reinterpret_cast<const uint4*>(src + c));
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * kLookupThreads * V;
+        if (c >= p.cols) break;
+        float e[V];
+        Elem<T>::unpack(raw[u], e);
+#pragma unroll
+        for (int q = 0; q < V; ++q) e[q] = inside ? e[q] * p.scale : none;
+        *reinterpret_cast<uint4*>(dst + c) = Elem<T>::pack(e);
+      }
+    } else {
+      T raw[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * kLookupThreads;
+        if (inside && c < p.cols) raw[u] = src[c];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * kLookupThreads;
+        if (c < p.cols) dst[c] = Elem<T>::put(inside ? Elem<T>::get(raw[u]) * p.scale : none);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------ sorting
+constexpr int kSortThreads = 256, kSortItems = 8, kSortTile = kSortThreads * kSortItems;
+constexpr int kSortBits = 8, kSortBins = 1 << kSortBits;
+
+struct SortParams {
+  int n, vocab, passes;
+  const long long* tokens;
+  int* key[2];               // the pass reads from one and writes to the other; the first reads the tokens
+  int* pos[2];
+  int* hist;                 // [blocks][bins]
+  unsigned char* met;        // [vocab]: whether the token occurs, or null
+  unsigned int* words;       // {arrived, left}, zero between calls
+  unsigned int* err;
+};
+
+// All blocks of the grid meet for the `round`-th time (from 1).  Cooperative launch; bounded all the same.
+__device__ __forceinline__ bool sort_meet(const SortParams& p, unsigned int round) {
+  __shared__ unsigned int ok;
+  if (gridDim.x == 1) {
+    __syncthreads();
+    return true;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    atomicAdd(&p.words[0], 1u);
+    const unsigned int want = round * gridDim.x;
+    const long long t0 = clock64();
+    unsigned int seen = 0;
+    ok = 1u;
+    while (true) {
+      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(&p.words[0]) : "memory");
+      if (seen >= want) break;
+      __nanosleep(32);
+      if (clock64() - t0 > kWaitLimitClocks) {
+        atomicExch(p.err, (unsigned int)kErrSortWait);
+        ok = 0u;
+        break;
+      }
+    }
+    __threadfence();
+  }
+  __syncthreads();
+  return ok != 0u;
+}
+
+// Stable sort of (token, row) by token, 8 bits a pass from the lowest.  A block has a run of whole tiles; in a pass it counts
+// its digits, meets the others, adds up for every digit what lies before its own first one, and
+// moves its items in order.  Tokens outside [0, vocab) get the key `vocab` and end up behind all others.
+__global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortParams p) {
+  __shared__ int base[kSortBins];                              // next place of a digit
+  __shared__ int warp_hist[kSortThreads / 32][kSortBins];
+  __shared__ int scan[kSortThreads / 32];
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int tiles = (p.n + kSortTile - 1) / kSortTile;
+  const int per_block = (tiles + gridDim.x - 1) / gridDim.x;
+  const int first = min((long long)p.n, (long long)blockIdx.x * per_block * kSortTile);
+  const int last = min((long long)p.n, ((long long)blockIdx.x + 1) * per_block * kSortTile);
+  if (p.met)
+    for (long long v = (long long)blockIdx.x * kSortThreads + t; v < p.vocab; v += (long long)gridDim.x * kSortThreads) p.met[v] = 0;
+  unsigned int round = 0;
+  for (int pass = 0; pass < p.passes; ++pass) {
+    const int shift = pass * kSortBits;
+    const int *key_in = p.key[pass & 1], *pos_in = p.pos[pass & 1];
+    int *key_out = p.key[(pass & 1) ^ 1], *pos_out = p.pos[(pass & 1) ^ 1];
+    auto key_of = [&](int i) -> int {
+      if (pass) return __ldcg(key_in + i);
+      const long long v = p.tokens[i];
+      return v >= 0 && v < p.vocab ? (int)v : p.vocab;
+    };
+    base[t] = 0;
+    __syncthreads();
+    for (int i = first + t; i < last; i += kSortThreads) atomicAdd(&base[(key_of(i) >> shift) & (kSortBins - 1)], 1);
+    __syncthreads();
+    p.hist[blockIdx.x * kSortBins + t] = base[t];
+    if (!sort_meet(p, ++round)) return;
+    // thread t: digit t's items in the blocks before this one, and in all of them
+    int before = 0, all = 0;
+    for (int b = 0; b < (int)gridDim.x; ++b) {
+      const int c = __ldcg(p.hist + b * kSortBins + t);
+      before += b < (int)blockIdx.x ? c : 0;
+      all += c;
+    }
+    int incl = all;
+    for (int x = 1; x < 32; x *= 2) {
+      const int o = __shfl_up_sync(0xffffffffu, incl, x);
+      if (lane >= x) incl += o;
+    }
+    if (lane == 31) scan[warp] = incl;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) incl += scan[w];
+    base[t] = incl - all + before;
+    __syncthreads();
+    for (int tile = first; tile < last; tile += kSortTile) {
+      // a warp has 256 items in a row, 32 at a time; an item's place among the warp's of its digit
+      int key[kSortItems], place[kSortItems];
+      for (int i = lane; i < kSortBins; i += 32) warp_hist[warp][i] = 0;
+      __syncwarp();
+#pragma unroll
+      for (int u = 0; u < kSortItems; ++u) {
+        const int i = tile + warp * (32 * kSortItems) + u * 32 + lane;
+        key[u] = i < last ? key_of(i) : -1;
+        const int digit = key[u] < 0 ? kSortBins : (key[u] >> shift) & (kSortBins - 1);
+        const unsigned same = __match_any_sync(0xffffffffu, digit);
+        const int ahead = __popc(same & ((1u << lane) - 1u));
+        int start = 0;
+        if (digit < kSortBins) start = warp_hist[warp][digit];
+        __syncwarp();
+        if (digit < kSortBins && ahead == 0) warp_hist[warp][digit] = start + __popc(same);
+        __syncwarp();
+        place[u] = start + ahead;
+      }
+      __syncthreads();
+      // thread t: where each warp's items of digit t begin
+      int at = base[t];
+      for (int w = 0; w < kSortThreads / 32; ++w) {
+        const int c = warp_hist[w][t];
+        warp_hist[w][t] = at;
+        at += c;
+      }
+      __syncthreads();
+      base[t] = at;
+#pragma unroll
+      for (int u = 0; u < kSortItems; ++u) {
+        if (key[u] < 0) continue;
+        const int i = tile + warp * (32 * kSortItems) + u * 32 + lane;
+        const int to = warp_hist[warp][(key[u] >> shift) & (kSortBins - 1)] + place[u];
+        key_out[to] = key[u];
+        pos_out[to] = pass ? __ldcg(pos_in + i) : i;
+        if (p.met && pass == p.passes - 1 && key[u] < p.vocab) p.met[key[u]] = 1;
+      }
+      __syncthreads();
+    }
+    if (pass + 1 < p.passes && !sort_meet(p, ++round)) return;
+  }
+  if (gridDim.x > 1 && t == 0) {
+    if (atomicAdd(&p.words[1], 1u) == gridDim.x - 1) p.words[0] = p.words[1] = 0u;   // the last one clears both
+  }
+}
+
+// ------------------------------------------------------------------------------------------ sums
+struct TableGradParams {
+  int n, vocab, cols, piece, pieces;   // sorted items; items of a piece, pieces
+  int tiles;                           // column tiles of a row
+  const int* key;
+  const int* pos;
+  const unsigned char* met;            // null: nothing is cleared
+  const void* dY;
+  long long lddy;
+  float scale;
+  int accumulate;
+  float* dE;
+  long long ldd;
+  float* part;                         // [2 pieces][ldp]: the run that a piece finds begun, and the one that it leaves open
+  long long ldp;
+  unsigned int sum_blocks;             // the blocks behind them clear the rows of tokens that do not occur
+  int vec_out;                         // dE takes 16-byte accesses
+};
+constexpr int kGradThreads = 128;
+template <typename T>
+__host__ __device__ constexpr int grad_columns() { return kGradThreads * Elem<T>::kVec; }
+
+// Column of the thread's element q in its tile: consecutive ones where rows take vectors, else one in 128.
+template <typename T, bool VEC>
+__device__ __forceinline__ int grad_column(int tile, int q) {
+  return tile * grad_columns<T>() + (VEC ? (int)threadIdx.x * Elem<T>::kVec + q : q * kGradThreads + (int)threadIdx.x);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_grad(const TableGradParams& p, int token, int tile, const float (&acc)[Elem<T>::kVec]) {
+  constexpr int V = Elem<T>::kVec;
+  float* out = p.dE + (long long)token * p.ldd;
+  if (VEC && p.vec_out) {
+    const int c = grad_column<T, VEC>(tile, 0);
+    if (c >= p.cols) return;
+#pragma unroll
+    for (int q = 0; q < V; q += 4) {
+      float4 o = make_float4(acc[q] * p.scale, acc[q + 1] * p.scale, acc[q + 2] * p.scale, acc[q + 3] * p.scale);
+      if (p.accumulate) {
+        const float4 old = *reinterpret_cast<const float4*>(out + c + q);
+        o.x += old.x; o.y += old.y; o.z += old.z; o.w += old.w;
+      }
+      *reinterpret_cast<float4*>(out + c + q) = o;
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      const int c = grad_column<T, VEC>(tile, q);
+      if (c < p.cols) out[c] = p.accumulate ? out[c] + acc[q] * p.scale : acc[q] * p.scale;
+    }
+  }
+}
+
+// A block adds the rows of one piece in one tile of columns.  Rows come four at a time; a run that lies inside the piece
+// is stored, the others' sums go to `part`.  The last blocks clear rows.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kGradThreads) table_grad_kernel(TableGradParams p) {
+  constexpr int V = Elem<T>::kVec, U = 4;
+  if (blockIdx.x >= p.sum_blocks) {
+    const unsigned int blk = blockIdx.x - p.sum_blocks, blocks = gridDim.x - p.sum_blocks;
+    for (long long v = blk; v < p.vocab; v += blocks) {
+      if (p.met[v]) continue;
+      float* out = p.dE + v * p.ldd;
+      if (p.vec_out) {
+        for (int c = threadIdx.x * 4; c < p.cols; c += kGradThreads * 4) *reinterpret_cast<float4*>(out + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+      } else {
+        for (int c = threadIdx.x; c < p.cols; c += kGradThreads) out[c] = 0.f;
+      }
+    }
+    return;
+  }
+  const int piece = (int)(blockIdx.x / p.tiles), tile = (int)(blockIdx.x - (unsigned)piece * p.tiles);
+  const int first = piece * p.piece, last = min(p.n, first + p.piece);
+  float acc[V];
+#pragma unroll
+  for (int q = 0; q < V; ++q) acc[q] = 0.f;
+  // tokens outside the vocabulary lie behind all others and have no row
+  int run = __ldg(p.key + first);
+  if (run >= p.vocab) return;
+  bool open = first > 0 && __ldg(p.key + first - 1) == run;          // begun in the piece before
+  auto leave = [&](bool goes_on) {
+    if (!open && !goes_on) {
+      store_grad<T, VEC>(p, run, tile, acc);
+    } else {
+      float* out = p.part + (2ll * piece + (open ? 0 : 1)) * p.ldp;
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        const int c = grad_column<T, VEC>(tile, q);
+        if (c < p.cols) out[c] = acc[q];
+      }
+    }
+  };
+  for (int i = first; i < last; i += U) {
+    int key[U];
+    uint4 raw[U];
+    T one[U][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      key[u] = i + u < last ? __ldg(p.key + i + u) : p.vocab;
+      if (key[u] < p.vocab) {
+        const T* src = static_cast<const T*>(p.dY) + (long long)__ldg(p.pos + i + u) * p.lddy;
+        if constexpr (VEC) {
+          const int c = grad_column<T, VEC>(tile, 0);
+          raw[u] = c < p.cols ? __ldcs(reinterpret_cast<const uint4*>(src + c)) : make_uint4(0u, 0u, 0u, 0u);
+        } else {
+#pragma unroll
+          for (int q = 0; q < V; ++q) {
+            const int c = grad_column<T, VEC>(tile, q);
+            one[u][q] = c < p.cols ? src[c] : Elem<T>::put(0.f);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (key[u] >= p.vocab) break;
+      if (key[u] != run) {
+        leave(false);
+        run = key[u];
+        open = false;
+#pragma unroll
+        for (int q = 0; q < V; ++q) acc[q] = 0.f;
+      }
+      float e[V];
+      if constexpr (VEC) {
+        Elem<T>::unpack(raw[u], e);
+      } else {
+#pragma unroll
+        for (int q = 0; q < V; ++q) e[q] = Elem<T>::get(one[u][q]);
+      }
+#pragma unroll
+      for (int q = 0; q < V; ++q) acc[q] += e[q];
+    }
+  }
+  leave(last < p.n && __ldg(p.key + last) == run);
+}
+
+// Runs that reach over pieces: the block of the piece in which one begins adds the parts of the others, in order.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kGradThreads) table_grad_join_kernel(TableGradParams p) {
+  constexpr int V = Elem<T>::kVec;
+  const int piece = (int)(blockIdx.x / p.tiles), tile = (int)(blockIdx.x - (unsigned)piece * p.tiles);
+  const int first = piece * p.piece, last = first + p.piece;
+  if (last >= p.n) return;
+  const int run = __ldg(p.key + last - 1);
+  if (run >= p.vocab || __ldg(p.key + last) != run) return;                            // ends here
+  if (first > 0 && __ldg(p.key + first) == run && __ldg(p.key + first - 1) == run) return;   // begun before
+  float acc[V];
+#pragma unroll
+  for (int q = 0; q < V; ++q) {
+    const int c = grad_column<T, VEC>(tile, q);
+    acc[q] = c < p.cols ? p.part[(2ll * piece + 1) * p.ldp + c] : 0.f;
+  }
+  for (int i = piece + 1; i < p.pieces && __ldg(p.key + (long long)i * p.piece) == run; ++i) {
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      const int c = grad_column<T, VEC>(tile, q);
+      if (c < p.cols) acc[q] += p.part[2ll * i * p.ldp + c];
+    }
+  }
+  store_grad<T, VEC>(p, run, tile, acc);
+}
+
+}  // namespace sgc
+
+namespace {
+
+using sgc::Carve;
+
+size_t elem_size(int dtype) { return dtype == SGEMM_CUBE_F32 ? 4 : 2; }
+bool bad_dtype(int dtype) { return dtype < SGEMM_CUBE_F32 || dtype > SGEMM_CUBE_BF16; }
+bool bad_scale(float s) { return !std::isfinite(s); }
+
+template <typename T>
+int launch_lookup(sgemm_cube_ctx* h, sgc::LookupParams p, bool vec, cudaStream_t st) {
+  const int span = sgc::kLookupThreads * sgc::kLookupItems * (vec ? sgc::Elem<T>::kVec : 1);
+  p.pieces = (p.cols + span - 1) / span;
+  const long long units = p.rows * p.pieces, cap = 0x7FFFFFFF;
+  const unsigned blocks = (unsigned)(units < cap ? units : cap);
+  if (vec) sgc::embedding_kernel<T, true><<<blocks, sgc::kLookupThreads, 0, st>>>(p);
+  else sgc::embedding_kernel<T, false><<<blocks, sgc::kLookupThreads, 0, st>>>(p);
+  return sgc::launched(h);
+}
+
+template <typename T>
+int launch_table_grad(sgemm_cube_ctx* h, sgc::TableGradParams p, bool vec, unsigned clear_blocks, cudaStream_t st) {
+  const unsigned blocks = p.sum_blocks + clear_blocks;
+  if (blocks == 0) return SGEMM_CUBE_OK;
+  if (vec) sgc::table_grad_kernel<T, true><<<blocks, sgc::kGradThreads, 0, st>>>(p);
+  else sgc::table_grad_kernel<T, false><<<blocks, sgc::kGradThreads, 0, st>>>(p);
+  int rc = sgc::launched(h);
+  if (rc || p.pieces < 2) return rc;
+  if (vec) sgc::table_grad_join_kernel<T, true><<<p.sum_blocks, sgc::kGradThreads, 0, st>>>(p);
+  else sgc::table_grad_join_kernel<T, false><<<p.sum_blocks, sgc::kGradThreads, 0, st>>>(p);
+  return sgc::launched(h);
+}
+
+int launch_sort(sgemm_cube_ctx* h, const sgc::SortParams& p, int blocks, cudaStream_t st) {
+  if (blocks > 1) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)blocks, 1, 1);
+    cfg.blockDim = dim3(sgc::kSortThreads, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute a;
+    a.id = cudaLaunchAttributeCooperative;
+    a.val.cooperative = 1;
+    cfg.attrs = &a;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, sgc::sort_tokens_kernel, p) == cudaSuccess) {
+      h->launches++;
+      return SGEMM_CUBE_OK;
+    }
+    cudaGetLastError();                          // a device that is partly occupied by others: one block does it
+  }
+  sgc::sort_tokens_kernel<<<1, sgc::kSortThreads, 0, st>>>(p);
+  return sgc::launched(h);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sgemm_cube_embedding(sgemm_cube_handle h, int rows, int vocab, int cols, int dtype, const int64_t* tokens, const void* table,
+                         int64_t ld, float scale, void* Y, int64_t ldy, void* stream) {
+  if (!h || bad_dims(rows, vocab, cols) || vocab < 1 || cols < 1 || ld < cols || ldy < cols || bad_dtype(dtype) || bad_scale(scale))
+    return SGEMM_CUBE_INVALID_ARG;
+  if (rows == 0) return SGEMM_CUBE_OK;
+  const size_t e = elem_size(dtype);
+  if (!tokens || !table || !Y || table == Y || misplaced(8, tokens) || misplaced(e, table, Y)) return SGEMM_CUBE_INVALID_ARG;
+  DeviceGuard g(h->device);
+  if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;
+  sgc::LookupParams p;
+  memset(&p, 0, sizeof(p));
+  p.rows = rows; p.vocab = vocab; p.cols = cols;
+  p.tokens = reinterpret_cast<const long long*>(tokens);
+  p.table = table; p.ld = ld;
+  p.scale = scale;
+  p.Y = Y; p.ldy = ldy;
+  const bool vec = sgc::rows_take_vectors(table, ld, cols, e) && sgc::rows_take_vectors(Y, ldy, cols, e);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (dtype == SGEMM_CUBE_F32) return launch_lookup<float>(h, p, vec, st);
+  if (dtype == SGEMM_CUBE_F16) return launch_lookup<__half>(h, p, vec, st);
+  return launch_lookup<__nv_bfloat16>(h, p, vec, st);
+}
+
+int sgemm_cube_embedding_backward(sgemm_cube_handle h, int rows, int vocab, int cols, int dtype, const int64_t* tokens,
+                                  const void* dY, int64_t lddy, float scale, int accumulate, float* dtable, int64_t ldd,
+                                  void* stream) {
+  if (!h || bad_dims(rows, vocab, cols) || vocab < 1 || cols < 1 || lddy < cols || ldd < cols || bad_dtype(dtype) || bad_scale(scale))
+    return SGEMM_CUBE_INVALID_ARG;
+  if (accumulate != 0 && accumulate != 1) return SGEMM_CUBE_INVALID_ARG;
+  const size_t e = elem_size(dtype);
+  if (!dtable || misplaced(4, dtable)) return SGEMM_CUBE_INVALID_ARG;
+  if (rows > 0 && (!tokens || !dY || misplaced(8, tokens) || misplaced(e, dY))) return SGEMM_CUBE_INVALID_ARG;
+  DeviceGuard g(h->device);
+  if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (rows == 0) {                               // empty sums
+    if (accumulate) return SGEMM_CUBE_OK;
+    if (cudaMemset2DAsync(dtable, (size_t)ldd * 4, 0, (size_t)cols * 4, vocab, st) != cudaSuccess) {
+      cudaGetLastError();
+      return SGEMM_CUBE_CUDA_ERROR;
+    }
+    return SGEMM_CUBE_OK;
+  }
+  // Pieces of 32 sorted rows, longer ones where there would be more than 4096.
+  const int piece = rows <= 32 * 4096 ? 32 : (int)(((long long)rows + 4095) / 4096);
+  sgc::TableGradParams p;
+  memset(&p, 0, sizeof(p));
+  p.n = rows; p.vocab = vocab; p.cols = cols;
+  p.piece = piece; p.pieces = (rows + piece - 1) / piece;
+  const int columns = dtype == SGEMM_CUBE_F32 ? sgc::grad_columns<float>() : sgc::grad_columns<__half>();
+  p.tiles = (cols + columns - 1) / columns;
+  p.dY = dY; p.lddy = lddy;
+  p.scale = scale;
+  p.accumulate = accumulate;
+  p.dE = dtable; p.ldd = ldd;
+  p.ldp = (int64_t)round_up((size_t)cols, 4);
+  if ((long long)p.pieces * p.tiles > 0x3FFFFFFF) return SGEMM_CUBE_INVALID_ARG;
+  p.sum_blocks = (unsigned)((long long)p.pieces * p.tiles);
+  p.vec_out = sgc::rows_take_vectors(dtable, ldd, cols, 4);
+  const bool vec = sgc::rows_take_vectors(dY, lddy, cols, e);
+  sgc::SortParams s;
+  memset(&s, 0, sizeof(s));
+  s.n = rows; s.vocab = vocab;
+  for (s.passes = 1; s.passes < 4 && (vocab >> (s.passes * sgc::kSortBits)) != 0; ++s.passes) {}
+  s.tokens = reinterpret_cast<const long long*>(tokens);
+  s.words = h->err_dev + sgc::kGridWords + 2;
+  s.err = h->err_dev;
+  const int sort_tiles = (rows + sgc::kSortTile - 1) / sgc::kSortTile;
+  const int blocks = sort_tiles < h->sm_count ? sort_tiles : h->sm_count;
+  int rc;
+  for (int pass = 0; pass < 2; ++pass) {         // sizes first, then pointers
+    Carve c;
+    c.base = pass ? static_cast<uint8_t*>(h->sort_ws) : nullptr;
+    for (int i = 0; i < 2; ++i) {
+      s.key[i] = c.take<int>((size_t)rows);
+      s.pos[i] = c.take<int>((size_t)rows);
+    }
+    s.hist = c.take<int>((size_t)blocks * sgc::kSortBins);
+    s.met = c.take<unsigned char>((size_t)vocab);
+    if (p.pieces > 1) p.part = c.take<float>((size_t)2 * p.pieces * p.ldp);
+    if (!pass && (rc = grow(h, &h->sort_ws, &h->sort_ws_bytes, c.used, st))) return rc;
+  }
+  if (accumulate) s.met = nullptr;
+  if ((rc = launch_sort(h, s, blocks, st))) return rc;
+  p.key = s.key[s.passes & 1];
+  p.pos = s.pos[s.passes & 1];
+  p.met = s.met;
+  const unsigned clear_blocks = accumulate ? 0u : (unsigned)(vocab < h->sm_count * 16 ? vocab : h->sm_count * 16);
+  if (dtype == SGEMM_CUBE_F32) return launch_table_grad<float>(h, p, vec, clear_blocks, st);
+  if (dtype == SGEMM_CUBE_F16) return launch_table_grad<__half>(h, p, vec, clear_blocks, st);
+  return launch_table_grad<__nv_bfloat16>(h, p, vec, clear_blocks, st);
+}
+
+}  // extern "C"

@@ -44,6 +44,8 @@
 #include <type_traits>
 
 #include "linear_epilogue.cuh"
+#include "loss_epilogue.cuh"
+#include "polynomial_epilogue.cuh"
 #include "ptx_sm100.cuh"
 
 namespace sgc {
@@ -286,13 +288,27 @@ __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[64]) 
 // K the contracted one, M the other (row-major A is K, row-major B is M).
 // 8192 x 16384 x 4096 under the power cap: forward with gelu and z 2416 us, dX 2256, dW 2262 (1365 to 1460 TFLOP/s of FP16
 // products); 1024 x 4096 x 1024, one wave: 33 bare, 50 with everything.
-enum LinearForm { kFormProduct = 0, kFormKM, kFormKK, kFormMM };
+// A form is such a layout and one of the epilogues that work on a finished tile: the layer's; a step of a matrix polynomial
+// (polynomial_epilogue.cuh); the logits' part in a softmax cross entropy (loss_epilogue.cuh).
+enum ProductLayout { kFormProduct = 0, kFormKM, kFormKK, kFormMM };
+enum ProductEpilogue { kEpiLinear = 0, kEpiPolynomial, kEpiLoss };
+__host__ __device__ constexpr int layout_of(int form) { return form & 3; }
+__host__ __device__ constexpr int epilogue_of(int form) { return form >> 2; }
+constexpr int form_of(ProductLayout layout, ProductEpilogue epilogue) { return (int)epilogue * 4 + (int)layout; }
 
 struct TcLinearParams : TcGemmParams {
   LinearEpilogue ep;
 };
+struct TcPolynomialParams : TcGemmParams {
+  PolynomialEpilogue ep;
+};
+struct TcLossParams : TcGemmParams {
+  LossEpilogue ep;
+};
 template <int FORM>
-using TcParams = std::conditional_t<FORM == kFormProduct, TcGemmParams, TcLinearParams>;
+using TcParams = std::conditional_t<FORM == kFormProduct, TcGemmParams,
+                                    std::conditional_t<epilogue_of(FORM) == kEpiLinear, TcLinearParams,
+                                                       std::conditional_t<epilogue_of(FORM) == kEpiPolynomial, TcPolynomialParams, TcLossParams>>>;
 
 // Linear forms: warps 10-15 store.  The accumulate warps hold 128 sums a thread and have no registers left
 // for bias, activation and residual, and while they work on those the tensor core waits; so they put a
@@ -315,8 +331,9 @@ __global__ void __launch_bounds__(tc_threads<FUSED, FORM>(), 1)
 tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmA1,
                const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmB1,
                const TcParams<FORM> p) {
-  constexpr bool A_MN = FORM == kFormMM;                            // A's rows (M) contiguous
-  constexpr bool B_MN = FORM != kFormKK;                            // B's columns (N) contiguous
+  constexpr bool A_MN = layout_of(FORM) == kFormMM;                 // A's rows (M) contiguous
+  constexpr bool B_MN = layout_of(FORM) != kFormKK;                 // B's columns (N) contiguous
+  constexpr int EPI = epilogue_of(FORM);
   static_assert(FORM == kFormProduct || (NTERMS == 3 && !FUSED && !REORD), "linear forms");
   using Cfg = TcCfg<NTERMS, PAIR, FUSED>;
   constexpr int BK = Cfg::BK;
@@ -418,7 +435,10 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
   // Work units: 128-row tiles, or 256-row pair tiles of which this CTA takes row block `cta_rank`.
   const int num_m = PAIR ? (p.M + 2 * kBM - 1) / (2 * kBM) : (p.M + kBM - 1) / kBM;
   const int num_n = (p.N + kBN - 1) / kBN;
-  const int num_tiles = num_m * num_n;
+  int num_tiles = num_m * num_n;
+  if constexpr (EPI == kEpiPolynomial) {
+    if (p.ep.symmetric) num_tiles = (int)lower_tiles(num_m, PAIR);
+  }
   const int ksplit = FUSED ? 1 : p.ksplit;
   // Linear forms with split-K: a cluster of `ksplit` blocks works on one tile, block `slice_rank` on its slice.
   const bool in_cluster = FORM != kFormProduct && ksplit > 1;
@@ -427,7 +447,10 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
   const int first_tile = (int)blockIdx.x / blocks_per_tile;
   const int tile_stride = (int)gridDim.x / blocks_per_tile;
   auto tile_rc = [&](int tile, int& tm, int& tn) {     // tm in units of 128 rows, tn of 256 columns
-    tile_coords(tile, num_m, num_n, tm, tn, PAIR ? SGC_PAIR_GROUP : 16);
+    bool lower = false;
+    if constexpr (EPI == kEpiPolynomial) lower = p.ep.symmetric != 0;
+    if (lower) lower_tile_coords(tile, PAIR, tm, tn);
+    else tile_coords(tile, num_m, num_n, tm, tn, PAIR ? SGC_PAIR_GROUP : 16);
     if (PAIR) tm = tm * 2 + (int)cta_rank;
   };
   const int num_kb = (p.K + BK - 1) / BK;                      // pipeline stages per tile
@@ -448,7 +471,11 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
     if constexpr (FORM != kFormProduct) {
       float* tile = p.ep.tiles + scratch_tile(unit, t) * kTileFloats;
       const int first = slice_rank * workers + w, step = ksplit * workers;
-      if (p.ep.vec)
+      if constexpr (EPI == kEpiPolynomial)
+        polynomial_store(p.ep, p.M, p.N, tile, ksplit, kTileFloats, tm * kBM, tn * kBN, first, step, lane);
+      else if constexpr (EPI == kEpiLoss)
+        loss_store(p.ep, p.M, p.N, tile, ksplit, kTileFloats, tm * kBM, tn * kBN, first, step, lane);
+      else if (p.ep.vec)
         linear_store_blocks(p.ep, p.D, p.ldd, p.M, p.N, tile, ksplit, kTileFloats, tm * kBM, tn * kBN, first, step, lane);
       else
         linear_store_rows(p.ep, p.D, p.ldd, p.M, p.N, tile, ksplit, kTileFloats, tm * kBM, tn * kBN, first, step, lane);
@@ -706,7 +733,9 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
         if constexpr (FORM == kFormProduct) {
           store_tile(p.D, p.ldd, vec_ok, (NTERMS == 1) ? p.accumulate : 0);
         } else {
-          const bool direct = p.ep.tiles == nullptr;
+          const bool direct = EPI == kEpiLinear && p.ep.tiles == nullptr;
+          bool rows_first = false;                 // along rows to the scratch of matrices that take no vectors
+          if constexpr (EPI == kEpiLinear) rows_first = !p.ep.vec;
           const int t = (int)(tiles_done & 1);
           float* tile = p.D;
           if (!direct) {
@@ -717,13 +746,15 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__
             }
             tile = p.ep.tiles + (scratch_tile(unit, t) + slice_rank) * kTileFloats;
           }
-          if (direct || !p.ep.vec) {
+          if (direct || rows_first) {
             // Straight to Y, with the way back; or along rows to the scratch of unaligned matrices, whose origin
             // is set back by the row and column that store_tile addresses.
-            if (direct) {
-              const PowerBack back = power_back(p.ep.exp_a, p.ep.exp_b);
+            if constexpr (EPI == kEpiLinear) {
+              if (direct) {
+                const PowerBack back = power_back(p.ep.exp_a, p.ep.exp_b);
 #pragma unroll
-              for (int j = 0; j < 128; ++j) S[j] = back(S[j]);
+                for (int j = 0; j < 128; ++j) S[j] = back(S[j]);
+              }
             }
             store_tile(direct ? tile : tile - ((long long)tm * kBM * kBN + tn * kBN), direct ? p.ldd : (long long)kBN,
                        direct ? vec_ok : true, 0);

@@ -3,33 +3,25 @@
 #include "ctx.cuh"
 #include "gemm_tc.cuh"
 #include "linear_kernels.cuh"
+#include "product_host.cuh"
 #include "short_batch.cuh"
 
 namespace {
 
+using sgc::blocks_for;
+using sgc::Carve;
+using sgc::check_operand;
+using sgc::is_packed;
+using sgc::kExpWords;
+using sgc::kGridWords;
+using sgc::kRangeWords;
+using sgc::launch_pack;
+using sgc::launched;
+using sgc::linear_config;
+using sgc::linear_product_any;
+using sgc::Packed;
 using sgc::PackJob;
-
-// Words of the handle's device scratch that the packing kernels use: running maxima and block counts of up to two jobs,
-// exponents of operands that a call packs itself, and the words in which the blocks of the one-launch kernels meet.
-// Every call leaves the first and the last four zero; after a kernel that gave up sgemm_cube_check does.
-constexpr int kRangeWords = 20, kExpWords = 24, kGridWords = 28;
-constexpr int kMaxSlices = 8;          // blocks of a portable cluster
-
-struct Packed {
-  const uint16_t* hi;
-  const uint16_t* lo;
-  int64_t ld;
-  const int* exp;
-};
-
-int blocks_for(const sgemm_cube_ctx* h, long long items) {
-  const long long b = (items + 255) / 256, cap = (long long)h->sm_count * 16;
-  return (int)(b < 1 ? 1 : (b < cap ? b : cap));
-}
-int launched(sgemm_cube_ctx* h) {
-  h->launches++;
-  return cudaGetLastError() == cudaSuccess ? SGEMM_CUBE_OK : SGEMM_CUBE_CUDA_ERROR;
-}
+using sgc::words_of;
 
 bool takes_vec4(const void* p, int64_t ld, int cols) { return aligned16(p) && ld % 4 == 0 && cols % 4 == 0; }
 
@@ -74,8 +66,10 @@ int launch_cooperative(sgemm_cube_ctx* h, void (*kernel)(P...), dim3 grid, cudaS
   return SGEMM_CUBE_OK;
 }
 
+}  // namespace
+
 // Range and split of one job, or of two in the same launches (the blocks in proportion to the elements).
-int launch_pack(sgemm_cube_ctx* h, const PackJob* jobs, int n, cudaStream_t st) {
+int sgc::launch_pack(sgemm_cube_ctx* h, const PackJob* jobs, int n, cudaStream_t st) {
   const long long ea = elements(jobs[0]), eb = n == 2 ? elements(jobs[1]) : 0;
   const PackJob& b = jobs[n == 2 ? 1 : 0];
   // one cooperative launch where the blocks that are resident at once hold everything
@@ -113,41 +107,8 @@ int launch_pack(sgemm_cube_ctx* h, const PackJob* jobs, int n, cudaStream_t st) 
   return SGEMM_CUBE_OK;
 }
 
-cudaLaunchConfig_t linear_config(size_t smem, unsigned cluster, cudaLaunchAttribute* attr, cudaStream_t st) {
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.blockDim = dim3(sgc::kLinearThreads, 1, 1);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  if (cluster > 1) {
-    attr->id = cudaLaunchAttributeClusterDimension;
-    attr->val.clusterDim.x = cluster; attr->val.clusterDim.y = 1; attr->val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-  }
-  return cfg;
-}
-// Kernel attributes, and how many clusters of pairs and of 2 to 8 split-K blocks are resident at once (the fewest
-// over the forms).
-template <int FORM, bool PAIR>
-int linear_attrs(sgemm_cube_ctx* h) {
-  auto kernel = sgc::tc_gemm_kernel<3, false, PAIR, false, FORM>;
-  constexpr size_t smem = sgc::TcCfg<3, PAIR, false>::SMEM_BYTES;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
-    cudaGetLastError();
-    return SGEMM_CUBE_CUDA_ERROR;
-  }
-  for (int c = 2; c <= (PAIR ? 2 : kMaxSlices); ++c) {
-    cudaLaunchAttribute a;
-    cudaLaunchConfig_t cfg = linear_config(smem, (unsigned)c, &a, nullptr);
-    cfg.gridDim = dim3((unsigned)(c * h->sm_count), 1, 1);
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
-    int& least = PAIR ? h->linear_pair_clusters : h->linear_slice_clusters[c];
-    if (n < least) least = n;
-  }
-  return SGEMM_CUBE_OK;
-}
+namespace {
+
 template <int NT, bool W_F32>
 int short_batch_attrs() {
   constexpr int smem = (int)sgc::ShortBatchCfg<NT, W_F32>::SMEM_BYTES;
@@ -160,130 +121,45 @@ int short_batch_attrs() {
   return SGEMM_CUBE_OK;
 }
 int linear_setup(sgemm_cube_ctx* h) {
-  if (h->linear_ready) return SGEMM_CUBE_OK;
-  h->linear_pair_clusters = h->sm_count;
-  for (int& n : h->linear_slice_clusters) n = h->sm_count;
+  sgc::ResidentClusters& k = h->linear_clusters;
+  if (k.ready) return SGEMM_CUBE_OK;
   int rc;
-  if ((rc = linear_attrs<sgc::kFormKM, false>(h)) || (rc = linear_attrs<sgc::kFormKK, false>(h)) ||
-      (rc = linear_attrs<sgc::kFormMM, false>(h)) || (rc = linear_attrs<sgc::kFormKM, true>(h)) ||
-      (rc = linear_attrs<sgc::kFormKK, true>(h)) || (rc = linear_attrs<sgc::kFormMM, true>(h)))
-    return rc;
   if ((rc = short_batch_attrs<16, false>()) || (rc = short_batch_attrs<32, false>()) || (rc = short_batch_attrs<64, false>()) ||
       (rc = short_batch_attrs<16, true>()) || (rc = short_batch_attrs<32, true>()) || (rc = short_batch_attrs<64, true>()))
     return rc;
-  h->linear_ready = true;
-  return SGEMM_CUBE_OK;
-}
-
-template <int FORM, bool PAIR>
-int launch_linear_kernel(sgemm_cube_ctx* h, const Packed& A, const Packed& B, const sgc::TcLinearParams& p,
-                         cudaStream_t st) {
-  using Cfg = sgc::TcCfg<3, PAIR, false>;
-  constexpr bool a_mn = FORM == sgc::kFormMM, b_mn = FORM != sgc::kFormKK;
-  CUtensorMap tm[4];
-  for (int w = 0; w < 2; ++w) {
-    const uint16_t* a = w ? A.lo : A.hi;
-    const uint16_t* b = w ? B.lo : B.hi;
-    const CUtensorMapDataType t = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    const CUtensorMapSwizzle z = CU_TENSOR_MAP_SWIZZLE_128B;
-    int rc = a_mn ? make_map(h, &tm[w], t, 2, a, p.M, p.K, A.ld, 64, Cfg::BK, z)
-                  : make_map(h, &tm[w], t, 2, a, p.K, p.M, A.ld, Cfg::BK, sgc::kBM, z);
-    if (rc) return rc;
-    rc = b_mn ? make_map(h, &tm[2 + w], t, 2, b, p.N, p.K, B.ld, 64, Cfg::BK, z)
-              : make_map(h, &tm[2 + w], t, 2, b, p.K, p.N, B.ld, Cfg::BK, Cfg::BN_CTA, z);
-    if (rc) return rc;
-  }
-  cudaLaunchAttribute attr;
-  const unsigned cluster = PAIR ? 2u : (unsigned)p.ksplit;
-  cudaLaunchConfig_t cfg = linear_config(Cfg::SMEM_BYTES, cluster, &attr, st);
-  const long long tiles = (long long)((p.M + (PAIR ? 2 : 1) * sgc::kBM - 1) / ((PAIR ? 2 : 1) * sgc::kBM)) *
-                          ((p.N + sgc::kBN - 1) / sgc::kBN);
-  const int cap = PAIR ? h->linear_pair_clusters : (cluster > 1 ? h->linear_slice_clusters[cluster] : h->sm_count);
-  cfg.gridDim = dim3(cluster * (unsigned)(tiles < cap ? tiles : cap), 1, 1);
-  h->launches++;
-  if (cudaLaunchKernelEx(&cfg, sgc::tc_gemm_kernel<3, false, PAIR, false, FORM>, tm[0], tm[1], tm[2], tm[3], p) !=
-      cudaSuccess) {
-    cudaGetLastError();
-    return SGEMM_CUBE_CUDA_ERROR;
-  }
-  return SGEMM_CUBE_OK;
-}
-
-// How many k slices, when the tiles leave half of the SMs idle: the clusters that are resident at once go
-// through the tiles in turns, and a turn takes as long as its slice; the fewest slices among those that take the
-// least time.  A slice is at least two k-blocks.
-int linear_slices(const sgemm_cube_ctx* h, long long tiles, int K, int chunk_k) {
-  if (!h->split_k) return 1;
-  if (tiles * 2 > h->sm_count) return 1;
-  const int chunks = (K + chunk_k - 1) / chunk_k;
-  int best = 1;
-  long long best_time = chunks;
-  for (int s = 2; s <= kMaxSlices && 2 * s <= chunks; ++s) {
-    const int per = (chunks + s - 1) / s, clusters = h->linear_slice_clusters[s];
-    if (clusters < 1 || (chunks + per - 1) / per != s) continue;      // the last slice would be empty
-    const long long time = (tiles + clusters - 1) / clusters * per;
-    if (time < best_time) { best_time = time; best = s; }
-  }
-  return best;
+  return sgc::product_setup<sgc::kFormKM, sgc::kFormKK, sgc::kFormMM>(h, k);
 }
 
 // C (M x N) = epilogue of A B on packed operands, termwise.
 template <int FORM>
 int linear_product(sgemm_cube_ctx* h, int M, int N, int K, const Packed& A, const Packed& B, float* Y, int64_t ldy,
                    sgc::LinearEpilogue ep, cudaStream_t st) {
-  int rc = linear_setup(h);
+  const int rc = linear_setup(h);
   if (rc) return rc;
   ep.exp_a = A.exp;
   ep.exp_b = B.exp;
   ep.vec = aligned16(Y) && ldy % 4 == 0 && (!ep.Z || (aligned16(ep.Z) && ep.ldz % 4 == 0)) &&
            (!ep.R || (aligned16(ep.R) && ep.ldr % 4 == 0));
-  constexpr int BK = sgc::TcCfg<3, false, false>::BK;
   sgc::TcLinearParams p;
   memset(&p, 0, sizeof(p));
   p.M = M; p.N = N; p.K = K;
   p.D = Y; p.ldd = ldy;
-  p.order = SGEMM_CUBE_TERMWISE;
-  p.kchunk_blocks = h->kblock_termwise / BK;
-  p.inv_scale = sgc::kPackInvScale;
-  p.scale = 1.f;
-  p.err = h->err_dev;
-  p.ksplit = 1;
   p.ep = ep;
-  const size_t tiles = (size_t)((M + sgc::kBM - 1) / sgc::kBM) * ((N + sgc::kBN - 1) / sgc::kBN);
-  const int slices = linear_slices(h, (long long)tiles, K, p.kchunk_blocks * BK);
-  if (slices > 1) {
-    rc = grow(h, &h->part_ws, &h->part_ws_bytes, tiles * slices * sgc::kTileFloats * 4, st);
-    if (rc) return rc;
-    const int chunks = (K + p.kchunk_blocks * BK - 1) / (p.kchunk_blocks * BK);
-    p.ksplit = slices;
-    p.kslice_blocks = (chunks + slices - 1) / slices * p.kchunk_blocks;
-    p.ep.tiles = static_cast<float*>(h->part_ws);
-    rc = launch_linear_kernel<FORM, false>(h, A, B, p, st);
-    if (rc != SGEMM_CUBE_CUDA_ERROR) return rc;
-    p.ksplit = 1;                                        // clusters that cannot be scheduled: whole k
-    p.kslice_blocks = 0;
-    p.ep.tiles = nullptr;
-  }
   // Nothing but the way back to do: the accumulate warps store to Y themselves.
-  if (ep.bias || ep.R || ep.Z || ep.act != SGEMM_CUBE_ACT_NONE) {
-    rc = grow(h, &h->tile_ws, &h->tile_ws_bytes, (size_t)h->sm_count * 2 * sgc::kTileFloats * 4, st);
-    if (rc) return rc;
-    p.ep.tiles = static_cast<float*>(h->tile_ws);
-  }
-  const bool pair = (h->cta_pair == 2 ? M > sgc::kBM : h->cta_pair == 1) && h->linear_pair_clusters > 0;
-  if (pair) {
-    rc = launch_linear_kernel<FORM, true>(h, A, B, p, st);
-    if (rc != SGEMM_CUBE_CUDA_ERROR || h->cta_pair != 2) return rc;
-  }
-  return launch_linear_kernel<FORM, false>(h, A, B, p, st);
+  const bool scratch = ep.bias || ep.R || ep.Z || ep.act != SGEMM_CUBE_ACT_NONE;
+  return sgc::run_product<FORM>(h, h->linear_clusters, A, B, p, scratch, st);
 }
 
-int linear_product_any(int form, sgemm_cube_ctx* h, int M, int N, int K, const Packed& A, const Packed& B, float* Y,
-                       int64_t ldy, const sgc::LinearEpilogue& ep, cudaStream_t st) {
+}  // namespace
+
+int sgc::linear_product_any(int form, sgemm_cube_ctx* h, int M, int N, int K, const Packed& A, const Packed& B, float* Y,
+                            int64_t ldy, const LinearEpilogue& ep, cudaStream_t st) {
   if (form == sgc::kFormKM) return linear_product<sgc::kFormKM>(h, M, N, K, A, B, Y, ldy, ep, st);
   if (form == sgc::kFormKK) return linear_product<sgc::kFormKK>(h, M, N, K, A, B, Y, ldy, ep, st);
   return linear_product<sgc::kFormMM>(h, M, N, K, A, B, Y, ldy, ep, st);
 }
+
+namespace {
 
 // ------------------------------------------------------------------------------------------ few rows
 // Which calls the FMA kernels take: their arithmetic grows with the rows, the tensor cores' costs a longer start
@@ -359,7 +235,7 @@ constexpr int kShortRows = 64, kShortMoreRows = 256, kShortMoreBlocks = 32;
 bool use_short_batch(const sgemm_cube_ctx* h, int M, int N, int K, int* slices) {
   const int nt = M <= 16 ? 16 : (M <= 32 ? 32 : 64);
   const long long tiles = (long long)((N + sgc::kShortN - 1) / sgc::kShortN) * ((M + nt - 1) / nt);
-  *slices = linear_slices(h, tiles, K, 2 * sgc::kShortK);
+  *slices = sgc::product_slices(h, h->linear_clusters, tiles, K, 2 * sgc::kShortK);
   if (M <= kShortRows) return true;
   const int blocks = (K + sgc::kShortK - 1) / sgc::kShortK;
   return M <= kShortMoreRows && tiles <= h->sm_count && (blocks + *slices - 1) / *slices <= kShortMoreBlocks;
@@ -404,9 +280,9 @@ int launch_short(sgemm_cube_ctx* h, const sgemm_cube_operand& W, const sgc::Shor
 }
 
 // ------------------------------------------------------------------------------------------ arguments
-bool is_packed(const sgemm_cube_operand* o) { return o->f32_dev == nullptr && o->hi_dev != nullptr; }
+}  // namespace
 
-int check_operand(const sgemm_cube_operand* o, int rows, int cols) {
+int sgc::check_operand(const sgemm_cube_operand* o, int rows, int cols) {
   if (!o) return SGEMM_CUBE_INVALID_ARG;
   if (rows == 0 || cols == 0) return SGEMM_CUBE_OK;              // an empty operand is not looked at
   if (o->f32_dev) return o->ld >= cols && !misplaced(4, o->f32_dev) ? SGEMM_CUBE_OK : SGEMM_CUBE_INVALID_ARG;
@@ -414,23 +290,15 @@ int check_operand(const sgemm_cube_operand* o, int rows, int cols) {
   if (!aligned16(o->hi_dev) || !aligned16(o->lo_dev) || o->ld16 % 8) return SGEMM_CUBE_MISALIGNED;
   return SGEMM_CUBE_OK;
 }
+namespace {
+
 bool bad_layout(int layout) { return layout != SGEMM_CUBE_WEIGHT_KN && layout != SGEMM_CUBE_WEIGHT_NK; }
 bool bad_act(int act) { return act < SGEMM_CUBE_ACT_NONE || act > SGEMM_CUBE_ACT_SILU; }
 
-// Pieces of the handle's workspace, in the order they are asked for.
-struct Carve {
-  size_t used = 0;
-  uint8_t* base = nullptr;
-  template <typename T>
-  T* take(size_t n) {
-    T* p = reinterpret_cast<T*>(base + used);
-    used += round_up(n * sizeof(T), 256);
-    return p;
-  }
-};
+}  // namespace
 
 // The words of an operand: its own, or (FP32) room in the workspace and a job that fills it.
-Packed words_of(const sgemm_cube_operand* o, int rows, int cols, Carve& c, int* exp, PackJob* jobs, int* n_jobs) {
+sgc::Packed sgc::words_of(const sgemm_cube_operand* o, int rows, int cols, Carve& c, int* exp, PackJob* jobs, int* n_jobs) {
   if (is_packed(o)) return Packed{o->hi_dev, o->lo_dev, o->ld16, o->exp_dev};
   const int64_t ld = (int64_t)round_up((size_t)cols, 8);
   uint16_t* hi = c.take<uint16_t>((size_t)rows * ld);
@@ -438,6 +306,13 @@ Packed words_of(const sgemm_cube_operand* o, int rows, int cols, Carve& c, int* 
   jobs[(*n_jobs)++] = pack_job(rows, cols, o->f32_dev, o->ld, hi, lo, ld, exp);
   return Packed{hi, lo, ld, exp};
 }
+
+bool sgc::linear_takes_few(sgemm_cube_ctx* h, int M, int N, int K, bool packed, bool nk) {
+  int slices;
+  return use_few_rows(M, N, K, packed, nk) || (linear_setup(h) == SGEMM_CUBE_OK && use_short_batch(h, M, N, K, &slices));
+}
+
+namespace {
 
 template <int ACT>
 int launch_dz(sgemm_cube_ctx* h, const PackJob& j, bool split, float* col_part, int chunks, int rows_per_chunk,

@@ -23,6 +23,7 @@ enum : unsigned int {
   kErrTileEmptyWait = 0x109,
   kErrTileFullWait = 0x10A,
   kErrPackWait = 0x10B,
+  kErrSortWait = 0x10C,
   kErrProbeWait = 0x1F0,
 };
 
