@@ -1,17 +1,20 @@
 // A matrix brought near the closest one with orthonormal rows (columns, where it has more rows), by Newton-Schulz products
 // (contract: include/sgemm_cube.h):
 //
-//   X = G / (|G|_F + eps);   steps times:  A = X X^T,  P = a + b A + c A A,  X <- P X;   O = scale X + beta R
+//   X = G / (|G|_F + eps);   steps times:  A = X X^T,  B = b A + c A A,  X <- a X + B X;   O = scale X + beta R
 //
-// (rows <= columns; else A = X^T X and X <- X P).  X, A and P live as FP16 words from the first pass to the last, written by the
-// epilogues of the products that make them (polynomial_epilogue.cuh): no pass of its own packs anything.  Their exponents
+// (rows <= columns; else A = X^T X and X <- a X + X B).  X, A and B live as FP16 words from the first pass to the last, written by
+// the epilogues of the products that make them (polynomial_epilogue.cuh): no pass of its own packs anything.  Their exponents
 // are known beforehand: the singular values of X lie in [0, s] with s = 1 at the start and the polynomial's largest value
 // on [0, s] after a step, and no entry of a matrix is larger than its largest singular value.
-// A and P are symmetric: half of their tiles are formed.
+// A and B are symmetric: half of their tiles are formed.  (a X is added in FP32: as a diagonal of B it went through the tensor
+// core's truncating sums, with 128 x 384 and five steps 2.8e-6 off where FP32 products are 1.7e-6.)
+// Small matrices take all of it in one launch (polynomial_chain.cuh).
 #include <cmath>
 
 #include "ctx.cuh"
 #include "elements.cuh"
+#include "polynomial_chain.cuh"
 #include "product_host.cuh"
 
 namespace sgc {
@@ -52,7 +55,6 @@ template <typename T>
 __global__ void __launch_bounds__(256)
 normalise_kernel(int rows, int cols, const T* __restrict__ G, long long ldg, int vec, const double* __restrict__ sums, int n_sums,
                  float eps, float pre, uint16_t* __restrict__ hi, uint16_t* __restrict__ lo, long long ldw) {
-  constexpr int V = Elem<T>::kVec;
   double s = 0.0;
   for (int i = threadIdx.x; i < n_sums; i += 256) s += sums[i];
   for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
@@ -61,37 +63,14 @@ normalise_kernel(int rows, int cols, const T* __restrict__ G, long long ldg, int
   __syncthreads();
   s = warp_sum[0];
   for (int w = 1; w < 8; ++w) s += warp_sum[w];
-  const double norm = sqrt(s) + (double)eps;
-  // (a matrix of zeros with eps = 0 stays one; a norm that is not finite makes every entry NaN)
-  const double scale = norm == 0.0 ? 0.0 : (isfinite(norm) ? 1.0 / norm : (double)NAN);
-  // two FP32 factors: 1 / norm can leave the FP32 range while the entries times it do not
-  const int e = scale != 0.0 && isfinite(scale) ? max(-126, min(126, ilogb(scale) / 2)) : 0;
-  const float f0 = pow2f(e), f1 = (float)(scale * (double)pow2f(-e)) * pre;
+  float f0, f1;
+  norm_factors(s, eps, pre, f0, f1);
   const int per_row = (cols + 7) >> 3;
   const long long total = (long long)rows * per_row, stride = (long long)gridDim.x * 256;
   for (long long it = (long long)blockIdx.x * 256 + threadIdx.x; it < total; it += stride) {
     const long long r = total < (1ll << 31) ? (long long)((uint32_t)it / (uint32_t)per_row) : it / per_row;
     const int c = (int)(it - r * per_row) << 3;
-    const T* at = G + r * ldg + c;
-    float v[8];
-    if (vec && c + 8 <= cols) {
-#pragma unroll
-      for (int i = 0; i < 8 / V; ++i) {
-        float x[V];
-        Elem<T>::unpack(*reinterpret_cast<const uint4*>(at + i * V), x);
-#pragma unroll
-        for (int q = 0; q < V; ++q) v[i * V + q] = x[q];
-      }
-    } else {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = c + q < cols ? Elem<T>::get(at[q]) : 0.f;
-    }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] *= f0;
-    uint4 h, l;
-    pack_words(v, f1, h, l);
-    *reinterpret_cast<uint4*>(hi + r * ldw + c) = h;
-    *reinterpret_cast<uint4*>(lo + r * ldw + c) = l;
+    normalise_eight(G + r * ldg + c, vec != 0, cols - c, f0, f1, hi + r * ldw + c, lo + r * ldw + c);
   }
 }
 
@@ -141,6 +120,7 @@ double largest_on(double s, double k0, double k1, double k2, int odd) {
 }
 // p with 2^p x below the largest FP16 number for |x| <= bound, a sixteenth of it left for rounding.
 int word_exponent(double bound) {
+  if (!(bound > 0.0)) return 0;                  // a matrix of zeros
   return 15 - (int)std::floor(std::log2(bound * 1.0625));
 }
 
@@ -167,7 +147,186 @@ int polynomial_product(sgemm_cube_ctx* h, int M, int N, int K, const Words& A, c
   return sgc::run_product<FORM>(h, h->polynomial_clusters, A.packed(), B.packed(), p, true, st);
 }
 
-constexpr int kMostSteps = 64;
+struct OrthogonalizeCall {
+  int rows, cols, dtype;
+  const void* G;
+  int64_t ldg;
+  int steps;
+  float eps;
+  const float* R;
+  int64_t ldr;
+  float scale, beta;
+  float* O;
+  int64_t ldo;
+  bool tall;
+  int n, m;                  // the shorter and the longer side
+  float pre;                 // 2^p of the first X
+  const sgc::ChainStep* step;
+  cudaStream_t st;
+  int vec_out() const { return aligned16(O) && ldo % 4 == 0 && (!R || (aligned16(R) && ldr % 4 == 0)); }
+};
+
+// One launch a product.
+int run_products(sgemm_cube_ctx* h, const OrthogonalizeCall& c) {
+  int rc = sgc::product_setup<sgc::kFormPolyKM, sgc::kFormPolyKK, sgc::kFormPolyMM>(h, h->polynomial_clusters);
+  if (rc) return rc;
+  const int blocks = sgc::blocks_for(h, (long long)c.rows * c.cols / 16 + 1);
+  Words X[2], A, B;
+  double* sums = nullptr;
+  for (int pass = 0; pass < 2; ++pass) {         // sizes first, then pointers
+    Carve w;
+    w.base = pass ? static_cast<uint8_t*>(h->poly_ws) : nullptr;
+    sums = w.take<double>((size_t)blocks);
+    X[0] = take_words(w, c.rows, c.cols);
+    X[1] = c.steps > 1 ? take_words(w, c.rows, c.cols) : X[0];
+    A = take_words(w, c.n, c.n);
+    B = take_words(w, c.n, c.n);
+    if (!pass && (rc = grow(h, &h->poly_ws, &h->poly_ws_bytes, w.used, c.st))) return rc;
+  }
+  rc = c.dtype == SGEMM_CUBE_F32   ? normalise<float>(h, c.rows, c.cols, c.G, c.ldg, sums, blocks, c.eps, c.pre, X[0], c.st)
+       : c.dtype == SGEMM_CUBE_F16 ? normalise<__half>(h, c.rows, c.cols, c.G, c.ldg, sums, blocks, c.eps, c.pre, X[0], c.st)
+                                   : normalise<__nv_bfloat16>(h, c.rows, c.cols, c.G, c.ldg, sums, blocks, c.eps, c.pre, X[0], c.st);
+  if (rc) return rc;
+  for (int i = 0; i < c.steps; ++i) {
+    const Words &x = X[i & 1], &next = X[(i + 1) & 1];
+    const sgc::ChainStep& f = c.step[i];
+    sgc::PolynomialEpilogue ep;
+    memset(&ep, 0, sizeof(ep));
+    ep.alpha = f.gram_alpha;
+    ep.hi = A.hi; ep.lo = A.lo; ep.ldw = A.ld;
+    ep.pre = f.gram_pre;
+    ep.symmetric = 1;
+    rc = c.tall ? polynomial_product<sgc::kFormPolyMM>(h, c.n, c.n, c.m, x, x, ep, c.st)
+                : polynomial_product<sgc::kFormPolyKK>(h, c.n, c.n, c.m, x, x, ep, c.st);
+    if (rc) return rc;
+    ep.alpha = f.square_alpha;
+    ep.r_hi = A.hi; ep.r_lo = A.lo; ep.ldr = A.ld;
+    ep.beta = f.square_beta;
+    ep.hi = B.hi; ep.lo = B.lo; ep.ldw = B.ld;
+    ep.pre = f.square_pre;
+    if ((rc = polynomial_product<sgc::kFormPolyKK>(h, c.n, c.n, c.n, A, A, ep, c.st))) return rc;
+    memset(&ep, 0, sizeof(ep));
+    ep.alpha = f.update_alpha;
+    ep.r_hi = x.hi; ep.r_lo = x.lo; ep.ldr = x.ld;
+    ep.beta = f.update_beta;
+    if (i + 1 < c.steps) {
+      ep.hi = next.hi; ep.lo = next.lo; ep.ldw = next.ld;
+      ep.pre = f.update_pre;
+    } else {
+      ep.Y = c.O; ep.ldy = c.ldo;
+      ep.kept = c.R; ep.ldk = c.ldr; ep.scale = c.scale; ep.keep = c.beta;
+      ep.vec = c.vec_out();
+    }
+    rc = c.tall ? polynomial_product<sgc::kFormPolyKK>(h, c.rows, c.cols, c.cols, x, B, ep, c.st)
+                : polynomial_product<sgc::kFormPolyKM>(h, c.rows, c.cols, c.rows, B, x, ep, c.st);
+    if (rc) return rc;
+  }
+  return SGEMM_CUBE_OK;
+}
+
+// Which matrices take the one launch: its tiles of 128 x 128 have no next tile's products to hide their epilogue behind, so it
+// loses to the larger kernel where that one is busy for long.
+bool takes_chain(int n, int m) { return n <= 1536 && (long long)n * m <= (1ll << 22); }
+
+// Slices of a product's tiles: the fewest clocks of about 1100 for a stage and 2500 for the meeting of a tile's blocks.
+sgc::ChainSplit chain_split(long long tiles, int K, int blocks) {
+  const int stages = (K + sgc::kChainBK - 1) / sgc::kChainBK;
+  sgc::ChainSplit best{(int)tiles, 1, stages};
+  long long least = (tiles + blocks - 1) / blocks * stages * 1100;
+  for (int s = 2; s <= sgc::kChainMostSlices && s <= stages && tiles * s <= blocks; ++s) {
+    const int per = (stages + s - 1) / s;
+    if ((stages + per - 1) / per != s) continue;                     // the last slice would be empty
+    const long long clocks = per * 1100ll + 2500 + 60 * s;
+    if (clocks < least) { least = clocks; best = sgc::ChainSplit{(int)tiles, s, per}; }
+  }
+  return best;
+}
+
+// All products in one cooperative launch; *done stays false where that cannot be had.
+template <typename T>
+int run_chain(sgemm_cube_ctx* h, const OrthogonalizeCall& c, bool* done) {
+  auto kernel = sgc::polynomial_chain_kernel<T>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sgc::kChainSmem) != cudaSuccess) {
+    cudaGetLastError();
+    return SGEMM_CUBE_CUDA_ERROR;
+  }
+  const long long side = (c.n + sgc::kChainTile - 1) / sgc::kChainTile, lower = side * (side + 1) / 2;
+  const long long all = side * ((c.m + sgc::kChainTile - 1) / sgc::kChainTile);
+  sgc::ChainParams p;
+  memset(&p, 0, sizeof(p));
+  p.gram = chain_split(lower, c.m, h->sm_count);
+  p.square = chain_split(lower, c.n, h->sm_count);
+  p.update = chain_split(all, c.n, h->sm_count);
+  // blocks: as many as the largest product has work for, and enough to read G
+  long long units = 1;
+  size_t scratch = 0;
+  for (const sgc::ChainSplit* s : {&p.gram, &p.square, &p.update}) {
+    const long long u = (long long)s->tiles * s->slices;
+    if (u > units) units = u;
+    if (s->slices > 1 && (size_t)u > scratch) scratch = (size_t)u;
+  }
+  const long long reading = (long long)c.rows * c.cols / (sgc::kChainThreads * 8) + 1;
+  if (reading > units) units = reading;
+  const int blocks = (int)(units < h->sm_count ? units : h->sm_count);
+  Words X[2], A, B;
+  p.count_stride = (int)(all > lower ? all : lower);
+  int rc;
+  for (int pass = 0; pass < 2; ++pass) {         // sizes first, then pointers
+    Carve w;
+    w.base = pass ? static_cast<uint8_t*>(h->poly_ws) : nullptr;
+    p.sums = w.take<double>((size_t)blocks);
+    p.counts = w.take<unsigned int>((size_t)3 * p.count_stride);
+    X[0] = take_words(w, c.rows, c.cols);
+    X[1] = c.steps > 1 ? take_words(w, c.rows, c.cols) : X[0];
+    A = take_words(w, c.n, c.n);
+    B = take_words(w, c.n, c.n);
+    p.scratch = w.take<float>(scratch * sgc::kChainTileFloats);
+    if (!pass && (rc = grow(h, &h->poly_ws, &h->poly_ws_bytes, w.used, c.st))) return rc;
+  }
+  sgc::ChainMaps maps;
+  const auto map = [&](CUtensorMap* to, const Words& w, int rows, int cols) {
+    const uint16_t* words[2] = {w.hi, w.lo};
+    for (int i = 0; i < 2; ++i) {
+      const int e = make_map(h, to + i, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, words[i], cols, rows, w.ld, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+      if (e) return e;
+    }
+    return (int)SGEMM_CUBE_OK;
+  };
+  if ((rc = map(maps.x[0], X[0], c.rows, c.cols)) || (rc = map(maps.x[1], X[1], c.rows, c.cols)) || (rc = map(maps.a, A, c.n, c.n)) ||
+      (rc = map(maps.b, B, c.n, c.n)))
+    return rc;
+  p.rows = c.rows; p.cols = c.cols; p.tall = c.tall; p.steps = c.steps;
+  p.G = c.G; p.ldg = c.ldg; p.vec = sgc::rows_take_vectors(c.G, c.ldg, c.cols, sizeof(T));
+  p.eps = c.eps; p.pre = c.pre;
+  for (int i = 0; i < 2; ++i) { p.x_hi[i] = X[i].hi; p.x_lo[i] = X[i].lo; }
+  p.a_hi = A.hi; p.a_lo = A.lo; p.b_hi = B.hi; p.b_lo = B.lo;
+  p.ldx = X[0].ld; p.lda = A.ld;
+  p.O = c.O; p.ldo = c.ldo; p.R = c.R; p.ldr = c.ldr; p.scale = c.scale; p.keep = c.beta; p.vec_out = c.vec_out();
+  p.chunk = h->kblock_termwise / sgc::kChainBK;
+  p.words = h->err_dev + sgc::kGridWords + 2;
+  p.err = h->err_dev;
+  memcpy(p.step, c.step, (size_t)c.steps * sizeof(sgc::ChainStep));
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((unsigned)blocks, 1, 1);
+  cfg.blockDim = dim3(sgc::kChainThreads, 1, 1);
+  cfg.dynamicSmemBytes = sgc::kChainSmem;
+  cfg.stream = c.st;
+  cudaLaunchAttribute a;
+  a.id = cudaLaunchAttributeCooperative;
+  a.val.cooperative = 1;
+  cfg.attrs = &a;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, maps, p) != cudaSuccess) {
+    cudaGetLastError();                          // a device that is partly occupied by others
+    return SGEMM_CUBE_OK;
+  }
+  h->launches++;
+  *done = true;
+  return SGEMM_CUBE_OK;
+}
+
+constexpr int kMostSteps = sgc::kChainMostSteps;
 constexpr double kMostBound = 0x1p20, kLeastBound = 0x1p-20;   // the words' exponents stay inside FP32's, squared and all
 
 }  // namespace
@@ -179,8 +338,8 @@ extern "C" int sgemm_cube_orthogonalize(sgemm_cube_handle h, int rows, int cols,
   if (!h || bad_dims(rows, cols) || dtype < SGEMM_CUBE_F32 || dtype > SGEMM_CUBE_BF16) return SGEMM_CUBE_INVALID_ARG;
   if (steps < 1 || steps > kMostSteps || !(eps >= 0.f) || !std::isfinite(eps) || !std::isfinite(scale) || !std::isfinite(beta))
     return SGEMM_CUBE_INVALID_ARG;
-  // what the words of X, A and P have to hold, step by step
-  double s = 1.0, bound_a[kMostSteps], bound_p[kMostSteps], bound_x[kMostSteps + 1];
+  // what the words of X, A and B have to hold, step by step
+  double s = 1.0, bound_a[kMostSteps], bound_b[kMostSteps], bound_x[kMostSteps + 1];
   float k[kMostSteps][3];
   bound_x[0] = s;
   for (int i = 0; i < steps; ++i) {
@@ -189,10 +348,10 @@ extern "C" int sgemm_cube_orthogonalize(sgemm_cube_handle h, int rows, int cols,
       if (!std::isfinite(k[i][q])) return SGEMM_CUBE_INVALID_ARG;
     }
     bound_a[i] = s * s;
-    bound_p[i] = largest_on(s, k[i][0], k[i][1], k[i][2], 0);
+    bound_b[i] = largest_on(s, 0.0, k[i][1], k[i][2], 0);
     s = largest_on(s, k[i][0], k[i][1], k[i][2], 1);
     bound_x[i + 1] = s;
-    if (!(s <= kMostBound && bound_p[i] <= kMostBound && s >= kLeastBound)) return SGEMM_CUBE_INVALID_ARG;
+    if (!(s <= kMostBound && bound_b[i] <= kMostBound && s >= kLeastBound)) return SGEMM_CUBE_INVALID_ARG;
   }
   if (rows == 0 || cols == 0) return SGEMM_CUBE_OK;
   const size_t elem = dtype == SGEMM_CUBE_F32 ? 4 : 2;
@@ -202,66 +361,30 @@ extern "C" int sgemm_cube_orthogonalize(sgemm_cube_handle h, int rows, int cols,
   DeviceGuard g(h->device);
   if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  int rc = sgc::product_setup<sgc::kFormPolyKM, sgc::kFormPolyKK, sgc::kFormPolyMM>(h, h->polynomial_clusters);
-  if (rc) return rc;
   const bool tall = rows > cols;
   const int n = tall ? cols : rows, m = tall ? rows : cols;
-  const int blocks = sgc::blocks_for(h, (long long)rows * cols / 16 + 1);
-  Words X[2], A, P;
-  double* sums = nullptr;
-  for (int pass = 0; pass < 2; ++pass) {         // sizes first, then pointers
-    Carve c;
-    c.base = pass ? static_cast<uint8_t*>(h->poly_ws) : nullptr;
-    sums = c.take<double>((size_t)blocks);
-    X[0] = take_words(c, rows, cols);
-    X[1] = steps > 1 ? take_words(c, rows, cols) : X[0];
-    A = take_words(c, n, n);
-    P = take_words(c, n, n);
-    if (!pass && (rc = grow(h, &h->poly_ws, &h->poly_ws_bytes, c.used, st))) return rc;
-  }
-  int px = word_exponent(bound_x[0]);
-  const float pre = std::ldexp(1.f, px);
-  rc = dtype == SGEMM_CUBE_F32   ? normalise<float>(h, rows, cols, G, ldg, sums, blocks, eps, pre, X[0], st)
-       : dtype == SGEMM_CUBE_F16 ? normalise<__half>(h, rows, cols, G, ldg, sums, blocks, eps, pre, X[0], st)
-                                 : normalise<__nv_bfloat16>(h, rows, cols, G, ldg, sums, blocks, eps, pre, X[0], st);
-  if (rc) return rc;
-  for (int i = 0; i < steps; ++i) {
-    const Words &x = X[i & 1], &next = X[(i + 1) & 1];
-    const int pa = word_exponent(bound_a[i]), pp = word_exponent(bound_p[i]), pn = word_exponent(bound_x[i + 1]);
-    sgc::PolynomialEpilogue ep;
-    // A = X X^T, or X^T X
-    memset(&ep, 0, sizeof(ep));
-    ep.alpha = std::ldexp(1.f, -2 * px);
-    ep.hi = A.hi; ep.lo = A.lo; ep.ldw = A.ld;
-    ep.pre = std::ldexp(1.f, pa);
-    ep.symmetric = 1;
-    rc = tall ? polynomial_product<sgc::kFormPolyMM>(h, n, n, m, x, x, ep, st)
-              : polynomial_product<sgc::kFormPolyKK>(h, n, n, m, x, x, ep, st);
-    if (rc) return rc;
-    // P = a + b A + c A A
-    ep.alpha = k[i][2] * std::ldexp(1.f, -2 * pa);
-    ep.r_hi = A.hi; ep.r_lo = A.lo; ep.ldr = A.ld;
-    ep.beta = k[i][1] * std::ldexp(1.f, -pa);
-    ep.diagonal = k[i][0];
-    ep.hi = P.hi; ep.lo = P.lo; ep.ldw = P.ld;
-    ep.pre = std::ldexp(1.f, pp);
-    if ((rc = polynomial_product<sgc::kFormPolyKK>(h, n, n, n, A, A, ep, st))) return rc;
-    // X <- P X, or X P; the last one to O
-    memset(&ep, 0, sizeof(ep));
-    ep.alpha = std::ldexp(1.f, -px - pp);
-    if (i + 1 < steps) {
-      ep.hi = next.hi; ep.lo = next.lo; ep.ldw = next.ld;
-      ep.pre = std::ldexp(1.f, pn);
-    } else {
-      ep.alpha *= scale;
-      ep.Y = O; ep.ldy = ldo;
-      ep.kept = R; ep.ldk = ldr; ep.keep = beta;
-      ep.vec = aligned16(O) && ldo % 4 == 0 && (!R || (aligned16(R) && ldr % 4 == 0));
-    }
-    rc = tall ? polynomial_product<sgc::kFormPolyKK>(h, rows, cols, cols, x, P, ep, st)
-              : polynomial_product<sgc::kFormPolyKM>(h, rows, cols, rows, P, x, ep, st);
-    if (rc) return rc;
+  // factors of the products, the words' exponents in them
+  sgc::ChainStep step[kMostSteps];
+  const int px0 = word_exponent(bound_x[0]);
+  for (int i = 0, px = px0; i < steps; ++i) {
+    const int pa = word_exponent(bound_a[i]), pb = word_exponent(bound_b[i]), pn = word_exponent(bound_x[i + 1]);
+    step[i].gram_alpha = std::ldexp(1.f, -2 * px);
+    step[i].gram_pre = std::ldexp(1.f, pa);
+    step[i].square_alpha = k[i][2] * std::ldexp(1.f, -2 * pa);
+    step[i].square_beta = k[i][1] * std::ldexp(1.f, -pa);
+    step[i].square_pre = std::ldexp(1.f, pb);
+    step[i].update_alpha = std::ldexp(1.f, -px - pb);
+    step[i].update_beta = k[i][0] * std::ldexp(1.f, -px);
+    step[i].update_pre = std::ldexp(1.f, pn);
     px = pn;
   }
-  return SGEMM_CUBE_OK;
+  OrthogonalizeCall c{rows, cols, dtype, G, ldg, steps, eps, R, ldr, scale, beta, O, ldo, tall, n, m, std::ldexp(1.f, px0), step, st};
+  bool done = false;
+  int rc = SGEMM_CUBE_OK;
+  if (takes_chain(n, m)) {
+    rc = dtype == SGEMM_CUBE_F32   ? run_chain<float>(h, c, &done)
+         : dtype == SGEMM_CUBE_F16 ? run_chain<__half>(h, c, &done)
+                                   : run_chain<__nv_bfloat16>(h, c, &done);
+  }
+  return done || rc ? rc : run_products(h, c);
 }

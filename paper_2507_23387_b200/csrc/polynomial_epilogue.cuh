@@ -1,7 +1,7 @@
 // One step of a matrix polynomial on packed operands: what becomes of a finished product of matrices that are kept as
 // FP16 words throughout,
 //
-//   v = alpha acc + beta R[row, col] + diagonal (row == col),
+//   v = alpha acc + beta R[row, col],
 //
 // acc the product of the words, R a matrix of words (its way back from words is in beta, the product's in alpha), v
 // stored as words of pre v, or as FP32 with a residual of its own.  A symmetric product (X X', the square of a symmetric
@@ -12,6 +12,7 @@
 #include <cstdint>
 #include <cuda_runtime.h>
 
+#include "elements.cuh"
 #include "linear_epilogue.cuh"
 #include "pack_job.cuh"
 #include "split_math.cuh"
@@ -19,18 +20,18 @@
 namespace sgc {
 
 struct PolynomialEpilogue {
-  float alpha, beta, diagonal, pre;
+  float alpha, beta, pre;
   const uint16_t* r_hi;       // words of R, or null; ld a multiple of 8, 16-byte aligned, as all words here
   const uint16_t* r_lo;
   long long ldr;
   uint16_t* hi;               // the result's words, or null
   uint16_t* lo;
   long long ldw;
-  float* Y;                   // where hi is null: Y = v + keep Y_old, FP32 of any alignment
+  float* Y;                   // where hi is null: Y = scale v + keep Y_old, FP32 of any alignment
   long long ldy;
   const float* kept;          // Y_old, or null; may be Y itself
   long long ldk;
-  float keep;
+  float scale, keep;
   int vec;                    // Y and the kept matrix take 16-byte accesses
   int symmetric;              // M == N, tiles that reach the lower triangle only; R is symmetric too
   float* tiles;               // as in LinearEpilogue
@@ -91,6 +92,71 @@ __device__ __forceinline__ void store_words(uint16_t* at, const uint4& w, uint32
   }
 }
 
+// Which of the elements (r, c .. c + 7) lie on or below the diagonal, and which of (r .. r + 7, c) strictly below it.
+__device__ __forceinline__ uint32_t on_or_below(int r, int c) {
+  const int under = r - c;
+  return under >= 7 ? 0xFFu : (under < 0 ? 0u : (2u << under) - 1u);
+}
+__device__ __forceinline__ uint32_t strictly_below(int r, int c) {
+  const int under = c - r;
+  return under < 0 ? 0xFFu : (under >= 7 ? 0u : 0xFFu & ~((2u << under) - 1u));
+}
+// y = scale v + keep k for up to eight columns, `left` of them inside the matrix.
+__device__ __forceinline__ void store_eight(float* y, const float* k, float scale, float keep, bool vec, int left, float (&v)[8]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] *= scale;
+  if (vec && left >= 8) {
+#pragma unroll
+    for (int q = 0; q < 8; q += 4) {
+      float4 o = make_float4(v[q], v[q + 1], v[q + 2], v[q + 3]);
+      if (k) {
+        const float4 old = *reinterpret_cast<const float4*>(k + q);
+        o.x = fmaf(keep, old.x, o.x); o.y = fmaf(keep, old.y, o.y);
+        o.z = fmaf(keep, old.z, o.z); o.w = fmaf(keep, old.w, o.w);
+      }
+      *reinterpret_cast<float4*>(y + q) = o;
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (q < left) y[q] = k ? fmaf(keep, k[q], v[q]) : v[q];
+  }
+}
+
+// 2^p / (norm + eps) as two FP32 factors (1 / norm can leave the FP32 range while the entries times it do not).  A matrix of
+// zeros with eps = 0 stays one; a norm that is not finite makes every entry NaN.
+__device__ __forceinline__ void norm_factors(double squares, float eps, float pre, float& f0, float& f1) {
+  const double norm = sqrt(squares) + (double)eps;
+  const double scale = norm == 0.0 ? 0.0 : (isfinite(norm) ? 1.0 / norm : (double)NAN);
+  const int e = scale != 0.0 && isfinite(scale) ? max(-126, min(126, ilogb(scale) / 2)) : 0;
+  f0 = pow2f(e);
+  f1 = (float)(scale * (double)pow2f(-e)) * pre;
+}
+// Words of f0 f1 G for eight columns, `left` of them inside the matrix (zeros behind them).
+template <typename T>
+__device__ __forceinline__ void normalise_eight(const T* at, bool vec, int left, float f0, float f1, uint16_t* hi, uint16_t* lo) {
+  constexpr int V = Elem<T>::kVec;
+  float v[8];
+  if (vec && left >= 8) {
+#pragma unroll
+    for (int i = 0; i < 8 / V; ++i) {
+      float x[V];
+      Elem<T>::unpack(*reinterpret_cast<const uint4*>(at + i * V), x);
+#pragma unroll
+      for (int q = 0; q < V; ++q) v[i * V + q] = x[q];
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = q < left ? Elem<T>::get(at[q]) : 0.f;
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] *= f0;
+  uint4 h, l;
+  pack_words(v, f1, h, l);
+  *reinterpret_cast<uint4*>(hi) = h;
+  *reinterpret_cast<uint4*>(lo) = l;
+}
+
 // Blocks of 32 x 32 of a finished tile, from `first` on every `step`-th (linear_epilogue.cuh describes the tile).  A
 // lane has eight columns of every eighth row; for the mirror image it has eight rows of four columns.
 __device__ __forceinline__ void polynomial_store(const PolynomialEpilogue& e, int M, int N, float* tile, int slices,
@@ -133,38 +199,14 @@ __device__ __forceinline__ void polynomial_store(const PolynomialEpilogue& e, in
           if (e.r_hi)
             unpack_words(*reinterpret_cast<const uint4*>(e.r_hi + r * e.ldr + c),
                          *reinterpret_cast<const uint4*>(e.r_lo + r * e.ldr + c), e.beta, v[u]);
-          if (e.diagonal != 0.f && (unsigned)(r - c) < 8u) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-              if (c + q == r) v[u][q] += e.diagonal;
-          }
           if (e.hi) {
             uint4 h, l;
             pack_words(v[u], e.pre, h, l);
-            // below and on the diagonal; the rest comes from the mirror image
-            const long long under = r - c;
-            const uint32_t take = !e.symmetric || under >= 7 ? 0xFFu : (under < 0 ? 0u : (2u << under) - 1u);
+            const uint32_t take = e.symmetric ? on_or_below((int)r, c) : 0xFFu;     // the rest comes from the mirror image
             store_words(e.hi + r * e.ldw + c, h, take);
             store_words(e.lo + r * e.ldw + c, l, take);
           } else {
-            float* y = e.Y + r * e.ldy + c;
-            const float* k = e.kept ? e.kept + r * e.ldk + c : nullptr;
-            if (e.vec && c + 8 <= N) {
-#pragma unroll
-              for (int q = 0; q < 8; q += 4) {
-                float4 o = make_float4(v[u][q], v[u][q + 1], v[u][q + 2], v[u][q + 3]);
-                if (k) {
-                  const float4 old = *reinterpret_cast<const float4*>(k + q);
-                  o.x = fmaf(e.keep, old.x, o.x); o.y = fmaf(e.keep, old.y, o.y);
-                  o.z = fmaf(e.keep, old.z, o.z); o.w = fmaf(e.keep, old.w, o.w);
-                }
-                *reinterpret_cast<float4*>(y + q) = o;
-              }
-            } else {
-#pragma unroll
-              for (int q = 0; q < 8; ++q)
-                if (c + q < N) y[q] = k ? fmaf(e.keep, k[q], v[u][q]) : v[u][q];
-            }
+            store_eight(e.Y + r * e.ldy + c, e.kept ? e.kept + r * e.ldk + c : nullptr, e.scale, e.keep, e.vec != 0, N - c, v[u]);
           }
         }
       }
@@ -187,8 +229,8 @@ __device__ __forceinline__ void polynomial_store(const PolynomialEpilogue& e, in
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const long long at = c + q;                            // element (r + i, at) goes to (at, r + i)
-      const long long under = at - r;                        // strictly below the diagonal: i > under
-      if (at >= N || under >= 7) continue;
+      const uint32_t take = strictly_below(r, c + q);
+      if (at >= N || take == 0u) continue;
       float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = e.alpha * (q == 0 ? f[i].x : (q == 1 ? f[i].y : (q == 2 ? f[i].z : f[i].w)));
@@ -197,7 +239,6 @@ __device__ __forceinline__ void polynomial_store(const PolynomialEpilogue& e, in
                      *reinterpret_cast<const uint4*>(e.r_lo + at * e.ldr + r), e.beta, v);
       uint4 h, l;
       pack_words(v, e.pre, h, l);
-      const uint32_t take = under < 0 ? 0xFFu : (0xFFu & ~((2u << under) - 1u));
       store_words(e.hi + at * e.ldw + r, h, take);
       store_words(e.lo + at * e.ldw + r, l, take);
     }

@@ -24,6 +24,7 @@ enum : unsigned int {
   kErrTileFullWait = 0x10A,
   kErrPackWait = 0x10B,
   kErrSortWait = 0x10C,
+  kErrChainWait = 0x10D,
   kErrProbeWait = 0x1F0,
 };
 
