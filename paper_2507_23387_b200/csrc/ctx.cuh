@@ -88,7 +88,7 @@ struct sgemm_cube_ctx {
   int max_pair_clusters[3] = {0, 0, 0};   // co-resident 2-CTA clusters: <1,false>, <3,false>, <3,true>
   EncodeTiledFn encode = nullptr;
   bool attrs_set = false;
-  sgc::ResidentClusters linear_clusters, polynomial_clusters, loss_clusters;
+  sgc::ResidentClusters linear_clusters, polynomial_clusters, loss_clusters, chain_clusters[3];   // (chain: by element type)
   int pack_once_blocks = 0, dz_once_blocks[5] = {0, 0, 0, 0, 0};   // resident blocks of the one-launch packing kernels
 };
 

@@ -11,6 +11,7 @@
 // core's truncating sums, with 128 x 384 and five steps 2.8e-6 off where FP32 products are 1.7e-6.)
 // Small matrices take all of it in one launch (polynomial_chain.cuh).
 #include <cmath>
+#include <type_traits>
 
 #include "ctx.cuh"
 #include "elements.cuh"
@@ -228,59 +229,97 @@ int run_products(sgemm_cube_ctx* h, const OrthogonalizeCall& c) {
 // loses to the larger kernel where that one is busy for long.
 bool takes_chain(int n, int m) { return n <= 1536 && (long long)n * m <= (1ll << 22); }
 
-// Slices of a product's tiles: the fewest clocks of about 1100 for a stage and 2500 for the meeting of a tile's blocks.
-sgc::ChainSplit chain_split(long long tiles, int K, int blocks) {
+// Slices of a product's tiles in a grid of clusters, and about how many clocks the product then takes: 1300 for a stage, 4000
+// until the first sums are there, 900 for two rows of a thread and 1500 for the meeting of a cluster.
+long long chain_split(long long tiles, int K, int blocks, int cluster, sgc::ChainSplit* split) {
   const int stages = (K + sgc::kChainBK - 1) / sgc::kChainBK;
-  sgc::ChainSplit best{(int)tiles, 1, stages};
-  long long least = (tiles + blocks - 1) / blocks * stages * 1100;
-  for (int s = 2; s <= sgc::kChainMostSlices && s <= stages && tiles * s <= blocks; ++s) {
+  long long least = 0;
+  for (int s = 1; s <= cluster && s <= stages; s *= 2) {
     const int per = (stages + s - 1) / s;
-    if ((stages + per - 1) / per != s) continue;                     // the last slice would be empty
-    const long long clocks = per * 1100ll + 2500 + 60 * s;
-    if (clocks < least) { least = clocks; best = sgc::ChainSplit{(int)tiles, s, per}; }
+    if (s > 1 && (tiles * s > blocks || (stages + per - 1) / per != s)) continue;      // (no slice may be empty)
+    const long long turns = (tiles * s + blocks - 1) / blocks;
+    const long long clocks = turns * (4000 + per * 1300ll + (s < 4 ? 4 / s : 1) * 1300ll) + (s > 1 ? 1500 : 0);
+    if (s == 1 || clocks < least) { least = clocks; *split = sgc::ChainSplit{(int)tiles, s, per}; }
   }
-  return best;
+  return least;
 }
 
-// All products in one cooperative launch; *done stays false where that cannot be had.
+cudaLaunchConfig_t chain_config(int blocks, int cluster, cudaLaunchAttribute* attr, cudaStream_t st) {
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((unsigned)blocks, 1, 1);
+  cfg.blockDim = dim3(sgc::kChainThreads, 1, 1);
+  cfg.dynamicSmemBytes = sgc::kChainSmem;
+  cfg.stream = st;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeCooperative;
+  attr[1].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cfg;
+}
+// How many clusters of 1 to 8 blocks are resident at once.
 template <typename T>
-int run_chain(sgemm_cube_ctx* h, const OrthogonalizeCall& c, bool* done) {
+int chain_setup(sgemm_cube_ctx* h) {
+  sgc::ResidentClusters& k = h->chain_clusters[sizeof(T) == 4 ? 0 : (std::is_same<T, __half>::value ? 1 : 2)];
+  if (k.ready) return SGEMM_CUBE_OK;
   auto kernel = sgc::polynomial_chain_kernel<T>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sgc::kChainSmem) != cudaSuccess) {
     cudaGetLastError();
     return SGEMM_CUBE_CUDA_ERROR;
   }
+  for (int c = 1; c <= sgc::kChainMostCluster; c *= 2) {
+    cudaLaunchAttribute a[2];
+    cudaLaunchConfig_t cfg = chain_config(c * h->sm_count, c, a, nullptr);
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
+    k.slices[c] = n * c < h->sm_count ? n : h->sm_count / c;
+  }
+  k.ready = true;
+  return SGEMM_CUBE_OK;
+}
+
+// All products in one cooperative launch; *done stays false where that cannot be had.
+template <typename T>
+int run_chain(sgemm_cube_ctx* h, const OrthogonalizeCall& c, bool* done) {
+  int rc = chain_setup<T>(h);
+  if (rc) return rc;
+  const sgc::ResidentClusters& k = h->chain_clusters[sizeof(T) == 4 ? 0 : (std::is_same<T, __half>::value ? 1 : 2)];
   const long long side = (c.n + sgc::kChainTile - 1) / sgc::kChainTile, lower = side * (side + 1) / 2;
   const long long all = side * ((c.m + sgc::kChainTile - 1) / sgc::kChainTile);
   sgc::ChainParams p;
   memset(&p, 0, sizeof(p));
-  p.gram = chain_split(lower, c.m, h->sm_count);
-  p.square = chain_split(lower, c.n, h->sm_count);
-  p.update = chain_split(all, c.n, h->sm_count);
-  // blocks: as many as the largest product has work for, and enough to read G
-  long long units = 1;
-  size_t scratch = 0;
-  for (const sgc::ChainSplit* s : {&p.gram, &p.square, &p.update}) {
-    const long long u = (long long)s->tiles * s->slices;
-    if (u > units) units = u;
-    if (s->slices > 1 && (size_t)u > scratch) scratch = (size_t)u;
+  // the cluster's size: larger ones share a tile among more blocks, smaller ones leave fewer SMs out
+  int cluster = 0, blocks = 0;
+  long long least = 0;
+  for (int s = 1; s <= sgc::kChainMostCluster; s *= 2) {
+    const int resident = k.slices[s] * s;
+    if (resident == 0) continue;
+    sgc::ChainSplit gram, square, update;
+    const long long clocks = chain_split(lower, c.m, resident, s, &gram) + chain_split(lower, c.n, resident, s, &square) +
+                             chain_split(all, c.n, resident, s, &update);
+    if (cluster && clocks >= least) continue;
+    least = clocks;
+    cluster = s;
+    p.gram = gram; p.square = square; p.update = update;
+    // blocks: as many as the largest product has work for, and enough to read G
+    long long units = (long long)c.rows * c.cols / (sgc::kChainThreads * 8) + 1;
+    for (const sgc::ChainSplit* q : {&gram, &square, &update})
+      if ((long long)q->tiles * q->slices > units) units = (long long)q->tiles * q->slices;
+    blocks = (int)(units < resident ? (units + s - 1) / s * s : resident);
   }
-  const long long reading = (long long)c.rows * c.cols / (sgc::kChainThreads * 8) + 1;
-  if (reading > units) units = reading;
-  const int blocks = (int)(units < h->sm_count ? units : h->sm_count);
+  if (!cluster) return SGEMM_CUBE_OK;
   Words X[2], A, B;
-  p.count_stride = (int)(all > lower ? all : lower);
-  int rc;
   for (int pass = 0; pass < 2; ++pass) {         // sizes first, then pointers
     Carve w;
     w.base = pass ? static_cast<uint8_t*>(h->poly_ws) : nullptr;
     p.sums = w.take<double>((size_t)blocks);
-    p.counts = w.take<unsigned int>((size_t)3 * p.count_stride);
     X[0] = take_words(w, c.rows, c.cols);
     X[1] = c.steps > 1 ? take_words(w, c.rows, c.cols) : X[0];
     A = take_words(w, c.n, c.n);
     B = take_words(w, c.n, c.n);
-    p.scratch = w.take<float>(scratch * sgc::kChainTileFloats);
     if (!pass && (rc = grow(h, &h->poly_ws, &h->poly_ws_bytes, w.used, c.st))) return rc;
   }
   sgc::ChainMaps maps;
@@ -306,18 +345,9 @@ int run_chain(sgemm_cube_ctx* h, const OrthogonalizeCall& c, bool* done) {
   p.words = h->err_dev + sgc::kGridWords + 2;
   p.err = h->err_dev;
   memcpy(p.step, c.step, (size_t)c.steps * sizeof(sgc::ChainStep));
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3((unsigned)blocks, 1, 1);
-  cfg.blockDim = dim3(sgc::kChainThreads, 1, 1);
-  cfg.dynamicSmemBytes = sgc::kChainSmem;
-  cfg.stream = c.st;
-  cudaLaunchAttribute a;
-  a.id = cudaLaunchAttributeCooperative;
-  a.val.cooperative = 1;
-  cfg.attrs = &a;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kernel, maps, p) != cudaSuccess) {
+  cudaLaunchAttribute attr[2];
+  const cudaLaunchConfig_t cfg = chain_config(blocks, cluster, attr, c.st);
+  if (cudaLaunchKernelEx(&cfg, sgc::polynomial_chain_kernel<T>, maps, p) != cudaSuccess) {
     cudaGetLastError();                          // a device that is partly occupied by others
     return SGEMM_CUBE_OK;
   }

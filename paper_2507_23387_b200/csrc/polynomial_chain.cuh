@@ -4,10 +4,10 @@
 //
 //   |G|_F, X = G / (|G|_F + eps);  steps times:  A = X X^T | B = b A + c A A | X <- a X + B X      (| all blocks meet)
 //
-// One block an SM, cooperative.  A unit is a 128 x 128 tile, or a slice of its k range: with S slices a tile the blocks of
-// a tile meet through L2 and each finishes 128 / S of its rows.  Warps 0-7 take the sums out of TMEM (k-blocks added in
-// FP32, as in gemm_tc.cuh) and finish the tile through shared memory, along rows and, for what is below the diagonal of a
-// symmetric product, along columns; warp 8 loads by TMA, warp 9 issues the MMAs.
+// One block an SM, cooperative, in clusters.  A unit is a 128 x 128 tile, or a slice of its k range: with S slices a tile (S
+// divides the cluster) S blocks of a cluster read each other's sums from shared memory and each finishes 128 / S of its rows.  Warps 0-7 take the sums out of TMEM (k-blocks added in
+// FP32, as in gemm_tc.cuh) and finish the tile through shared memory (the ring, which is idle by then), along rows and, for
+// what is below the diagonal of a symmetric product, along columns; warp 8 loads by TMA, warp 9 issues the MMAs.
 // Words are written by ordinary stores and read by TMA in the next phase: a proxy fence stands on both sides of the meeting.
 #pragma once
 
@@ -25,15 +25,15 @@ constexpr int kChainThreads = 320, kChainEpiThreads = 256;
 constexpr uint32_t kChainWords = kChainTile * kChainBK * 2;              // one word of one operand's tile
 constexpr uint32_t kChainStageBytes = 4 * kChainWords;                   // A hi, A lo, B hi, B lo
 constexpr uint32_t kChainRing = kChainStages * kChainStageBytes;
-constexpr int kChainPitch = 130, kChainRows = 64;                        // finishing: 64 rows at a time, 130 floats apart
-constexpr uint32_t kChainSmem = kChainRing + kChainRows * kChainPitch * 4 + 256 + 1024;
-constexpr int kChainMostSteps = 64, kChainMostSlices = 16;
-constexpr int kChainTileFloats = kChainTile * kChainTile;
+constexpr int kChainPitch = 132;                                         // finishing: rows of a tile, 132 floats apart, in the ring
+static_assert(kChainTile * kChainPitch * 4 <= kChainRing, "a finished tile fits the ring");
+constexpr uint32_t kChainSmem = kChainRing + 256 + 1024;
+constexpr int kChainMostSteps = 64, kChainMostCluster = 8;
 
 struct ChainStep {           // factors of a step's three products (powers of two for the words' exponents in them)
   float gram_alpha, gram_pre, square_alpha, square_beta, square_pre, update_alpha, update_beta, update_pre;
 };
-struct ChainSplit {          // tiles of a product, slices of a tile, 64-deep stages of a slice
+struct ChainSplit {          // tiles of a product, slices of a tile (a power of two), 64-deep stages of a slice
   int tiles, slices, per;
 };
 struct ChainParams {
@@ -52,10 +52,7 @@ struct ChainParams {
   int vec_out;
   int chunk;                 // stages of a k-block
   ChainSplit gram, square, update;
-  float* scratch;            // [units][128 x 128]
   double* sums;              // [blocks]
-  unsigned int* counts;      // [3][most tiles]: slices of a tile that are there, over all steps
-  int count_stride;
   unsigned int* words;       // {arrived, left} of the grid, zero between calls
   unsigned int* err;
   ChainStep step[kChainMostSteps];
@@ -65,13 +62,14 @@ struct ChainMaps {
 };
 
 __device__ __forceinline__ void fence_proxy_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
-__device__ __forceinline__ unsigned int load_acquire(const unsigned int* p) {
+// Relaxed: the fences around them stand alone (a releasing addition or acquiring loads in the loop each add one of their own).
+__device__ __forceinline__ unsigned int load_relaxed(const unsigned int* p) {
   unsigned int v;
-  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
   return v;
 }
-__device__ __forceinline__ void add_release(unsigned int* p) {
-  asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(1u) : "memory");
+__device__ __forceinline__ void add_relaxed(unsigned int* p) {
+  asm volatile("red.relaxed.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(1u) : "memory");
 }
 // The 256 threads of the first eight warps meet; true if `ok` is for all of them.
 __device__ __forceinline__ bool chain_agree(bool ok) {
@@ -90,7 +88,7 @@ __device__ __forceinline__ bool chain_agree(bool ok) {
 // Waits, bounded, until *p is at least `want`.
 __device__ __forceinline__ bool chain_wait(const unsigned int* p, unsigned int want, volatile uint32_t* abort_flag, unsigned int* err) {
   const long long t0 = clock64();
-  while (load_acquire(p) < want) {
+  while (load_relaxed(p) < want) {
     if (*abort_flag) return false;
     if (clock64() - t0 > kWaitLimitClocks) {
       *abort_flag = 1u;
@@ -101,19 +99,27 @@ __device__ __forceinline__ bool chain_wait(const unsigned int* p, unsigned int w
   }
   return true;
 }
-// All blocks of the grid meet for the `round`-th time (from 1); what they stored is there for loads and TMA behind it.
+// All blocks of the grid meet for the `round`-th time (from 1); what they stored is there for loads and, behind a proxy
+// fence of the thread that issues it, for TMA.  One thread's fences stand for the block's stores, which the barrier has put
+// before them (every thread fencing for itself took 3000 to 5000 clocks a meeting).
 __device__ __forceinline__ bool chain_meet(const ChainParams& p, unsigned int round, volatile uint32_t* abort_flag) {
-  fence_proxy_async_global();
-  __threadfence();
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag == 0u) {
-    add_release(&p.words[0]);
+    __threadfence();
+    fence_proxy_async_global();
+    add_relaxed(&p.words[0]);
     chain_wait(&p.words[0], round * gridDim.x, abort_flag, p.err);
     __threadfence();
   }
   __syncthreads();
-  fence_proxy_async_global();
   return *abort_flag == 0u;
+}
+
+// Four floats of shared memory of a block of the cluster.
+__device__ __forceinline__ float4 load_peer(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
 }
 
 // Tile `t` of the lower triangle, row by row.
@@ -131,13 +137,14 @@ __global__ void __launch_bounds__(kChainThreads, 1)
 polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_constant__ ChainParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* stage = reinterpret_cast<float*>(smem + kChainRing);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kChainRing + kChainRows * kChainPitch * 4);
+  float* stage = reinterpret_cast<float*>(smem);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kChainRing);
   uint64_t* full_bar = bars;                          // [stages]  TMA -> MMA
   uint64_t* empty_bar = bars + kChainStages;          // [stages]  MMA -> TMA
   uint64_t* tfull_bar = bars + 2 * kChainStages;      // [3]  MMA -> sums: hi*hi regions 0 and 1, corrections
   uint64_t* tempty_bar = tfull_bar + 3;               // [3]  sums -> MMA
-  uint64_t* drain_bar = tempty_bar + 3;
+  uint64_t* ring_bar = tempty_bar + 3;                // finishing -> TMA: the ring may be filled again
+  uint64_t* drain_bar = ring_bar + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_bar + 1);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   double* block_sums = reinterpret_cast<double*>(stage);
@@ -154,9 +161,14 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
       mbar_init(&tfull_bar[r], 1);
       mbar_init(&tempty_bar[r], kChainEpiThreads / 32);
     }
+    mbar_init(ring_bar, kChainEpiThreads / 32);
     mbar_init(drain_bar, 1);
     *abort_flag = 0u;
     fence_mbar_init();
+  }
+  if (warp == 8 && lane < 8) {
+    const CUtensorMap* all = maps.x[0];
+    tma_prefetch_desc(all + lane);
   }
   if (warp == 9) {
     tmem_alloc(tmem_slot, 512);
@@ -197,8 +209,6 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
       for (int w = 1; w < kChainThreads / 32; ++w) s += block_sums[w];
       p.sums[blockIdx.x] = s;
     }
-    if (blockIdx.x == 0)
-      for (int i = tid; i < 3 * p.count_stride; i += kChainThreads) p.counts[i] = 0u;
     go = chain_meet(p, ++round, abort_flag);
   }
   if (go) {
@@ -237,6 +247,8 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
       kb0 = slice * split.per;
       kb1 = min(num_kb, kb0 + split.per);
     };
+    // With slices every block has at most one unit; the cluster meets once, when all sums of its tiles are in shared memory.
+    const bool sliced = split.slices > 1;
     // A's and B's rows (or, MN-major, columns) of a tile and their k, by majorness
     const bool a_mn = kind == 0 && tall, b_mn = (kind == 0 && tall) || (kind == 2 && !tall);
     if (warp < 8) {
@@ -244,7 +256,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
       const int quarter = warp & 3, half = warp >> 2;
       const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * 64;
       const float alpha = kind == 0 ? f.gram_alpha : (kind == 1 ? f.square_alpha : f.update_alpha);
-      const float beta = kind == 1 ? f.square_beta : f.update_beta;
+      const float beta = kind == 0 ? 0.f : (kind == 1 ? f.square_beta : f.update_beta);
       const bool last = phase == phases - 1;
       const float pre = kind == 0 ? f.gram_pre : (kind == 1 ? f.square_pre : f.update_pre);
       const uint16_t* r_hi = kind == 0 ? nullptr : (kind == 1 ? p.a_hi : p.x_hi[cur]);
@@ -252,9 +264,12 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
       uint16_t* w_hi = kind == 0 ? p.a_hi : (kind == 1 ? p.b_hi : p.x_hi[cur ^ 1]);
       uint16_t* w_lo = kind == 0 ? p.a_lo : (kind == 1 ? p.b_lo : p.x_lo[cur ^ 1]);
       const long long ld = symmetric ? p.lda : p.ldx;
+      // Rows of a tile that a block finishes.
+      const int share = kChainTile / split.slices;
       for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
         int tm, tn, slice, kb0, kb1;
         unit_of(unit, tm, tn, slice, kb0, kb1);
+        const int r0 = slice * share;
         const int unit_chunks = (kb1 - kb0 + p.chunk - 1) / p.chunk;
         float S[64];
         bool ok = true;
@@ -300,117 +315,118 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
           __syncwarp();
           if (lane == 0) mbar_arrive(&tempty_bar[2]);
         }
-        // Rows of the tile that this block finishes, 64 at a time at most.
-        const int share = split.slices == 1 ? kChainRows : ((kChainTile + split.slices - 1) / split.slices + 7) / 8 * 8;
-        const int passes = split.slices == 1 ? 2 : 1;
-        if (split.slices > 1) {
-          // the slice's sums to L2, four columns of a row in a piece, the 128 rows next to each other
-          if (ok) {
-            float4* out = reinterpret_cast<float4*>(p.scratch + (long long)unit * kChainTileFloats) + quarter * 32 + lane;
+        if (ok) {
+          float* out = stage + (quarter * 32 + lane) * kChainPitch + half * 64;
 #pragma unroll
-            for (int c = 0; c < 16; ++c)
-              __stcg(out + (half * 16 + c) * kChainTile, make_float4(S[4 * c], S[4 * c + 1], S[4 * c + 2], S[4 * c + 3]));
-          }
-          __threadfence();
-          ok = chain_agree(ok);
-          if (!ok) break;
-          if (tid == 0) {
-            unsigned int* count = p.counts + kind * p.count_stride + unit / split.slices;
-            add_release(count);
-            ok = chain_wait(count, (unsigned int)(step + 1) * split.slices, abort_flag, p.err);
-            __threadfence();
-          }
-          ok = chain_agree(ok);
-          if (!ok) break;
+          for (int c = 0; c < 64; c += 4) *reinterpret_cast<float4*>(out + c) = make_float4(S[c], S[c + 1], S[c + 2], S[c + 3]);
         }
-        const int row_first = split.slices == 1 ? 0 : slice * share;
-        for (int pass = 0; pass < passes; ++pass) {
-          const int r0 = row_first + pass * kChainRows;                  // within the tile
-          const int rows = min(share, kChainTile - r0);
-          if (split.slices == 1) {
-            if (ok && (quarter >> 1) == pass) {
-              float* out = stage + ((quarter & 1) * 32 + lane) * kChainPitch + half * 64;
+        // A lane has four columns of a row, a warp every eighth row, four of them at a time; R's words come one turn ahead.
+        // Loops, not straight lines: what a block runs through once a phase comes from the instruction cache's far end (16 rows
+        // unrolled took four times as long).
+        const int cg = lane * 4, c = tn * kChainTile + cg;
+        const bool mirror = symmetric && tm != tn;           // (a tile on the diagonal holds its own mirror image)
+        const int row_end = min(share, M - tm * kChainTile - r0);
+        int lr = c < N ? warp : kChainTile;
+        long long at_r = (long long)(tm * kChainTile + r0 + lr) * ld + c;
+        uint2 rh[4], rl[4];
+        auto ask = [&](int row, long long at) {
 #pragma unroll
-              for (int c = 0; c < 64; c += 2) *reinterpret_cast<float2*>(out + c) = make_float2(S[c], S[c + 1]);
+          for (int j = 0; j < 4; ++j) {
+            rh[j] = rl[j] = make_uint2(0u, 0u);
+            if (r_hi && row + 8 * j < row_end) {
+              rh[j] = __ldcg(reinterpret_cast<const uint2*>(r_hi + at + 8 * j * ld));
+              rl[j] = __ldcg(reinterpret_cast<const uint2*>(r_lo + at + 8 * j * ld));
             }
+          }
+        };
+        ask(lr, at_r);
+        if (sliced) cluster_sync_all();
+        ok = chain_agree(ok);
+        if (!ok) break;
+        const uint32_t first_peer = cluster_ctarank() & ~(uint32_t)(split.slices - 1);
+#pragma unroll 1
+        for (; lr < row_end; lr += 32, at_r += 32 * ld) {
+          float* at = stage + (r0 + lr) * kChainPitch + cg;
+          float4 v[4];
+          if (!sliced) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float4*>(at + 8 * j * kChainPitch);   // (the ring goes on behind the tile)
           } else {
-            const float4* in = reinterpret_cast<const float4*>(p.scratch + (long long)(unit - slice) * kChainTileFloats);
-            for (int i = tid; i < rows * 32; i += kChainEpiThreads) {
-              const int c4 = i / rows, r = i - c4 * rows;
-              const float4* at = in + c4 * kChainTile + r0 + r;
-              float4 v = __ldcg(at);
-#pragma unroll 4
-              for (int s = 1; s < split.slices; ++s) {
-                const float4 o = __ldcg(at + s * (kChainTileFloats / 4));
-                v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+            for (int s = 0; s < split.slices; ++s) {         // in a fixed order; a block begins with its own, so that they do
+              const uint32_t peer = mapa_u32(smem_u32(at), first_peer + ((slice + s) & (split.slices - 1)));   // not all read one
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                if (lr + 8 * j < row_end) {
+                  const float4 t = load_peer(peer + 8 * j * kChainPitch * 4);
+                  v[j].x += t.x; v[j].y += t.y; v[j].z += t.z; v[j].w += t.w;
+                }
               }
-              float* out = stage + r * kChainPitch + c4 * 4;
-              *reinterpret_cast<float2*>(out) = make_float2(v.x, v.y);
-              *reinterpret_cast<float2*>(out + 2) = make_float2(v.z, v.w);
             }
           }
-          ok = chain_agree(ok);
-          if (!ok) break;
-          for (int i = tid; i < rows * 16; i += kChainEpiThreads) {
-            const int lr = i >> 4, r = tm * kChainTile + r0 + lr, c = tn * kChainTile + (i & 15) * 8;
-            if (r >= M || c >= N) continue;
-            float* at = stage + lr * kChainPitch + (i & 15) * 8;
-            float v[8];
 #pragma unroll
-            for (int q = 0; q < 8; q += 2) {
-              const float2 t = *reinterpret_cast<const float2*>(at + q);
-              v[q] = alpha * t.x; v[q + 1] = alpha * t.y;
-            }
-            if (r_hi)
-              unpack_words(__ldcg(reinterpret_cast<const uint4*>(r_hi + r * ld + c)),
-                           __ldcg(reinterpret_cast<const uint4*>(r_lo + r * ld + c)), beta, v);
+          for (int j = 0; j < 4; ++j) {
+            v[j].x *= alpha; v[j].y *= alpha; v[j].z *= alpha; v[j].w *= alpha;
+            unpack_words(rh[j], rl[j], beta, v[j]);
+          }
+          ask(lr + 32, at_r + 32 * ld);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (lr + 8 * j >= row_end) break;
+            if (mirror) *reinterpret_cast<float4*>(at + 8 * j * kChainPitch) = v[j];
             if (last) {
-              store_eight(p.O + r * p.ldo + c, p.R ? p.R + r * p.ldr + c : nullptr, p.scale, p.keep, p.vec_out != 0, N - c, v);
-              continue;
-            }
-            uint4 h, l;
-            pack_words(v, pre, h, l);
-            const uint32_t take = symmetric ? on_or_below(r, c) : 0xFFu;
-            store_words(w_hi + r * ld + c, h, take);
-            store_words(w_lo + r * ld + c, l, take);
-            if (symmetric) {
-#pragma unroll
-              for (int q = 0; q < 8; q += 2) *reinterpret_cast<float2*>(at + q) = make_float2(v[q], v[q + 1]);
+              const long long r = tm * kChainTile + r0 + lr + 8 * j;
+              store_four(p.O + r * p.ldo + c, p.R ? p.R + r * p.ldr + c : nullptr, p.scale, p.keep, p.vec_out != 0, N - c, v[j]);
+            } else {
+              uint2 h, l;
+              pack_words(v[j], pre, h, l);
+              *reinterpret_cast<uint2*>(w_hi + at_r + 8 * j * ld) = h;
+              *reinterpret_cast<uint2*>(w_lo + at_r + 8 * j * ld) = l;
             }
           }
+        }
+        if (mirror) {
           chain_agree(true);
-          if (symmetric) {
-            // the mirror image of what is strictly below the diagonal: eight rows of a column
-            const int groups = rows >> 3;
-            for (int i = tid; i < groups * kChainTile; i += kChainEpiThreads) {
-              const int col = i / groups, g = i - col * groups;
-              const int c = tn * kChainTile + col, r = tm * kChainTile + r0 + g * 8;
-              if (c >= N || r >= M) continue;
-              const uint32_t take = strictly_below(r, c);
-              if (take == 0u) continue;
+          // eight rows of a column, to the row of that number
+          // (up to four of a warp's lanes next to each other: 64 bytes of a row, and its reads meet in few banks)
+          const int groups = share >> 3, wide = groups < 4 ? 1 : 2;
+#pragma unroll 1
+          for (int i = tid; i < groups * kChainTile; i += kChainEpiThreads) {
+            const int col = (i >> wide) & (kChainTile - 1), g = ((i & ((1 << wide) - 1)) + ((i >> wide) / kChainTile << wide)) * 8;
+            const int row = tn * kChainTile + col;
+            if (row < N && g < row_end) {
               float v[8];
 #pragma unroll
-              for (int q = 0; q < 8; ++q) v[q] = stage[(g * 8 + q) * kChainPitch + col];
+              for (int q = 0; q < 8; ++q) v[q] = stage[(r0 + g + q) * kChainPitch + col];
               uint4 h, l;
               pack_words(v, pre, h, l);
-              store_words(w_hi + c * ld + r, h, take);
-              store_words(w_lo + c * ld + r, l, take);
+              const long long to = (long long)row * ld + tm * kChainTile + r0 + g;
+              *reinterpret_cast<uint4*>(w_hi + to) = h;
+              *reinterpret_cast<uint4*>(w_lo + to) = l;
             }
-            chain_agree(true);
           }
         }
-        if (!ok) break;
+        // (the ring's next user is TMA: the accesses above are put before it)
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ring_bar);
       }
+      if (sliced && (int)blockIdx.x >= units) cluster_sync_all();
     } else if (warp == 8) {
       // ------------------------------------------------------------------ TMA producer
       if (lane == 0) {
+        fence_proxy_async_global();
         const CUtensorMap* a = kind == 0 ? maps.x[cur] : (kind == 1 ? maps.a : (tall ? maps.x[cur] : maps.b));
         const CUtensorMap* b = kind == 0 ? maps.x[cur] : (kind == 1 ? maps.a : (tall ? maps.b : maps.x[cur]));
         bool ok = true;
         for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
           int tm, tn, slice, kb0, kb1;
           unit_of(unit, tm, tn, slice, kb0, kb1);
-          for (int kb = kb0; kb < kb1; ++kb, ++it) {
+          ok = mbar_wait_bounded(ring_bar, (units_done & 1) ^ 1, abort_flag, p.err, kErrProducerEmptyWait);
+          ++units_done;
+          for (int kb = kb0; kb < kb1 && ok; ++kb, ++it) {
             const uint32_t s = it % kChainStages;
             ok = mbar_wait_bounded(&empty_bar[s], ((it / kChainStages) & 1) ^ 1, abort_flag, p.err, kErrProducerEmptyWait);
             if (!ok) break;
@@ -432,6 +448,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
             mbar_wait_clocks(&full_bar[(it - d) % kChainStages], ((it - d) / kChainStages) & 1, kAbortDrainClocks);
       }
       __syncwarp();
+      if (sliced) cluster_sync_all();
     } else {
       // ------------------------------------------------------------------ MMA issuer
       if (lane == 0) {
@@ -463,7 +480,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
               ok = mbar_wait_bounded(&full_bar[s], (it / kChainStages) & 1, abort_flag, p.err, kErrMmaFullWait);
               if (!ok) break;
               tc_fence_after_sync();
-              const uint32_t st = smem_u32(smem + s * kChainStageBytes) >> 4;
+              const uint32_t st = (smem_u32(smem + s * kChainStageBytes) & 0x3FFFFu) >> 4;    // (without the rank in the cluster)
               const uint32_t a_hi = a_lo0 + st, a_lo = a_hi + (kChainWords >> 4);
               const uint32_t b_hi = b_lo0 + st + 2 * (kChainWords >> 4), b_lo = b_hi + (kChainWords >> 4);
 #pragma unroll
@@ -481,6 +498,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
         }
       }
       __syncwarp();
+      if (sliced) cluster_sync_all();
     }
     if (phase + 1 < phases) go = chain_meet(p, ++round, abort_flag);
   }
@@ -497,6 +515,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
     tc_fence_after_sync();
     tmem_dealloc(tmem_base, 512);
   }
+  cluster_sync_all();                                        // (no block ends while another of its cluster may read its sums)
   if (tid == 0 && *abort_flag == 0u) {
     if (atomicAdd(&p.words[1], 1u) == gridDim.x - 1) p.words[0] = p.words[1] = 0u;      // the last one clears both
   }

@@ -80,6 +80,19 @@ __device__ __forceinline__ void pack_words(const float (&v)[8], float pre, uint4
   split_two(v[4] * pre, v[5] * pre, scale, hi.z, lo.z);
   split_two(v[6] * pre, v[7] * pre, scale, hi.w, lo.w);
 }
+// The same for four elements.
+__device__ __forceinline__ void unpack_words(const uint2& hi, const uint2& lo, float f, float4& v) {
+  const float f_lo = f * kPackInvScale;
+  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&hi.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi.y));
+  const float2 c = __half22float2(*reinterpret_cast<const __half2*>(&lo.x)), d = __half22float2(*reinterpret_cast<const __half2*>(&lo.y));
+  v.x = fmaf(f, a.x, fmaf(f_lo, c.x, v.x)); v.y = fmaf(f, a.y, fmaf(f_lo, c.y, v.y));
+  v.z = fmaf(f, b.x, fmaf(f_lo, d.x, v.z)); v.w = fmaf(f, b.y, fmaf(f_lo, d.y, v.w));
+}
+__device__ __forceinline__ void pack_words(const float4& v, float pre, uint2& hi, uint2& lo) {
+  const float scale = pow2f(kPackScaleExp);
+  split_two(v.x * pre, v.y * pre, scale, hi.x, lo.x);
+  split_two(v.z * pre, v.w * pre, scale, hi.y, lo.y);
+}
 // Eight words to `at`, or those of them that `take` has a bit for.
 __device__ __forceinline__ void store_words(uint16_t* at, const uint4& w, uint32_t take) {
   if (take == 0xFFu) {
@@ -120,6 +133,22 @@ __device__ __forceinline__ void store_eight(float* y, const float* k, float scal
 #pragma unroll
     for (int q = 0; q < 8; ++q)
       if (q < left) y[q] = k ? fmaf(keep, k[q], v[q]) : v[q];
+  }
+}
+
+__device__ __forceinline__ void store_four(float* y, const float* k, float scale, float keep, bool vec, int left, float4 v) {
+  v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
+  if (vec && left >= 4) {
+    if (k) {
+      const float4 old = *reinterpret_cast<const float4*>(k);
+      v.x = fmaf(keep, old.x, v.x); v.y = fmaf(keep, old.y, v.y); v.z = fmaf(keep, old.z, v.z); v.w = fmaf(keep, old.w, v.w);
+    }
+    *reinterpret_cast<float4*>(y) = v;
+  } else {
+    y[0] = k ? fmaf(keep, k[0], v.x) : v.x;
+    if (left > 1) y[1] = k ? fmaf(keep, k[1], v.y) : v.y;
+    if (left > 2) y[2] = k ? fmaf(keep, k[2], v.z) : v.z;
+    if (left > 3) y[3] = k ? fmaf(keep, k[3], v.w) : v.w;
   }
 }
 
