@@ -26,10 +26,27 @@ struct LookupParams {
 };
 constexpr int kLookupThreads = 128, kLookupItems = 4;
 
-// A block copies a piece of a row: 16-byte vectors or (rows that are not on 16-byte boundaries) single elements.
+// 16 bytes from an address that is a multiple of the element's size: the 4-byte words that hold them (each holds a byte of
+// them, so none lies outside what may be read), shifted.
+template <typename T>
+__device__ __forceinline__ uint4 load_shifted(const T* at) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(at);
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(a & ~uintptr_t(3));
+  uint4 v = make_uint4(__ldg(w), __ldg(w + 1), __ldg(w + 2), __ldg(w + 3));
+  if (sizeof(T) == 2 && (a & 2)) {
+    const uint32_t x = __ldg(w + 4);
+    v.x = __funnelshift_r(v.x, v.y, 16); v.y = __funnelshift_r(v.y, v.z, 16);
+    v.z = __funnelshift_r(v.z, v.w, 16); v.w = __funnelshift_r(v.w, x, 16);
+  }
+  return v;
+}
+
+// A block copies a piece of a row in 16-byte vectors; where the two rows do not meet 16-byte boundaries at the same
+// columns (VEC false) these lie on Y's boundaries, their source comes in 4-byte words, and what is left of the row at both
+// ends goes by elements.  (All of it by elements: 30001 x 1001 FP16 40 us.)
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kLookupThreads) embedding_kernel(LookupParams p) {
-  constexpr int V = VEC ? Elem<T>::kVec : 1, U = kLookupItems;
+  constexpr int V = Elem<T>::kVec, U = kLookupItems;
   for (long long unit = blockIdx.x; unit < p.rows * p.pieces; unit += gridDim.x) {
     const long long row = p.pieces == 1 ? unit : unit / p.pieces;
     const int c0 = (int)(unit - row * p.pieces) * (kLookupThreads * V * U) + threadIdx.x * V;
@@ -56,24 +73,36 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_kernel(LookupParams 
         *reinterpret_cast<uint4*>(dst + c) = Elem<T>::pack(e);
       }
     } else {
-      T raw[U];
+      const int head = min(p.cols, (int)((16 - (reinterpret_cast<uintptr_t>(dst) & 15)) % 16 / sizeof(T)));
+      const int end = head + (p.cols - head) / V * V;
+      uint4 raw[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * kLookupThreads;
-        if (inside && c < p.cols) raw[u] = src[c];
+        const int c = head + c0 + u * kLookupThreads * V;
+        if (inside && c < end) raw[u] = load_shifted(src + c);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * kLookupThreads;
-        if (c < p.cols) dst[c] = Elem<T>::put(inside ? Elem<T>::get(raw[u]) * p.scale : none);
+        const int c = head + c0 + u * kLookupThreads * V;
+        if (c >= end) break;
+        float e[V];
+        Elem<T>::unpack(raw[u], e);
+#pragma unroll
+        for (int q = 0; q < V; ++q) e[q] = inside ? e[q] * p.scale : none;
+        *reinterpret_cast<uint4*>(dst + c) = Elem<T>::pack(e);
+      }
+      if (c0 < kLookupThreads * V) {                         // the row's first piece: both ends
+        const int i = threadIdx.x, c = i < head ? i : end + i - head;
+        if (c < p.cols) dst[c] = Elem<T>::put(inside ? Elem<T>::get(src[c]) * p.scale : none);
       }
     }
   }
 }
 
 // ------------------------------------------------------------------------------------------ sorting
-constexpr int kSortThreads = 256, kSortItems = 8, kSortTile = kSortThreads * kSortItems;
-constexpr int kSortBits = 8, kSortBins = 1 << kSortBits;
+constexpr int kSortThreads = 512, kSortItems = 4, kSortTile = kSortThreads * kSortItems;
+constexpr int kSortBits = 9, kSortBins = 1 << kSortBits;        // two passes for vocabularies up to 2^18
+static_assert(kSortThreads == kSortBins, "a thread has a digit");
 
 struct SortParams {
   int n, vocab, passes;
@@ -95,16 +124,15 @@ __device__ __forceinline__ bool sort_meet(const SortParams& p, unsigned int roun
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    __threadfence();
-    atomicAdd(&p.words[0], 1u);
+    __threadfence();                                           // the block's stores, which the barrier has put before this
+    asm volatile("red.relaxed.gpu.global.add.u32 [%0], %1;" ::"l"(&p.words[0]), "r"(1u) : "memory");
     const unsigned int want = round * gridDim.x;
     const long long t0 = clock64();
     unsigned int seen = 0;
     ok = 1u;
     while (true) {
-      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(&p.words[0]) : "memory");
+      asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(&p.words[0]) : "memory");
       if (seen >= want) break;
-      __nanosleep(32);
       if (clock64() - t0 > kWaitLimitClocks) {
         atomicExch(p.err, (unsigned int)kErrSortWait);
         ok = 0u;
@@ -117,7 +145,7 @@ __device__ __forceinline__ bool sort_meet(const SortParams& p, unsigned int roun
   return ok != 0u;
 }
 
-// Stable sort of (token, row) by token, 8 bits a pass from the lowest.  A block has a run of whole tiles; in a pass it counts
+// Stable sort of (token, row) by token, 9 bits a pass from the lowest.  A block has a run of whole tiles; in a pass it counts
 // its digits, meets the others, adds up for every digit what lies before its own first one, and
 // moves its items in order.  Tokens outside [0, vocab) get the key `vocab` and end up behind all others.
 __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortParams p) {
@@ -143,16 +171,28 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortParams p)
     };
     base[t] = 0;
     __syncthreads();
-    for (int i = first + t; i < last; i += kSortThreads) atomicAdd(&base[(key_of(i) >> shift) & (kSortBins - 1)], 1);
+    for (int i = first + t; i < last; i += kSortTile) {
+      int key[kSortItems];
+#pragma unroll
+      for (int u = 0; u < kSortItems; ++u) key[u] = i + u * kSortThreads < last ? key_of(i + u * kSortThreads) : -1;
+#pragma unroll
+      for (int u = 0; u < kSortItems; ++u)
+        if (key[u] >= 0) atomicAdd(&base[(key[u] >> shift) & (kSortBins - 1)], 1);
+    }
     __syncthreads();
     p.hist[blockIdx.x * kSortBins + t] = base[t];
     if (!sort_meet(p, ++round)) return;
     // thread t: digit t's items in the blocks before this one, and in all of them
     int before = 0, all = 0;
-    for (int b = 0; b < (int)gridDim.x; ++b) {
-      const int c = __ldcg(p.hist + b * kSortBins + t);
-      before += b < (int)blockIdx.x ? c : 0;
-      all += c;
+    for (int b0 = 0; b0 < (int)gridDim.x; b0 += 8) {
+      int c[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) c[u] = b0 + u < (int)gridDim.x ? __ldcg(p.hist + (b0 + u) * kSortBins + t) : 0;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        before += b0 + u < (int)blockIdx.x ? c[u] : 0;
+        all += c[u];
+      }
     }
     int incl = all;
     for (int x = 1; x < 32; x *= 2) {
@@ -165,7 +205,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortParams p)
     base[t] = incl - all + before;
     __syncthreads();
     for (int tile = first; tile < last; tile += kSortTile) {
-      // a warp has 256 items in a row, 32 at a time; an item's place among the warp's of its digit
+      // a warp has 128 items in a row, 32 at a time; an item's place among the warp's of its digit
       int key[kSortItems], place[kSortItems];
       for (int i = lane; i < kSortBins; i += 32) warp_hist[warp][i] = 0;
       __syncwarp();
@@ -236,7 +276,8 @@ __host__ __device__ constexpr int grad_columns() { return kGradThreads * Elem<T>
 // Column of the thread's element q in its tile: consecutive ones where rows take vectors, else one in 128.
 template <typename T, bool VEC>
 __device__ __forceinline__ int grad_column(int tile, int q) {
-  return tile * grad_columns<T>() + (VEC ? (int)threadIdx.x * Elem<T>::kVec + q : q * kGradThreads + (int)threadIdx.x);
+  const int t = (int)threadIdx.x % kGradThreads;
+  return tile * grad_columns<T>() + (VEC ? t * Elem<T>::kVec + q : q * kGradThreads + t);
 }
 template <typename T, bool VEC>
 __device__ __forceinline__ void store_grad(const TableGradParams& p, int token, int tile, const float (&acc)[Elem<T>::kVec]) {
@@ -347,28 +388,42 @@ __global__ void __launch_bounds__(kGradThreads) table_grad_kernel(TableGradParam
   leave(last < p.n && __ldg(p.key + last) == run);
 }
 
-// Runs that reach over pieces: the block of the piece in which one begins adds the parts of the others, in order.
+// Runs that reach over pieces: the block of the piece in which one begins adds the parts of the others, in order, eight loads
+// at a time.  (Eight groups of threads with an eighth of the parts each, or eight pieces a block, are faster for a token in 2000
+// of 30001 rows, 26 us as a plain loop, and slower where no token is in that many: 8192 rows 15 us where this takes 7.)
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kGradThreads) table_grad_join_kernel(TableGradParams p) {
   constexpr int V = Elem<T>::kVec;
   const int piece = (int)(blockIdx.x / p.tiles), tile = (int)(blockIdx.x - (unsigned)piece * p.tiles);
   const int first = piece * p.piece, last = first + p.piece;
   if (last >= p.n) return;
-  const int run = __ldg(p.key + last - 1);
-  if (run >= p.vocab || __ldg(p.key + last) != run) return;                            // ends here
-  if (first > 0 && __ldg(p.key + first) == run && __ldg(p.key + first - 1) == run) return;   // begun before
+  const int run = __ldg(p.key + last - 1), next = __ldg(p.key + last), start = __ldg(p.key + first);
+  const int before = first > 0 ? __ldg(p.key + first - 1) : -1;
+  if (run >= p.vocab || next != run || (start == run && before == run)) return;        // ends here, or begun before
+  int end = piece + 1;                                                                 // behind the pieces that find it begun
+  while (true) {
+    const int i = end + (int)threadIdx.x;
+    const int found = __syncthreads_count(i < p.pieces && __ldg(p.key + (long long)i * p.piece) == run);
+    end += found;
+    if (found < kGradThreads) break;
+  }
   float acc[V];
+  int col[V];
 #pragma unroll
   for (int q = 0; q < V; ++q) {
-    const int c = grad_column<T, VEC>(tile, q);
-    acc[q] = c < p.cols ? p.part[(2ll * piece + 1) * p.ldp + c] : 0.f;
+    col[q] = grad_column<T, VEC>(tile, q);
+    acc[q] = col[q] < p.cols ? p.part[(2ll * piece + 1) * p.ldp + col[q]] : 0.f;
   }
-  for (int i = piece + 1; i < p.pieces && __ldg(p.key + (long long)i * p.piece) == run; ++i) {
+  for (int i0 = piece + 1; i0 < end; i0 += 8) {
+    float part[8][V];
 #pragma unroll
-    for (int q = 0; q < V; ++q) {
-      const int c = grad_column<T, VEC>(tile, q);
-      if (c < p.cols) acc[q] += p.part[2ll * i * p.ldp + c];
-    }
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int q = 0; q < V; ++q) part[u][q] = i0 + u < end && col[q] < p.cols ? p.part[2ll * (i0 + u) * p.ldp + col[q]] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int q = 0; q < V; ++q) acc[q] += part[u][q];
   }
   store_grad<T, VEC>(p, run, tile, acc);
 }
@@ -385,7 +440,7 @@ bool bad_scale(float s) { return !std::isfinite(s); }
 
 template <typename T>
 int launch_lookup(sgemm_cube_ctx* h, sgc::LookupParams p, bool vec, cudaStream_t st) {
-  const int span = sgc::kLookupThreads * sgc::kLookupItems * (vec ? sgc::Elem<T>::kVec : 1);
+  const int span = sgc::kLookupThreads * sgc::kLookupItems * sgc::Elem<T>::kVec;
   p.pieces = (p.cols + span - 1) / span;
   const long long units = p.rows * p.pieces, cap = 0x7FFFFFFF;
   const unsigned blocks = (unsigned)(units < cap ? units : cap);

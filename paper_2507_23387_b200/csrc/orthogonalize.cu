@@ -225,18 +225,19 @@ int run_products(sgemm_cube_ctx* h, const OrthogonalizeCall& c) {
   return SGEMM_CUBE_OK;
 }
 
-// Which matrices take the one launch: its tiles of 128 x 128 have no next tile's products to hide their epilogue behind, so it
-// loses to the larger kernel where that one is busy for long.
-bool takes_chain(int n, int m) { return n <= 1536 && (long long)n * m <= (1ll << 22); }
+// Which matrices take the one launch: its tiles of 128 x 128 fetch twice as many bytes for a product as the larger kernel's pairs and
+// have no next tile's products to hide their epilogue behind.  Five steps, one launch and a launch a product: 128 x 384 133 and
+// 318 us, 2048 x 512 187 and 523, 1024 x 8192 767 and 933, 2048 x 2048 664 and 820; 3000 x 3000 2416 and 2036.
+bool takes_chain(int n, int m) { return (double)n * n * m <= 1.2e10; }
 
 // Slices of a product's tiles in a grid of clusters, and about how many clocks the product then takes: 1300 for a stage, 4000
 // until the first sums are there, 900 for two rows of a thread and 1500 for the meeting of a cluster.
 long long chain_split(long long tiles, int K, int blocks, int cluster, sgc::ChainSplit* split) {
   const int stages = (K + sgc::kChainBK - 1) / sgc::kChainBK;
   long long least = 0;
-  for (int s = 1; s <= cluster && s <= stages; s *= 2) {
+  for (int s = 1; s <= cluster; s *= 2) {
     const int per = (stages + s - 1) / s;
-    if (s > 1 && (tiles * s > blocks || (stages + per - 1) / per != s)) continue;      // (no slice may be empty)
+    if (s > 1 && tiles * s > blocks) continue;
     const long long turns = (tiles * s + blocks - 1) / blocks;
     const long long clocks = turns * (4000 + per * 1300ll + (s < 4 ? 4 / s : 1) * 1300ll) + (s > 1 ? 1500 : 0);
     if (s == 1 || clocks < least) { least = clocks; *split = sgc::ChainSplit{(int)tiles, s, per}; }

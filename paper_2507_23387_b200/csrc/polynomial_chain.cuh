@@ -115,6 +115,11 @@ __device__ __forceinline__ bool chain_meet(const ChainParams& p, unsigned int ro
   return *abort_flag == 0u;
 }
 
+// All threads of the cluster meet, warp by warp (the barrier wants whole warps).
+__device__ __forceinline__ void chain_cluster_meet() {
+  __syncwarp();
+  cluster_sync_all();
+}
 // Four floats of shared memory of a block of the cluster.
 __device__ __forceinline__ float4 load_peer(uint32_t addr) {
   float4 v;
@@ -296,12 +301,13 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
           __syncwarp();
           if (lane == 0) mbar_arrive(&tempty_bar[r]);
         }
-        if (ok) {
+        const bool empty = kb0 >= kb1;                       // a slice behind the end: its block finishes rows all the same
+        if (ok && !empty) {
           ok = mbar_wait_bounded(&tfull_bar[2], units_done & 1, abort_flag, p.err, kErrEpiTmemFullWait);
           ok = __all_sync(0xffffffffu, ok);
         }
-        ++units_done;
-        if (ok) {
+        if (!empty) ++units_done;
+        if (ok && !empty) {
           tc_fence_after_sync();
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
@@ -315,7 +321,12 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
           __syncwarp();
           if (lane == 0) mbar_arrive(&tempty_bar[2]);
         }
-        if (ok) {
+        if (empty) {
+          float4* out = reinterpret_cast<float4*>(stage) + tid;
+#pragma unroll 1
+          for (int i = 0; i < kChainTile * kChainPitch / 4; i += kChainEpiThreads)
+            if (i + tid < kChainTile * kChainPitch / 4) out[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        } else if (ok) {
           float* out = stage + (quarter * 32 + lane) * kChainPitch + half * 64;
 #pragma unroll
           for (int c = 0; c < 64; c += 4) *reinterpret_cast<float4*>(out + c) = make_float4(S[c], S[c + 1], S[c + 2], S[c + 3]);
@@ -340,7 +351,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
           }
         };
         ask(lr, at_r);
-        if (sliced) cluster_sync_all();
+        if (sliced) chain_cluster_meet();
         ok = chain_agree(ok);
         if (!ok) break;
         const uint32_t first_peer = cluster_ctarank() & ~(uint32_t)(split.slices - 1);
@@ -411,9 +422,9 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
         // (the ring's next user is TMA: the accesses above are put before it)
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(ring_bar);
+        if (lane == 0 && !empty) mbar_arrive(ring_bar);
       }
-      if (sliced && (int)blockIdx.x >= units) cluster_sync_all();
+      if (sliced && (int)blockIdx.x >= units) chain_cluster_meet();
     } else if (warp == 8) {
       // ------------------------------------------------------------------ TMA producer
       if (lane == 0) {
@@ -424,6 +435,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
         for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
           int tm, tn, slice, kb0, kb1;
           unit_of(unit, tm, tn, slice, kb0, kb1);
+          if (kb0 >= kb1) break;
           ok = mbar_wait_bounded(ring_bar, (units_done & 1) ^ 1, abort_flag, p.err, kErrProducerEmptyWait);
           ++units_done;
           for (int kb = kb0; kb < kb1 && ok; ++kb, ++it) {
@@ -447,8 +459,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
           for (uint32_t d = 1; d <= kChainStages && d <= it; ++d)
             mbar_wait_clocks(&full_bar[(it - d) % kChainStages], ((it - d) / kChainStages) & 1, kAbortDrainClocks);
       }
-      __syncwarp();
-      if (sliced) cluster_sync_all();
+      if (sliced) chain_cluster_meet();
     } else {
       // ------------------------------------------------------------------ MMA issuer
       if (lane == 0) {
@@ -466,6 +477,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
         for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x, ++units_done) {
           int tm, tn, slice, kb0, kb1;
           unit_of(unit, tm, tn, slice, kb0, kb1);
+          if (kb0 >= kb1) break;
           const uint32_t d_x = tmem_base + 2 * kChainTile;
           for (int c0 = kb0; c0 < kb1 && ok; c0 += p.chunk, ++chunks_done) {
             const uint32_t r = chunks_done & 1, d_main = tmem_base + r * kChainTile;
@@ -497,8 +509,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
           if (ok) umma_commit(&tfull_bar[2]);
         }
       }
-      __syncwarp();
-      if (sliced) cluster_sync_all();
+      if (sliced) chain_cluster_meet();
     }
     if (phase + 1 < phases) go = chain_meet(p, ++round, abort_flag);
   }
@@ -515,7 +526,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
     tc_fence_after_sync();
     tmem_dealloc(tmem_base, 512);
   }
-  cluster_sync_all();                                        // (no block ends while another of its cluster may read its sums)
+  chain_cluster_meet();                                      // (no block ends while another of its cluster may read its sums)
   if (tid == 0 && *abort_flag == 0u) {
     if (atomicAdd(&p.words[1], 1u) == gridDim.x - 1) p.words[0] = p.words[1] = 0u;      // the last one clears both
   }
