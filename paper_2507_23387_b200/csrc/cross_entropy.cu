@@ -16,28 +16,6 @@ namespace sgc {
 
 constexpr int kFormLossKM = form_of(kFormKM, kEpiLoss), kFormLossKK = form_of(kFormKK, kEpiLoss);
 
-// The pairs of logits that are there already (few rows: the linear layer's own forms wrote them).  A warp takes 64
-// columns of a row, two a lane.
-__global__ void __launch_bounds__(256)
-logit_parts_kernel(int rows, int vocab, const float* __restrict__ Z, long long ldz, const long long* __restrict__ targets,
-                   float* __restrict__ target_logit, float2* __restrict__ parts, long long ldp) {
-  const int lane = threadIdx.x & 31;
-  const int per_row = (vocab + kLossColumns - 1) / kLossColumns;
-  const long long total = (long long)rows * per_row;
-  for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < total; w += (long long)gridDim.x * 8) {
-    const long long r = w / per_row;
-    const int piece = (int)(w - r * per_row), c = piece * kLossColumns + lane * 2;
-    const float* z = Z + r * ldz + c;
-    float v[2];
-    v[0] = c < vocab ? z[0] : -INFINITY;
-    v[1] = c + 1 < vocab ? z[1] : -INFINITY;
-    const long long t = targets[r];
-    if (t >= c && t < c + 2 && t < vocab) target_logit[r] = v[t - c];
-    const float2 part = softmax_part(v, 32);
-    if (lane == 0) parts[r * ldp + piece] = part;
-  }
-}
-
 struct LossJoinParams {
   int rows, vocab, per_row;
   const float2* parts;
@@ -47,52 +25,128 @@ struct LossJoinParams {
   float* loss;              // or null
   float* lse;               // or null
   float2* stats;            // (m, 1 / sum) of a row, or null
+  const float* dloss;       // with the words below: the exponent of dz' words, |dz| <= |dloss| of a row with a target
+  unsigned int* range;      // {largest so far, blocks that are through}, zero between calls
+  int* exp;
+  unsigned int* counts;     // cleared for the gradient's kernel, or null
+  int n_counts;
 };
+// lse and loss of a row from its (largest, sum).  loss = (m - z_t) + log sum: the difference of two logits keeps its digits,
+// whatever their size.
+__device__ __forceinline__ void finish_row(const LossJoinParams& p, long long r, float2 acc, float target_logit) {
+  const bool none = acc.x == -INFINITY && acc.y == 0.f;              // no logit above -inf
+  const float log_sum = logf(acc.y);
+  const long long t = p.targets[r];
+  float loss = 0.f;
+  if (t >= p.vocab) loss = NAN;
+  else if (t >= 0) loss = none ? INFINITY : (acc.x - target_logit) + log_sum;
+  if (p.loss) p.loss[r] = loss;
+  if (p.lse) p.lse[r] = none ? -INFINITY : acc.x + log_sum;
+  if (p.stats) p.stats[r] = make_float2(none ? 0.f : acc.x, none ? 0.f : 1.f / acc.y);
+}
 __device__ __forceinline__ float2 join_parts(float2 a, float2 b) {
   const float m = fmaxf(a.x, b.x);
   if (m == -INFINITY) return make_float2(m, a.y + b.y);              // both 0, or NaN
   return make_float2(m, a.y * expf(a.x - m) + b.y * expf(b.x - m));
 }
-// lse and loss of a row from its pairs; a block a row.  The pairs of a thread are joined in their order, the threads' in
-// a fixed tree.  loss = (m - z_t) + log sum: the difference of two logits keeps its digits, whatever their size.
-__global__ void __launch_bounds__(128) loss_join_kernel(LossJoinParams p) {
-  const long long r = blockIdx.x;
-  float2 acc = make_float2(-INFINITY, 0.f);
-  for (int i = threadIdx.x; i < p.per_row; i += 128) acc = join_parts(acc, p.parts[r * p.ldp + i]);
+// A block's (largest, sum), in thread 0: the threads' in a fixed tree.
+template <int WARPS>
+__device__ __forceinline__ float2 join_block(float2 acc) {
   for (int x = 16; x > 0; x >>= 1) {
     const float2 o = make_float2(__shfl_xor_sync(0xffffffffu, acc.x, x), __shfl_xor_sync(0xffffffffu, acc.y, x));
     acc = join_parts(acc, o);
   }
-  __shared__ float2 warp_part[4];
+  __shared__ float2 warp_part[WARPS];
   if ((threadIdx.x & 31) == 0) warp_part[threadIdx.x >> 5] = acc;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 4; ++w) acc = join_parts(acc, warp_part[w]);
-    const bool none = acc.x == -INFINITY && acc.y == 0.f;            // no logit above -inf
-    const float log_sum = logf(acc.y);
-    const long long t = p.targets[r];
-    float loss = 0.f;
-    if (t >= p.vocab) loss = NAN;
-    else if (t >= 0) loss = none ? INFINITY : (acc.x - p.target_logit[r]) + log_sum;
-    if (p.loss) p.loss[r] = loss;
-    if (p.lse) p.lse[r] = none ? -INFINITY : acc.x + log_sum;
-    if (p.stats) p.stats[r] = make_float2(none ? 0.f : acc.x, none ? 0.f : 1.f / acc.y);
+  if (threadIdx.x == 0)
+    for (int w = 1; w < WARPS; ++w) acc = join_parts(acc, warp_part[w]);
+  return acc;
+}
+
+// lse and loss of a row from its pairs: a block a row, or (WARP) a warp a row where there are few pairs.  A thread joins its pairs
+// in their order.
+template <bool WARP>
+__global__ void __launch_bounds__(128) loss_join_kernel(LossJoinParams p) {
+  constexpr int T = WARP ? 32 : 128;
+  const int t = threadIdx.x % T;
+  if (p.counts)
+    for (int i = blockIdx.x * 128 + threadIdx.x; i < p.n_counts; i += gridDim.x * 128) p.counts[i] = 0u;
+  const long long r = WARP ? (long long)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+  float2 acc = make_float2(-INFINITY, 0.f);
+  if (r < p.rows)
+    for (int i0 = t; i0 < p.per_row; i0 += 4 * T) {
+      float2 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = i0 + u * T < p.per_row ? p.parts[r * p.ldp + i0 + u * T] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) acc = join_parts(acc, v[u]);
+    }
+  if constexpr (WARP) {
+    for (int x = 16; x > 0; x >>= 1)
+      acc = join_parts(acc, make_float2(__shfl_xor_sync(0xffffffffu, acc.x, x), __shfl_xor_sync(0xffffffffu, acc.y, x)));
+  } else {
+    acc = join_block<4>(acc);
+  }
+  if (t == 0 && r < p.rows) finish_row(p, r, acc, p.target_logit[r]);
+  if (p.exp) {
+    uint32_t m = t == 0 && r < p.rows && p.targets[r] >= 0 ? finite_bits(p.dloss[r]) : 0u;
+    if constexpr (WARP) {
+      __shared__ uint32_t most[4];
+      if (t == 0) most[threadIdx.x >> 5] = m;
+      __syncthreads();
+      m = max(max(most[0], most[1]), max(most[2], most[3]));
+    }
+    if (threadIdx.x == 0) {
+      if (m) atomicMax(&p.range[0], m);
+      __threadfence();
+      if (atomicAdd(&p.range[1], 1u) == gridDim.x - 1) {             // the last block: the exponent, and zeros for the next call
+        __threadfence();
+        *p.exp = pack_exponent(atomicExch(&p.range[0], 0u));
+        atomicExch(&p.range[1], 0u);
+      }
+    }
   }
 }
 
-// The exponent of dz' words: |dz| <= |dloss| of a row with a target.  One block.
-__global__ void __launch_bounds__(1024)
-loss_exponent_kernel(int rows, const float* __restrict__ dloss, const long long* __restrict__ targets, int* exp) {
-  uint32_t m = 0;
-  for (int r = threadIdx.x; r < rows; r += 1024)
-    if (targets[r] >= 0) m = max(m, finite_bits(dloss[r]));
-  m = __reduce_max_sync(0xffffffffu, m);
-  __shared__ uint32_t warp_max[32];
-  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = m;
-  __syncthreads();
-  if (threadIdx.x < 32) {
-    m = __reduce_max_sync(0xffffffffu, warp_max[threadIdx.x]);
-    if (threadIdx.x == 0) *exp = pack_exponent(m);
+// The same from logits that are there already (few rows: the linear layer's own forms wrote them, they are in L2): a
+// cluster of blocks has a row, and its first block joins their pairs.  Rows start on 16 bytes.
+constexpr int kRowThreads = 256;
+__global__ void __launch_bounds__(kRowThreads) loss_rows_kernel(LossJoinParams p, const float* __restrict__ Z, long long ldz) {
+  __shared__ float2 pairs[8];                                        // of the cluster's blocks, in the first
+  const int ranks = (int)cluster_size(), rank = (int)cluster_ctarank();
+  const long long r = blockIdx.x / ranks;
+  const float4* z = reinterpret_cast<const float4*>(Z + r * ldz);
+  float2 acc = make_float2(-INFINITY, 0.f);
+  constexpr int U = 4;
+  const int quads = (p.vocab + 3) / 4, step = ranks * kRowThreads;
+  for (int i0 = rank * kRowThreads + threadIdx.x; i0 < quads; i0 += U * step) {
+    float v[4 * U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * step;
+      float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      if (i < quads) q = z[i];
+      const int left = p.vocab - 4 * i;                              // (what stands behind the row's end is not looked at)
+      v[4 * u] = q.x;
+      v[4 * u + 1] = left > 1 ? q.y : -INFINITY;
+      v[4 * u + 2] = left > 2 ? q.z : -INFINITY;
+      v[4 * u + 3] = left > 3 ? q.w : -INFINITY;
+    }
+    acc = join_parts(acc, softmax_part(v, 1));
+  }
+  acc = join_block<kRowThreads / 32>(acc);
+  if (threadIdx.x == 0) {
+    const uint32_t at = mapa_u32(smem_u32(&pairs[rank]), 0);
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(acc.x), "f"(acc.y) : "memory");
+  }
+  __syncwarp();
+  cluster_sync_all();
+  if (rank == 0 && threadIdx.x == 0) {
+    acc = pairs[0];
+    for (int k = 1; k < ranks; ++k) acc = join_parts(acc, pairs[k]);
+    const long long t = p.targets[r];
+    finish_row(p, r, acc, t >= 0 && t < p.vocab ? Z[r * ldz + t] : 0.f);
   }
 }
 
@@ -108,38 +162,56 @@ struct LossGradParams {
   long long ldw;
   const int* exp;
   float* col_part;          // [chunks][vocab] column sums of dz, or null
+  unsigned int* counts;     // [blocks in x]: chunks that are there, zero before the launch
+  float* dbias;             // the chunks' sums in their order, added to what is there for the second piece and on
+  int add;
 };
 // dz = dloss (exp(z - m) / sum - 1[t]) of a piece of rows, as words, with its column sums.  A lane has eight columns; the warps
-// of a block take every eighth row of its chunk.  Bound by memory: 8 bytes a logit.
+// of a block take every eighth row of its chunk, and the last block of a column adds the chunks' sums.  Bound by memory: 8 bytes
+// a logit (2048 x 131072 343 us, 6.3 TB/s).
 __global__ void __launch_bounds__(256) loss_grad_kernel(LossGradParams p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = blockIdx.x * 256 + lane * 8;
   const int r_end = min(p.rows, (int)(blockIdx.y + 1) * p.rows_per_chunk);
   const float pre = p.hi ? pow2f(*p.exp) : 1.f;
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int r = blockIdx.y * p.rows_per_chunk + warp; r < r_end; r += 8) {
-    if (c >= p.vocab) break;
-    const float* z = p.Z + (long long)r * p.ldz + c;                 // rows are 8 floats wide at least, zeros behind the end
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(z));
-    const float4 b = __ldcs(reinterpret_cast<const float4*>(z + 4));
-    const float2 st = p.stats[r];
-    const long long t = p.targets[r];
-    float g = t >= 0 ? p.dloss[r] : 0.f;
-    if (t >= p.vocab) g = NAN;
-    const bool none = st.y == 0.f;                                   // nothing is allowed: no gradient
-    const float w = none ? 0.f : g * st.y;
-    float d[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  constexpr int U = 2;
+  for (int r0 = blockIdx.y * p.rows_per_chunk + warp; r0 < r_end && c < p.vocab; r0 += 8 * U) {
+    float4 a[U], b[U];
+    float2 st[U];
+    long long t[U];
+    float g[U];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      d[q] = c + q < p.vocab && t >= 0 ? w * fast_exp2((d[q] - st.x) * kLog2e) : 0.f;
-      if (c + q == t && !none) d[q] -= g;
-      sum[q] += d[q];
+    for (int u = 0; u < U; ++u) {
+      const int r = min(r0 + 8 * u, r_end - 1);
+      const float* z = p.Z + (long long)r * p.ldz + c;               // (rows are 8 floats wide at least)
+      a[u] = __ldcs(reinterpret_cast<const float4*>(z));
+      b[u] = __ldcs(reinterpret_cast<const float4*>(z + 4));
+      st[u] = p.stats[r];
+      t[u] = p.targets[r];
+      g[u] = p.dloss[r];
     }
-    if (p.hi) {
-      uint4 h, l;
-      pack_words(d, pre, h, l);
-      *reinterpret_cast<uint4*>(p.hi + (long long)r * p.ldw + c) = h;
-      *reinterpret_cast<uint4*>(p.lo + (long long)r * p.ldw + c) = l;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + 8 * u;
+      if (r >= r_end) break;
+      float weight = t[u] >= 0 ? g[u] : 0.f;
+      if (t[u] >= p.vocab) weight = NAN;
+      const bool none = st[u].y == 0.f;                              // nothing is allowed: no gradient
+      const float w = none ? 0.f : weight * st[u].y;
+      float d[8] = {a[u].x, a[u].y, a[u].z, a[u].w, b[u].x, b[u].y, b[u].z, b[u].w};
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        d[q] = c + q < p.vocab && t[u] >= 0 ? w * fast_exp2((d[q] - st[u].x) * kLog2e) : 0.f;
+        if (c + q == t[u] && !none) d[q] -= weight;
+        sum[q] += d[q];
+      }
+      if (p.hi) {
+        uint4 h, l;
+        pack_words(d, pre, h, l);
+        *reinterpret_cast<uint4*>(p.hi + (long long)r * p.ldw + c) = h;
+        *reinterpret_cast<uint4*>(p.lo + (long long)r * p.ldw + c) = l;
+      }
     }
   }
   if (p.col_part) {
@@ -153,17 +225,19 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(LossGradParams p) {
       for (int w = 1; w < 8; ++w) s += part[w][threadIdx.x];
       p.col_part[(long long)blockIdx.y * p.vocab + col] = s;
     }
-  }
-}
-
-__global__ void __launch_bounds__(256)
-loss_column_sums_kernel(const float* __restrict__ part, int chunks, int cols, float* __restrict__ out) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
-  float s = part[c];
+    __shared__ bool last;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(&p.counts[blockIdx.x], 1u) == gridDim.y - 1;
+    __syncthreads();
+    if (last && col < p.vocab) {
+      __threadfence();
+      float s = p.add ? p.dbias[col] : 0.f;
 #pragma unroll 8
-  for (int i = 1; i < chunks; ++i) s += part[(long long)i * cols + c];
-  out[c] = s;
+      for (int i = 0; i < (int)gridDim.y; ++i) s += __ldcg(p.col_part + (long long)i * p.vocab + col);
+      p.dbias[col] = s;
+    }
+  }
 }
 
 }  // namespace sgc
@@ -176,7 +250,7 @@ using sgc::PackJob;
 
 constexpr size_t kPieceBytes = (size_t)1 << 30;          // logits of a piece of rows
 constexpr int kPieceRows = 1 << 22;                      // (small vocabularies)
-constexpr int kGradRows = 256;                           // rows of a column sum's part
+constexpr int kGradRows = 256, kGradRowsLeast = 32;      // rows of a column sum's part
 
 int loss_setup(sgemm_cube_ctx* h) {
   return sgc::product_setup<sgc::kFormLossKM, sgc::kFormLossKK>(h, h->loss_clusters);
@@ -202,14 +276,41 @@ int loss_product(sgemm_cube_ctx* h, int M, int N, int K, const Packed& X, const 
   return sgc::run_product<FORM>(h, h->loss_clusters, X, W, p, true, st);
 }
 
-int launch_join(sgemm_cube_ctx* h, int rows, int vocab, const sgc::LossEpilogue& ep, float* loss, float* lse, float2* stats, cudaStream_t st) {
+sgc::LossJoinParams join_params(int rows, int vocab, const sgc::LossEpilogue& ep, float* loss, float* lse) {
   sgc::LossJoinParams j;
+  memset(&j, 0, sizeof(j));
   j.rows = rows; j.vocab = vocab; j.per_row = (vocab + sgc::kLossColumns - 1) / sgc::kLossColumns;
   j.parts = ep.parts; j.ldp = ep.ldp;
   j.targets = ep.targets; j.target_logit = ep.target_logit;
-  j.loss = loss; j.lse = lse; j.stats = stats;
-  sgc::loss_join_kernel<<<(unsigned)rows, 128, 0, st>>>(j);
+  j.loss = loss; j.lse = lse;
+  return j;
+}
+int launch_join(sgemm_cube_ctx* h, const sgc::LossJoinParams& j, cudaStream_t st) {
+  if (j.per_row <= 512) sgc::loss_join_kernel<true><<<(unsigned)((j.rows + 3) / 4), 128, 0, st>>>(j);
+  else sgc::loss_join_kernel<false><<<(unsigned)j.rows, 128, 0, st>>>(j);
   return sgc::launched(h);
+}
+int launch_rows(sgemm_cube_ctx* h, const sgc::LossJoinParams& j, const float* Z, int64_t ldz, cudaStream_t st) {
+  // blocks of a row: pieces of at least 4096 columns, while the SMs have room
+  int ranks = 1;
+  while (ranks < 8 && (long long)j.rows * ranks < 2 * h->sm_count && j.vocab / (2 * ranks) >= 4096) ranks *= 2;
+  for (;; ranks = 1) {                           // clusters that cannot be scheduled: one block a row
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute a;
+    a.id = cudaLaunchAttributeClusterDimension;
+    a.val.clusterDim.x = (unsigned)ranks; a.val.clusterDim.y = 1; a.val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(j.rows * ranks), 1, 1);
+    cfg.blockDim = dim3(sgc::kRowThreads, 1, 1);
+    cfg.stream = st;
+    cfg.attrs = &a;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, sgc::loss_rows_kernel, j, Z, (long long)ldz) == cudaSuccess) break;
+    cudaGetLastError();
+    if (ranks == 1) return SGEMM_CUBE_CUDA_ERROR;
+  }
+  h->launches++;
+  return SGEMM_CUBE_OK;
 }
 
 bool bad_layout(int layout) { return layout != SGEMM_CUBE_WEIGHT_KN && layout != SGEMM_CUBE_WEIGHT_NK; }
@@ -252,19 +353,19 @@ int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K, const sge
   for (int pass = 0; pass < 2; ++pass) {         // sizes first, then pointers
     Carve c;
     c.base = pass ? static_cast<uint8_t*>(h->loss_ws) : nullptr;
-    ep.parts = c.take<float2>((size_t)M * per_row);
-    ep.target_logit = c.take<float>((size_t)M);
-    if (few) Z = c.take<float>((size_t)M * ldz);
+    if (few) {
+      Z = c.take<float>((size_t)M * ldz);
+    } else {
+      ep.parts = c.take<float2>((size_t)M * per_row);
+      ep.target_logit = c.take<float>((size_t)M);
+    }
     if (!pass && (rc = grow(h, &h->loss_ws, &h->loss_ws_bytes, c.used, st))) return rc;
   }
   if (few) {
     // few rows: the layer's kernels for them, whose logits stay in L2
     rc = sgemm_cube_linear(h, M, N, K, X, W, weight_layout, bias, nullptr, 0, SGEMM_CUBE_ACT_NONE, Z, ldz, nullptr, 0, stream);
     if (rc) return rc;
-    sgc::logit_parts_kernel<<<sgc::blocks_for(h, (long long)M * per_row * 32), 256, 0, st>>>(
-        M, N, Z, ldz, ep.targets, ep.target_logit, ep.parts, ep.ldp);
-    if ((rc = sgc::launched(h))) return rc;
-    return launch_join(h, M, N, ep, loss, lse, nullptr, st);
+    return launch_rows(h, join_params(M, N, ep, loss, lse), Z, ldz, st);
   }
   PackJob jobs[2];
   int n_jobs = 0;
@@ -281,7 +382,7 @@ int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K, const sge
   if (n_jobs && (rc = sgc::launch_pack(h, jobs, n_jobs, st))) return rc;
   rc = nk ? loss_product<sgc::kFormLossKK>(h, M, N, K, px, pw, ep, st) : loss_product<sgc::kFormLossKM>(h, M, N, K, px, pw, ep, st);
   if (rc) return rc;
-  return launch_join(h, M, N, ep, loss, lse, nullptr, st);
+  return launch_join(h, join_params(M, N, ep, loss, lse), st);
 }
 
 int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, const sgemm_cube_operand* X,
@@ -316,7 +417,10 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
     const long long pieces = ((long long)M + piece - 1) / piece;
     piece = (int)round_up((size_t)((M + pieces - 1) / pieces), 256);
   }
-  const int chunks = (M + kGradRows - 1) / kGradRows + (M + piece - 1) / piece;     // (every piece rounds up)
+  // rows of a part: enough parts for eight blocks an SM
+  int grad_rows = kGradRows;
+  while (grad_rows > kGradRowsLeast && (long long)((N + 255) / 256) * ((piece + grad_rows - 1) / grad_rows) < 8 * h->sm_count) grad_rows /= 2;
+  const int chunks = (piece + grad_rows - 1) / grad_rows, col_blocks = (N + 255) / 256;
   sgc::LossEpilogue ep;
   memset(&ep, 0, sizeof(ep));
   ep.bias = bias;
@@ -325,6 +429,7 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
   float2* stats = nullptr;
   uint16_t *ghi = nullptr, *glo = nullptr;
   float* col_part = nullptr;
+  unsigned int* counts = nullptr;
   float* target_logit = nullptr;
   for (int pass = 0; pass < 2; ++pass) {         // sizes first, then pointers
     Carve c;
@@ -337,7 +442,10 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
       ghi = c.take<uint16_t>((size_t)piece * ldz);
       glo = c.take<uint16_t>((size_t)piece * ldz);
     }
-    if (dbias) col_part = c.take<float>((size_t)chunks * N);
+    if (dbias) {
+      col_part = c.take<float>((size_t)chunks * N);
+      counts = c.take<unsigned int>((size_t)col_blocks);
+    }
     if (!pass && (rc = grow(h, &h->loss_ws, &h->loss_ws_bytes, c.used, st))) return rc;
   }
   ep.target_logit = target_logit;
@@ -354,32 +462,33 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
     if (!pass && c.used && (rc = grow(h, &h->ws, &h->ws_bytes, c.used, st))) return rc;
   }
   if (n_jobs && (rc = sgc::launch_pack(h, jobs, n_jobs, st))) return rc;
-  if (split) {
-    sgc::loss_exponent_kernel<<<1, 1024, 0, st>>>(M, dloss, reinterpret_cast<const long long*>(targets), exps + 2);
-    if ((rc = sgc::launched(h))) return rc;
-  }
-  int chunk0 = 0;
   for (int r0 = 0; r0 < M; r0 += piece) {
     const int rows = M - r0 < piece ? M - r0 : piece;
     const Packed x{px.hi + (int64_t)r0 * px.ld, px.lo + (int64_t)r0 * px.ld, px.ld, px.exp};
     ep.targets = reinterpret_cast<const long long*>(targets) + r0;
     rc = nk ? loss_product<sgc::kFormLossKK>(h, rows, N, K, x, pw, ep, st) : loss_product<sgc::kFormLossKM>(h, rows, N, K, x, pw, ep, st);
     if (rc) return rc;
-    if ((rc = launch_join(h, rows, N, ep, loss ? loss + r0 : nullptr, lse ? lse + r0 : nullptr, stats, st))) return rc;
+    sgc::LossJoinParams j = join_params(rows, N, ep, loss ? loss + r0 : nullptr, lse ? lse + r0 : nullptr);
+    j.stats = stats;
+    j.dloss = dloss + r0;
+    j.range = h->err_dev + sgc::kRangeWords;
+    j.exp = split ? exps + 2 : nullptr;
+    j.counts = counts; j.n_counts = col_blocks;
+    if ((rc = launch_join(h, j, st))) return rc;
     sgc::LossGradParams p;
     memset(&p, 0, sizeof(p));
-    p.rows = rows; p.vocab = N; p.rows_per_chunk = kGradRows;
+    p.rows = rows; p.vocab = N; p.rows_per_chunk = grad_rows;
     p.Z = ep.Z; p.ldz = ldz;
     p.stats = stats;
     p.dloss = dloss + r0;
     p.targets = ep.targets;
     p.hi = ghi; p.lo = glo; p.ldw = ldz;
     p.exp = exps + 2;
-    p.col_part = dbias ? col_part + (size_t)chunk0 * N : nullptr;
-    const int row_chunks = (rows + kGradRows - 1) / kGradRows;
-    sgc::loss_grad_kernel<<<dim3((unsigned)((N + 255) / 256), (unsigned)row_chunks, 1), 256, 0, st>>>(p);
+    p.col_part = col_part; p.counts = counts;
+    p.dbias = dbias; p.add = r0 > 0;
+    const int row_chunks = (rows + grad_rows - 1) / grad_rows;
+    sgc::loss_grad_kernel<<<dim3((unsigned)col_blocks, (unsigned)row_chunks, 1), 256, 0, st>>>(p);
     if ((rc = sgc::launched(h))) return rc;
-    chunk0 += row_chunks;
     const Packed dz{ghi, glo, ldz, exps + 2};
     sgc::LinearEpilogue le;
     memset(&le, 0, sizeof(le));
@@ -391,10 +500,6 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
               : sgc::linear_product_any(sgc::kFormMM, h, K, N, rows, x, dz, dW, lddw, le, st);
       if (rc) return rc;
     }
-  }
-  if (dbias) {
-    sgc::loss_column_sums_kernel<<<(unsigned)((N + 255) / 256), 256, 0, st>>>(col_part, chunk0, N, dbias);
-    return sgc::launched(h);
   }
   return SGEMM_CUBE_OK;
 }
