@@ -2,7 +2,7 @@
 
 One residual block without attention, everything in FP32, every product on the three-product kernel:
 
-    x  = E[token]                          rows of the embedding (a torch gather)
+    x  = E[token]                          sgemm_cube_embedding
     n  = norm(x; g1, c1)                   sgemm_cube_layer_norm
     h  = gelu(n W1' + b1)                  sgemm_cube_linear, keeping Z = n W1' + b1
     y  = h W2' + b2 + x                    sgemm_cube_linear with the residual
@@ -12,11 +12,15 @@ One residual block without attention, everything in FP32, every product on the t
 
 The loss is -mean(logp) - entropy_weight * mean(entropy) over the rows whose next token is known
 (negative: none).  `Model.gradients` walks the same list backwards through the `_backward` entry points;
-`Model.step` adds plain gradient descent.  Every buffer is made once for the largest batch.  `Sampler` keeps the
+`Model.step` adds plain gradient descent.  Every buffer is made once for the largest batch.  A model with keep_logits=False
+has no room for l: the last two lines and their gradients are one call, sgemm_cube_cross_entropy_backward (no entropy then),
+and `Model.loss` is sgemm_cube_cross_entropy.  With orthogonal=... the step orthogonalises the updates of W1 and W2
+(sgemm_cube_orthogonalize, into the weight).  `Sampler` keeps the
 weights packed and answers the most likely next tokens of a few sequences at a time.  `python -m` of this file
 trains on a fixed random successor table and prints the loss, then what the sampler learned:
 
     python -m paper_2507_23387_b200.lm_step [--tokens 1024] [--width 512] [--hidden 2048] [--vocab 8192] [--steps 60]
+                                            [--no-logits] [--orthogonal 0.02]
 """
 import argparse
 
@@ -30,7 +34,8 @@ NK, GELU = binding.WEIGHT_NK, binding.ACT_GELU
 class Model:
     """Weights, gradients and the buffers of one training step of at most `tokens` rows."""
 
-    def __init__(self, handle, tokens, width, hidden, vocab, seed=0):
+    def __init__(self, handle, tokens, width, hidden, vocab, seed=0, keep_logits=True):
+        self.keep_logits = keep_logits
         self.h, self.device = handle, torch.device("cuda", handle.device)
         g = torch.Generator(device=self.device).manual_seed(seed)
 
@@ -53,48 +58,75 @@ class Model:
 
         self.rows = {                                    # one row a token
             "x": buffer(tokens, width), "n": buffer(tokens, width), "y": buffer(tokens, width), "f": buffer(tokens, width),
-            "z": buffer(tokens, hidden), "a": buffer(tokens, hidden), "l": buffer(tokens, vocab),
+            "z": buffer(tokens, hidden), "a": buffer(tokens, hidden),
             "dx": buffer(tokens, width), "dy": buffer(tokens, width), "da": buffer(tokens, hidden),
             "mean1": buffer(tokens), "rstd1": buffer(tokens), "mean2": buffer(tokens), "rstd2": buffer(tokens),
             "logp": buffer(tokens), "entropy": buffer(tokens), "stats": buffer(tokens, 2),
         }
+        if keep_logits:
+            self.rows["l"] = buffer(tokens, vocab)
 
-    def forward(self, tokens, targets):
-        """Views of the buffers for these rows, filled up to logp, entropy and stats."""
+    def features(self, tokens):
+        """Views of the buffers for these rows, filled up to f."""
         h, w = self.h, self.weights
         r = {k: v[:tokens.numel()] for k, v in self.rows.items()}
-        torch.index_select(w["E"], 0, tokens, out=r["x"])
+        h.sgemm_cube_embedding(tokens, w["E"], r["x"])
         h.sgemm_cube_layer_norm(r["x"], r["n"], w["g1"], w["c1"], mean=r["mean1"], rstd=r["rstd1"])
         h.sgemm_cube_linear(r["n"], w["W1"], r["a"], bias=w["b1"], activation=GELU, preact=r["z"], weight_layout=NK)
         h.sgemm_cube_linear(r["a"], w["W2"], r["y"], bias=w["b2"], residual=r["x"], weight_layout=NK)
         h.sgemm_cube_layer_norm(r["y"], r["f"], w["g2"], w["c2"], mean=r["mean2"], rstd=r["rstd2"])
+        return r
+
+    def forward(self, tokens, targets):
+        """The same up to logp, entropy and stats."""
+        h, w, r = self.h, self.weights, self.features(tokens)
         h.sgemm_cube_linear(r["f"], w["H"], r["l"], weight_layout=NK)
         h.sgemm_cube_token_logprobs(r["l"], targets, r["logp"], entropy=r["entropy"], stats=r["stats"])
         return r
 
+    def loss(self, tokens, targets):
+        """The mean of -logp over the known targets (a tensor of one value), without logits or gradients."""
+        r, known = self.features(tokens), (targets >= 0).float()
+        self.h.sgemm_cube_cross_entropy(r["f"], self.weights["H"], targets, r["logp"], weight_layout=NK)
+        return r["logp"].sum() / known.sum().clamp(min=1.0)
+
     def gradients(self, tokens, targets, entropy_weight=0.0):
         """The loss (a tensor of one value); its gradients of all weights go to self.grads."""
         h, w, g = self.h, self.weights, self.grads
-        r = self.forward(tokens, targets)
         known = (targets >= 0).float()
         share = known / known.sum().clamp(min=1.0)
-        loss = -(share * (r["logp"] + entropy_weight * r["entropy"])).sum()
-        h.sgemm_cube_token_logprobs_backward(r["l"], targets, r["stats"], r["l"], dlogp=-share, entropy=r["entropy"],
-                                             dentropy=-entropy_weight * share)     # in the place of the logits
-        h.sgemm_cube_linear_backward(r["l"], r["f"], w["H"], dX=r["dx"], dW=g["H"], weight_layout=NK)
+        if self.keep_logits:
+            r = self.forward(tokens, targets)
+            loss = -(share * (r["logp"] + entropy_weight * r["entropy"])).sum()
+            h.sgemm_cube_token_logprobs_backward(r["l"], targets, r["stats"], r["l"], dlogp=-share, entropy=r["entropy"],
+                                                 dentropy=-entropy_weight * share)     # in the place of the logits
+            h.sgemm_cube_linear_backward(r["l"], r["f"], w["H"], dX=r["dx"], dW=g["H"], weight_layout=NK)
+        else:
+            assert entropy_weight == 0.0, "the entropy needs the logits"
+            r = self.features(tokens)
+            h.sgemm_cube_cross_entropy_backward(r["f"], w["H"], targets, share, dX=r["dx"], dW=g["H"], loss=r["logp"],
+                                                weight_layout=NK)
+            loss = (share * r["logp"]).sum()
         h.sgemm_cube_layer_norm_backward(r["dx"], r["y"], r["mean2"], r["rstd2"], r["dy"], w["g2"], g["g2"], g["c2"])
         h.sgemm_cube_linear_backward(r["dy"], r["a"], w["W2"], dX=r["da"], dW=g["W2"], dbias=g["b2"], weight_layout=NK)
         h.sgemm_cube_linear_backward(r["da"], r["n"], w["W1"], dX=r["dx"], dW=g["W1"], dbias=g["b1"], preact=r["z"],
                                      activation=GELU, weight_layout=NK)
         h.sgemm_cube_layer_norm_backward(r["dx"], r["x"], r["mean1"], r["rstd1"], r["dx"], w["g1"], g["g1"], g["c1"])
         r["dx"].add_(r["dy"])                                                      # the residual's path round the block
-        g["E"].zero_().index_add_(0, tokens, r["dx"])
+        h.sgemm_cube_embedding_backward(tokens, r["dx"], g["E"])
         return loss
 
-    def step(self, tokens, targets, rate, entropy_weight=0.0):
+    def step(self, tokens, targets, rate, entropy_weight=0.0, orthogonal=0.0, decay=0.0):
+        """One step of gradient descent; with `orthogonal` > 0 the updates of W1 and W2 are that rate times the
+        orthogonalised gradient, behind a decay of the weight."""
         loss = self.gradients(tokens, targets, entropy_weight)
         for k, v in self.weights.items():
-            v.sub_(self.grads[k], alpha=rate)
+            if orthogonal > 0.0 and k in ("W1", "W2"):
+                # singular values of about one, so entries of about rows^-1/2 times this where rows > columns
+                scale = orthogonal * max(1.0, v.shape[0] / v.shape[1]) ** 0.5
+                self.h.sgemm_cube_orthogonalize(self.grads[k], v, scale=-scale, residual=v, beta=1.0 - orthogonal * decay)
+            else:
+                v.sub_(self.grads[k], alpha=rate)
         return loss
 
 
@@ -121,7 +153,7 @@ class Sampler:
         the vocabulary (a row with nothing allowed has log probabilities of -inf)."""
         h, w, p, s = self.h, self.w, self.packed, tokens.numel()
         x, n, a, l = self.x[:s], self.n[:s], self.a[:s], self.l[:s]
-        torch.index_select(w["E"], 0, tokens, out=x)
+        h.sgemm_cube_embedding(tokens, w["E"], x)
         h.sgemm_cube_layer_norm(x, n, w["g1"], w["c1"])
         h.sgemm_cube_linear(n, p["W1"], a, bias=w["b1"], activation=GELU, weight_layout=NK)
         h.sgemm_cube_linear(a, p["W2"], x, bias=w["b2"], residual=x, weight_layout=NK)
@@ -139,14 +171,16 @@ def main():
     for name, value in (("tokens", 1024), ("width", 512), ("hidden", 2048), ("vocab", 8192), ("steps", 60)):
         ap.add_argument("--" + name, type=int, default=value)
     ap.add_argument("--rate", type=float, default=4.0)
+    ap.add_argument("--no-logits", action="store_true", help="the loss and its gradients without room for the logits")
+    ap.add_argument("--orthogonal", type=float, default=0.0, help="rate of orthogonalised updates of W1 and W2")
     args = ap.parse_args()
     h = binding.Handle(0)
-    model = Model(h, args.tokens, args.width, args.hidden, args.vocab)
+    model = Model(h, args.tokens, args.width, args.hidden, args.vocab, keep_logits=not args.no_logits)
     gen = torch.Generator(device=model.device).manual_seed(1)
     successor = torch.randperm(args.vocab, generator=gen, device=model.device)
     tokens = torch.randint(0, args.vocab, (args.tokens,), generator=gen, device=model.device)
     for i in range(args.steps):
-        loss = model.step(tokens, successor[tokens], args.rate)
+        loss = model.step(tokens, successor[tokens], args.rate, orthogonal=args.orthogonal)
         if i % 10 == 0 or i == args.steps - 1:
             print("step %4d  loss %.4f" % (i, float(loss)))
     logp, top = Sampler(model, 8).next(tokens[:8])
