@@ -49,6 +49,17 @@ __device__ __forceinline__ float2 join_parts(float2 a, float2 b) {
   if (m == -INFINITY) return make_float2(m, a.y + b.y);              // both 0, or NaN
   return make_float2(m, a.y * expf(a.x - m) + b.y * expf(b.x - m));
 }
+// The largest |dloss| so far; the last of `blocks` makes the exponent of it and leaves zeros for the next call.
+__device__ __forceinline__ void publish_weight(const LossJoinParams& p, uint32_t m, unsigned int blocks) {
+  if (m) atomicMax(&p.range[0], m);
+  __threadfence();
+  if (atomicAdd(&p.range[1], 1u) == blocks - 1) {
+    __threadfence();
+    *p.exp = pack_exponent(atomicExch(&p.range[0], 0u));
+    atomicExch(&p.range[1], 0u);
+  }
+}
+
 // A block's (largest, sum), in thread 0: the threads' in a fixed tree.
 template <int WARPS>
 __device__ __forceinline__ float2 join_block(float2 acc) {
@@ -97,15 +108,7 @@ __global__ void __launch_bounds__(128) loss_join_kernel(LossJoinParams p) {
       __syncthreads();
       m = max(max(most[0], most[1]), max(most[2], most[3]));
     }
-    if (threadIdx.x == 0) {
-      if (m) atomicMax(&p.range[0], m);
-      __threadfence();
-      if (atomicAdd(&p.range[1], 1u) == gridDim.x - 1) {             // the last block: the exponent, and zeros for the next call
-        __threadfence();
-        *p.exp = pack_exponent(atomicExch(&p.range[0], 0u));
-        atomicExch(&p.range[1], 0u);
-      }
-    }
+    if (threadIdx.x == 0) publish_weight(p, m, gridDim.x);
   }
 }
 
@@ -115,6 +118,8 @@ constexpr int kRowThreads = 256;
 __global__ void __launch_bounds__(kRowThreads) loss_rows_kernel(LossJoinParams p, const float* __restrict__ Z, long long ldz) {
   __shared__ float2 pairs[8];                                        // of the cluster's blocks, in the first
   const int ranks = (int)cluster_size(), rank = (int)cluster_ctarank();
+  if (p.counts)
+    for (int i = blockIdx.x * kRowThreads + threadIdx.x; i < p.n_counts; i += gridDim.x * kRowThreads) p.counts[i] = 0u;
   const long long r = blockIdx.x / ranks;
   const float4* z = reinterpret_cast<const float4*>(Z + r * ldz);
   float2 acc = make_float2(-INFINITY, 0.f);
@@ -147,6 +152,7 @@ __global__ void __launch_bounds__(kRowThreads) loss_rows_kernel(LossJoinParams p
     for (int k = 1; k < ranks; ++k) acc = join_parts(acc, pairs[k]);
     const long long t = p.targets[r];
     finish_row(p, r, acc, t >= 0 && t < p.vocab ? Z[r * ldz + t] : 0.f);
+    if (p.exp) publish_weight(p, t >= 0 ? finite_bits(p.dloss[r]) : 0u, (unsigned)p.rows);
   }
 }
 
@@ -154,6 +160,7 @@ struct LossGradParams {
   int rows, vocab, rows_per_chunk;
   const float* Z;
   long long ldz;
+  float* dz;                // dz in FP32 too, in the place of Z, or null
   const float2* stats;
   const float* dloss;
   const long long* targets;
@@ -206,6 +213,11 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(LossGradParams p) {
         if (c + q == t[u] && !none) d[q] -= weight;
         sum[q] += d[q];
       }
+      if (p.dz) {
+        float* out = p.dz + (long long)r * p.ldz + c;
+        *reinterpret_cast<float4*>(out) = make_float4(d[0], d[1], d[2], d[3]);
+        *reinterpret_cast<float4*>(out + 4) = make_float4(d[4], d[5], d[6], d[7]);
+      }
       if (p.hi) {
         uint4 h, l;
         pack_words(d, pre, h, l);
@@ -238,6 +250,87 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(LossGradParams p) {
       p.dbias[col] = s;
     }
   }
+}
+
+// dX for few rows and an FP32 weight stored outputs x inputs: dX[m, k] = sum over n of dz[m, n] W[n, k], in FP32.  The weight's
+// rows stream past the few rows of dz once, and the long sum over the vocabulary is shared by many blocks: a block has 128
+// columns of k and a run of n, a warp four rows of W in every 32, a lane four columns; the blocks' sums are added in order.
+// Bound by memory: 4 bytes an entry of W for up to 16 rows (arithmetic: 32 FMA a byte and 16 rows, half of what the SMs have).
+// (The linear layer's form for few rows shares a sum among 8 blocks at most: one row of 65536 x 1024 230 us of the call's 471.)
+constexpr int kSumRows = 256, kSumMost = 16;             // rows of W between two loads of dz; rows of dz
+template <int MR, bool VEC>
+__global__ void __launch_bounds__(256)
+weighted_rows_kernel(int M, int N, int K, const float* __restrict__ dz, long long ldz, const float* __restrict__ W, long long ldw, int run,
+                     float* __restrict__ part) {
+  __shared__ __align__(16) float d[MR][kSumRows];
+  __shared__ __align__(16) float sums[8][4][128];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x * 128;
+  const int n_first = (int)min((long long)N, (long long)blockIdx.y * run), n_end = (int)min((long long)N, (long long)(blockIdx.y + 1) * run);
+  int col[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) col[q] = c0 + (VEC ? lane * 4 + q : q * 32 + lane);
+  float acc[MR][4];
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc[m][q] = 0.f;
+  for (int n0 = n_first; n0 < n_end; n0 += kSumRows) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < MR * kSumRows; i += 256) {
+      const int m = i / kSumRows, n = n0 + i % kSumRows;
+      d[m][i % kSumRows] = m < M && n < n_end ? dz[m * ldz + n] : 0.f;
+    }
+    __syncthreads();
+    const int rows = min(kSumRows, n_end - n0);
+#pragma unroll 2
+    for (int i = warp * 4; i < rows; i += 32) {
+      float w[4][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float* at = W + (long long)(n0 + i + j) * ldw;
+        const bool in = i + j < rows;
+        if (VEC) {
+          const float4 v = in && col[0] < K ? __ldcs(reinterpret_cast<const float4*>(at + col[0])) : make_float4(0.f, 0.f, 0.f, 0.f);
+          w[j][0] = v.x; w[j][1] = v.y; w[j][2] = v.z; w[j][3] = v.w;
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) w[j][q] = in && col[q] < K ? __ldcs(at + col[q]) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < MR; ++m) {
+        const float4 f = *reinterpret_cast<const float4*>(&d[m][i]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          acc[m][q] = fmaf(f.x, w[0][q], fmaf(f.y, w[1][q], fmaf(f.z, w[2][q], fmaf(f.w, w[3][q], acc[m][q]))));
+      }
+    }
+  }
+#pragma unroll
+  for (int m0 = 0; m0 < MR; m0 += 4) {
+    __syncthreads();
+#pragma unroll
+    for (int m = m0; m < m0 + 4 && m < MR; ++m)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sums[warp][m - m0][col[q] - c0] = acc[m][q];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4 * 128; i += 256) {
+      const int m = m0 + i / 128, c = c0 + i % 128;
+      if (m >= M || c >= K || m >= MR) continue;
+      float s = sums[0][i / 128][i % 128];
+      for (int w = 1; w < 8; ++w) s += sums[w][i / 128][i % 128];
+      part[((long long)blockIdx.y * M + m) * K + c] = s;
+    }
+  }
+}
+__global__ void __launch_bounds__(256)
+sum_runs_kernel(int M, int K, const float* __restrict__ part, int runs, float* __restrict__ dX, long long lddx) {
+  const int c = blockIdx.x * 256 + threadIdx.x, m = blockIdx.y;
+  if (c >= K) return;
+  float s = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < runs; ++i) s += part[((long long)i * M + m) * K + c];
+  dX[m * lddx + c] = s;
 }
 
 }  // namespace sgc
@@ -311,6 +404,31 @@ int launch_rows(sgemm_cube_ctx* h, const sgc::LossJoinParams& j, const float* Z,
   }
   h->launches++;
   return SGEMM_CUBE_OK;
+}
+
+// dX of few rows by the kernel above: how many runs of the vocabulary, about four blocks an SM, and the launches.
+int sum_runs(const sgemm_cube_ctx* h, int N, int K, int* run) {
+  const int tiles = (K + 127) / 128;
+  int runs = (4 * h->sm_count + tiles - 1) / tiles;
+  const int most = (N + sgc::kSumRows - 1) / sgc::kSumRows;
+  if (runs > most) runs = most;
+  *run = (int)round_up((size_t)((N + runs - 1) / runs), 32);
+  return (N + *run - 1) / *run;
+}
+template <int MR>
+int launch_weighted_rows(sgemm_cube_ctx* h, int M, int N, int K, const float* dz, int64_t ldz, const sgemm_cube_operand* W, float* part,
+                         float* dX, int64_t lddx, cudaStream_t st) {
+  int run;
+  const int runs = sum_runs(h, N, K, &run);
+  const dim3 grid((unsigned)((K + 127) / 128), (unsigned)runs, 1);
+  if (aligned16(W->f32_dev) && W->ld % 4 == 0 && K % 4 == 0)
+    sgc::weighted_rows_kernel<MR, true><<<grid, 256, 0, st>>>(M, N, K, dz, ldz, W->f32_dev, W->ld, run, part);
+  else
+    sgc::weighted_rows_kernel<MR, false><<<grid, 256, 0, st>>>(M, N, K, dz, ldz, W->f32_dev, W->ld, run, part);
+  const int rc = sgc::launched(h);
+  if (rc) return rc;
+  sgc::sum_runs_kernel<<<dim3((unsigned)((K + 255) / 256), (unsigned)M, 1), 256, 0, st>>>(M, K, part, runs, dX, lddx);
+  return sgc::launched(h);
 }
 
 bool bad_layout(int layout) { return layout != SGEMM_CUBE_WEIGHT_KN && layout != SGEMM_CUBE_WEIGHT_NK; }
@@ -431,9 +549,17 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
   float* col_part = nullptr;
   unsigned int* counts = nullptr;
   float* target_logit = nullptr;
+  // (before the sizes: what the forms for few rows are chosen by has to be known)
+  const bool few = !sgc::is_packed(X) && sgc::linear_takes_few(h, M, N, K, sgc::is_packed(W), nk) &&
+                   (!dX || sgc::linear_takes_few(h, M, K, N, sgc::is_packed(W), !nk));
+  float* sum_part = nullptr;
   for (int pass = 0; pass < 2; ++pass) {         // sizes first, then pointers
     Carve c;
     c.base = pass ? static_cast<uint8_t*>(h->loss_ws) : nullptr;
+    if (few && dX && nk && !sgc::is_packed(W) && M <= sgc::kSumMost) {
+      int run;
+      sum_part = c.take<float>((size_t)sum_runs(h, N, K, &run) * M * K);
+    }
     ep.parts = c.take<float2>((size_t)piece * per_row);
     target_logit = c.take<float>((size_t)piece);
     stats = c.take<float2>((size_t)piece);
@@ -453,6 +579,73 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
   int n_jobs = 0;
   int* exps = reinterpret_cast<int*>(h->err_dev + sgc::kExpWords);
   Packed px{}, pw{};
+  const auto grad = [&](int r0, int rows, float* dz) {
+    sgc::LossGradParams p;
+    memset(&p, 0, sizeof(p));
+    p.rows = rows; p.vocab = N; p.rows_per_chunk = grad_rows;
+    p.Z = ep.Z; p.ldz = ldz;
+    p.dz = dz;
+    p.stats = stats;
+    p.dloss = dloss + r0;
+    p.targets = reinterpret_cast<const long long*>(targets) + r0;
+    p.hi = ghi; p.lo = glo; p.ldw = ldz;
+    p.exp = exps + 2;
+    p.col_part = col_part; p.counts = counts;
+    p.dbias = dbias; p.add = r0 > 0;
+    sgc::loss_grad_kernel<<<dim3((unsigned)col_blocks, (unsigned)((rows + grad_rows - 1) / grad_rows), 1), 256, 0, st>>>(p);
+    return sgc::launched(h);
+  };
+  const auto rows_of_join = [&](int r0, int rows) {
+    sgc::LossJoinParams j = join_params(rows, N, ep, loss ? loss + r0 : nullptr, lse ? lse + r0 : nullptr);
+    j.stats = stats;
+    j.dloss = dloss + r0;
+    j.range = h->err_dev + sgc::kRangeWords;
+    j.exp = split ? exps + 2 : nullptr;
+    j.counts = counts; j.n_counts = col_blocks;
+    return j;
+  };
+  const auto weight_gradient = [&](const Packed& x, int rows, sgc::LinearEpilogue le) {
+    const Packed dz{ghi, glo, ldz, exps + 2};
+    return nk ? sgc::linear_product_any(sgc::kFormMM, h, N, K, rows, dz, x, dW, lddw, le, st)
+              : sgc::linear_product_any(sgc::kFormMM, h, K, N, rows, x, dz, dW, lddw, le, st);
+  };
+  sgc::LinearEpilogue plain;
+  memset(&plain, 0, sizeof(plain));
+  // Few rows (one piece): the weight's bytes decide, so both products with it take forms that read it as it is, or, where a row of
+  // it does not start on 16 bytes and more than a few rows of X ask for that, pack it once for both.
+  const bool packed_w = sgc::is_packed(W);
+  if (few) {
+    const bool as_it_is = packed_w || M <= 4 || (aligned16(W->f32_dev) && W->ld % 4 == 0);
+    if (dW || !as_it_is) {
+      for (int pass = 0; pass < 2; ++pass) {
+        Carve c;
+        c.base = pass ? static_cast<uint8_t*>(h->ws) : nullptr;
+        n_jobs = 0;
+        if (!as_it_is) pw = sgc::words_of(W, w_rows, w_cols, c, exps + 1, jobs, &n_jobs);
+        if (dW) px = sgc::words_of(X, M, K, c, exps + 3, jobs, &n_jobs);
+        if (!pass && (rc = grow(h, &h->ws, &h->ws_bytes, c.used, st))) return rc;
+      }
+      if ((rc = sgc::launch_pack(h, jobs, n_jobs, st))) return rc;
+    }
+    const sgemm_cube_operand words{nullptr, 0, pw.hi, pw.lo, pw.ld, pw.exp};
+    const sgemm_cube_operand* w = as_it_is ? W : &words;
+    rc = sgemm_cube_linear(h, M, N, K, X, w, weight_layout, bias, nullptr, 0, SGEMM_CUBE_ACT_NONE, ep.Z, ldz, nullptr, 0, stream);
+    if (rc) return rc;
+    ep.targets = reinterpret_cast<const long long*>(targets);
+    if ((rc = launch_rows(h, rows_of_join(0, M), ep.Z, ldz, st)) || (rc = grad(0, M, dX ? ep.Z : nullptr))) return rc;
+    if (dX && sum_part) {
+      rc = M == 1   ? launch_weighted_rows<1>(h, M, N, K, ep.Z, ldz, W, sum_part, dX, lddx, st)
+           : M == 2 ? launch_weighted_rows<2>(h, M, N, K, ep.Z, ldz, W, sum_part, dX, lddx, st)
+           : M <= 4 ? launch_weighted_rows<4>(h, M, N, K, ep.Z, ldz, W, sum_part, dX, lddx, st)
+           : M <= 8 ? launch_weighted_rows<8>(h, M, N, K, ep.Z, ldz, W, sum_part, dX, lddx, st)
+                    : launch_weighted_rows<16>(h, M, N, K, ep.Z, ldz, W, sum_part, dX, lddx, st);
+    } else if (dX) {
+      const sgemm_cube_operand dz{ep.Z, ldz, nullptr, nullptr, 0, nullptr};
+      rc = sgemm_cube_linear(h, M, K, N, &dz, w, nk ? SGEMM_CUBE_WEIGHT_KN : SGEMM_CUBE_WEIGHT_NK, nullptr, nullptr, 0,
+                             SGEMM_CUBE_ACT_NONE, dX, lddx, nullptr, 0, stream);
+    }
+    return rc || !dW ? rc : weight_gradient(px, M, plain);
+  }
   for (int pass = 0; pass < 2; ++pass) {
     Carve c;
     c.base = pass ? static_cast<uint8_t*>(h->ws) : nullptr;
@@ -468,37 +661,14 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
     ep.targets = reinterpret_cast<const long long*>(targets) + r0;
     rc = nk ? loss_product<sgc::kFormLossKK>(h, rows, N, K, x, pw, ep, st) : loss_product<sgc::kFormLossKM>(h, rows, N, K, x, pw, ep, st);
     if (rc) return rc;
-    sgc::LossJoinParams j = join_params(rows, N, ep, loss ? loss + r0 : nullptr, lse ? lse + r0 : nullptr);
-    j.stats = stats;
-    j.dloss = dloss + r0;
-    j.range = h->err_dev + sgc::kRangeWords;
-    j.exp = split ? exps + 2 : nullptr;
-    j.counts = counts; j.n_counts = col_blocks;
-    if ((rc = launch_join(h, j, st))) return rc;
-    sgc::LossGradParams p;
-    memset(&p, 0, sizeof(p));
-    p.rows = rows; p.vocab = N; p.rows_per_chunk = grad_rows;
-    p.Z = ep.Z; p.ldz = ldz;
-    p.stats = stats;
-    p.dloss = dloss + r0;
-    p.targets = ep.targets;
-    p.hi = ghi; p.lo = glo; p.ldw = ldz;
-    p.exp = exps + 2;
-    p.col_part = col_part; p.counts = counts;
-    p.dbias = dbias; p.add = r0 > 0;
-    const int row_chunks = (rows + grad_rows - 1) / grad_rows;
-    sgc::loss_grad_kernel<<<dim3((unsigned)col_blocks, (unsigned)row_chunks, 1), 256, 0, st>>>(p);
-    if ((rc = sgc::launched(h))) return rc;
+    if ((rc = launch_join(h, rows_of_join(r0, rows), st)) || (rc = grad(r0, rows, nullptr))) return rc;
     const Packed dz{ghi, glo, ldz, exps + 2};
-    sgc::LinearEpilogue le;
-    memset(&le, 0, sizeof(le));
-    if (dX && (rc = sgc::linear_product_any(nk ? sgc::kFormKM : sgc::kFormKK, h, rows, K, N, dz, pw, dX + (int64_t)r0 * lddx, lddx, le, st)))
+    if (dX && (rc = sgc::linear_product_any(nk ? sgc::kFormKM : sgc::kFormKK, h, rows, K, N, dz, pw, dX + (int64_t)r0 * lddx, lddx, plain, st)))
       return rc;
     if (dW) {
+      sgc::LinearEpilogue le = plain;
       if (r0 > 0) { le.R = dW; le.ldr = lddw; }
-      rc = nk ? sgc::linear_product_any(sgc::kFormMM, h, N, K, rows, dz, x, dW, lddw, le, st)
-              : sgc::linear_product_any(sgc::kFormMM, h, K, N, rows, x, dz, dW, lddw, le, st);
-      if (rc) return rc;
+      if ((rc = weight_gradient(x, rows, le))) return rc;
     }
   }
   return SGEMM_CUBE_OK;

@@ -44,12 +44,15 @@ __device__ __forceinline__ uint4 load_shifted(const T* at) {
 // A block copies a piece of a row in 16-byte vectors; where the two rows do not meet 16-byte boundaries at the same
 // columns (VEC false) these lie on Y's boundaries, their source comes in 4-byte words, and what is left of the row at both
 // ends goes by elements.  (All of it by elements: 30001 x 1001 FP16 40 us.)
-template <typename T, bool VEC>
+// TH threads have a row's piece, the block's others rows of their own.
+template <typename T, bool VEC, int TH>
 __global__ void __launch_bounds__(kLookupThreads) embedding_kernel(LookupParams p) {
   constexpr int V = Elem<T>::kVec, U = kLookupItems;
-  for (long long unit = blockIdx.x; unit < p.rows * p.pieces; unit += gridDim.x) {
+  constexpr int side = kLookupThreads / TH;
+  const int t_row = (int)threadIdx.x % TH;
+  for (long long unit = (long long)blockIdx.x * side + (int)threadIdx.x / TH; unit < p.rows * p.pieces; unit += (long long)gridDim.x * side) {
     const long long row = p.pieces == 1 ? unit : unit / p.pieces;
-    const int c0 = (int)(unit - row * p.pieces) * (kLookupThreads * V * U) + threadIdx.x * V;
+    const int c0 = (int)(unit - row * p.pieces) * (TH * V * U) + t_row * V;
     const long long t = __ldg(p.tokens + row);
     const bool inside = t >= 0 && t < p.vocab;
     const T* src = static_cast<const T*>(p.table) + (inside ? t : 0) * p.ld;
@@ -59,12 +62,12 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_kernel(LookupParams 
       uint4 raw[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * kLookupThreads * V;
+        const int c = c0 + u * TH * V;
         if (inside && c < p.cols) raw[u] = __ldg(reinterpret_cast<const uint4*>(src + c));
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * kLookupThreads * V;
+        const int c = c0 + u * TH * V;
         if (c >= p.cols) break;
         float e[V];
         Elem<T>::unpack(raw[u], e);
@@ -78,12 +81,12 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_kernel(LookupParams 
       uint4 raw[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int c = head + c0 + u * kLookupThreads * V;
+        const int c = head + c0 + u * TH * V;
         if (inside && c < end) raw[u] = load_shifted(src + c);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int c = head + c0 + u * kLookupThreads * V;
+        const int c = head + c0 + u * TH * V;
         if (c >= end) break;
         float e[V];
         Elem<T>::unpack(raw[u], e);
@@ -91,8 +94,8 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_kernel(LookupParams 
         for (int q = 0; q < V; ++q) e[q] = inside ? e[q] * p.scale : none;
         *reinterpret_cast<uint4*>(dst + c) = Elem<T>::pack(e);
       }
-      if (c0 < kLookupThreads * V) {                         // the row's first piece: both ends
-        const int i = threadIdx.x, c = i < head ? i : end + i - head;
+      if (c0 < TH * V) {                         // the row's first piece: both ends
+        const int i = t_row, c = i < head ? i : end + i - head;
         if (c < p.cols) dst[c] = Elem<T>::put(inside ? Elem<T>::get(src[c]) * p.scale : none);
       }
     }
@@ -103,6 +106,7 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_kernel(LookupParams 
 constexpr int kSortThreads = 512, kSortItems = 4, kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBits = 9, kSortBins = 1 << kSortBits;        // two passes for vocabularies up to 2^18
 static_assert(kSortThreads == kSortBins, "a thread has a digit");
+constexpr int kSortFew = 1024;                                  // items that are ranked by counting
 
 struct SortParams {
   int n, vocab, passes;
@@ -110,7 +114,8 @@ struct SortParams {
   int* key[2];               // the pass reads from one and writes to the other; the first reads the tokens
   int* pos[2];
   int* hist;                 // [blocks][bins]
-  unsigned char* met;        // [vocab]: whether the token occurs, or null
+  unsigned char* met;        // [vocab rounded up to 16]: whether the token occurs, or null
+  int clear;                 // the flags are cleared here first
   unsigned int* words;       // {arrived, left}, zero between calls
   unsigned int* err;
 };
@@ -157,8 +162,28 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortParams p)
   const int per_block = (tiles + gridDim.x - 1) / gridDim.x;
   const int first = min((long long)p.n, (long long)blockIdx.x * per_block * kSortTile);
   const int last = min((long long)p.n, ((long long)blockIdx.x + 1) * per_block * kSortTile);
-  if (p.met)
-    for (long long v = (long long)blockIdx.x * kSortThreads + t; v < p.vocab; v += (long long)gridDim.x * kSortThreads) p.met[v] = 0;
+  if (p.clear)
+    for (long long v = (long long)blockIdx.x * kSortThreads + t; v < (p.vocab + 15) / 16; v += (long long)gridDim.x * kSortThreads)
+      reinterpret_cast<uint4*>(p.met)[v] = make_uint4(0u, 0u, 0u, 0u);
+  if (p.n <= kSortFew) {
+    // One block: an item's place is the number of items that come before it.
+    __shared__ int keys[kSortFew];
+    for (int i = t; i < p.n; i += kSortThreads) {
+      const long long v = p.tokens[i];
+      keys[i] = v >= 0 && v < p.vocab ? (int)v : p.vocab;
+    }
+    __syncthreads();                                           // (the flags are cleared, too)
+    for (int i = t; i < p.n; i += kSortThreads) {
+      const int own = keys[i];
+      int place = 0;
+#pragma unroll 8
+      for (int j = 0; j < p.n; ++j) place += keys[j] < own || (keys[j] == own && j < i) ? 1 : 0;
+      p.key[p.passes & 1][place] = own;
+      p.pos[p.passes & 1][place] = i;
+      if (p.met && own < p.vocab) p.met[own] = 1;
+    }
+    return;
+  }
   unsigned int round = 0;
   for (int pass = 0; pass < p.passes; ++pass) {
     const int shift = pass * kSortBits;
@@ -270,21 +295,19 @@ struct TableGradParams {
   int vec_out;                         // dE takes 16-byte accesses
 };
 constexpr int kGradThreads = 128;
-template <typename T>
-__host__ __device__ constexpr int grad_columns() { return kGradThreads * Elem<T>::kVec; }
 
-// Column of the thread's element q in its tile: consecutive ones where rows take vectors, else one in 128.
-template <typename T, bool VEC>
+// Column of the thread's element q in its tile of TH threads: consecutive ones where rows take vectors, else TH apart.
+template <typename T, bool VEC, int TH>
 __device__ __forceinline__ int grad_column(int tile, int q) {
-  const int t = (int)threadIdx.x % kGradThreads;
-  return tile * grad_columns<T>() + (VEC ? t * Elem<T>::kVec + q : q * kGradThreads + t);
+  const int t = (int)threadIdx.x % TH;
+  return tile * (TH * Elem<T>::kVec) + (VEC ? t * Elem<T>::kVec + q : q * TH + t);
 }
-template <typename T, bool VEC>
+template <typename T, bool VEC, int TH>
 __device__ __forceinline__ void store_grad(const TableGradParams& p, int token, int tile, const float (&acc)[Elem<T>::kVec]) {
   constexpr int V = Elem<T>::kVec;
   float* out = p.dE + (long long)token * p.ldd;
   if (VEC && p.vec_out) {
-    const int c = grad_column<T, VEC>(tile, 0);
+    const int c = grad_column<T, VEC, TH>(tile, 0);
     if (c >= p.cols) return;
 #pragma unroll
     for (int q = 0; q < V; q += 4) {
@@ -298,31 +321,38 @@ __device__ __forceinline__ void store_grad(const TableGradParams& p, int token, 
   } else {
 #pragma unroll
     for (int q = 0; q < V; ++q) {
-      const int c = grad_column<T, VEC>(tile, q);
+      const int c = grad_column<T, VEC, TH>(tile, q);
       if (c < p.cols) out[c] = p.accumulate ? out[c] + acc[q] * p.scale : acc[q] * p.scale;
     }
   }
 }
 
-// A block adds the rows of one piece in one tile of columns.  Rows come four at a time; a run that lies inside the piece
+// TH threads add the rows of one piece in one tile of columns; a block has 128 / TH pieces side by side.  Rows come four at a time; a run that lies inside the piece
 // is stored, the others' sums go to `part`.  The last blocks clear rows.
-template <typename T, bool VEC>
+template <typename T, bool VEC, int TH>
 __global__ void __launch_bounds__(kGradThreads) table_grad_kernel(TableGradParams p) {
   constexpr int V = Elem<T>::kVec, U = 4;
   if (blockIdx.x >= p.sum_blocks) {
     const unsigned int blk = blockIdx.x - p.sum_blocks, blocks = gridDim.x - p.sum_blocks;
-    for (long long v = blk; v < p.vocab; v += blocks) {
-      if (p.met[v]) continue;
-      float* out = p.dE + v * p.ldd;
-      if (p.vec_out) {
-        for (int c = threadIdx.x * 4; c < p.cols; c += kGradThreads * 4) *reinterpret_cast<float4*>(out + c) = make_float4(0.f, 0.f, 0.f, 0.f);
-      } else {
-        for (int c = threadIdx.x; c < p.cols; c += kGradThreads) out[c] = 0.f;
+    // eight rows at a time: their flags come together; a warp, or all threads, for a row
+    for (long long v0 = blk * 8ll; v0 < p.vocab; v0 += blocks * 8ll) {
+      const uint2 f = *reinterpret_cast<const uint2*>(p.met + v0);   // (flags behind the vocabulary are not looked at)
+      const int lane = threadIdx.x % TH, mine = threadIdx.x / TH, step = kGradThreads / TH;
+      for (int i = mine; i < 8 && v0 + i < p.vocab; i += step) {
+        if ((i < 4 ? f.x >> (8 * i) : f.y >> (8 * i - 32)) & 0xFFu) continue;
+        float* out = p.dE + (v0 + i) * p.ldd;
+        if (p.vec_out) {
+          for (int c = lane * 4; c < p.cols; c += TH * 4) *reinterpret_cast<float4*>(out + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+          for (int c = lane; c < p.cols; c += TH) out[c] = 0.f;
+        }
       }
     }
     return;
   }
-  const int piece = (int)(blockIdx.x / p.tiles), tile = (int)(blockIdx.x - (unsigned)piece * p.tiles);
+  const int group = (int)(blockIdx.x / p.tiles), tile = (int)(blockIdx.x - (unsigned)group * p.tiles);
+  const int piece = group * (kGradThreads / TH) + (int)threadIdx.x / TH;
+  if (piece >= p.pieces) return;
   const int first = piece * p.piece, last = min(p.n, first + p.piece);
   float acc[V];
 #pragma unroll
@@ -333,12 +363,12 @@ __global__ void __launch_bounds__(kGradThreads) table_grad_kernel(TableGradParam
   bool open = first > 0 && __ldg(p.key + first - 1) == run;          // begun in the piece before
   auto leave = [&](bool goes_on) {
     if (!open && !goes_on) {
-      store_grad<T, VEC>(p, run, tile, acc);
+      store_grad<T, VEC, TH>(p, run, tile, acc);
     } else {
       float* out = p.part + (2ll * piece + (open ? 0 : 1)) * p.ldp;
 #pragma unroll
       for (int q = 0; q < V; ++q) {
-        const int c = grad_column<T, VEC>(tile, q);
+        const int c = grad_column<T, VEC, TH>(tile, q);
         if (c < p.cols) out[c] = acc[q];
       }
     }
@@ -353,12 +383,12 @@ __global__ void __launch_bounds__(kGradThreads) table_grad_kernel(TableGradParam
       if (key[u] < p.vocab) {
         const T* src = static_cast<const T*>(p.dY) + (long long)__ldg(p.pos + i + u) * p.lddy;
         if constexpr (VEC) {
-          const int c = grad_column<T, VEC>(tile, 0);
+          const int c = grad_column<T, VEC, TH>(tile, 0);
           raw[u] = c < p.cols ? __ldcs(reinterpret_cast<const uint4*>(src + c)) : make_uint4(0u, 0u, 0u, 0u);
         } else {
 #pragma unroll
           for (int q = 0; q < V; ++q) {
-            const int c = grad_column<T, VEC>(tile, q);
+            const int c = grad_column<T, VEC, TH>(tile, q);
             one[u][q] = c < p.cols ? src[c] : Elem<T>::put(0.f);
           }
         }
@@ -391,8 +421,8 @@ __global__ void __launch_bounds__(kGradThreads) table_grad_kernel(TableGradParam
 // Runs that reach over pieces: the block of the piece in which one begins adds the parts of the others, in order, eight loads
 // at a time.  (Eight groups of threads with an eighth of the parts each, or eight pieces a block, are faster for a token in 2000
 // of 30001 rows, 26 us as a plain loop, and slower where no token is in that many: 8192 rows 15 us where this takes 7.)
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kGradThreads) table_grad_join_kernel(TableGradParams p) {
+template <typename T, bool VEC, int TH>
+__global__ void __launch_bounds__(TH) table_grad_join_kernel(TableGradParams p) {
   constexpr int V = Elem<T>::kVec;
   const int piece = (int)(blockIdx.x / p.tiles), tile = (int)(blockIdx.x - (unsigned)piece * p.tiles);
   const int first = piece * p.piece, last = first + p.piece;
@@ -405,13 +435,13 @@ __global__ void __launch_bounds__(kGradThreads) table_grad_join_kernel(TableGrad
     const int i = end + (int)threadIdx.x;
     const int found = __syncthreads_count(i < p.pieces && __ldg(p.key + (long long)i * p.piece) == run);
     end += found;
-    if (found < kGradThreads) break;
+    if (found < TH) break;
   }
   float acc[V];
   int col[V];
 #pragma unroll
   for (int q = 0; q < V; ++q) {
-    col[q] = grad_column<T, VEC>(tile, q);
+    col[q] = grad_column<T, VEC, TH>(tile, q);
     acc[q] = col[q] < p.cols ? p.part[(2ll * piece + 1) * p.ldp + col[q]] : 0.f;
   }
   for (int i0 = piece + 1; i0 < end; i0 += 8) {
@@ -425,7 +455,7 @@ __global__ void __launch_bounds__(kGradThreads) table_grad_join_kernel(TableGrad
 #pragma unroll
       for (int q = 0; q < V; ++q) acc[q] += part[u][q];
   }
-  store_grad<T, VEC>(p, run, tile, acc);
+  store_grad<T, VEC, TH>(p, run, tile, acc);
 }
 
 }  // namespace sgc
@@ -438,28 +468,47 @@ size_t elem_size(int dtype) { return dtype == SGEMM_CUBE_F32 ? 4 : 2; }
 bool bad_dtype(int dtype) { return dtype < SGEMM_CUBE_F32 || dtype > SGEMM_CUBE_BF16; }
 bool bad_scale(float s) { return !std::isfinite(s); }
 
-template <typename T>
+template <typename T, int TH>
 int launch_lookup(sgemm_cube_ctx* h, sgc::LookupParams p, bool vec, cudaStream_t st) {
-  const int span = sgc::kLookupThreads * sgc::kLookupItems * sgc::Elem<T>::kVec;
+  const int span = TH * sgc::kLookupItems * sgc::Elem<T>::kVec, side = sgc::kLookupThreads / TH;
   p.pieces = (p.cols + span - 1) / span;
-  const long long units = p.rows * p.pieces, cap = 0x7FFFFFFF;
+  const long long units = (p.rows * p.pieces + side - 1) / side, cap = 0x7FFFFFFF;
   const unsigned blocks = (unsigned)(units < cap ? units : cap);
-  if (vec) sgc::embedding_kernel<T, true><<<blocks, sgc::kLookupThreads, 0, st>>>(p);
-  else sgc::embedding_kernel<T, false><<<blocks, sgc::kLookupThreads, 0, st>>>(p);
+  if (vec) sgc::embedding_kernel<T, true, TH><<<blocks, sgc::kLookupThreads, 0, st>>>(p);
+  else sgc::embedding_kernel<T, false, TH><<<blocks, sgc::kLookupThreads, 0, st>>>(p);
   return sgc::launched(h);
 }
-
+// As few threads as have a vector each, 16 at least (both ends of a row that is off the boundaries are theirs too): 32768 rows of
+// 128 FP32 10 us, 20 with 128 threads a row.
 template <typename T>
+int launch_lookup(sgemm_cube_ctx* h, const sgc::LookupParams& p, bool vec, cudaStream_t st) {
+  constexpr int V = sgc::Elem<T>::kVec;
+  if (p.cols <= 16 * V) return launch_lookup<T, 16>(h, p, vec, st);
+  if (p.cols <= 32 * V) return launch_lookup<T, 32>(h, p, vec, st);
+  return p.cols <= 64 * V ? launch_lookup<T, 64>(h, p, vec, st) : launch_lookup<T, 128>(h, p, vec, st);
+}
+
+template <typename T, int TH>
 int launch_table_grad(sgemm_cube_ctx* h, sgc::TableGradParams p, bool vec, unsigned clear_blocks, cudaStream_t st) {
+  constexpr int columns = TH * sgc::Elem<T>::kVec, side = sgc::kGradThreads / TH;
+  p.tiles = (p.cols + columns - 1) / columns;
+  const long long joins = (long long)p.pieces * p.tiles;
+  if (joins > 0x3FFFFFFF) return SGEMM_CUBE_INVALID_ARG;
+  p.sum_blocks = (unsigned)((long long)((p.pieces + side - 1) / side) * p.tiles);
   const unsigned blocks = p.sum_blocks + clear_blocks;
-  if (blocks == 0) return SGEMM_CUBE_OK;
-  if (vec) sgc::table_grad_kernel<T, true><<<blocks, sgc::kGradThreads, 0, st>>>(p);
-  else sgc::table_grad_kernel<T, false><<<blocks, sgc::kGradThreads, 0, st>>>(p);
+  if (vec) sgc::table_grad_kernel<T, true, TH><<<blocks, sgc::kGradThreads, 0, st>>>(p);
+  else sgc::table_grad_kernel<T, false, TH><<<blocks, sgc::kGradThreads, 0, st>>>(p);
   int rc = sgc::launched(h);
   if (rc || p.pieces < 2) return rc;
-  if (vec) sgc::table_grad_join_kernel<T, true><<<p.sum_blocks, sgc::kGradThreads, 0, st>>>(p);
-  else sgc::table_grad_join_kernel<T, false><<<p.sum_blocks, sgc::kGradThreads, 0, st>>>(p);
+  if (vec) sgc::table_grad_join_kernel<T, true, TH><<<(unsigned)joins, TH, 0, st>>>(p);
+  else sgc::table_grad_join_kernel<T, false, TH><<<(unsigned)joins, TH, 0, st>>>(p);
   return sgc::launched(h);
+}
+template <typename T>
+int launch_table_grad(sgemm_cube_ctx* h, const sgc::TableGradParams& p, bool vec, unsigned clear_blocks, cudaStream_t st) {
+  constexpr int V = sgc::Elem<T>::kVec;
+  if (p.cols <= 32 * V) return launch_table_grad<T, 32>(h, p, vec, clear_blocks, st);
+  return p.cols <= 64 * V ? launch_table_grad<T, 64>(h, p, vec, clear_blocks, st) : launch_table_grad<T, 128>(h, p, vec, clear_blocks, st);
 }
 
 int launch_sort(sgemm_cube_ctx* h, const sgc::SortParams& p, int blocks, cudaStream_t st) {
@@ -537,15 +586,11 @@ int sgemm_cube_embedding_backward(sgemm_cube_handle h, int rows, int vocab, int 
   memset(&p, 0, sizeof(p));
   p.n = rows; p.vocab = vocab; p.cols = cols;
   p.piece = piece; p.pieces = (rows + piece - 1) / piece;
-  const int columns = dtype == SGEMM_CUBE_F32 ? sgc::grad_columns<float>() : sgc::grad_columns<__half>();
-  p.tiles = (cols + columns - 1) / columns;
   p.dY = dY; p.lddy = lddy;
   p.scale = scale;
   p.accumulate = accumulate;
   p.dE = dtable; p.ldd = ldd;
   p.ldp = (int64_t)round_up((size_t)cols, 4);
-  if ((long long)p.pieces * p.tiles > 0x3FFFFFFF) return SGEMM_CUBE_INVALID_ARG;
-  p.sum_blocks = (unsigned)((long long)p.pieces * p.tiles);
   p.vec_out = sgc::rows_take_vectors(dtable, ldd, cols, 4);
   const bool vec = sgc::rows_take_vectors(dY, lddy, cols, e);
   sgc::SortParams s;
@@ -566,11 +611,18 @@ int sgemm_cube_embedding_backward(sgemm_cube_handle h, int rows, int vocab, int 
       s.pos[i] = c.take<int>((size_t)rows);
     }
     s.hist = c.take<int>((size_t)blocks * sgc::kSortBins);
-    s.met = c.take<unsigned char>((size_t)vocab);
+    s.met = c.take<unsigned char>(round_up((size_t)vocab, 16));
     if (p.pieces > 1) p.part = c.take<float>((size_t)2 * p.pieces * p.ldp);
     if (!pass && (rc = grow(h, &h->sort_ws, &h->sort_ws_bytes, c.used, st))) return rc;
   }
   if (accumulate) s.met = nullptr;
+  if (s.met) {                                   // 8 turns of the sort's blocks at the most, else a launch of its own
+    s.clear = (size_t)vocab <= (size_t)blocks * sgc::kSortThreads * 16 * 8;
+    if (!s.clear && cudaMemsetAsync(s.met, 0, (size_t)vocab, st) != cudaSuccess) {
+      cudaGetLastError();
+      return SGEMM_CUBE_CUDA_ERROR;
+    }
+  }
   if ((rc = launch_sort(h, s, blocks, st))) return rc;
   p.key = s.key[s.passes & 1];
   p.pos = s.pos[s.passes & 1];
