@@ -499,7 +499,7 @@ int sgemm_cube_embedding(sgemm_cube_handle h, int rows, int vocab, int cols, int
  * (accumulate == 1: such rows are left alone).  Tokens outside [0, vocab) have no row and take no part.
  * The sums are FP32 over rows in their order, in pieces of at least 32 of the sorted rows: the same from call to call.
  *   dY_dev  rows x cols of `dtype`;  dtable_dev  vocab x cols FP32, ldd >= cols.  Any alignment, no overlap.
- * Workspace: 16 bytes a row, 1 byte a token of the vocabulary, 8192 rows of cols FP32 at most.
+ * Workspace: 16 bytes a row, 1 byte a token of the vocabulary, and FP32 rows of cols: two for every 32 rows, 8192 at most.
  * Errors: INVALID_ARG, ALLOC_FAILED, CUDA_ERROR. */
 int sgemm_cube_embedding_backward(sgemm_cube_handle h, int rows, int vocab, int cols, int dtype,
                                   const int64_t* tokens_dev, const void* dY_dev, int64_t lddy, float scale,
@@ -523,8 +523,8 @@ int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K,
  * may be NULL and is then not computed.  A row whose every logit is -inf has no gradient.  dz is packed with one exponent, from the largest
  * |dloss| of a row with a target, as sgemm_cube_linear_backward packs its dz.  Outputs must not overlap inputs or each
  * other.  M == 0: dW and dbias are zero.
- * Workspace: as above, and 2 GiB or 8 bytes for every logit, whichever is less (256 rows at the least): more rows are taken
- * in pieces, whose dW are added up.
+ * Workspace: as above, and 2 GiB or 8 bytes for every logit, whichever is less (256 rows at the least), with up to a quarter
+ * more for sums; more rows are taken in pieces, whose dW are added up.
  * Errors: INVALID_ARG, MISALIGNED (packed operands), ALLOC_FAILED, CUDA_ERROR. */
 int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K,
                                       const sgemm_cube_operand* X, const sgemm_cube_operand* W, int weight_layout,
@@ -539,7 +539,7 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K,
  *   coefficients  3 * steps floats (HOST): a, b, c of every step; NULL: 3.4445, -4.7750, 2.0315 in all of them
  *   R_dev  rows x cols FP32 (ldr >= cols) or NULL (no second term): the weight that is updated, with beta = 1 - rate * decay and a scale
  *     of -rate times what the sizes ask for; may be O_dev itself (then ldr == ldo)
- *   O_dev  rows x cols FP32 (written); may be G_dev where that is FP32 (G is read before O is written)
+ *   O_dev  rows x cols FP32 (written); may be G_dev where that is FP32 (then ldo == ldg; G is read before O is written)
  * All matrices of the iteration are kept as two FP16 words (22 bits) with exponents that follow from the coefficients:
  * entries of X keep 22 bits down to 2^-29 of the largest singular value.  The products are those of sgemm_cube, termwise; the sum of
  * squares is FP64, so G may have any FP32 size.  An infinite or NaN entry makes every entry of X NaN.  Zeros give zeros.

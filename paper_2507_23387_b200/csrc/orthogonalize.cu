@@ -389,6 +389,7 @@ extern "C" int sgemm_cube_orthogonalize(sgemm_cube_handle h, int rows, int cols,
   if (!G || !O || ldg < cols || ldo < cols || (R && ldr < cols)) return SGEMM_CUBE_INVALID_ARG;
   if (misplaced(elem, G) || misplaced(4, O, R)) return SGEMM_CUBE_INVALID_ARG;
   if (R == O && ldr != ldo && rows > 1) return SGEMM_CUBE_INVALID_ARG;
+  if (G == O && (dtype != SGEMM_CUBE_F32 || (ldg != ldo && rows > 1))) return SGEMM_CUBE_INVALID_ARG;
   DeviceGuard g(h->device);
   if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;
   cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -365,7 +365,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
           } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
+#pragma unroll 4
             for (int s = 0; s < split.slices; ++s) {         // in a fixed order; a block begins with its own, so that they do
               const uint32_t peer = mapa_u32(smem_u32(at), first_peer + ((slice + s) & (split.slices - 1)));   // not all read one
 #pragma unroll

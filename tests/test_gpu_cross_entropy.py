@@ -135,6 +135,23 @@ def test_backward(h, m, n, k, layout):
     assert m <= 256 or all(torch.equal(a, b) for a, b in zip(first, second))
 
 
+# few rows, all of whose products read the weight as it is, packed or on odd addresses; long sums over the vocabulary
+@pytest.mark.parametrize("layout", [WEIGHT_KN, WEIGHT_NK])
+@pytest.mark.parametrize("m,n,k", [(1, 20000, 128), (2, 3001, 130), (4, 9999, 77), (6, 700, 1000), (9, 5003, 260), (16, 12001, 99), (17, 4000, 64),
+                                   (40, 2050, 131), (150, 1500, 200)])
+def test_gradients_of_few_rows(h, m, n, k, layout):
+    c = Case(m, n, k, layout, seed=m)
+    first = c.check_backward(h)
+    assert all(torch.equal(a, b) for a, b in zip(first, c.check_backward(h)))
+    packed = PackedMatrix(*c.w.shape)
+    h.sgemm_cube_pack(c.w, packed)
+    c.check_backward(h, w=packed)
+    c.check_forward(h, w=packed)
+    odd = strided(c.w, c.w.shape[1] + 5, 1)
+    c.check_backward(h, w=odd)
+    c.check_forward(h, w=odd)
+
+
 @pytest.mark.parametrize("pair", [0, 1, 2])
 @pytest.mark.parametrize("split", [0, 1])
 def test_kernel_variants(pair, split):

@@ -190,12 +190,13 @@ def test_refusals(h):
              o=o.data_ptr(), ldo=cols):
         return lib.sgemm_cube_orthogonalize(h._h, rows, cols, dtype, g, ldg, steps, k, eps, scale, r, ldr, beta, o, ldo, None)
 
-    assert call() == 0 and call(r=None) == 0 and call(r=o.data_ptr()) == 0
+    assert call() == 0 and call(r=None) == 0 and call(r=o.data_ptr()) == 0 and call(o=g.data_ptr()) == 0
+    assert call(rows=1, o=g.data_ptr(), ldo=cols + 1) == 0         # one row has no leading dimension
     before = h.sgemm_cube_launch_count()
     nan = float("nan")
     for bad in (dict(rows=-1), dict(cols=2 ** 31 - 1), dict(dtype=3), dict(g=None), dict(o=None), dict(g=g.data_ptr() + 2), dict(o=o.data_ptr() + 1),
                 dict(r=r.data_ptr() + 2), dict(ldg=cols - 1), dict(ldo=cols - 1), dict(ldr=cols - 1), dict(steps=0), dict(steps=65), dict(eps=-1.0),
-                dict(eps=nan), dict(scale=nan), dict(beta=float("inf")), dict(r=o.data_ptr(), ldo=cols + 1),
+                dict(eps=nan), dict(scale=nan), dict(beta=float("inf")), dict(r=o.data_ptr(), ldo=cols + 1), dict(o=g.data_ptr(), ldo=cols + 1), dict(o=g.data_ptr(), dtype=1),
                 dict(k=(f * 6)(1, 0, 0, nan, 0, 0)), dict(k=(f * 6)(0, 0, 0, 1, 0, 0)), dict(k=(f * 6)(2000, 0, 0, 2000, 0, 0))):
         assert call(**bad) == INVALID_ARG, bad
     assert h.sgemm_cube_launch_count() == before
