@@ -327,6 +327,16 @@ __device__ __forceinline__ void store_grad(const TableGradParams& p, int token, 
   }
 }
 
+// Zeros for `len` floats, by all threads of a block.
+__device__ __forceinline__ void clear_run(float* out, long long len) {
+  const long long head = min(len, (long long)((16 - (reinterpret_cast<uintptr_t>(out) & 15)) % 16 / 4)), quads = (len - head) / 4;
+  float4* body = reinterpret_cast<float4*>(out + head);
+#pragma unroll 4
+  for (long long i = threadIdx.x; i < quads; i += kGradThreads) body[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (threadIdx.x < head) out[threadIdx.x] = 0.f;
+  if (threadIdx.x < len - head - 4 * quads) out[head + 4 * quads + threadIdx.x] = 0.f;
+}
+
 // TH threads add the rows of one piece in one tile of columns; a block has 128 / TH pieces side by side.  Rows come four at a time; a run that lies inside the piece
 // is stored, the others' sums go to `part`.  The last blocks clear rows.
 template <typename T, bool VEC, int TH>
@@ -334,18 +344,17 @@ __global__ void __launch_bounds__(kGradThreads) table_grad_kernel(TableGradParam
   constexpr int V = Elem<T>::kVec, U = 4;
   if (blockIdx.x >= p.sum_blocks) {
     const unsigned int blk = blockIdx.x - p.sum_blocks, blocks = gridDim.x - p.sum_blocks;
-    // eight rows at a time: their flags come together; a warp, or all threads, for a row
-    for (long long v0 = blk * 8ll; v0 < p.vocab; v0 += blocks * 8ll) {
-      const uint2 f = *reinterpret_cast<const uint2*>(p.met + v0);   // (flags behind the vocabulary are not looked at)
-      const int lane = threadIdx.x % TH, mine = threadIdx.x / TH, step = kGradThreads / TH;
-      for (int i = mine; i < 8 && v0 + i < p.vocab; i += step) {
-        if ((i < 4 ? f.x >> (8 * i) : f.y >> (8 * i - 32)) & 0xFFu) continue;
-        float* out = p.dE + (v0 + i) * p.ldd;
-        if (p.vec_out) {
-          for (int c = lane * 4; c < p.cols; c += TH * 4) *reinterpret_cast<float4*>(out + c) = make_float4(0.f, 0.f, 0.f, 0.f);
-        } else {
-          for (int c = lane; c < p.cols; c += TH) out[c] = 0.f;
-        }
+    // 8 or (short rows) 32 rows at a time: their flags come together, and rows that follow each other are cleared as one
+    const int rows = p.cols < 1024 ? 32 : 8, lane = threadIdx.x & 31;
+    const bool flat = p.ldd == p.cols;
+    for (long long v0 = (long long)blk * rows; v0 < p.vocab; v0 += (long long)blocks * rows) {
+      uint32_t left = __ballot_sync(0xffffffffu, lane < rows && v0 + lane < p.vocab && p.met[v0 + lane] == 0);
+      while (left) {
+        const int first = __ffs(left) - 1;
+        const uint32_t behind = ~(left >> first);                      // the run's first row that is not to be cleared
+        const int run = flat ? (behind ? __ffs(behind) - 1 : 32) : 1;
+        left &= run + first >= 32 ? (1u << first) - 1u : ~(((1u << run) - 1u) << first);
+        clear_run(p.dE + (v0 + first) * p.ldd, (long long)run * p.cols);
       }
     }
     return;
