@@ -252,20 +252,30 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(LossGradParams p) {
   }
 }
 
-// dX for few rows and an FP32 weight stored outputs x inputs: dX[m, k] = sum over n of dz[m, n] W[n, k], in FP32.  The weight's
-// rows stream past the few rows of dz once, and the long sum over the vocabulary is shared by many blocks: a block has 128
-// columns of k and a run of n, a warp four rows of W in every 32, a lane four columns; the blocks' sums are added in order.
-// Bound by memory: 4 bytes an entry of W for up to 16 rows (arithmetic: 32 FMA a byte and 16 rows, half of what the SMs have).
-// (The linear layer's form for few rows shares a sum among 8 blocks at most: one row of 65536 x 1024 230 us of the call's 471.)
-constexpr int kSumRows = 256, kSumMost = 16;             // rows of W between two loads of dz; rows of dz
+// Products of few rows with an FP32 matrix, in FP32, up to 16 rows at a time: Y[m, j] = sum over i of A[m, i] W(i, j).  The matrix streams
+// past the rows once, and a long sum is shared by many blocks, whose parts are added in order.  Bound by memory, 4 bytes an
+// entry of W (16 FMA for those 4 bytes are half of what the SMs have).  Used where the linear layer's forms for few rows have no
+// work for all SMs (they share a sum among 8 blocks at most: dX of one row of 65536 x 1024 took 230 us, here 60), or would have to
+// pack W first because its rows are not on 16 bytes.
+struct FewProduct {
+  int M, J, I;               // rows, outputs, length of the sums
+  const float* A;
+  long long lda;
+  const float* W;
+  long long ldw;
+  int run;                   // of a block's sum; a multiple of 32
+  float* part;               // [runs][M_all][J], at this group's first row
+  long long part_stride;     // M_all * J
+};
+constexpr int kFewChunk = 256, kFewMost = 16;           // entries of a sum between two loads of A; rows
+
+// W's rows are the summed index: a block has 128 outputs and a run of rows, a warp four rows in every 32, a lane four outputs.
 template <int MR, bool VEC>
-__global__ void __launch_bounds__(256)
-weighted_rows_kernel(int M, int N, int K, const float* __restrict__ dz, long long ldz, const float* __restrict__ W, long long ldw, int run,
-                     float* __restrict__ part) {
-  __shared__ __align__(16) float d[MR][kSumRows];
+__global__ void __launch_bounds__(256) few_rows_sums_kernel(FewProduct p) {
+  __shared__ __align__(16) float d[MR][kFewChunk];
   __shared__ __align__(16) float sums[8][4][128];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x * 128;
-  const int n_first = (int)min((long long)N, (long long)blockIdx.y * run), n_end = (int)min((long long)N, (long long)(blockIdx.y + 1) * run);
+  const int n_first = (int)min((long long)p.I, (long long)blockIdx.y * p.run), n_end = (int)min((long long)p.I, (long long)(blockIdx.y + 1) * p.run);
   int col[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) col[q] = c0 + (VEC ? lane * 4 + q : q * 32 + lane);
@@ -274,27 +284,27 @@ weighted_rows_kernel(int M, int N, int K, const float* __restrict__ dz, long lon
   for (int m = 0; m < MR; ++m)
 #pragma unroll
     for (int q = 0; q < 4; ++q) acc[m][q] = 0.f;
-  for (int n0 = n_first; n0 < n_end; n0 += kSumRows) {
+  for (int n0 = n_first; n0 < n_end; n0 += kFewChunk) {
     __syncthreads();
-    for (int i = threadIdx.x; i < MR * kSumRows; i += 256) {
-      const int m = i / kSumRows, n = n0 + i % kSumRows;
-      d[m][i % kSumRows] = m < M && n < n_end ? dz[m * ldz + n] : 0.f;
+    for (int i = threadIdx.x; i < MR * kFewChunk; i += 256) {
+      const int m = i / kFewChunk, n = n0 + i % kFewChunk;
+      d[m][i % kFewChunk] = m < p.M && n < n_end ? p.A[m * p.lda + n] : 0.f;
     }
     __syncthreads();
-    const int rows = min(kSumRows, n_end - n0);
+    const int rows = min(kFewChunk, n_end - n0);
 #pragma unroll 2
     for (int i = warp * 4; i < rows; i += 32) {
       float w[4][4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float* at = W + (long long)(n0 + i + j) * ldw;
+        const float* at = p.W + (long long)(n0 + i + j) * p.ldw;
         const bool in = i + j < rows;
         if (VEC) {
-          const float4 v = in && col[0] < K ? __ldcs(reinterpret_cast<const float4*>(at + col[0])) : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float4 v = in && col[0] < p.J ? __ldcs(reinterpret_cast<const float4*>(at + col[0])) : make_float4(0.f, 0.f, 0.f, 0.f);
           w[j][0] = v.x; w[j][1] = v.y; w[j][2] = v.z; w[j][3] = v.w;
         } else {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) w[j][q] = in && col[q] < K ? __ldcs(at + col[q]) : 0.f;
+          for (int q = 0; q < 4; ++q) w[j][q] = in && col[q] < p.J ? __ldcs(at + col[q]) : 0.f;
         }
       }
 #pragma unroll
@@ -316,21 +326,143 @@ weighted_rows_kernel(int M, int N, int K, const float* __restrict__ dz, long lon
     __syncthreads();
     for (int i = threadIdx.x; i < 4 * 128; i += 256) {
       const int m = m0 + i / 128, c = c0 + i % 128;
-      if (m >= M || c >= K || m >= MR) continue;
+      if (m >= p.M || c >= p.J || m >= MR) continue;
       float s = sums[0][i / 128][i % 128];
       for (int w = 1; w < 8; ++w) s += sums[w][i / 128][i % 128];
-      part[((long long)blockIdx.y * M + m) * K + c] = s;
+      p.part[blockIdx.y * p.part_stride + (long long)m * p.J + c] = s;
     }
   }
 }
+
+// W's rows are the outputs: a warp has four of them and a run of the sum, a lane every 32nd vector (or entry) of it.
+template <int MR, bool VEC>
+__global__ void __launch_bounds__(256) few_rows_dots_kernel(FewProduct p) {
+  __shared__ __align__(16) float d[MR][kFewChunk];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long j0 = (long long)blockIdx.x * 32 + warp * 4;
+  const int n_first = (int)min((long long)p.I, (long long)blockIdx.y * p.run), n_end = (int)min((long long)p.I, (long long)(blockIdx.y + 1) * p.run);
+  float acc[MR][4];
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc[m][q] = 0.f;
+  for (int n0 = n_first; n0 < n_end; n0 += kFewChunk) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < MR * kFewChunk; i += 256) {
+      const int m = i / kFewChunk, n = n0 + i % kFewChunk;
+      d[m][i % kFewChunk] = m < p.M && n < n_end ? p.A[m * p.lda + n] : 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < kFewChunk / 128; ++g) {                      // 128 entries of the sum: four a lane
+      float w[4][4];
+      const int at = VEC ? g * 128 + lane * 4 : g * 128 + lane;
+      if (n0 + g * 128 >= n_end) break;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float* row = p.W + (j0 + j) * p.ldw + n0;
+        if (VEC) {
+          const float4 v = j0 + j < p.J && n0 + at < n_end ? __ldcs(reinterpret_cast<const float4*>(row + at)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          w[j][0] = v.x; w[j][1] = v.y; w[j][2] = v.z; w[j][3] = v.w;
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) w[j][q] = j0 + j < p.J && n0 + at + q * 32 < n_end ? __ldcs(row + at + q * 32) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < MR; ++m) {
+        float f[4];
+        if (VEC) {
+          const float4 v = *reinterpret_cast<const float4*>(&d[m][at]);
+          f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) f[q] = d[m][at + q * 32];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[m][j] = fmaf(f[0], w[j][0], fmaf(f[1], w[j][1], fmaf(f[2], w[j][2], fmaf(f[3], w[j][3], acc[m][j]))));
+      }
+    }
+  }
+  // the lanes' sums of a row, in a fixed tree; lane j keeps output j's
+#pragma unroll
+  for (int m = 0; m < MR; ++m) {
+    float mine = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float s = acc[m][j];
+#pragma unroll
+      for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
+      if (lane == j) mine = s;
+    }
+    if (m < p.M && lane < 4 && j0 + lane < p.J) p.part[blockIdx.y * p.part_stride + (long long)m * p.J + j0 + lane] = mine;
+  }
+}
+// dW for few rows: out[r, c] = sum over m of a[m, r] b[m, c], in FP32, up to 64 of them.  A block has 256 rows and 128 columns of the
+// result, a warp four rows at a time, a lane four columns: bound by the result's bytes up to about 32 rows, then by FMA.
+// (The tensor cores' tiles store a matrix with rows on odd addresses by elements, a row a thread: 8 rows, 100001 x 999, 560 us.)
+constexpr int kOuterMost = 64, kOuterRows = 256;
+template <bool VEC>
 __global__ void __launch_bounds__(256)
-sum_runs_kernel(int M, int K, const float* __restrict__ part, int runs, float* __restrict__ dX, long long lddx) {
+few_outer_kernel(int M, int R, int C, const float* __restrict__ a, long long lda, const float* __restrict__ b, long long ldb,
+                 float* __restrict__ out, long long ldo) {
+  __shared__ __align__(16) float bs[kOuterMost][128];
+  __shared__ __align__(16) float as[kOuterMost][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x * 128;
+  for (int i = threadIdx.x; i < M * 128; i += 256) {
+    const int m = i / 128, c = i % 128;
+    // (a lane's four columns next to each other in either layout)
+    const int at = VEC ? c : (c % 32) * 4 + c / 32;
+    bs[m][at] = c0 + c < C ? b[m * ldb + c0 + c] : 0.f;
+  }
+  const long long r_first = (long long)blockIdx.y * kOuterRows;
+  const long long r_end = min((long long)R, r_first + kOuterRows);
+  for (long long r0 = r_first; r0 < r_end; r0 += 32) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < M * 32; i += 256) {
+      const int m = i / 32, r = i % 32;
+      as[m][r] = r0 + r < r_end ? a[m * lda + r0 + r] : 0.f;
+    }
+    __syncthreads();
+    float acc[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[j][q] = 0.f;
+#pragma unroll 4
+    for (int m = 0; m < M; ++m) {
+      const float4 x = *reinterpret_cast<const float4*>(&as[m][warp * 4]), y = *reinterpret_cast<const float4*>(&bs[m][lane * 4]);
+      const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[j][q] = fmaf(xs[j], ys[q], acc[j][q]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const long long r = r0 + warp * 4 + j;
+      if (r >= r_end) break;
+      float* to = out + r * ldo + c0;
+      if (VEC) {
+        if (c0 + lane * 4 < C) __stcs(reinterpret_cast<float4*>(to + lane * 4), make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]));
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (c0 + q * 32 + lane < C) __stcs(to + q * 32 + lane, acc[j][q]);
+      }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256)
+sum_runs_kernel(int M, int J, const float* __restrict__ part, int runs, const float* __restrict__ bias, float* __restrict__ Y, long long ldy) {
   const int c = blockIdx.x * 256 + threadIdx.x, m = blockIdx.y;
-  if (c >= K) return;
+  if (c >= J) return;
   float s = 0.f;
 #pragma unroll 8
-  for (int i = 0; i < runs; ++i) s += part[((long long)i * M + m) * K + c];
-  dX[m * lddx + c] = s;
+  for (int i = 0; i < runs; ++i) s += part[((long long)i * M + m) * J + c];
+  Y[m * ldy + c] = bias ? s + bias[c] : s;
 }
 
 }  // namespace sgc
@@ -406,29 +538,87 @@ int launch_rows(sgemm_cube_ctx* h, const sgc::LossJoinParams& j, const float* Z,
   return SGEMM_CUBE_OK;
 }
 
-// dX of few rows by the kernel above: how many runs of the vocabulary, about four blocks an SM, and the launches.
-int sum_runs(const sgemm_cube_ctx* h, int N, int K, int* run) {
-  const int tiles = (K + 127) / 128;
+// Products by the kernels above: how many runs the sums are cut into, about four blocks an SM.
+int few_runs(const sgemm_cube_ctx* h, int J, int I, bool dots, int* run) {
+  const int tiles = dots ? (int)(((long long)J + 31) / 32) : (int)(((long long)J + 127) / 128);
   int runs = (4 * h->sm_count + tiles - 1) / tiles;
-  const int most = (N + sgc::kSumRows - 1) / sgc::kSumRows;
+  const int most = (I + 2 * sgc::kFewChunk - 1) / (2 * sgc::kFewChunk);
   if (runs > most) runs = most;
-  *run = (int)round_up((size_t)((N + runs - 1) / runs), 32);
-  return (N + *run - 1) / *run;
+  *run = (int)round_up((size_t)(((long long)I + runs - 1) / runs), 32);
+  return (int)(((long long)I + *run - 1) / *run);
+}
+size_t few_part(const sgemm_cube_ctx* h, int M, int J, int I, bool dots) {
+  int run;
+  return (size_t)few_runs(h, J, I, dots, &run) * M * J;
 }
 template <int MR>
-int launch_weighted_rows(sgemm_cube_ctx* h, int M, int N, int K, const float* dz, int64_t ldz, const sgemm_cube_operand* W, float* part,
-                         float* dX, int64_t lddx, cudaStream_t st) {
-  int run;
-  const int runs = sum_runs(h, N, K, &run);
-  const dim3 grid((unsigned)((K + 127) / 128), (unsigned)runs, 1);
-  if (aligned16(W->f32_dev) && W->ld % 4 == 0 && K % 4 == 0)
-    sgc::weighted_rows_kernel<MR, true><<<grid, 256, 0, st>>>(M, N, K, dz, ldz, W->f32_dev, W->ld, run, part);
-  else
-    sgc::weighted_rows_kernel<MR, false><<<grid, 256, 0, st>>>(M, N, K, dz, ldz, W->f32_dev, W->ld, run, part);
-  const int rc = sgc::launched(h);
-  if (rc) return rc;
-  sgc::sum_runs_kernel<<<dim3((unsigned)((K + 255) / 256), (unsigned)M, 1), 256, 0, st>>>(M, K, part, runs, dX, lddx);
+int launch_few(sgemm_cube_ctx* h, const sgc::FewProduct& p, bool dots, bool vec, int runs, cudaStream_t st) {
+  if (dots) {
+    const dim3 grid((unsigned)(((long long)p.J + 31) / 32), (unsigned)runs, 1);
+    if (vec) sgc::few_rows_dots_kernel<MR, true><<<grid, 256, 0, st>>>(p);
+    else sgc::few_rows_dots_kernel<MR, false><<<grid, 256, 0, st>>>(p);
+  } else {
+    const dim3 grid((unsigned)(((long long)p.J + 127) / 128), (unsigned)runs, 1);
+    if (vec) sgc::few_rows_sums_kernel<MR, true><<<grid, 256, 0, st>>>(p);
+    else sgc::few_rows_sums_kernel<MR, false><<<grid, 256, 0, st>>>(p);
+  }
   return sgc::launched(h);
+}
+// Y (M x J) = A (M x I) W + bias; W's rows are the outputs (dots) or the summed index.
+int few_product(sgemm_cube_ctx* h, int M, int J, int I, const float* A, int64_t lda, const float* W, int64_t ldw, bool dots, const float* bias,
+                float* part, float* Y, int64_t ldy, cudaStream_t st) {
+  sgc::FewProduct p;
+  memset(&p, 0, sizeof(p));
+  p.J = J; p.I = I;
+  p.lda = lda;
+  p.W = W; p.ldw = ldw;
+  p.part_stride = (long long)M * J;
+  const int runs = few_runs(h, J, I, dots, &p.run);
+  const bool vec = aligned16(W) && ldw % 4 == 0 && (dots ? I : J) % 4 == 0;
+  for (int m0 = 0; m0 < M; m0 += sgc::kFewMost) {
+    p.M = M - m0 < sgc::kFewMost ? M - m0 : sgc::kFewMost;
+    p.A = A + m0 * lda;
+    p.part = part + (long long)m0 * J;
+    const int rc = p.M == 1   ? launch_few<1>(h, p, dots, vec, runs, st)
+                   : p.M == 2 ? launch_few<2>(h, p, dots, vec, runs, st)
+                   : p.M <= 4 ? launch_few<4>(h, p, dots, vec, runs, st)
+                   : p.M <= 8 ? launch_few<8>(h, p, dots, vec, runs, st)
+                              : launch_few<16>(h, p, dots, vec, runs, st);
+    if (rc) return rc;
+  }
+  sgc::sum_runs_kernel<<<dim3((unsigned)(((long long)J + 255) / 256), (unsigned)M, 1), 256, 0, st>>>(M, J, part, runs, bias, Y, ldy);
+  return sgc::launched(h);
+}
+bool on_16_bytes(const sgemm_cube_operand* W) { return aligned16(W->f32_dev) && W->ld % 4 == 0; }
+// Logits: an FP32 weight whose rows are not on 16 bytes would be packed first, three times its bytes; up to eight rows read it as
+// it is instead (8 x 100001 x 999 126 us, 370 packed; but 14 263 and, of 32 rows in two groups, twice the packed time).
+bool few_logits(int M, const sgemm_cube_operand* W) { return W->f32_dev && M > 4 && M <= 8 && !on_16_bytes(W); }
+// dX: the linear layer's forms have about J / 128 tiles of up to 8 blocks; where that leaves more than half of the SMs idle for every
+// group of 16 rows, W is read once for each group instead (20 x 168 outputs of a sum of 78984: the call 335 -> 197 us; but 53 x 384
+// of 27468 185 -> 210 without that bound).  On odd addresses up to 8 rows.
+bool few_dx(const sgemm_cube_ctx* h, int M, int J, const sgemm_cube_operand* W) {
+  if (!W->f32_dev) return false;
+  if (M <= 8) return true;
+  const int groups = (M + sgc::kFewMost - 1) / sgc::kFewMost, tiles = (J + 127) / 128, blocks = tiles * 2 <= h->sm_count ? tiles * 8 : tiles;
+  return on_16_bytes(W) && J % 4 == 0 && M <= 4 * sgc::kFewMost && (groups == 1 || 2ll * groups * blocks < h->sm_count);
+}
+// dW: by FMA where memory bounds that, or the tensor cores' tiles would store by elements.
+bool few_dw(int M, const float* dW, int64_t lddw) { return M <= (aligned16(dW) && lddw % 4 == 0 ? 32 : sgc::kOuterMost); }
+int few_outer(sgemm_cube_ctx* h, int M, int R, int C, const float* a, int64_t lda, const float* b, int64_t ldb, float* out, int64_t ldo,
+              cudaStream_t st) {
+  // columns in x: the blocks that run at the same time write the same rows
+  const long long rows = ((long long)R + sgc::kOuterRows - 1) / sgc::kOuterRows;
+  const bool vec = aligned16(out) && ldo % 4 == 0 && C % 4 == 0;
+  for (long long y0 = 0; y0 < rows; y0 += 65535) {       // (the grid's limit)
+    const long long r0 = y0 * sgc::kOuterRows, some = rows - y0 < 65535 ? rows - y0 : 65535;
+    const long long left = (long long)R - r0, here = left < some * sgc::kOuterRows ? left : some * sgc::kOuterRows;
+    const dim3 grid((unsigned)(((long long)C + 127) / 128), (unsigned)some, 1);
+    if (vec) sgc::few_outer_kernel<true><<<grid, 256, 0, st>>>(M, (int)here, C, a + r0, lda, b, ldb, out + r0 * ldo, ldo);
+    else sgc::few_outer_kernel<false><<<grid, 256, 0, st>>>(M, (int)here, C, a + r0, lda, b, ldb, out + r0 * ldo, ldo);
+    const int rc = sgc::launched(h);
+    if (rc) return rc;
+  }
+  return SGEMM_CUBE_OK;
 }
 
 bool bad_layout(int layout) { return layout != SGEMM_CUBE_WEIGHT_KN && layout != SGEMM_CUBE_WEIGHT_NK; }
@@ -466,13 +656,15 @@ int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K, const sge
   ep.bias = bias;
   ep.targets = reinterpret_cast<const long long*>(targets);
   ep.ldp = per_row;
-  float* Z = nullptr;
+  float *Z = nullptr, *part = nullptr;
   const int64_t ldz = (int64_t)round_up((size_t)N, 8);
+  const bool by_fma = few && few_logits(M, W);
   for (int pass = 0; pass < 2; ++pass) {         // sizes first, then pointers
     Carve c;
     c.base = pass ? static_cast<uint8_t*>(h->loss_ws) : nullptr;
     if (few) {
       Z = c.take<float>((size_t)M * ldz);
+      if (by_fma) part = c.take<float>(few_part(h, M, N, K, nk));
     } else {
       ep.parts = c.take<float2>((size_t)M * per_row);
       ep.target_logit = c.take<float>((size_t)M);
@@ -480,8 +672,9 @@ int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K, const sge
     if (!pass && (rc = grow(h, &h->loss_ws, &h->loss_ws_bytes, c.used, st))) return rc;
   }
   if (few) {
-    // few rows: the layer's kernels for them, whose logits stay in L2
-    rc = sgemm_cube_linear(h, M, N, K, X, W, weight_layout, bias, nullptr, 0, SGEMM_CUBE_ACT_NONE, Z, ldz, nullptr, 0, stream);
+    // few rows: kernels for them, whose logits stay in L2
+    if (by_fma) rc = few_product(h, M, N, K, X->f32_dev, X->ld, W->f32_dev, W->ld, nk, bias, part, Z, ldz, st);
+    else rc = sgemm_cube_linear(h, M, N, K, X, W, weight_layout, bias, nullptr, 0, SGEMM_CUBE_ACT_NONE, Z, ldz, nullptr, 0, stream);
     if (rc) return rc;
     return launch_rows(h, join_params(M, N, ep, loss, lse), Z, ldz, st);
   }
@@ -552,14 +745,13 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
   // (before the sizes: what the forms for few rows are chosen by has to be known)
   const bool few = !sgc::is_packed(X) && sgc::linear_takes_few(h, M, N, K, sgc::is_packed(W), nk) &&
                    (!dX || sgc::linear_takes_few(h, M, K, N, sgc::is_packed(W), !nk));
-  float* sum_part = nullptr;
+  const bool fma_logits = few && few_logits(M, W), fma_dx = few && dX && few_dx(h, M, K, W), fma_dw = few && dW && few_dw(M, dW, lddw);
+  float *sum_part = nullptr, *logit_part = nullptr;
   for (int pass = 0; pass < 2; ++pass) {         // sizes first, then pointers
     Carve c;
     c.base = pass ? static_cast<uint8_t*>(h->loss_ws) : nullptr;
-    if (few && dX && nk && !sgc::is_packed(W) && M <= sgc::kSumMost) {
-      int run;
-      sum_part = c.take<float>((size_t)sum_runs(h, N, K, &run) * M * K);
-    }
+    if (fma_dx) sum_part = c.take<float>(few_part(h, M, K, N, !nk));
+    if (fma_logits) logit_part = c.take<float>(few_part(h, M, N, K, nk));
     ep.parts = c.take<float2>((size_t)piece * per_row);
     target_logit = c.take<float>((size_t)piece);
     stats = c.take<float2>((size_t)piece);
@@ -579,7 +771,7 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
   int n_jobs = 0;
   int* exps = reinterpret_cast<int*>(h->err_dev + sgc::kExpWords);
   Packed px{}, pw{};
-  const auto grad = [&](int r0, int rows, float* dz) {
+  const auto grad = [&](int r0, int rows, float* dz, bool words) {
     sgc::LossGradParams p;
     memset(&p, 0, sizeof(p));
     p.rows = rows; p.vocab = N; p.rows_per_chunk = grad_rows;
@@ -588,7 +780,7 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
     p.stats = stats;
     p.dloss = dloss + r0;
     p.targets = reinterpret_cast<const long long*>(targets) + r0;
-    p.hi = ghi; p.lo = glo; p.ldw = ldz;
+    if (words) { p.hi = ghi; p.lo = glo; p.ldw = ldz; }
     p.exp = exps + 2;
     p.col_part = col_part; p.counts = counts;
     p.dbias = dbias; p.add = r0 > 0;
@@ -615,36 +807,38 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
   // it does not start on 16 bytes and more than a few rows of X ask for that, pack it once for both.
   const bool packed_w = sgc::is_packed(W);
   if (few) {
-    const bool as_it_is = packed_w || M <= 4 || (aligned16(W->f32_dev) && W->ld % 4 == 0);
-    if (dW || !as_it_is) {
+    // (nothing that follows has to pack the weight)
+    const bool as_it_is = packed_w || on_16_bytes(W) || ((fma_logits || M <= 4) && (!dX || fma_dx || M <= 4));
+    const bool words = dW && !fma_dw;              // of X and dz
+    if (words || !as_it_is) {
       for (int pass = 0; pass < 2; ++pass) {
         Carve c;
         c.base = pass ? static_cast<uint8_t*>(h->ws) : nullptr;
         n_jobs = 0;
         if (!as_it_is) pw = sgc::words_of(W, w_rows, w_cols, c, exps + 1, jobs, &n_jobs);
-        if (dW) px = sgc::words_of(X, M, K, c, exps + 3, jobs, &n_jobs);
+        if (words) px = sgc::words_of(X, M, K, c, exps + 3, jobs, &n_jobs);
         if (!pass && (rc = grow(h, &h->ws, &h->ws_bytes, c.used, st))) return rc;
       }
       if ((rc = sgc::launch_pack(h, jobs, n_jobs, st))) return rc;
     }
-    const sgemm_cube_operand words{nullptr, 0, pw.hi, pw.lo, pw.ld, pw.exp};
-    const sgemm_cube_operand* w = as_it_is ? W : &words;
-    rc = sgemm_cube_linear(h, M, N, K, X, w, weight_layout, bias, nullptr, 0, SGEMM_CUBE_ACT_NONE, ep.Z, ldz, nullptr, 0, stream);
+    const sgemm_cube_operand packed{nullptr, 0, pw.hi, pw.lo, pw.ld, pw.exp};
+    const sgemm_cube_operand* w = as_it_is ? W : &packed;
+    if (fma_logits && as_it_is) rc = few_product(h, M, N, K, X->f32_dev, X->ld, W->f32_dev, W->ld, nk, bias, logit_part, ep.Z, ldz, st);
+    else rc = sgemm_cube_linear(h, M, N, K, X, w, weight_layout, bias, nullptr, 0, SGEMM_CUBE_ACT_NONE, ep.Z, ldz, nullptr, 0, stream);
     if (rc) return rc;
     ep.targets = reinterpret_cast<const long long*>(targets);
-    if ((rc = launch_rows(h, rows_of_join(0, M), ep.Z, ldz, st)) || (rc = grad(0, M, dX ? ep.Z : nullptr))) return rc;
-    if (dX && sum_part) {
-      rc = M == 1   ? launch_weighted_rows<1>(h, M, N, K, ep.Z, ldz, W, sum_part, dX, lddx, st)
-           : M == 2 ? launch_weighted_rows<2>(h, M, N, K, ep.Z, ldz, W, sum_part, dX, lddx, st)
-           : M <= 4 ? launch_weighted_rows<4>(h, M, N, K, ep.Z, ldz, W, sum_part, dX, lddx, st)
-           : M <= 8 ? launch_weighted_rows<8>(h, M, N, K, ep.Z, ldz, W, sum_part, dX, lddx, st)
-                    : launch_weighted_rows<16>(h, M, N, K, ep.Z, ldz, W, sum_part, dX, lddx, st);
+    if ((rc = launch_rows(h, rows_of_join(0, M), ep.Z, ldz, st)) || (rc = grad(0, M, dX || fma_dw ? ep.Z : nullptr, words))) return rc;
+    if (fma_dx) {
+      rc = few_product(h, M, K, N, ep.Z, ldz, W->f32_dev, W->ld, !nk, nullptr, sum_part, dX, lddx, st);
     } else if (dX) {
       const sgemm_cube_operand dz{ep.Z, ldz, nullptr, nullptr, 0, nullptr};
       rc = sgemm_cube_linear(h, M, K, N, &dz, w, nk ? SGEMM_CUBE_WEIGHT_KN : SGEMM_CUBE_WEIGHT_NK, nullptr, nullptr, 0,
                              SGEMM_CUBE_ACT_NONE, dX, lddx, nullptr, 0, stream);
     }
-    return rc || !dW ? rc : weight_gradient(px, M, plain);
+    if (rc || !dW) return rc;
+    if (!fma_dw) return weight_gradient(px, M, plain);
+    return nk ? few_outer(h, M, N, K, ep.Z, ldz, X->f32_dev, X->ld, dW, lddw, st)
+              : few_outer(h, M, K, N, X->f32_dev, X->ld, ep.Z, ldz, dW, lddw, st);
   }
   for (int pass = 0; pass < 2; ++pass) {
     Carve c;
@@ -661,7 +855,7 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
     ep.targets = reinterpret_cast<const long long*>(targets) + r0;
     rc = nk ? loss_product<sgc::kFormLossKK>(h, rows, N, K, x, pw, ep, st) : loss_product<sgc::kFormLossKM>(h, rows, N, K, x, pw, ep, st);
     if (rc) return rc;
-    if ((rc = launch_join(h, rows_of_join(r0, rows), st)) || (rc = grad(r0, rows, nullptr))) return rc;
+    if ((rc = launch_join(h, rows_of_join(r0, rows), st)) || (rc = grad(r0, rows, nullptr, split))) return rc;
     const Packed dz{ghi, glo, ldz, exps + 2};
     if (dX && (rc = sgc::linear_product_any(nk ? sgc::kFormKM : sgc::kFormKK, h, rows, K, N, dz, pw, dX + (int64_t)r0 * lddx, lddx, plain, st)))
       return rc;
