@@ -399,6 +399,33 @@ __global__ void __launch_bounds__(256) few_rows_dots_kernel(FewProduct p) {
     if (m < p.M && lane < 4 && j0 + lane < p.J) p.part[blockIdx.y * p.part_stride + (long long)m * p.J + j0 + lane] = mine;
   }
 }
+// An FP32 matrix copied to rows on 16 bytes (`quads` of them a row; zeros behind the end), where TMA can read it.
+__global__ void __launch_bounds__(256)
+realign_kernel(long long rows, int cols, const float* __restrict__ W, long long ldw, float4* __restrict__ out, int quads) {
+  const long long total = rows * quads, stride = (long long)gridDim.x * 256;
+  constexpr int U = 4;
+  for (long long i0 = (long long)blockIdx.x * 256 + threadIdx.x; i0 < total; i0 += U * stride) {
+    float4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + u * stride;
+      if (i >= total) break;
+      const long long r = total < (1ll << 31) ? (long long)((uint32_t)i / (uint32_t)quads) : i / quads;
+      const int c = (int)(i - r * quads) * 4;
+      const float* at = W + r * ldw + c;
+      v[u].x = __ldcs(at);
+      v[u].y = c + 1 < cols ? __ldcs(at + 1) : 0.f;
+      v[u].z = c + 2 < cols ? __ldcs(at + 2) : 0.f;
+      v[u].w = c + 3 < cols ? __ldcs(at + 3) : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + u * stride;
+      if (i < total) out[i] = v[u];
+    }
+  }
+}
+
 // dW for few rows: out[r, c] = sum over m of a[m, r] b[m, c], in FP32, up to 64 of them.  A block has 256 rows and 128 columns of the
 // result, a warp four rows at a time, a lane four columns: bound by the result's bytes up to about 32 rows, then by FMA.
 // (The tensor cores' tiles store a matrix with rows on odd addresses by elements, a row a thread: 8 rows, 100001 x 999, 560 us.)
@@ -575,8 +602,9 @@ int few_product(sgemm_cube_ctx* h, int M, int J, int I, const float* A, int64_t 
   p.part_stride = (long long)M * J;
   const int runs = few_runs(h, J, I, dots, &p.run);
   const bool vec = aligned16(W) && ldw % 4 == 0 && (dots ? I : J) % 4 == 0;
-  for (int m0 = 0; m0 < M; m0 += sgc::kFewMost) {
-    p.M = M - m0 < sgc::kFewMost ? M - m0 : sgc::kFewMost;
+  const int most = vec ? sgc::kFewMost : 8;      // (16 rows by single entries: 1.7 TB/s where 8 take 3.2)
+  for (int m0 = 0; m0 < M; m0 += most) {
+    p.M = M - m0 < most ? M - m0 : most;
     p.A = A + m0 * lda;
     p.part = part + (long long)m0 * J;
     const int rc = p.M == 1   ? launch_few<1>(h, p, dots, vec, runs, st)
@@ -590,12 +618,12 @@ int few_product(sgemm_cube_ctx* h, int M, int J, int I, const float* A, int64_t 
   return sgc::launched(h);
 }
 bool on_16_bytes(const sgemm_cube_operand* W) { return aligned16(W->f32_dev) && W->ld % 4 == 0; }
-// Logits: an FP32 weight whose rows are not on 16 bytes would be packed first, three times its bytes; up to eight rows read it as
-// it is instead (8 x 100001 x 999 126 us, 370 packed; but 14 263 and, of 32 rows in two groups, twice the packed time).
-bool few_logits(int M, const sgemm_cube_operand* W) { return W->f32_dev && M > 4 && M <= 8 && !on_16_bytes(W); }
+// Logits: an FP32 weight whose rows are not on 16 bytes would be copied or packed first; up to 16 rows, eight at a time, read it as
+// it is instead (100001 x 999: 8 rows 126 us, 370 packed; 14 rows 252, 295 copied and 345 packed).
+bool few_logits(int M, const sgemm_cube_operand* W) { return W->f32_dev && M > 4 && M <= 16 && !on_16_bytes(W); }
 // dX: the linear layer's forms have about J / 128 tiles of up to 8 blocks; where that leaves more than half of the SMs idle for every
 // group of 16 rows, W is read once for each group instead (20 x 168 outputs of a sum of 78984: the call 335 -> 197 us; but 53 x 384
-// of 27468 185 -> 210 without that bound).  On odd addresses up to 8 rows.
+// of 27468 185 -> 210 without that bound).  On odd addresses up to 8 rows (16 of 45889 x 3664, all gradients: 997 us, 847 packed).
 bool few_dx(const sgemm_cube_ctx* h, int M, int J, const sgemm_cube_operand* W) {
   if (!W->f32_dev) return false;
   if (M <= 8) return true;
@@ -673,8 +701,21 @@ int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K, const sge
   }
   if (few) {
     // few rows: kernels for them, whose logits stay in L2
+    const int w_rows = nk ? N : K, w_cols = nk ? K : N, quads = (w_cols + 3) / 4;
+    const sgemm_cube_operand* w = W;
+    sgemm_cube_operand copy{nullptr, 4ll * quads, nullptr, nullptr, 0, nullptr};
+    if (!by_fma && W->f32_dev && M > 8 && !on_16_bytes(W)) {
+      // Rows on odd addresses: the layer would pack the weight, 12 bytes an entry and 4 to read the words; a copy that its kernel can
+      // read by TMA moves 8 and 4.
+      if ((rc = grow(h, &h->ws, &h->ws_bytes, (size_t)w_rows * quads * 16, st))) return rc;
+      copy.f32_dev = static_cast<const float*>(h->ws);
+      w = &copy;
+      sgc::realign_kernel<<<sgc::blocks_for(h, (long long)w_rows * quads / 4 + 1), 256, 0, st>>>(w_rows, w_cols, W->f32_dev, W->ld,
+                                                                                                static_cast<float4*>(h->ws), quads);
+      if ((rc = sgc::launched(h))) return rc;
+    }
     if (by_fma) rc = few_product(h, M, N, K, X->f32_dev, X->ld, W->f32_dev, W->ld, nk, bias, part, Z, ldz, st);
-    else rc = sgemm_cube_linear(h, M, N, K, X, W, weight_layout, bias, nullptr, 0, SGEMM_CUBE_ACT_NONE, Z, ldz, nullptr, 0, stream);
+    else rc = sgemm_cube_linear(h, M, N, K, X, w, weight_layout, bias, nullptr, 0, SGEMM_CUBE_ACT_NONE, Z, ldz, nullptr, 0, stream);
     if (rc) return rc;
     return launch_rows(h, join_params(M, N, ep, loss, lse), Z, ldz, st);
   }
