@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(256) few_rows_sums_kernel(FewProduct p) {
     }
     __syncthreads();
     const int rows = min(kFewChunk, n_end - n0);
-#pragma unroll 2
+#pragma unroll 1
     for (int i = warp * 4; i < rows; i += 32) {
       float w[4][4];
 #pragma unroll
@@ -427,15 +427,16 @@ realign_kernel(long long rows, int cols, const float* __restrict__ W, long long 
 }
 
 // dW for few rows: out[r, c] = sum over m of a[m, r] b[m, c], in FP32, up to 64 of them.  A block has 256 rows and 128 columns of the
-// result, a warp four rows at a time, a lane four columns: bound by the result's bytes up to about 32 rows, then by FMA.
+// result, a warp eight rows at a time, a lane four columns: bound by the result's bytes for few rows, then by FMA.
 // (The tensor cores' tiles store a matrix with rows on odd addresses by elements, a row a thread: 8 rows, 100001 x 999, 560 us.)
 constexpr int kOuterMost = 64, kOuterRows = 256;
-template <bool VEC>
+template <int MOST, bool VEC>
 __global__ void __launch_bounds__(256)
 few_outer_kernel(int M, int R, int C, const float* __restrict__ a, long long lda, const float* __restrict__ b, long long ldb,
                  float* __restrict__ out, long long ldo) {
-  __shared__ __align__(16) float bs[kOuterMost][128];
-  __shared__ __align__(16) float as[kOuterMost][32];
+  constexpr int CHUNK = MOST <= 16 ? kOuterRows : 64;                // rows of the result between two loads of a
+  __shared__ __align__(16) float bs[MOST][128];
+  __shared__ __align__(16) float as[MOST][CHUNK];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x * 128;
   for (int i = threadIdx.x; i < M * 128; i += 256) {
     const int m = i / 128, c = i % 128;
@@ -445,30 +446,35 @@ few_outer_kernel(int M, int R, int C, const float* __restrict__ a, long long lda
   }
   const long long r_first = (long long)blockIdx.y * kOuterRows;
   const long long r_end = min((long long)R, r_first + kOuterRows);
-  for (long long r0 = r_first; r0 < r_end; r0 += 32) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < M * 32; i += 256) {
-      const int m = i / 32, r = i % 32;
-      as[m][r] = r0 + r < r_end ? a[m * lda + r0 + r] : 0.f;
+  for (long long r0 = r_first; r0 < r_end; r0 += 64) {
+    const int at = (int)(r0 - r_first) % CHUNK;
+    if (at == 0) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < M * CHUNK; i += 256) {
+        const int m = i / CHUNK, r = i % CHUNK;
+        as[m][r] = r0 + r < r_end ? a[m * lda + r0 + r] : 0.f;
+      }
+      __syncthreads();
     }
-    __syncthreads();
-    float acc[4][4];
+    float acc[8][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) acc[j][q] = 0.f;
-#pragma unroll 4
+#pragma unroll 2
     for (int m = 0; m < M; ++m) {
-      const float4 x = *reinterpret_cast<const float4*>(&as[m][warp * 4]), y = *reinterpret_cast<const float4*>(&bs[m][lane * 4]);
-      const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+      const float4 x = *reinterpret_cast<const float4*>(&as[m][at + warp * 8]);
+      const float4 z = *reinterpret_cast<const float4*>(&as[m][at + warp * 8 + 4]);
+      const float4 y = *reinterpret_cast<const float4*>(&bs[m][lane * 4]);
+      const float xs[8] = {x.x, x.y, x.z, x.w, z.x, z.y, z.z, z.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[j][q] = fmaf(xs[j], ys[q], acc[j][q]);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const long long r = r0 + warp * 4 + j;
+    for (int j = 0; j < 8; ++j) {
+      const long long r = r0 + warp * 8 + j;
       if (r >= r_end) break;
       float* to = out + r * ldo + c0;
       if (VEC) {
@@ -641,8 +647,9 @@ int few_outer(sgemm_cube_ctx* h, int M, int R, int C, const float* a, int64_t ld
     const long long r0 = y0 * sgc::kOuterRows, some = rows - y0 < 65535 ? rows - y0 : 65535;
     const long long left = (long long)R - r0, here = left < some * sgc::kOuterRows ? left : some * sgc::kOuterRows;
     const dim3 grid((unsigned)(((long long)C + 127) / 128), (unsigned)some, 1);
-    if (vec) sgc::few_outer_kernel<true><<<grid, 256, 0, st>>>(M, (int)here, C, a + r0, lda, b, ldb, out + r0 * ldo, ldo);
-    else sgc::few_outer_kernel<false><<<grid, 256, 0, st>>>(M, (int)here, C, a + r0, lda, b, ldb, out + r0 * ldo, ldo);
+    const auto kernel = M <= 16 ? (vec ? sgc::few_outer_kernel<16, true> : sgc::few_outer_kernel<16, false>)
+                                : (vec ? sgc::few_outer_kernel<sgc::kOuterMost, true> : sgc::few_outer_kernel<sgc::kOuterMost, false>);
+    kernel<<<grid, 256, 0, st>>>(M, (int)here, C, a + r0, lda, b, ldb, out + r0 * ldo, ldo);
     const int rc = sgc::launched(h);
     if (rc) return rc;
   }

@@ -41,10 +41,10 @@ inline bool bad_dims(D... d) { return ((d < 0 || d > 0x7FFF0000) || ...); }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 namespace sgc {
-// How many clusters of a family of product kernels are resident at once: pairs, and 2 to 8 blocks with a k slice each.
+// How many clusters of a family of product kernels are resident at once: pairs, and 2 to 8 (one-launch updates: 16) blocks with a k slice each.
 struct ResidentClusters {
   bool ready = false;          // kernel attributes set, the counts below known
-  int pairs = 0, slices[9] = {0};
+  int pairs = 0, slices[17] = {0};
 };
 }  // namespace sgc
 

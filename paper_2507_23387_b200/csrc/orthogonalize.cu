@@ -231,7 +231,7 @@ int run_products(sgemm_cube_ctx* h, const OrthogonalizeCall& c) {
 bool takes_chain(int n, int m) { return (double)n * n * m <= 1.2e10; }
 
 // Slices of a product's tiles in a grid of clusters, and about how many clocks the product then takes: 1300 for a stage, 4000
-// until the first sums are there, 900 for two rows of a thread and 1500 for the meeting of a cluster.
+// until the first sums are there, 1300 for every 32 rows of a block, and 1500 for the meeting of a cluster, 3000 of one of 16.
 long long chain_split(long long tiles, int K, int blocks, int cluster, sgc::ChainSplit* split) {
   const int stages = (K + sgc::kChainBK - 1) / sgc::kChainBK;
   long long least = 0;
@@ -239,7 +239,7 @@ long long chain_split(long long tiles, int K, int blocks, int cluster, sgc::Chai
     const int per = (stages + s - 1) / s;
     if (s > 1 && tiles * s > blocks) continue;
     const long long turns = (tiles * s + blocks - 1) / blocks;
-    const long long clocks = turns * (4000 + per * 1300ll + (s < 4 ? 4 / s : 1) * 1300ll) + (s > 1 ? 1500 : 0);
+    const long long clocks = turns * (4000 + per * 1300ll + (s < 4 ? 4 / s : 1) * 1300ll) + (s > 8 ? 3000 : (s > 1 ? 1500 : 0));
     if (s == 1 || clocks < least) { least = clocks; *split = sgc::ChainSplit{(int)tiles, s, per}; }
   }
   return least;
@@ -260,13 +260,14 @@ cudaLaunchConfig_t chain_config(int blocks, int cluster, cudaLaunchAttribute* at
   cfg.numAttrs = 2;
   return cfg;
 }
-// How many clusters of 1 to 8 blocks are resident at once.
+// How many clusters of 1 to 16 blocks are resident at once.
 template <typename T>
 int chain_setup(sgemm_cube_ctx* h) {
   sgc::ResidentClusters& k = h->chain_clusters[sizeof(T) == 4 ? 0 : (std::is_same<T, __half>::value ? 1 : 2)];
   if (k.ready) return SGEMM_CUBE_OK;
   auto kernel = sgc::polynomial_chain_kernel<T>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sgc::kChainSmem) != cudaSuccess) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sgc::kChainSmem) != cudaSuccess ||
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
     cudaGetLastError();
     return SGEMM_CUBE_CUDA_ERROR;
   }

@@ -28,7 +28,7 @@ constexpr uint32_t kChainRing = kChainStages * kChainStageBytes;
 constexpr int kChainPitch = 132;                                         // finishing: rows of a tile, 132 floats apart, in the ring
 static_assert(kChainTile * kChainPitch * 4 <= kChainRing, "a finished tile fits the ring");
 constexpr uint32_t kChainSmem = kChainRing + 256 + 1024;
-constexpr int kChainMostSteps = 64, kChainMostCluster = 8;
+constexpr int kChainMostSteps = 64, kChainMostCluster = 16;
 
 struct ChainStep {           // factors of a step's three products (powers of two for the words' exponents in them)
   float gram_alpha, gram_pre, square_alpha, square_beta, square_pre, update_alpha, update_beta, update_pre;
@@ -402,7 +402,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
           chain_agree(true);
           // eight rows of a column, to the row of that number
           // (up to four of a warp's lanes next to each other: 64 bytes of a row, and its reads meet in few banks)
-          const int groups = share >> 3, wide = groups < 4 ? 1 : 2;
+          const int groups = share >> 3, wide = groups < 2 ? 0 : (groups < 4 ? 1 : 2);
 #pragma unroll 1
           for (int i = tid; i < groups * kChainTile; i += kChainEpiThreads) {
             const int col = (i >> wide) & (kChainTile - 1), g = ((i & ((1 << wide) - 1)) + ((i >> wide) / kChainTile << wide)) * 8;
