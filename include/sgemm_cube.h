@@ -509,7 +509,7 @@ int sgemm_cube_embedding_backward(sgemm_cube_handle h, int rows, int vocab, int 
  *   lse_dev[r]  = log sum_j exp(z[r, j])
  *   loss_dev[r] = lse[r] - z[r, t], t = targets_dev[r]; 0 where t < 0 (no target), NaN where t >= N
  * Either may be NULL, not both.  X, W, weight_layout and bias as in sgemm_cube_linear, whose products these are (its forms for few rows
- * among them); a bias of -inf takes a token out.  A row whose every logit is -inf has lse -inf and, with a target, loss +inf.
+ * among them, and FP32 multiplication for up to 64 rows); a bias of -inf takes a token out.  A row whose every logit is -inf has lse -inf and, with a target, loss +inf.
  * M >= 0, N >= 1, K >= 1.  Workspace: what sgemm_cube_linear takes to pack its operands, and M N / 8 bytes.
  * Errors: INVALID_ARG, MISALIGNED (packed operands), ALLOC_FAILED, CUDA_ERROR. */
 int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K,

@@ -253,8 +253,8 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(LossGradParams p) {
 }
 
 // Products of few rows with an FP32 matrix, in FP32, up to 16 rows at a time: Y[m, j] = sum over i of A[m, i] W(i, j).  The matrix streams
-// past the rows once, and a long sum is shared by many blocks, whose parts are added in order.  Bound by memory, 4 bytes an
-// entry of W (16 FMA for those 4 bytes are half of what the SMs have).  Used where the linear layer's forms for few rows have no
+// past the rows once, and a long sum is shared by many blocks, whose parts are added in order.  4 bytes an entry of W, latency above
+// a few rows (12 rows of 65536 x 1024 119 us, 2.3 TB/s: 64 sums a thread leave 16 warps an SM).  Used where the linear layer's forms for few rows have no
 // work for all SMs (they share a sum among 8 blocks at most: dX of one row of 65536 x 1024 took 230 us, here 60), or would have to
 // pack W first because its rows are not on 16 bytes.
 struct FewProduct {
@@ -513,13 +513,6 @@ constexpr int kGradRows = 256, kGradRowsLeast = 32;      // rows of a column sum
 int loss_setup(sgemm_cube_ctx* h) {
   return sgc::product_setup<sgc::kFormLossKM, sgc::kFormLossKK>(h, h->loss_clusters);
 }
-
-struct LossCall {
-  int M, N, K;
-  bool nk;
-  const float* bias;
-  const int64_t* targets;
-};
 
 template <int FORM>
 int loss_product(sgemm_cube_ctx* h, int M, int N, int K, const Packed& X, const Packed& W, sgc::LossEpilogue ep, cudaStream_t st) {
