@@ -271,6 +271,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
       const long long ld = symmetric ? p.lda : p.ldx;
       // Rows of a tile that a block finishes.
       const int share = kChainTile / split.slices;
+      const int filled = (num_kb + split.per - 1) / split.per;       // slices that hold sums
       for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
         int tm, tn, slice, kb0, kb1;
         unit_of(unit, tm, tn, slice, kb0, kb1);
@@ -321,12 +322,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
           __syncwarp();
           if (lane == 0) mbar_arrive(&tempty_bar[2]);
         }
-        if (empty) {
-          float4* out = reinterpret_cast<float4*>(stage) + tid;
-#pragma unroll 1
-          for (int i = 0; i < kChainTile * kChainPitch / 4; i += kChainEpiThreads)
-            if (i + tid < kChainTile * kChainPitch / 4) out[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        } else if (ok) {
+        if (ok && !empty) {
           float* out = stage + (quarter * 32 + lane) * kChainPitch + half * 64;
 #pragma unroll
           for (int c = 0; c < 64; c += 4) *reinterpret_cast<float4*>(out + c) = make_float4(S[c], S[c + 1], S[c + 2], S[c + 3]);
@@ -365,9 +361,11 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
           } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            int from = slice < filled ? slice : slice % filled;      // in a fixed order; a block begins with its own, so that
 #pragma unroll 4
-            for (int s = 0; s < split.slices; ++s) {         // in a fixed order; a block begins with its own, so that they do
-              const uint32_t peer = mapa_u32(smem_u32(at), first_peer + ((slice + s) & (split.slices - 1)));   // not all read one
+            for (int s = 0; s < filled; ++s) {                       // they do not all read one
+              const uint32_t peer = mapa_u32(smem_u32(at), first_peer + from);
+              from = from + 1 < filled ? from + 1 : 0;
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 if (lr + 8 * j < row_end) {
