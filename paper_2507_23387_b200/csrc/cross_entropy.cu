@@ -618,7 +618,7 @@ int few_product(sgemm_cube_ctx* h, int M, int J, int I, const float* A, int64_t 
 }
 bool on_16_bytes(const sgemm_cube_operand* W) { return aligned16(W->f32_dev) && W->ld % 4 == 0; }
 // Logits: an FP32 weight whose rows are not on 16 bytes would be copied or packed first; up to 16 rows, eight at a time, read it as
-// it is instead (100001 x 999: 8 rows 126 us, 370 packed; 14 rows 252, 295 copied and 345 packed).
+// it is instead (100001 x 999: 8 rows 126 us, 370 packed; 14 rows 218, 295 copied and 345 packed).
 bool few_logits(int M, const sgemm_cube_operand* W) { return W->f32_dev && M > 4 && M <= 16 && !on_16_bytes(W); }
 // dX: the linear layer's forms have about J / 128 tiles of up to 8 blocks; where that leaves more than half of the SMs idle for every
 // group of 16 rows, W is read once for each group instead (20 x 168 outputs of a sum of 78984: the call 335 -> 197 us; but 53 x 384

@@ -226,8 +226,8 @@ int run_products(sgemm_cube_ctx* h, const OrthogonalizeCall& c) {
 }
 
 // Which matrices take the one launch: its tiles of 128 x 128 fetch twice as many bytes for a product as the larger kernel's pairs and
-// have no next tile's products to hide their epilogue behind.  Five steps, one launch and a launch a product: 128 x 384 133 and
-// 318 us, 2048 x 512 187 and 523, 1024 x 8192 767 and 933, 2048 x 2048 664 and 820; 3000 x 3000 2416 and 2036.
+// have no next tile's products to hide their epilogue behind.  Five steps, one launch and a launch a product: 128 x 384 123 and
+// 318 us, 2048 x 512 186 and 523, 1024 x 8192 758 and 933, 2048 x 2048 664 and 820; 3000 x 3000 2416 and 2036.
 bool takes_chain(int n, int m) { return (double)n * n * m <= 1.2e10; }
 
 // Slices of a product's tiles in a grid of clusters, and about how many clocks the product then takes: 1300 for a stage, 4000
