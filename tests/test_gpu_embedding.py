@@ -147,6 +147,23 @@ def test_gradient_strides(h, dtype, cols, ldy, ldd, off):
     assert bool(torch.isnan(buf[~inside]).all())
 
 
+@pytest.mark.parametrize("vocab,cols,ldd,off", [(41, 4096, 4096, 0), (41, 4096, 4096, 1), (3, 20000, 20000, 31), (3, 20000, 20003, 17),
+                                                (4096, 12, 12, 32), (9001, 5, 5, 7), (1000, 33, 40, 3), (1, 1, 1, 5), (130, 127, 127, 30)])
+@pytest.mark.parametrize("met", ["none", "few", "ends", "every other"])
+def test_rows_without_tokens_are_zeros_and_nothing_else_is_written(h, vocab, cols, ldd, off, met):
+    """Zeros go out in pieces that begin at their own addresses, inside rows and across them."""
+    tokens = {"none": torch.tensor([-1, vocab]), "few": torch.tensor([vocab // 2, vocab // 3, vocab // 2]),
+              "ends": torch.tensor([0, vocab - 1]), "every other": torch.arange(0, vocab, 2)}[met].to(DEV)
+    dy = torch.ones(len(tokens), cols, device=DEV)
+    grad, buf = wide(vocab, cols, ldd, offset=off)
+    h.sgemm_cube_embedding_backward(tokens, dy, grad)
+    keep = tokens[(tokens >= 0) & (tokens < vocab)]
+    assert torch.equal(grad, torch.bincount(keep, minlength=vocab).float()[:, None].expand(vocab, cols))
+    inside = torch.zeros(len(buf), dtype=torch.bool, device=DEV)
+    torch.as_strided(inside, (vocab, cols), (ldd, 1), off).fill_(True)
+    assert bool(buf[~inside].isnan().all())
+
+
 def test_gradient_of_infinite_rows_stays_in_their_tokens(h):
     rows, cols = 200, 9
     tokens, dy = torch.arange(rows, device=DEV) % 20, rand(10, rows, cols)
