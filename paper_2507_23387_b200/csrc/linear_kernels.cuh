@@ -45,18 +45,25 @@ pack_range_kernel(PackJob a, PackJob b, unsigned int blocks_a, unsigned int* wor
   const unsigned int nblk = second ? gridDim.x - blocks_a : blocks_a;
   const unsigned int blk = second ? blockIdx.x - blocks_a : blockIdx.x;
   uint32_t m = 0;
-  // Items are 4 elements of a row (vector) or single elements; every thread has four in flight.
-  const long long per_row = j.vec ? j.cols >> 2 : j.cols;
-  const long long total = (long long)j.rows * per_row;
+  // Items are 4 elements of a row (vector) or single elements; every thread has four in flight.  Rows behind one another are one
+  // vector, whatever their width; what lies in front of its first 16 bytes and behind its last is the first block's.
+  const bool flat = j.ldx == j.cols, quads = flat || j.vec;
+  const long long all = (long long)j.rows * j.cols;
+  const int head = flat ? (int)min(all, (long long)((16 - (reinterpret_cast<uintptr_t>(j.X) & 15)) % 16 / 4)) : 0;
+  const long long per_row = quads ? j.cols >> 2 : j.cols;
+  const long long total = flat ? (all - head) >> 2 : (long long)j.rows * per_row;
   const long long stride = (long long)nblk * 256;
-  const bool flat = j.ldx == j.cols;
+  if (flat && blk == 0) {
+    if ((int)threadIdx.x < head) m = finite_bits(j.X[threadIdx.x]);
+    if (head + 4 * total + threadIdx.x < all) m = max(m, finite_bits(j.X[head + 4 * total + threadIdx.x]));
+  }
   auto at = [&](long long it) -> const float* {
-    if (flat) return j.X + it * (j.vec ? 4 : 1);
+    if (flat) return j.X + head + it * 4;
     const long long r = total < (1ll << 31) ? (long long)((uint32_t)it / (uint32_t)per_row) : it / per_row;
     return j.X + r * j.ldx + (it - r * per_row) * (j.vec ? 4 : 1);
   };
   long long it = (long long)blk * 256 + threadIdx.x;
-  if (j.vec) {
+  if (quads) {
     for (; it + 3 * stride < total; it += 4 * stride) {
       float4 v[4];
 #pragma unroll
@@ -147,6 +154,21 @@ dz_range_kernel(PackJob j, float* __restrict__ col_part, int rows_per_chunk, uns
   if (words) publish_amax(m, words, words + 2, gridDim.x * gridDim.y, j.exp);
 }
 
+// Eight elements of a row on any address, out of the three 16-byte words that hold them (both passes over 50001 x 1001 107 us; by
+// elements 111, and 130 with the range pass by elements, too).  The caller sees that those lie in the matrix.
+__device__ __forceinline__ void load_eight(const float* src, float (&v)[8]) {
+  const uintptr_t addr = reinterpret_cast<uintptr_t>(src);
+  const float4* words = reinterpret_cast<const float4*>(addr & ~uintptr_t(15));
+  const bool one = addr & 4, two = addr & 8;
+  const float4 a = words[0], b = words[1], c = words[2];
+  const float w[12] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, c.y, c.z, c.w};
+  float s[11];
+#pragma unroll
+  for (int q = 0; q < 11; ++q) s[q] = one ? w[q + 1] : w[q];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = two ? s[q + 2] : s[q];
+}
+
 // The split of one or two matrices (or of dz): 2^p x as hi, lo words.  Item: 8 consecutive elements of a
 // row.  Bytes per element: 4 (dz: 8) read, 4 written: bound by memory (16384 x 4096 81 us, 6.6 TB/s; the range pass
 // before it 54, 5 TB/s beside the writing back of what the kernels before left in L2; dz of 8192 x 16384 with gelu
@@ -157,6 +179,7 @@ __device__ __forceinline__ void pack_items(const PackJob& j, long long first, lo
   const float scale = pow2f(kPackScaleExp);
   const int per_row = (j.cols + 7) >> 3;
   const long long total = (long long)j.rows * per_row;
+  const float* end = j.X + (long long)(j.rows - 1) * j.ldx + j.cols;
   // From the end to the start: the range pass before read from start to end, so what it read last is
   // still in L2.
   for (long long it = total - 1 - first; it >= 0; it -= stride) {
@@ -168,6 +191,8 @@ __device__ __forceinline__ void pack_items(const PackJob& j, long long first, lo
       const float4 a = *reinterpret_cast<const float4*>(src);
       const float4 b = *reinterpret_cast<const float4*>(src + 4);
       v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else if (!DZ && c + 8 <= j.cols && src - j.X >= 3 && end - src >= 12) {
+      load_eight(src, v);
     } else {
 #pragma unroll
       for (int q = 0; q < 8; ++q) v[q] = c + q < j.cols ? src[q] : 0.f;
