@@ -399,16 +399,18 @@ __global__ void __launch_bounds__(256) few_rows_dots_kernel(FewProduct p) {
     if (m < p.M && lane < 4 && j0 + lane < p.J) p.part[blockIdx.y * p.part_stride + (long long)m * p.J + j0 + lane] = mine;
   }
 }
-// An FP32 matrix copied to rows on 16 bytes (`quads` of them a row; zeros behind the end), where TMA can read it.
+// An FP32 matrix copied to rows on 16 bytes (`quads` of them a row; zeros behind the end), where TMA can read it.  Blocks follow each other
+// in memory (100001 x 999 122 us, 6.5 TB/s; threads a grid apart 143), from the end on: the product finds the matrix' start in L2.
+constexpr int kRealignBlock = 1024;                    // 16-byte words that a block copies at a time
 __global__ void __launch_bounds__(256)
 realign_kernel(long long rows, int cols, const float* __restrict__ W, long long ldw, float4* __restrict__ out, int quads) {
-  const long long total = rows * quads, stride = (long long)gridDim.x * 256;
-  constexpr int U = 4;
-  for (long long i0 = (long long)blockIdx.x * 256 + threadIdx.x; i0 < total; i0 += U * stride) {
+  const long long total = rows * quads;
+  constexpr int U = kRealignBlock / 256;
+  for (long long i0 = (long long)(gridDim.x - 1 - blockIdx.x) * kRealignBlock + threadIdx.x; i0 < total; i0 += (long long)gridDim.x * kRealignBlock) {
     float4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long long i = i0 + u * stride;
+      const long long i = i0 + u * 256;
       if (i >= total) break;
       const long long r = total < (1ll << 31) ? (long long)((uint32_t)i / (uint32_t)quads) : i / quads;
       const int c = (int)(i - r * quads) * 4;
@@ -420,7 +422,7 @@ realign_kernel(long long rows, int cols, const float* __restrict__ W, long long 
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long long i = i0 + u * stride;
+      const long long i = i0 + u * 256;
       if (i < total) out[i] = v[u];
     }
   }
@@ -618,7 +620,7 @@ int few_product(sgemm_cube_ctx* h, int M, int J, int I, const float* A, int64_t 
 }
 bool on_16_bytes(const sgemm_cube_operand* W) { return aligned16(W->f32_dev) && W->ld % 4 == 0; }
 // Logits: an FP32 weight whose rows are not on 16 bytes would be copied or packed first; up to 16 rows, eight at a time, read it as
-// it is instead (100001 x 999: 8 rows 126 us, 370 packed; 14 rows 218, 295 copied and 345 packed).
+// it is instead (100001 x 999: 8 rows 126 us, 370 packed; 14 rows 218, 275 copied and 345 packed).
 bool few_logits(int M, const sgemm_cube_operand* W) { return W->f32_dev && M > 4 && M <= 16 && !on_16_bytes(W); }
 // dX: the linear layer's forms have about J / 128 tiles of up to 8 blocks; where that leaves more than half of the SMs idle for every
 // group of 16 rows, W is read once for each group instead (20 x 168 outputs of a sum of 78984: the call 335 -> 197 us; but 53 x 384
@@ -710,8 +712,9 @@ int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K, const sge
       if ((rc = grow(h, &h->ws, &h->ws_bytes, (size_t)w_rows * quads * 16, st))) return rc;
       copy.f32_dev = static_cast<const float*>(h->ws);
       w = &copy;
-      sgc::realign_kernel<<<sgc::blocks_for(h, (long long)w_rows * quads / 4 + 1), 256, 0, st>>>(w_rows, w_cols, W->f32_dev, W->ld,
-                                                                                                static_cast<float4*>(h->ws), quads);
+      const long long pieces = ((long long)w_rows * quads + sgc::kRealignBlock - 1) / sgc::kRealignBlock;
+      sgc::realign_kernel<<<(unsigned)(pieces < (1 << 24) ? pieces : 1 << 24), 256, 0, st>>>(w_rows, w_cols, W->f32_dev, W->ld,
+                                                                                             static_cast<float4*>(h->ws), quads);
       if ((rc = sgc::launched(h))) return rc;
     }
     if (by_fma) rc = few_product(h, M, N, K, X->f32_dev, X->ld, W->f32_dev, W->ld, nk, bias, part, Z, ldz, st);
