@@ -164,6 +164,22 @@ def test_rows_without_tokens_are_zeros_and_nothing_else_is_written(h, vocab, col
     assert bool(buf[~inside].isnan().all())
 
 
+@pytest.mark.parametrize("rows", [255, 256, 257, 383, 385, 1023, 1025, 2047, 4099, 8191, 8192, 8193])
+@pytest.mark.parametrize("vocab", [1, 3, 700, 300000])
+def test_gradient_on_both_sides_of_what_is_ranked_and_sorted(h, rows, vocab):
+    tokens, dy = tokens_like_text(31, rows, vocab), rand(32, rows, 12)
+    tokens[::7] = vocab
+    tokens[rows // 2:rows // 2 + 40] = -1
+    tokens[-1] = vocab - 1
+    want, bound = want_gradient(tokens, dy, vocab, 1.0)
+    got = torch.full((vocab, 12), float("nan"), device=DEV)
+    for accumulate in (False, True):
+        h.sgemm_cube_embedding_backward(tokens, dy, got, accumulate=accumulate)
+        # the second call adds what is there: one more rounding of the doubled sums
+        total = want * (2 if accumulate else 1)
+        assert bool(((got.double() - total).abs() <= bound * (2 if accumulate else 1) + U * total.abs() * accumulate).all())
+
+
 def test_gradient_of_infinite_rows_stays_in_their_tokens(h):
     rows, cols = 200, 9
     tokens, dy = torch.arange(rows, device=DEV) % 20, rand(10, rows, cols)
