@@ -119,10 +119,14 @@ double largest_on(double s, double k0, double k1, double k2, int odd) {
     if (roots[i] > 0.0 && roots[i] < s * s) most = std::fmax(most, f(std::sqrt(roots[i])));
   return most;
 }
-// p with 2^p x below the largest FP16 number for |x| <= bound, a sixteenth of it left for rounding.
+// p with 2^p x below the largest FP16 number for |x| <= bound, a sixteenth of it left for rounding.  At most 60, which X and A do not
+// reach: a smaller B vanishes beside a X (a step of B alone would leave less than the smallest singular value that is allowed), its
+// words lose bits from 2^-95 on, and 2^p stays FP32's whatever the coefficients.
+constexpr int kMostWordExponent = 60;
 int word_exponent(double bound) {
   if (!(bound > 0.0)) return 0;                  // a matrix of zeros
-  return 15 - (int)std::floor(std::log2(bound * 1.0625));
+  const double p = 15.0 - std::floor(std::log2(bound * 1.0625));
+  return p < kMostWordExponent ? (int)p : kMostWordExponent;
 }
 
 template <typename T>
@@ -359,7 +363,7 @@ int run_chain(sgemm_cube_ctx* h, const OrthogonalizeCall& c, bool* done) {
 }
 
 constexpr int kMostSteps = sgc::kChainMostSteps;
-constexpr double kMostBound = 0x1p20, kLeastBound = 0x1p-20;   // the words' exponents stay inside FP32's, squared and all
+constexpr double kMostBound = 0x1p20, kLeastBound = 0x1p-20;   // X's and A's exponents stay inside FP32's, squared and all; B's: word_exponent
 
 }  // namespace
 
