@@ -118,6 +118,7 @@ constexpr int kRowThreads = 256;
 __global__ void __launch_bounds__(kRowThreads) loss_rows_kernel(LossJoinParams p, const float* __restrict__ Z, long long ldz) {
   __shared__ float2 pairs[8];                                        // of the cluster's blocks, in the first
   const int ranks = (int)cluster_size(), rank = (int)cluster_ctarank();
+  cluster_started();                                                 // waited for in front of the store to the first block
   if (p.counts)
     for (int i = blockIdx.x * kRowThreads + threadIdx.x; i < p.n_counts; i += gridDim.x * kRowThreads) p.counts[i] = 0u;
   const long long r = blockIdx.x / ranks;
@@ -141,6 +142,8 @@ __global__ void __launch_bounds__(kRowThreads) loss_rows_kernel(LossJoinParams p
     acc = join_parts(acc, softmax_part(v, 1));
   }
   acc = join_block<kRowThreads / 32>(acc);
+  __syncwarp();
+  cluster_wait_started();                                            // the first block runs before anyone writes to it
   if (threadIdx.x == 0) {
     const uint32_t at = mapa_u32(smem_u32(&pairs[rank]), 0);
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(acc.x), "f"(acc.y) : "memory");
