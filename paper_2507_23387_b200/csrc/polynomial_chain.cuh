@@ -102,17 +102,23 @@ __device__ __forceinline__ bool chain_wait(const unsigned int* p, unsigned int w
 // All blocks of the grid meet for the `round`-th time (from 1); what they stored is there for loads and, behind a proxy
 // fence of the thread that issues it, for TMA.  One thread's fences stand for the block's stores, which the barrier has put
 // before them (every thread fencing for itself took 3000 to 5000 clocks a meeting).
+// The answer is the first thread's, in a word that nobody writes before the next meeting: one for all threads.
 __device__ __forceinline__ bool chain_meet(const ChainParams& p, unsigned int round, volatile uint32_t* abort_flag) {
+  volatile uint32_t* met = abort_flag + 1;
   __syncthreads();
-  if (threadIdx.x == 0 && *abort_flag == 0u) {
-    __threadfence();
-    fence_proxy_async_global();
-    add_relaxed(&p.words[0]);
-    chain_wait(&p.words[0], round * gridDim.x, abort_flag, p.err);
-    __threadfence();
+  if (threadIdx.x == 0) {
+    bool ok = *abort_flag == 0u;
+    if (ok) {
+      __threadfence();
+      fence_proxy_async_global();
+      add_relaxed(&p.words[0]);
+      ok = chain_wait(&p.words[0], round * gridDim.x, abort_flag, p.err);
+      __threadfence();
+    }
+    *met = ok;
   }
   __syncthreads();
-  return *abort_flag == 0u;
+  return *met != 0u;
 }
 
 // All threads of the cluster meet, warp by warp (the barrier wants whole warps).
@@ -151,7 +157,7 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
   uint64_t* ring_bar = tempty_bar + 3;                // finishing -> TMA: the ring may be filled again
   uint64_t* drain_bar = ring_bar + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_bar + 1);
-  volatile uint32_t* abort_flag = tmem_slot + 1;
+  volatile uint32_t* abort_flag = tmem_slot + 1;      // and, behind it, chain_meet's word
   double* block_sums = reinterpret_cast<double*>(stage);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const bool tall = p.tall != 0;
@@ -236,7 +242,8 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
   uint32_t it = 0;                                           // stages: producer and MMA thread each count them
   uint32_t chunks_done = 0, units_done = 0;                  // k-blocks and units: MMA thread and sums
   const int phases = 3 * p.steps;
-  for (int phase = 0; phase < phases && go; ++phase) {
+  int phase = 0;
+  for (; phase < phases && go; ++phase) {
     const int step = phase / 3, kind = phase - 3 * step;
     const ChainStep& f = p.step[step];
     const ChainSplit split = kind == 0 ? p.gram : (kind == 1 ? p.square : p.update);
@@ -510,6 +517,14 @@ polynomial_chain_kernel(const __grid_constant__ ChainMaps maps, const __grid_con
       if (sliced) chain_cluster_meet();
     }
     if (phase + 1 < phases) go = chain_meet(p, ++round, abort_flag);
+  }
+
+  // A wait ran out: the block has nothing more to do, but others of its cluster may be through that wait and read its shared memory
+  // yet.  It stays, and meets them as often as they meet it, so that no phase's meeting is taken for another one's.
+#pragma unroll 1
+  for (; phase < phases; ++phase) {
+    const int kind = phase % 3;
+    if ((kind == 0 ? p.gram : (kind == 1 ? p.square : p.update)).slices > 1) chain_cluster_meet();
   }
 
   // ---------------------------------------------------------------------- teardown
