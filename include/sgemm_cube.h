@@ -626,7 +626,8 @@ int sgemm_cube_last_kernel_clock(sgemm_cube_handle h, uint64_t* sm_cycles_out, u
  * SGEMM_CUBE_DEVICE_TIMEOUT.  Neither function below makes a GEMM kernel fail.
  *
  * sgemm_cube_debug_inject_error: host-made failure.  Waits for the device, then copies `code`
- * into the error word, as if a kernel had recorded it.
+ * into the error word, as if a kernel had recorded it; with 0x10C (the sorting of an embedding's gradient) it also leaves the
+ * count of the blocks that had met, as that kernel does.
  * sgemm_cube_debug_wait_timeout: enqueues a one-CTA kernel in which one thread runs the kernels'
  * bounded wait, with a limit of `limit_clocks` SM clocks (1 .. 10^8), on a barrier that nothing
  * signals; the wait gives up after the limit and records code 0x1F0.  The kernel then ends

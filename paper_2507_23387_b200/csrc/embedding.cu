@@ -153,6 +153,8 @@ __device__ __forceinline__ bool sort_meet(const SortParams& p, unsigned int roun
 // Stable sort of (token, row) by token, 9 bits a pass from the lowest.  A block has a run of whole tiles; in a pass it counts
 // its digits, meets the others, adds up for every digit what lies before its own first one, and
 // moves its items in order.  Tokens outside [0, vocab) get the key `vocab` and end up behind all others.
+// After a wait that ran out, until sgemm_cube_check has cleared the words, counts and items may be anything that the workspace held: places
+// are looked at before they are written to, here, and tokens and rows before they are used, in the sums.
 __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortParams p) {
   __shared__ int base[kSortBins];                              // next place of a digit
   __shared__ int warp_hist[kSortThreads / 32][kSortBins];
@@ -263,6 +265,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortParams p)
         if (key[u] < 0) continue;
         const int i = tile + warp * (32 * kSortItems) + u * 32 + lane;
         const int to = warp_hist[warp][(key[u] >> shift) & (kSortBins - 1)] + place[u];
+        if ((unsigned)to >= (unsigned)p.n) continue;
         key_out[to] = key[u];
         pos_out[to] = pass ? __ldcg(pos_in + i) : i;
         if (p.met && pass == p.passes - 1 && key[u] < p.vocab) p.met[key[u]] = 1;
@@ -356,6 +359,8 @@ struct TableGradParams {
 };
 constexpr int kGradThreads = 128, kClearPiece = 4096;   // threads; floats that a block clears at a time
 
+__device__ __forceinline__ bool is_token(const TableGradParams& p, int key) { return (unsigned)key < (unsigned)p.vocab; }
+
 // Column of the thread's element q in its tile of TH threads: consecutive ones where rows take vectors, else TH apart.
 template <typename T, bool VEC, int TH>
 __device__ __forceinline__ int grad_column(int tile, int q) {
@@ -440,7 +445,7 @@ __global__ void __launch_bounds__(kGradThreads) table_grad_kernel(TableGradParam
   for (int q = 0; q < V; ++q) acc[q] = 0.f;
   // tokens outside the vocabulary lie behind all others and have no row
   int run = __ldg(p.key + first);
-  if (run >= p.vocab) return;
+  if (!is_token(p, run)) return;
   bool open = first > 0 && __ldg(p.key + first - 1) == run;          // begun in the piece before
   auto leave = [&](bool goes_on) {
     if (!open && !goes_on) {
@@ -461,8 +466,8 @@ __global__ void __launch_bounds__(kGradThreads) table_grad_kernel(TableGradParam
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       key[u] = i + u < last ? __ldg(p.key + i + u) : p.vocab;
-      if (key[u] < p.vocab) {
-        const T* src = static_cast<const T*>(p.dY) + (long long)__ldg(p.pos + i + u) * p.lddy;
+      if (is_token(p, key[u])) {
+        const T* src = static_cast<const T*>(p.dY) + (long long)min((unsigned)__ldg(p.pos + i + u), (unsigned)(p.n - 1)) * p.lddy;
         if constexpr (VEC) {
           const int c = grad_column<T, VEC, TH>(tile, 0);
           raw[u] = c < p.cols ? __ldcs(reinterpret_cast<const uint4*>(src + c)) : make_uint4(0u, 0u, 0u, 0u);
@@ -477,7 +482,7 @@ __global__ void __launch_bounds__(kGradThreads) table_grad_kernel(TableGradParam
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (key[u] >= p.vocab) break;
+      if (!is_token(p, key[u])) break;
       if (key[u] != run) {
         leave(false);
         run = key[u];
@@ -510,7 +515,7 @@ __global__ void __launch_bounds__(TH) table_grad_join_kernel(TableGradParams p) 
   if (last >= p.n) return;
   const int run = __ldg(p.key + last - 1), next = __ldg(p.key + last), start = __ldg(p.key + first);
   const int before = first > 0 ? __ldg(p.key + first - 1) : -1;
-  if (run >= p.vocab || next != run || (start == run && before == run)) return;        // ends here, or begun before
+  if (!is_token(p, run) || next != run || (start == run && before == run)) return;     // ends here, or begun before
   int end = piece + 1;                                                                 // behind the pieces that find it begun
   while (true) {
     const int i = end + (int)threadIdx.x;

@@ -13,6 +13,7 @@
 #include "ctx.cuh"
 #include "gemm_tc.cuh"
 #include "probe_kernel.cuh"
+#include "product_host.cuh"
 #include "split_kernel.cuh"
 
 namespace {
@@ -1035,6 +1036,13 @@ int sgemm_cube_debug_inject_error(sgemm_cube_handle h, uint32_t code) {
   if (!g.ok) return SGEMM_CUBE_CUDA_ERROR;
   if (cudaDeviceSynchronize() != cudaSuccess ||
       cudaMemcpy(h->err_dev, &code, sizeof(code), cudaMemcpyHostToDevice) != cudaSuccess) {
+    cudaGetLastError();
+    return SGEMM_CUBE_CUDA_ERROR;
+  }
+  // what the blocks that did meet have counted stays, too, until sgemm_cube_check
+  const unsigned int counted = 1u << 16;
+  if (code == sgc::kErrSortWait &&
+      cudaMemcpy(h->err_dev + sgc::kGridWords + 2, &counted, sizeof(counted), cudaMemcpyHostToDevice) != cudaSuccess) {
     cudaGetLastError();
     return SGEMM_CUBE_CUDA_ERROR;
   }
