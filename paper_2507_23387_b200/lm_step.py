@@ -31,6 +31,11 @@ from . import binding
 NK, GELU = binding.WEIGHT_NK, binding.ACT_GELU
 
 
+def _indices(tokens):
+    """Tokens as the library reads them: 64 bits, next to each other (a view or a 32-bit tensor is copied)."""
+    return tokens.long().contiguous()
+
+
 class Model:
     """Weights, gradients and the buffers of one training step of at most `tokens` rows."""
 
@@ -70,7 +75,7 @@ class Model:
         """Views of the buffers for these rows, filled up to f."""
         h, w = self.h, self.weights
         r = {k: v[:tokens.numel()] for k, v in self.rows.items()}
-        h.sgemm_cube_embedding(tokens, w["E"], r["x"])
+        h.sgemm_cube_embedding(_indices(tokens), w["E"], r["x"])
         h.sgemm_cube_layer_norm(r["x"], r["n"], w["g1"], w["c1"], mean=r["mean1"], rstd=r["rstd1"])
         h.sgemm_cube_linear(r["n"], w["W1"], r["a"], bias=w["b1"], activation=GELU, preact=r["z"], weight_layout=NK)
         h.sgemm_cube_linear(r["a"], w["W2"], r["y"], bias=w["b2"], residual=r["x"], weight_layout=NK)
@@ -113,7 +118,7 @@ class Model:
                                      activation=GELU, weight_layout=NK)
         h.sgemm_cube_layer_norm_backward(r["dx"], r["x"], r["mean1"], r["rstd1"], r["dx"], w["g1"], g["g1"], g["c1"])
         r["dx"].add_(r["dy"])                                                      # the residual's path round the block
-        h.sgemm_cube_embedding_backward(tokens, r["dx"], g["E"])
+        h.sgemm_cube_embedding_backward(_indices(tokens), r["dx"], g["E"])
         return loss
 
     def step(self, tokens, targets, rate, entropy_weight=0.0, orthogonal=0.0, decay=0.0):
@@ -153,7 +158,7 @@ class Sampler:
         the vocabulary (a row with nothing allowed has log probabilities of -inf)."""
         h, w, p, s = self.h, self.w, self.packed, tokens.numel()
         x, n, a, l = self.x[:s], self.n[:s], self.a[:s], self.l[:s]
-        h.sgemm_cube_embedding(tokens, w["E"], x)
+        h.sgemm_cube_embedding(_indices(tokens), w["E"], x)
         h.sgemm_cube_layer_norm(x, n, w["g1"], w["c1"])
         h.sgemm_cube_linear(n, p["W1"], a, bias=w["b1"], activation=GELU, weight_layout=NK)
         h.sgemm_cube_linear(a, p["W2"], x, bias=w["b2"], residual=x, weight_layout=NK)
