@@ -770,7 +770,8 @@ int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K, 
   // rows of a piece: whole tiles of pairs, pieces of about the same size
   long long most = (long long)(kPieceBytes / (4 * (size_t)ldz)) / 256 * 256;
   if (most > kPieceRows) most = kPieceRows;
-  int piece = most < 256 ? 256 : (most < M ? (int)most : M);
+  if (most < 256) most = 256;
+  int piece = most < M ? (int)most : M;
   if (piece < M) {
     const long long pieces = ((long long)M + piece - 1) / piece;
     piece = (int)round_up((size_t)((M + pieces - 1) / pieces), 256);
