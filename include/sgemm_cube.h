@@ -505,12 +505,16 @@ int sgemm_cube_embedding_backward(sgemm_cube_handle h, int rows, int vocab, int 
                                   const int64_t* tokens_dev, const void* dY_dev, int64_t lddy, float scale,
                                   int accumulate, float* dtable_dev, int64_t ldd, void* stream);
 
-/* Softmax cross entropy of a linear layer over a vocabulary of N tokens, without the logits z = X W + b:
+/* Softmax cross entropy of a linear layer over a vocabulary of N tokens, from the layer's inputs; the logits z = X W + b are no operand
+ * and are not returned:
  *   lse_dev[r]  = log sum_j exp(z[r, j])
  *   loss_dev[r] = lse[r] - z[r, t], t = targets_dev[r]; 0 where t < 0 (no target), NaN where t >= N
  * Either may be NULL, not both.  X, W, weight_layout and bias as in sgemm_cube_linear, whose products these are (its forms for few rows
  * among them, and FP32 multiplication for up to 64 rows); a bias of -inf takes a token out.  A row whose every logit is -inf has lse -inf and, with a target, loss +inf.
- * M >= 0, N >= 1, K >= 1.  Workspace: what sgemm_cube_linear takes to pack its operands, and M N / 8 bytes.
+ * M >= 0, N >= 1, K >= 1.  Workspace: what sgemm_cube_linear takes to pack its operands, and M N / 8 bytes: the logits stay in tiles.  Where
+ * sgemm_cube_linear has forms for few rows (up to 64, of narrow layers up to 256) it holds the logits instead, 4 bytes each, and for an FP32 W
+ * with rows off 16-byte boundaries a copy of it (4 bytes an entry) or, for 5 to 16 rows, parts of the logits' sums (another 4 bytes
+ * a logit, and 5 MB).
  * Errors: INVALID_ARG, MISALIGNED (packed operands), ALLOC_FAILED, CUDA_ERROR. */
 int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K,
                              const sgemm_cube_operand* X, const sgemm_cube_operand* W, int weight_layout,
@@ -523,8 +527,10 @@ int sgemm_cube_cross_entropy(sgemm_cube_handle h, int M, int N, int K,
  * may be NULL and is then not computed.  A row whose every logit is -inf has no gradient.  dz is packed with one exponent, from the largest
  * |dloss| of a row with a target, as sgemm_cube_linear_backward packs its dz.  Outputs must not overlap inputs or each
  * other.  M == 0: dW and dbias are zero.
- * Workspace: as above, and 2 GiB or 8 bytes for every logit, whichever is less (256 rows at the least), with up to a quarter
- * more for sums; more rows are taken in pieces, whose dW are added up.
+ * Workspace: what sgemm_cube_linear takes to pack its operands, and 8 bytes for every logit (rows of them rounded up to 8), twice what a matrix
+ * of them takes, but 2 GiB at the most (256 rows of them where those are more); more rows are taken in pieces, whose dW are added up.  Beside that for sums:
+ * an eighth of a byte a logit, 12 bytes a row and, with dbias, 4 bytes a token for every 32 rows (or part of them) of a piece; for few rows as
+ * above parts of the logits' sums, and of those of dX (4 bytes an entry, and 20 MB).
  * Errors: INVALID_ARG, MISALIGNED (packed operands), ALLOC_FAILED, CUDA_ERROR. */
 int sgemm_cube_cross_entropy_backward(sgemm_cube_handle h, int M, int N, int K,
                                       const sgemm_cube_operand* X, const sgemm_cube_operand* W, int weight_layout,

@@ -1,13 +1,13 @@
-// Softmax cross entropy of a linear layer's outputs over a large vocabulary, without the logits, and its gradients
+// Softmax cross entropy of a linear layer's outputs over a large vocabulary, from the layer's inputs, and its gradients
 // (contracts: include/sgemm_cube.h).
 //
 //   z = X W + b,  lse = log sum_j exp(z_j),  loss = lse - z_t,  dz = dloss (exp(z - lse) - 1[t]),
 //   dX = dz W^T,  dW = X^T dz,  db = column sums of dz.
 //
 // Forward: the logits stay in the product's tiles; (largest, sum) of every 64 of them is what a tile leaves behind
-// (loss_epilogue.cuh), and one pass over those pairs gives lse and the loss.
+// (loss_epilogue.cuh), and one pass over those pairs gives lse and the loss.  (Few rows: the linear layer's forms for them write the logits.)
 // Gradients: a piece of the rows at a time.  Its logits (1 GiB at most) go to the workspace once and are turned into
-// the FP16 words of dz, which both products read: three products in all.  (In pieces of the vocabulary a piece's logits would have to
+// the FP16 words of dz (as much again), which both products read: three products in all.  (In pieces of the vocabulary a piece's logits would have to
 // be formed a second time once lse is known: four products.)  The words' exponent is known before them, |dz| <= |dloss|.
 #include "ctx.cuh"
 #include "product_host.cuh"

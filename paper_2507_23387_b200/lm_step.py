@@ -13,8 +13,9 @@ One residual block without attention, everything in FP32, every product on the t
 The loss is -mean(logp) - entropy_weight * mean(entropy) over the rows whose next token is known
 (negative: none).  `Model.gradients` walks the same list backwards through the `_backward` entry points;
 `Model.step` adds plain gradient descent.  Every buffer is made once for the largest batch.  A model with keep_logits=False
-has no room for l: the last two lines and their gradients are one call, sgemm_cube_cross_entropy_backward (no entropy then),
-and `Model.loss` is sgemm_cube_cross_entropy.  With orthogonal=... the step orthogonalises the updates of W1 and W2
+keeps no l: the last two lines and their gradients are one call, sgemm_cube_cross_entropy_backward (no entropy then), whose workspace
+holds the logits of a piece of the rows and the words of their gradient (8 bytes a logit, 2 GiB at the most).  `Model.loss` is
+sgemm_cube_cross_entropy, which keeps logits of few rows only.  With orthogonal=... the step orthogonalises the updates of W1 and W2
 (sgemm_cube_orthogonalize, into the weight).  `Sampler` keeps the
 weights packed and answers the most likely next tokens of a few sequences at a time.  `python -m` of this file
 trains on a fixed random successor table and prints the loss, then what the sampler learned:
@@ -176,7 +177,7 @@ def main():
     for name, value in (("tokens", 1024), ("width", 512), ("hidden", 2048), ("vocab", 8192), ("steps", 60)):
         ap.add_argument("--" + name, type=int, default=value)
     ap.add_argument("--rate", type=float, default=4.0)
-    ap.add_argument("--no-logits", action="store_true", help="the loss and its gradients without room for the logits")
+    ap.add_argument("--no-logits", action="store_true", help="the loss and its gradients in one call, no matrix of logits in the model")
     ap.add_argument("--orthogonal", type=float, default=0.0, help="rate of orthogonalised updates of W1 and W2")
     args = ap.parse_args()
     h = binding.Handle(0)
