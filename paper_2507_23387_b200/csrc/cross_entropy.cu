@@ -582,18 +582,29 @@ size_t few_part(const sgemm_cube_ctx* h, int M, int J, int I, bool dots) {
   int run;
   return (size_t)few_runs(h, J, I, dots, &run) * M * J;
 }
-template <int MR>
-int launch_few(sgemm_cube_ctx* h, const sgc::FewProduct& p, bool dots, bool vec, int runs, cudaStream_t st) {
+template <int MR, bool VEC>
+int launch_few(sgemm_cube_ctx* h, const sgc::FewProduct& p, bool dots, int runs, cudaStream_t st) {
   if (dots) {
     const dim3 grid((unsigned)(((long long)p.J + 31) / 32), (unsigned)runs, 1);
-    if (vec) sgc::few_rows_dots_kernel<MR, true><<<grid, 256, 0, st>>>(p);
-    else sgc::few_rows_dots_kernel<MR, false><<<grid, 256, 0, st>>>(p);
+    sgc::few_rows_dots_kernel<MR, VEC><<<grid, 256, 0, st>>>(p);
   } else {
     const dim3 grid((unsigned)(((long long)p.J + 127) / 128), (unsigned)runs, 1);
-    if (vec) sgc::few_rows_sums_kernel<MR, true><<<grid, 256, 0, st>>>(p);
-    else sgc::few_rows_sums_kernel<MR, false><<<grid, 256, 0, st>>>(p);
+    sgc::few_rows_sums_kernel<MR, VEC><<<grid, 256, 0, st>>>(p);
   }
   return sgc::launched(h);
+}
+// (16 rows by single entries: 1.7 TB/s where 8 take 3.2)
+template <bool VEC>
+constexpr int few_most() { return VEC ? sgc::kFewMost : 8; }
+template <bool VEC>
+int launch_few(sgemm_cube_ctx* h, const sgc::FewProduct& p, bool dots, int runs, cudaStream_t st) {
+  if (p.M == 1) return launch_few<1, VEC>(h, p, dots, runs, st);
+  if (p.M == 2) return launch_few<2, VEC>(h, p, dots, runs, st);
+  if (p.M <= 4) return launch_few<4, VEC>(h, p, dots, runs, st);
+  if constexpr (few_most<VEC>() > 8) {
+    if (p.M > 8) return launch_few<few_most<VEC>(), VEC>(h, p, dots, runs, st);
+  }
+  return launch_few<8, VEC>(h, p, dots, runs, st);
 }
 // Y (M x J) = A (M x I) W + bias; W's rows are the outputs (dots) or the summed index.
 int few_product(sgemm_cube_ctx* h, int M, int J, int I, const float* A, int64_t lda, const float* W, int64_t ldw, bool dots, const float* bias,
@@ -606,16 +617,12 @@ int few_product(sgemm_cube_ctx* h, int M, int J, int I, const float* A, int64_t 
   p.part_stride = (long long)M * J;
   const int runs = few_runs(h, J, I, dots, &p.run);
   const bool vec = aligned16(W) && ldw % 4 == 0 && (dots ? I : J) % 4 == 0;
-  const int most = vec ? sgc::kFewMost : 8;      // (16 rows by single entries: 1.7 TB/s where 8 take 3.2)
+  const int most = vec ? few_most<true>() : few_most<false>();
   for (int m0 = 0; m0 < M; m0 += most) {
     p.M = M - m0 < most ? M - m0 : most;
     p.A = A + m0 * lda;
     p.part = part + (long long)m0 * J;
-    const int rc = p.M == 1   ? launch_few<1>(h, p, dots, vec, runs, st)
-                   : p.M == 2 ? launch_few<2>(h, p, dots, vec, runs, st)
-                   : p.M <= 4 ? launch_few<4>(h, p, dots, vec, runs, st)
-                   : p.M <= 8 ? launch_few<8>(h, p, dots, vec, runs, st)
-                              : launch_few<16>(h, p, dots, vec, runs, st);
+    const int rc = vec ? launch_few<true>(h, p, dots, runs, st) : launch_few<false>(h, p, dots, runs, st);
     if (rc) return rc;
   }
   sgc::sum_runs_kernel<<<dim3((unsigned)(((long long)J + 255) / 256), (unsigned)M, 1), 256, 0, st>>>(M, J, part, runs, bias, Y, ldy);
