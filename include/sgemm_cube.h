@@ -109,7 +109,7 @@ enum {
    * (tile, slice); the slices' sums go to a workspace (grown with cudaMalloc on first use) and a
    * reduction kernel adds them in slice order (termwise: hi*hi sums and correction sums
    * separately, combined once).  This is one more level of the blocked summation of Sec. 4.5 and
-   * is deterministic.  0: never split. */
+   * is deterministic.  0: never split.  (Orthogonalised updates split the k range of their products under the same option.) */
   SGEMM_CUBE_OPT_SPLIT_K = 5
 };
 

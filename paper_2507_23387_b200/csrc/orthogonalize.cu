@@ -300,7 +300,7 @@ int run_chain(sgemm_cube_ctx* h, const OrthogonalizeCall& c, bool* done) {
   // the cluster's size: larger ones share a tile among more blocks, smaller ones leave fewer SMs out
   int cluster = 0, blocks = 0;
   long long least = 0;
-  for (int s = 1; s <= sgc::kChainMostCluster; s *= 2) {
+  for (int s = 1; s <= (h->split_k ? sgc::kChainMostCluster : 1); s *= 2) {      // (clusters are for slices of a k range)
     const int resident = k.slices[s] * s;
     if (resident == 0) continue;
     sgc::ChainSplit gram, square, update;
